@@ -531,6 +531,102 @@ int kvmem_recall_step_host(kvmem_pool_t* pool, int32_t session_first, int32_t n_
                            size_t select_workspace_bytes, void* attend_workspace /*DEVICE*/,
                            size_t attend_workspace_bytes, void* stream);
 
+/* ---- decode over a view: drafted tokens, accumulated weights, eviction ---------------------------
+ * What a serving loop does with an execution view between two recall steps (Sec. 4.1, Sec. 5.2: decode
+ * extends the view at its tail; the multi-token prediction of Sec. 5.1 verifies several drafted tokens
+ * at once): attention of drafted tokens over view and tail, the attention weight every view token has
+ * gathered, and eviction of the tokens that gathered least.
+ *
+ * Tail: tokens newer than the view that do not fill a block yet, token-major like the input of
+ * kvmem_append_blocks (whole blocks of it can be handed to that call as they are).  Session s holds
+ * n_tokens[s] committed tokens in rows [0, n_tokens[s]), its drafted tokens in the n_q[s] rows behind them.
+ * Rows behind those are not used, whatever they hold. */
+typedef struct {
+    const void* k;           /* DEVICE bf16 [n_sessions][cap_tokens][n_layers][n_kv_heads][head_dim], 16-byte aligned */
+    const void* v;           /* the same for the values                                                                */
+    int32_t cap_tokens;      /* at least n_q_tokens                                                                    */
+    const int32_t* n_tokens; /* DEVICE int32 [n_sessions]; n_tokens[s] + n_q[s] must not exceed cap_tokens             */
+} kvmem_tail_t;
+
+/* Attention of a tree of drafted tokens over view and tail.  For every drafted token i < n_q[s] of session s, layer l
+ * and head h, with T = min(n_sel[s] * block_tokens, view_cap_tokens):
+ *     visible(i) = the T view tokens, the committed tail tokens, and each drafted token j < n_q[s] whose bit j is set in
+ *                  mask[s][i]
+ *     out = softmax over visible(i) of (q_i . k * scale), times v          lse = ln sum over visible(i) of exp(q_i . k * scale)
+ * A token that sees nothing gets out = 0 and lse = -inf.  A token that is not visible to i does not reach i's result,
+ * whatever its key and value hold (infinities and NaN included).
+ *   q        DEVICE bf16 [n_sessions][n_q_tokens][L][H][d], n_q_tokens in [1, 64]
+ *   n_q      DEVICE int32 [n_sessions] drafted tokens of each session (clamped to [0, n_q_tokens]); NULL: n_q_tokens each.
+ *            out and lse of the tokens behind n_q[s] are left as they were
+ *   mask     DEVICE uint64 [n_sessions][n_q_tokens]: bit j of word i says whether drafted token i sees drafted token j (an
+ *            ancestor in the tree, and itself); bits at n_q[s] and above count as clear.  NULL: a chain (token i sees
+ *            0 .. i), which is also the form for a single token
+ *   tail     HOST struct; NULL: no tail, the drafted tokens see the view alone (mask must be NULL)
+ *   out      DEVICE bf16 [n_sessions][n_q_tokens][L][H][d]: the result is complete, nothing is left to merge, so it
+ *            is rounded once to the type the next layer reads
+ *   lse      DEVICE fp32 [n_sessions][n_q_tokens][L][H]
+ *   scale    0 selects 1/sqrt(head_dim)
+ *   workspace  DEVICE, kvmem_tree_workspace_bytes(), 256-byte aligned; contents undefined afterwards.  Calls that may overlap
+ *            on the GPU (two streams, two captured graphs) need one each
+ * kvmem_view_tree_attend reads a materialised view (any block size the pool accepts); kvmem_paged_tree_attend reads the
+ * selected blocks' pages through the block table in the order of sel_ids (block sizes that divide 64 tokens or are a
+ * multiple of it), as kvmem_paged_attend does, with its rule for ids out of range.  Built for head_dim 128.  HBM traffic:
+ * one read of the view up to 256 query rows (n_q_tokens * H/G) per KV head, one per 256 rows above.
+ * An n_tokens[s] outside [0, cap_tokens - n_q[s]] is clamped to it and reported as KVMEM_E_DEVICE_RANGE.
+ * Errors: KVMEM_E_INVALID (pointers, sizes, n_q_tokens, tail too short), KVMEM_E_UNSUPPORTED, KVMEM_E_CAPACITY (workspace),
+ * KVMEM_E_STATE (an FP8 repository, paged form). */
+size_t kvmem_tree_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens);
+int kvmem_view_tree_attend(kvmem_pool_t* pool, int32_t n_sessions, const void* q /*DEVICE*/, int32_t n_q_tokens,
+                           const int32_t* n_q /*DEVICE, may be NULL*/, const uint64_t* mask /*DEVICE, may be NULL*/,
+                           const void* view_k /*DEVICE*/, const void* view_v /*DEVICE*/, int32_t view_cap_tokens,
+                           const int32_t* n_sel /*DEVICE*/, const kvmem_tail_t* tail /*HOST, may be NULL*/, float scale,
+                           void* out /*DEVICE*/, float* lse /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes,
+                           void* stream);
+int kvmem_paged_tree_attend(kvmem_pool_t* pool, int32_t session_first, int32_t n_sessions, const void* q /*DEVICE*/,
+                            int32_t n_q_tokens, const int32_t* n_q /*DEVICE, may be NULL*/,
+                            const uint64_t* mask /*DEVICE, may be NULL*/, const int32_t* sel_ids /*DEVICE*/, int32_t sel_stride,
+                            const int32_t* n_sel /*DEVICE*/, const kvmem_tail_t* tail /*HOST, may be NULL*/, float scale,
+                            void* out /*DEVICE*/, float* lse /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes,
+                            void* stream);
+
+/* kvmem_view_tree_attend for a chain (mask NULL) that also accumulates the attention weight of every view token:
+ *     mass[s][l][g][t] = decay * mass[s][l][g][t] + sum over tokens i < n_q[s] and the heads h of KV head g of
+ *                        exp(q_i . k_t * scale - lse[s][i][l][h])                     for t < T
+ * (fp32 throughout, a fixed order of addition: the same bits from run to run).  Entries at T and above are left as they
+ * were.  The weights are those of the whole softmax, tail included.
+ *   mass   DEVICE fp32 [n_sessions][L][G][view_cap_tokens]; decay finite and non-negative (1: plain sum)
+ *   workspace  DEVICE, kvmem_mass_workspace_bytes(), 256-byte aligned
+ * n_q_tokens * (H/G) <= 64.  Other arguments and errors as above. */
+size_t kvmem_mass_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens,
+                                  int32_t view_cap_tokens);
+int kvmem_view_attend_mass(kvmem_pool_t* pool, int32_t n_sessions, const void* q /*DEVICE*/, int32_t n_q_tokens,
+                           const int32_t* n_q /*DEVICE, may be NULL*/, const void* view_k /*DEVICE*/,
+                           const void* view_v /*DEVICE*/, int32_t view_cap_tokens, const int32_t* n_sel /*DEVICE*/,
+                           const kvmem_tail_t* tail /*HOST, may be NULL*/, float scale, float* mass /*DEVICE*/, float decay,
+                           void* out /*DEVICE*/, float* lse /*DEVICE*/, void* workspace /*DEVICE*/, size_t workspace_bytes,
+                           void* stream);
+
+/* Evict the tokens of a view that gathered the least attention weight: per session, layer and KV head, with
+ * T = min(n_sel[s] * block_tokens, view_cap_tokens), C = keep_blocks * block_tokens and K = min(C, T), the tokens kept are
+ * the first min(n_sink_tokens, K), the last min(n_recent_tokens, what is left of K), and of the others those with the
+ * largest mass, equal weights to the lower token, until K are kept (every head keeps its own tokens).  They are moved in
+ * ascending order to rows [0, K) of another view, their weights with them; n_sel_out[s] = min(keep_blocks, T /
+ * block_tokens) is that view's length in blocks, so that kvmem_view_attend and the calls above read it as any other.
+ * Rows behind K are left as they were.  Any fp32 weight is ordered by its value (a NaN counts as larger than every number).
+ *   dst_k, dst_v  DEVICE bf16 [n_sessions][L][G][dst_cap_tokens][d], 128-byte aligned, dst_cap_tokens >= C; must not overlap the view
+ *   dst_mass      DEVICE fp32 [n_sessions][L][G][dst_cap_tokens]; must not overlap mass
+ *   kept          DEVICE int32 [n_sessions][L][G][C] receives the kept tokens' places in the old view, or NULL
+ *   n_sel_out     DEVICE int32 [n_sessions]; may be n_sel itself
+ *   workspace     DEVICE, kvmem_evict_workspace_bytes(), 256-byte aligned
+ * Errors: KVMEM_E_INVALID, KVMEM_E_CAPACITY, KVMEM_E_UNSUPPORTED (head_dim other than 128). */
+size_t kvmem_evict_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t keep_blocks);
+int kvmem_view_evict(kvmem_pool_t* pool, int32_t n_sessions, const void* view_k /*DEVICE*/, const void* view_v /*DEVICE*/,
+                     int32_t view_cap_tokens, const int32_t* n_sel /*DEVICE*/, const float* mass /*DEVICE*/,
+                     int32_t keep_blocks, int32_t n_sink_tokens, int32_t n_recent_tokens, void* dst_k /*DEVICE*/,
+                     void* dst_v /*DEVICE*/, int32_t dst_cap_tokens, float* dst_mass /*DEVICE*/,
+                     int32_t* kept /*DEVICE, may be NULL*/, int32_t* n_sel_out /*DEVICE*/, void* workspace /*DEVICE*/,
+                     size_t workspace_bytes, void* stream);
+
 /* ---- inspection ------------------------------------------------------------------------------ */
 
 /* Mean-K index of a session: DEVICE bf16 [n_layers][n_kv_heads][max_blocks_per_session][head_dim]

@@ -5,6 +5,7 @@ from .kvmem import (  # noqa: F401
     Pool,
     PoolConfig,
     SelectParams,
+    Tail,
     View,
     budget_blocks,
     load_library,

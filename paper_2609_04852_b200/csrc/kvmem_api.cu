@@ -1071,6 +1071,189 @@ int kvmem_view_cache_attend(kvmem_pool_t* p, const void* q, int32_t n_q_tokens, 
     return KVMEM_OK;
 }
 
+// ---- decode over a view: drafted tokens, accumulated weights, eviction ----
+
+// [p, p + n) and [q, q + m) share a byte
+static bool overlap(const void* p, size_t n, const void* q, size_t m) {
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    return a < b + m && b < a + n;
+}
+
+static size_t tree_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t n_q_tokens, int32_t mass_cap, const char* who) {
+    const char* why = "";
+    if (!cfg || !config_valid(*cfg, &why) || n_sessions < 1 || n_sessions > 65535 || n_q_tokens < 1 || n_q_tokens > kMaxDrafted || mass_cap < 0) {
+        set_error("invalid arguments to %s", who);
+        return 0;
+    }
+    return tree_workspace_bytes(*cfg, n_sessions, n_q_tokens, mass_cap);
+}
+
+size_t kvmem_tree_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t n_q_tokens) {
+    return tree_bytes(cfg, n_sessions, n_q_tokens, 0, "kvmem_tree_workspace_bytes");
+}
+
+size_t kvmem_mass_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t n_q_tokens, int32_t view_cap_tokens) {
+    if (view_cap_tokens < 1) { set_error("view_cap_tokens must be positive"); return 0; }
+    return tree_bytes(cfg, n_sessions, n_q_tokens, view_cap_tokens, "kvmem_mass_workspace_bytes");
+}
+
+// what the three attention calls check alike; fills the arguments that do not depend on where the keys live
+static int tree_common(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32_t n_q_tokens, const int32_t* n_q,
+                       const uint64_t* mask, const int32_t* n_sel, const kvmem_tail_t* tail, float scale, void* out, float* lse,
+                       const void* workspace, const char* who, TreeArgs* a) {
+    if (n_sessions < 1 || n_sessions > 65535) { set_error("n_sessions must be in [1, 65535]"); return KVMEM_E_INVALID; }
+    if (!q || !n_sel || !out || !lse || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256)) {
+        set_error("%s: null or misaligned pointer", who);
+        return KVMEM_E_INVALID;
+    }
+    if (n_q_tokens < 1 || n_q_tokens > kMaxDrafted) { set_error("n_q_tokens must be in [1, %d]", kMaxDrafted); return KVMEM_E_INVALID; }
+    if (p->cfg.head_dim != 128) { set_error("attention kernel is built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
+    if (!(scale >= 0.0f) || !std::isfinite(scale)) { set_error("scale must be finite and non-negative (0 selects 1/sqrt(d))"); return KVMEM_E_INVALID; }
+    if (tail) {
+        if (!tail->k || !tail->v || !tail->n_tokens || !aligned(tail->k, 16) || !aligned(tail->v, 16)) {
+            set_error("%s: null or misaligned tail pointer", who);
+            return KVMEM_E_INVALID;
+        }
+        if (tail->cap_tokens < n_q_tokens || (int64_t)tail->cap_tokens * n_sessions > INT32_MAX) {
+            set_error("the tail holds %d tokens per session: at least n_q_tokens = %d are needed, and n_sessions * cap_tokens must stay below 2^31",
+                      tail->cap_tokens, n_q_tokens);
+            return KVMEM_E_INVALID;
+        }
+    } else if (mask) {
+        set_error("a mask says which drafted keys a token sees: it needs a tail that holds them");
+        return KVMEM_E_INVALID;
+    }
+    const Geometry& g = p->geo;
+    a->q = (const __nv_bfloat16*)q; a->n_q = n_q; a->mask = (const unsigned long long*)mask; a->n_sel = n_sel;
+    if (tail) { a->tail_k = (const __nv_bfloat16*)tail->k; a->tail_v = (const __nv_bfloat16*)tail->v; a->n_tail = tail->n_tokens; a->tail_cap = tail->cap_tokens; }
+    a->out = (__nv_bfloat16*)out; a->lse = lse; a->status = p->status_dev;
+    a->ns = n_sessions; a->M = n_q_tokens; a->L = g.L; a->H = g.H; a->G = g.G; a->r = g.r; a->rows = n_q_tokens * g.r; a->B = g.B;
+    a->scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)g.d);
+    return KVMEM_OK;
+}
+
+static int tree_view(kvmem_pool_t* p, const void* view_k, const void* view_v, int32_t view_cap_tokens, const char* who, TreeArgs* a) {
+    if (!view_k || !view_v || !aligned(view_k, 128) || !aligned(view_v, 128)) {
+        set_error("%s: null or misaligned pointer (views need 128-byte alignment)", who);
+        return KVMEM_E_INVALID;
+    }
+    if (view_cap_tokens < p->cfg.block_tokens || view_cap_tokens % p->cfg.block_tokens != 0) {
+        set_error("view_cap_tokens must be a positive multiple of block_tokens");
+        return KVMEM_E_INVALID;
+    }
+    a->view_k = (const __nv_bfloat16*)view_k; a->view_v = (const __nv_bfloat16*)view_v; a->cap = view_cap_tokens;
+    return KVMEM_OK;
+}
+
+int kvmem_view_tree_attend(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32_t n_q_tokens, const int32_t* n_q,
+                           const uint64_t* mask, const void* view_k, const void* view_v, int32_t view_cap_tokens,
+                           const int32_t* n_sel, const kvmem_tail_t* tail, float scale, void* out, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    TreeArgs a{};
+    int rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, mask, n_sel, tail, scale, out, lse, workspace, "kvmem_view_tree_attend", &a);
+    if (rc == KVMEM_OK) rc = tree_view(p, view_k, view_v, view_cap_tokens, "kvmem_view_tree_attend", &a);
+    if (rc != KVMEM_OK) return rc;
+    const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, 0);
+    if (workspace_bytes < need) { set_error("tree workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
+    cudaError_t e = launch_tree(*p, a, workspace, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("tree attention kernel launch", e);
+    return KVMEM_OK;
+}
+
+int kvmem_paged_tree_attend(kvmem_pool_t* p, int32_t session_first, int32_t n_sessions, const void* q, int32_t n_q_tokens,
+                            const int32_t* n_q, const uint64_t* mask, const int32_t* sel_ids, int32_t sel_stride,
+                            const int32_t* n_sel, const kvmem_tail_t* tail, float scale, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    if (!sessions_ok(p, session_first, n_sessions)) return KVMEM_E_INVALID;
+    if (!pages_are(p, false, "kvmem_paged_tree_attend")) return KVMEM_E_STATE;
+    TreeArgs a{};
+    const int rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, mask, n_sel, tail, scale, out, lse, workspace, "kvmem_paged_tree_attend", &a);
+    if (rc != KVMEM_OK) return rc;
+    if (!paged_block_size_ok(p, false, "kvmem_paged_tree_attend")) return KVMEM_E_UNSUPPORTED;
+    if (!sel_ids || sel_stride < 1 || (int64_t)sel_stride * p->cfg.block_tokens > INT32_MAX - 256) {
+        set_error("kvmem_paged_tree_attend: sel_ids is null, or sel_stride is not positive or too long");
+        return KVMEM_E_INVALID;
+    }
+    const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, 0);
+    if (workspace_bytes < need) { set_error("tree workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
+    a.sel_ids = sel_ids; a.sel_stride = sel_stride; a.cap = sel_stride * p->cfg.block_tokens;
+    a.pages = p->pages; a.tables = p->tables; a.nblocks_dev = p->nblocks_dev; a.session_first = session_first;
+    a.max_bps = p->geo.max_bps; a.max_blocks = p->geo.max_blocks;
+    cudaError_t e = launch_tree(*p, a, workspace, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("paged tree attention kernel launch", e);
+    return KVMEM_OK;
+}
+
+int kvmem_view_attend_mass(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32_t n_q_tokens, const int32_t* n_q,
+                           const void* view_k, const void* view_v, int32_t view_cap_tokens, const int32_t* n_sel,
+                           const kvmem_tail_t* tail, float scale, float* mass, float decay, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    TreeArgs a{};
+    int rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, nullptr, n_sel, tail, scale, out, lse, workspace, "kvmem_view_attend_mass", &a);
+    if (rc == KVMEM_OK) rc = tree_view(p, view_k, view_v, view_cap_tokens, "kvmem_view_attend_mass", &a);
+    if (rc != KVMEM_OK) return rc;
+    if (!mass || !aligned(mass, 16)) { set_error("kvmem_view_attend_mass: mass must be a 16-byte aligned device pointer"); return KVMEM_E_INVALID; }
+    if (!(decay >= 0.0f) || !std::isfinite(decay)) { set_error("decay must be finite and non-negative"); return KVMEM_E_INVALID; }
+    if (a.rows > 64) { set_error("n_q_tokens * (H/G) = %d exceeds 64 rows per call", a.rows); return KVMEM_E_UNSUPPORTED; }
+    const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, view_cap_tokens);
+    if (workspace_bytes < need) { set_error("weight workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
+    a.mass = mass; a.decay = decay;
+    cudaError_t e = launch_tree(*p, a, workspace, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("attention with weights kernel launch", e);
+    return KVMEM_OK;
+}
+
+size_t kvmem_evict_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t keep_blocks) {
+    const char* why = "";
+    if (!cfg || !config_valid(*cfg, &why) || n_sessions < 1 || n_sessions > 65535 || keep_blocks < 1) {
+        set_error("invalid arguments to kvmem_evict_workspace_bytes");
+        return 0;
+    }
+    return evict_workspace_bytes(*cfg, n_sessions, keep_blocks);
+}
+
+int kvmem_view_evict(kvmem_pool_t* p, int32_t n_sessions, const void* view_k, const void* view_v, int32_t view_cap_tokens,
+                     const int32_t* n_sel, const float* mass, int32_t keep_blocks, int32_t n_sink_tokens, int32_t n_recent_tokens,
+                     void* dst_k, void* dst_v, int32_t dst_cap_tokens, float* dst_mass, int32_t* kept, int32_t* n_sel_out,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    if (n_sessions < 1 || n_sessions > 65535) { set_error("n_sessions must be in [1, 65535]"); return KVMEM_E_INVALID; }
+    if (!view_k || !view_v || !n_sel || !mass || !dst_k || !dst_v || !dst_mass || !n_sel_out || !workspace || !aligned(view_k, 128) ||
+        !aligned(view_v, 128) || !aligned(dst_k, 128) || !aligned(dst_v, 128) || !aligned(mass, 16) || !aligned(dst_mass, 16) ||
+        !aligned(workspace, 256)) {
+        set_error("kvmem_view_evict: null or misaligned pointer (views need 128-byte alignment)");
+        return KVMEM_E_INVALID;
+    }
+    if (p->cfg.head_dim != 128) { set_error("the eviction kernels are built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
+    const int B = p->cfg.block_tokens;
+    if (view_cap_tokens < B || view_cap_tokens % B != 0 || keep_blocks < 1 || (int64_t)keep_blocks * B > dst_cap_tokens) {
+        set_error("view_cap_tokens must be a positive multiple of block_tokens and the destination hold keep_blocks >= 1 blocks");
+        return KVMEM_E_INVALID;
+    }
+    if (n_sink_tokens < 0 || n_recent_tokens < 0) { set_error("n_sink_tokens and n_recent_tokens must not be negative"); return KVMEM_E_INVALID; }
+    const size_t heads = (size_t)n_sessions * p->geo.L * p->geo.G;
+    const size_t src_b = heads * view_cap_tokens * 256, dst_b = heads * dst_cap_tokens * 256;
+    if (overlap(view_k, src_b, dst_k, dst_b) || overlap(view_k, src_b, dst_v, dst_b) || overlap(view_v, src_b, dst_k, dst_b) ||
+        overlap(view_v, src_b, dst_v, dst_b) || overlap(dst_k, dst_b, dst_v, dst_b) ||
+        overlap(mass, heads * view_cap_tokens * 4, dst_mass, heads * dst_cap_tokens * 4)) {
+        set_error("kvmem_view_evict moves tokens out of place: source and destination overlap");
+        return KVMEM_E_INVALID;
+    }
+    const size_t need = evict_workspace_bytes(p->cfg, n_sessions, keep_blocks);
+    if (workspace_bytes < need) { set_error("evict workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
+    EvictArgs a{};
+    a.view_k = (const __nv_bfloat16*)view_k; a.view_v = (const __nv_bfloat16*)view_v; a.n_sel = n_sel; a.mass = mass;
+    a.dst_k = (__nv_bfloat16*)dst_k; a.dst_v = (__nv_bfloat16*)dst_v; a.dst_mass = dst_mass; a.kept = kept; a.n_sel_out = n_sel_out;
+    a.ns = n_sessions; a.LG = p->geo.L * p->geo.G; a.B = B; a.cap = view_cap_tokens; a.dst_cap = dst_cap_tokens; a.keep = keep_blocks;
+    a.n_sink = n_sink_tokens; a.n_recent = n_recent_tokens;
+    cudaError_t e = launch_evict(*p, a, workspace, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("eviction kernel launch", e);
+    return KVMEM_OK;
+}
+
 int kvmem_get_index(kvmem_pool_t* p, int32_t session, const void** index, int32_t* n_blocks) {
     if (!pool_ok(p)) return KVMEM_E_STATE;
     if (!sessions_ok(p, session, 1)) return KVMEM_E_INVALID;

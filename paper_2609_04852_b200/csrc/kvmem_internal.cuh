@@ -242,4 +242,41 @@ cudaError_t launch_attend(const kvmem_pool& p, int n_sessions, const __nv_bfloat
                           cudaStream_t st, const int32_t* sel_ids = nullptr, int sel_stride = 0, int session_first = 0,
                           const PagedSource* alt = nullptr, int rope_first_position = -1);
 
+// ---- decode over a view: drafted tokens, accumulated weights, eviction ----
+constexpr int kMaxDrafted = 64;      // drafted tokens per session: one bit each in a mask word
+struct TreeArgs {
+    const __nv_bfloat16* q;          // [ns][M][L][H][d]
+    const int32_t* n_q;              // [ns] or null
+    const unsigned long long* mask;  // [ns][M] or null (a chain)
+    const __nv_bfloat16 *view_k, *view_v;   // [ns][LG][cap][d], or null: the pages
+    const int32_t* n_sel;            // [ns]
+    const int32_t *sel_ids, *tables, *nblocks_dev;
+    const __nv_bfloat16* pages;
+    const __nv_bfloat16 *tail_k, *tail_v;   // [ns][tail_cap][LG][d], or null
+    const int32_t* n_tail;
+    __nv_bfloat16* out;              // [ns][M][L][H][d]
+    float* lse;                      // [ns][M][L][H]
+    float* mass;                     // [ns][LG][cap] or null
+    int32_t* status;
+    int ns, M, L, H, G, r, rows, B;
+    int cap, tail_cap;               // capacity in tokens of a session's view (paged: of its selection) and tail
+    int session_first, sel_stride, max_bps, max_blocks;
+    float scale, decay;
+};
+size_t tree_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int mass_cap_tokens);
+cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace, cudaStream_t st);
+
+struct EvictArgs {
+    const __nv_bfloat16 *view_k, *view_v;   // [ns][LG][cap][d]
+    const int32_t* n_sel;
+    const float* mass;               // [ns][LG][cap]
+    __nv_bfloat16 *dst_k, *dst_v;    // [ns][LG][dst_cap][d]
+    float* dst_mass;                 // [ns][LG][dst_cap]
+    int32_t* kept;                   // [ns][LG][C], C = keep * B
+    int32_t* n_sel_out;
+    int ns, LG, B, cap, dst_cap, keep, n_sink, n_recent;
+};
+size_t evict_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int keep_blocks);
+cudaError_t launch_evict(const kvmem_pool& p, const EvictArgs& a, void* workspace, cudaStream_t st);
+
 }  // namespace kvmem

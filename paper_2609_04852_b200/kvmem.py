@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import Optional, Sequence, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
@@ -34,6 +34,10 @@ class PoolConfig(C.Structure):
                                                                    ("fp8_k_scale", C.c_float), ("fp8_v_scale", C.c_float)]
 
 
+class TailStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("cap_tokens", C.c_int32), ("n_tokens", C.c_void_p)]
+
+
 class SelectParams(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("budget_blocks", "max_view_tokens", "mandatory_tokens",
                                           "n_sink_blocks", "n_recent_blocks")]
@@ -55,7 +59,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         raise FileNotFoundError(f"{path} is missing: build it with paper_2609_04852_b200._build.build()")
     L = C.CDLL(path)
     vp, i32, sz, f32 = C.c_void_p, C.c_int32, C.c_size_t, C.c_float
-    cfgp, prmp = C.POINTER(PoolConfig), C.POINTER(SelectParams)
+    cfgp, prmp, tailp = C.POINTER(PoolConfig), C.POINTER(SelectParams), C.POINTER(TailStruct)
     sig = {
         "kvmem_pool_bytes": (sz, [cfgp]),
         "kvmem_budget_blocks": (i32, [prmp, i32, i32]),
@@ -101,6 +105,13 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "kvmem_view_attend_fp8": (C.c_int, [vp, i32, vp, i32, vp, vp, i32, vp, f32, f32, f32, vp, vp, vp, sz, vp]),
         "kvmem_view_attend_static": (C.c_int, [vp, i32, vp, i32, vp, vp, i32, vp, f32, vp, vp, vp]),
         "kvmem_selftest_wait_timeout": (C.c_int, [vp, C.c_uint32, vp, vp]),
+        "kvmem_tree_workspace_bytes": (sz, [cfgp, i32, i32]),
+        "kvmem_mass_workspace_bytes": (sz, [cfgp, i32, i32, i32]),
+        "kvmem_evict_workspace_bytes": (sz, [cfgp, i32, i32]),
+        "kvmem_view_tree_attend": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, tailp, f32, vp, vp, vp, sz, vp]),
+        "kvmem_paged_tree_attend": (C.c_int, [vp, i32, i32, vp, i32, vp, vp, vp, i32, vp, tailp, f32, vp, vp, vp, sz, vp]),
+        "kvmem_view_attend_mass": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i32, vp, tailp, f32, vp, f32, vp, vp, vp, sz, vp]),
+        "kvmem_view_evict": (C.c_int, [vp, i32, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]),
         "kvmem_step_staging_bytes": (sz, [cfgp, i32, i32]),
         "kvmem_recall_step_host": (C.c_int, [vp, i32, i32, vp, i32, prmp, vp, i32, vp, vp, vp, i32, f32, vp, vp,
                                              vp, sz, vp, sz, vp, sz, vp]),
@@ -125,7 +136,8 @@ EXPORTED = ("kvmem_pool_bytes", "kvmem_budget_blocks", "kvmem_select_workspace_b
             "kvmem_score_host_staging_bytes", "kvmem_score_host_index", "kvmem_materialize_fp8", "kvmem_view_attend_fp8",
             "kvmem_materialize_attend_rope", "kvmem_paged_attend_fp8", "kvmem_materialize_attend_fp8",
             "kvmem_paged_attend_fp8_rope", "kvmem_selftest_wait_timeout", "kvmem_materialize_delta",
-            "kvmem_materialize_fp8_rope")
+            "kvmem_materialize_fp8_rope", "kvmem_tree_workspace_bytes", "kvmem_view_tree_attend", "kvmem_paged_tree_attend",
+            "kvmem_mass_workspace_bytes", "kvmem_view_attend_mass", "kvmem_evict_workspace_bytes", "kvmem_view_evict")
 
 
 def _check(status: int) -> None:
@@ -180,6 +192,15 @@ def set_option(name: str, value: int) -> None:
 
 
 @dataclass
+class Tail:
+    """Tokens behind a view that fill no block yet: k, v bf16 [n_sessions][cap_tokens][L][G][d]; n_tokens int32
+    [n_sessions] committed ones on the device, with the drafted tokens in the rows behind them."""
+    k: torch.Tensor
+    v: torch.Tensor
+    n_tokens: torch.Tensor
+
+
+@dataclass
 class View:
     """Execution view buffers: bf16 [n_sessions][L][G][cap_tokens][d] each."""
     k: torch.Tensor
@@ -210,6 +231,8 @@ class Pool:
         self._host_ws: Optional[torch.Tensor] = None
         self._host_staging: Optional[torch.Tensor] = None
         self._staging: Optional[torch.Tensor] = None
+        self._decode_ws: Optional[torch.Tensor] = None
+        self._decode_ws_all: List[torch.Tensor] = []
 
     # ---- lifetime
     def close(self) -> None:
@@ -393,6 +416,106 @@ class Pool:
                                           _dev(view.v, torch.bfloat16), view.cap_tokens, _dev(n_sel, torch.int32),
                                           scale, _dev(out, torch.float32), _dev(lse, torch.float32),
                                           ws.data_ptr(), ws.numel(), _stream()))
+
+    # ---- decode over a view: drafted tokens, accumulated weights, eviction
+    def _place(self, name: str, t: torch.Tensor, dtype, shape) -> int:
+        """Pointer of a contiguous tensor of this dtype and shape on the pool's device; ValueError for any other."""
+        if not t.is_cuda or t.device != self.device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {self.device}, got "
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (strided)'}")
+        return t.data_ptr()
+
+    def _decode_workspace(self, need: int, workspace: Optional[torch.Tensor]) -> Tuple[int, int]:
+        if need == 0:
+            raise KvmemError(E_INVALID, self.lib.kvmem_last_error().decode())
+        if workspace is not None:
+            return self._place("workspace", workspace, torch.uint8, (workspace.numel(),)), workspace.numel()
+        if self._decode_ws is None or self._decode_ws.numel() < need:
+            # a captured graph may still replay on a smaller one, so those are kept; each is at least twice the one before
+            size = need if self._decode_ws is None else max(need, 2 * self._decode_ws.numel())
+            self._decode_ws_all.append(torch.empty(size, dtype=torch.uint8, device=self.device))
+            self._decode_ws = self._decode_ws_all[-1]
+        return self._decode_ws.data_ptr(), self._decode_ws.numel()
+
+    def _decode_common(self, q, n_sel, tail, out, lse, n_q):
+        c = self.cfg
+        if q.dim() != 5:
+            raise ValueError("q: expected [n_sessions][n_q_tokens][L][H][d]")
+        ns, M = q.shape[:2]
+        shape = (ns, M, c.n_layers, c.n_q_heads, c.head_dim)
+        qp = self._place("q", q, torch.bfloat16, shape)
+        np_ = self._place("n_sel", n_sel, torch.int32, (ns,))
+        op, lp = self._place("out", out, torch.bfloat16, shape), self._place("lse", lse, torch.float32, shape[:4])
+        nq = None if n_q is None else self._place("n_q", n_q, torch.int32, (ns,))
+        tp = None
+        if tail is not None:
+            cap = tail.k.shape[1] if tail.k.dim() == 5 else -1
+            ts = (ns, cap, c.n_layers, c.n_kv_heads, c.head_dim)
+            tp = C.byref(TailStruct(self._place("tail.k", tail.k, torch.bfloat16, ts), self._place("tail.v", tail.v, torch.bfloat16, ts),
+                                    cap, self._place("tail.n_tokens", tail.n_tokens, torch.int32, (ns,))))
+        return ns, M, qp, np_, tp, op, lp, nq
+
+    def _view_of(self, name: str, view: View, ns: int) -> Tuple[int, int, int]:
+        c = self.cfg
+        shape = (ns, c.n_layers, c.n_kv_heads, view.cap_tokens, c.head_dim)
+        return self._place(name + ".k", view.k, torch.bfloat16, shape), self._place(name + ".v", view.v, torch.bfloat16, shape), view.cap_tokens
+
+    def view_tree_attend(self, q: torch.Tensor, view: View, n_sel: torch.Tensor, tail: Optional[Tail], out: torch.Tensor,
+                         lse: torch.Tensor, mask: Optional[torch.Tensor] = None, n_q: Optional[torch.Tensor] = None,
+                         scale: float = 0.0, workspace: Optional[torch.Tensor] = None) -> None:
+        """Attention of up to 64 drafted tokens per session over view and tail: q bf16 [n_sessions][M][L][H][d], mask
+        int64 [n_sessions][M] (bit j of word i: token i sees drafted token j; None: a chain), n_q int32 [n_sessions]
+        drafted tokens in use, out bf16 like q, lse fp32 [n_sessions][M][L][H].  Calls that may overlap on the GPU (other
+        streams, other captured graphs) need a workspace each (kvmem_tree_workspace_bytes); None: the pool's own."""
+        ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
+        vk, vv, cap = self._view_of("view", view, ns)
+        mp = None if mask is None else self._place("mask", mask, torch.int64, (ns, M))
+        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes(C.byref(self.cfg), ns, M), workspace)
+        _check(self.lib.kvmem_view_tree_attend(self.handle, ns, qp, M, nq, mp, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, _stream()))
+
+    def paged_tree_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, tail: Optional[Tail],
+                          out: torch.Tensor, lse: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                          n_q: Optional[torch.Tensor] = None, scale: float = 0.0, session_first: int = 0,
+                          workspace: Optional[torch.Tensor] = None) -> None:
+        """view_tree_attend straight over the selected blocks' pages: sel_ids int32 [n_sessions][stride]."""
+        ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
+        sp = self._place("sel_ids", sel_ids, torch.int32, (ns, sel_ids.shape[-1]))
+        mp = None if mask is None else self._place("mask", mask, torch.int64, (ns, M))
+        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes(C.byref(self.cfg), ns, M), workspace)
+        _check(self.lib.kvmem_paged_tree_attend(self.handle, session_first, ns, qp, M, nq, mp, sp, sel_ids.shape[-1], np_, tp,
+                                                scale, op, lp, wp, wn, _stream()))
+
+    def view_attend_mass(self, q: torch.Tensor, view: View, n_sel: torch.Tensor, mass: torch.Tensor, out: torch.Tensor,
+                         lse: torch.Tensor, tail: Optional[Tail] = None, n_q: Optional[torch.Tensor] = None, decay: float = 1.0,
+                         scale: float = 0.0, workspace: Optional[torch.Tensor] = None) -> None:
+        """view_tree_attend for a chain that also sets mass fp32 [n_sessions][L][G][cap_tokens] to decay * mass + the
+        attention weight of each view token, summed over the query rows of its KV head (n_q_tokens * H/G <= 64)."""
+        c = self.cfg
+        ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
+        vk, vv, cap = self._view_of("view", view, ns)
+        ap = self._place("mass", mass, torch.float32, (ns, c.n_layers, c.n_kv_heads, cap))
+        wp, wn = self._decode_workspace(self.lib.kvmem_mass_workspace_bytes(C.byref(self.cfg), ns, M, cap), workspace)
+        _check(self.lib.kvmem_view_attend_mass(self.handle, ns, qp, M, nq, vk, vv, cap, np_, tp, scale, ap, decay, op, lp, wp, wn,
+                                               _stream()))
+
+    def view_evict(self, view: View, n_sel: torch.Tensor, mass: torch.Tensor, dst: View, n_sel_out: torch.Tensor,
+                   dst_mass: torch.Tensor, kept: Optional[torch.Tensor] = None, keep_blocks: Optional[int] = None,
+                   n_sink_tokens: int = 0, n_recent_tokens: int = 0, workspace: Optional[torch.Tensor] = None) -> None:
+        """Keep the keep_blocks (default: dst's capacity) * block_tokens tokens of each KV head with the largest mass,
+        the first n_sink_tokens and last n_recent_tokens among them, and move them in order to dst; n_sel_out int32
+        [n_sessions] receives dst's lengths in blocks, kept int32 [n_sessions][L][G][keep_blocks * B] the tokens' places."""
+        c = self.cfg
+        ns = n_sel.shape[0]
+        keep = dst.cap_tokens // c.block_tokens if keep_blocks is None else keep_blocks
+        vk, vv, cap = self._view_of("view", view, ns)
+        dk, dv, dcap = self._view_of("dst", dst, ns)
+        heads = (ns, c.n_layers, c.n_kv_heads)
+        ap, dp = self._place("mass", mass, torch.float32, (*heads, cap)), self._place("dst_mass", dst_mass, torch.float32, (*heads, dcap))
+        kp = None if kept is None else self._place("kept", kept, torch.int32, (*heads, keep * c.block_tokens))
+        np_, no = self._place("n_sel", n_sel, torch.int32, (ns,)), self._place("n_sel_out", n_sel_out, torch.int32, (ns,))
+        wp, wn = self._decode_workspace(self.lib.kvmem_evict_workspace_bytes(C.byref(self.cfg), ns, keep), workspace)
+        _check(self.lib.kvmem_view_evict(self.handle, ns, vk, vv, cap, np_, ap, keep, n_sink_tokens, n_recent_tokens, dk, dv, dcap,
+                                         dp, kp, no, wp, wn, _stream()))
 
     def materialize_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, view: View,
                            out: torch.Tensor, lse: torch.Tensor, scale: float = 0.0, session_first: int = 0) -> None:

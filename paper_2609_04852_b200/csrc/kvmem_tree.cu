@@ -1,21 +1,67 @@
 // Attention of drafted tokens over a view (or the selected pages) and the tail of tokens behind it, and the weights it
-// leaves on the view:   out_i = sum_t p_it v_t,  p_it = exp(x_it - lse_i),  x_it = scale q_i . k_t,
+// leaves on the view:   out_i = sum_t p_it v_t,  p_it = exp(x_it - lse_i),  x_it = scale q_i . k_t over the t that i sees,
 //                       mass_t = decay mass_t + sum_i p_it.
-// A warp per query row walks the tokens 32 at a time: a lane takes one token's logit, the maximum and the sum run along
-// (online softmax, fp32), then the lanes share out the 128 dimensions of the values.  The weights are a second pass once
-// the log-sum-exp is known, a thread per token.
+//
+// The query rows of a KV head (drafted tokens x query heads that share it) are the rows of one or two 128-row tiles, the
+// tokens come in tiles of 128: view tiles first, then tail tiles (committed and drafted tokens).  Per tile
+//     S = Q K^T   tcgen05.mma, both operands in shared memory, 128 x 128 fp32 accumulators in tensor memory
+//     P = exp2(S scale log2e - ref)   a thread per row: one TMEM lane, so maximum and sum need no shuffles
+//     O += P V    tcgen05.mma, P as bf16 in tensor memory (in the place of S), V from shared memory
+// Two slots (S, P and O each: 2 x 256 columns, all of tensor memory) keep the tensor pipe and the special-function unit
+// busy in turn: with up to 128 rows the slots take tiles alternately and are merged at the end like two splits; with more
+// rows slot w is row tile w and both read the same K and V tile.  One warp fetches tiles with TMA (128-byte swizzle) into a
+// ring of 32 KiB slots, one issues the MMAs, eight hold the rows.
+//
+// ref is a running maximum that moves only when a row's logits pass it by 8 (in powers of two): O is then rescaled in
+// tensor memory.  Until then the weights may reach 2^8, which costs neither fp32 nor bf16 any precision.
+//
+// Work: the tiles of all (session, KV head, row group) lie on one line, cut into as many equal parts as there are CTAs
+// (one per SM), so that sessions of any lengths keep all SMs busy to the end.  A CTA's share of one head is a segment;
+// each leaves unnormalised sums, row references and row sums, and tree_merge_kernel joins a head's segments in order: the
+// result depends on the sizes alone, not on timing.  Lengths are read on the device.
+//
+// Tokens that nobody may see: their logits are replaced before they are used, and their values are cleared in shared
+// memory before the second product (0 x NaN).  A drafted token's value that is not finite would reach the tokens that do
+// not see it in the same way: such elements are cleared too, and the merge adds them to the rows that see them.
+#include <cudaTypedefs.h>
 #include <math.h>
 
 #include <algorithm>
 
 #include "kvmem_internal.cuh"
+#include "kvmem_ptx.cuh"
+#include "kvmem_t5.cuh"
 
 namespace kvmem {
 
 constexpr int kTreeD = 128;
+constexpr int kTreeTile = 128;                    // tokens per tile
+constexpr int kTreeHalf = kTreeTile * 128;        // bytes of one 64-dim half of a 128-row operand tile (16 KiB)
+constexpr int kTreeSlot = 2 * kTreeHalf;          // a K, V or Q tile
+constexpr int kTreeRows = 128;                    // rows of a row tile: TMEM lanes
+constexpr int kTreeThreads = 64 + 256;            // TMA warp, MMA warp, two groups of four row warps
+constexpr int kTreeRing1 = 6, kTreeRing2 = 5;     // ring slots beside one or two Q tiles: 224 KiB in all
+constexpr float kTreeSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
+constexpr size_t kTreeSmem = (size_t)(1 + kTreeRing1) * kTreeSlot + 1024;
+static_assert(1 + kTreeRing1 == 2 + kTreeRing2, "both forms take the same shared memory");
+constexpr uint32_t kTreeIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
+constexpr uint32_t kTreeIdescO = kTreeIdescS | (1u << 16);                                        // B with dims contiguous (V as it lies)
+constexpr uint32_t kTreeVStep = (uint32_t)kTreeHalf >> 4;      // leading offset of V's descriptor: from dims 0..63 to 64..127
 
 struct TreeSpan {
     int n_view, n_tail, n_q;      // view tokens, committed tail tokens, drafted tokens of the session
+    int view_tiles, tiles;        // tiles of the view, tiles of view and tail
+};
+
+struct TreeWork {
+    TreeArgs a;
+    int row_tiles, row_groups, rows_slot;   // row tiles per CTA (1, 2), groups of them per head, rows stored per slot
+    float* part_o;                // [segment][slot][rows_slot][128]
+    float2* part_ml;              // [segment][slot][rows_slot]: (reference, sum of weights), log2 domain
+    unsigned long long* part_nf;  // [segment]: a byte per row warp, set where it cleared a drafted value that is not finite
+    long long* start;             // [ns + 1]: tiles of the sessions before, in head units; filled by CTA 0
+    float* lse2;                  // [ns][LG][rows]: log-sum-exp in the log2 domain (weights only)
+    float* logits;                // [ns][LG][rows][cap]: scaled logits, log2 domain (weights only)
 };
 
 __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& a, int s, bool report) {
@@ -28,98 +74,594 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& a, int s, bool rep
         t.n_tail = min(max(n, 0), a.tail_cap - t.n_q);
         if (report && t.n_tail != n) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
     }
+    t.view_tiles = (t.n_view + kTreeTile - 1) / kTreeTile;
+    t.tiles = t.n_q > 0 ? t.view_tiles + (a.tail_k ? (t.n_tail + t.n_q + kTreeTile - 1) / kTreeTile : 0) : 0;
     return t;
 }
 
-// row of 128 elements of token t (view tokens first, then the tail) of KV head lg
-__device__ __forceinline__ size_t view_row(const TreeArgs& a, int s, int lg, int t) {
-    return (((size_t)s * a.L * a.G + lg) * a.cap + t) * kTreeD;
-}
-__device__ __forceinline__ size_t tail_row(const TreeArgs& a, int s, int lg, int t) {
-    return (((size_t)s * a.tail_cap + t) * a.L * a.G + lg) * kTreeD;
-}
-__device__ __forceinline__ size_t page_row(const TreeArgs& a, int s, int lg, int t, bool value) {
-    const int id = a.sel_ids[(size_t)s * a.sel_stride + t / a.B];
-    int pg = -1;
-    if (id >= 0 && id < a.nblocks_dev[a.session_first + s]) pg = a.tables[(size_t)(a.session_first + s) * a.max_bps + id];
-    if (pg < 0 || pg >= a.max_blocks) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); pg = 0; }
-    return ((((size_t)pg * 2 + (value ? 1 : 0)) * a.L * a.G + lg) * a.B + t % a.B) * kTreeD;
+// drafted tokens that drafted token m sees, those in use only
+__device__ __forceinline__ unsigned long long tree_bits(const TreeArgs& a, int s, int m, int n_q) {
+    const unsigned long long all = n_q >= 64 ? ~0ull : (1ull << n_q) - 1;
+    return all & (a.mask ? a.mask[(size_t)s * a.M + m] : (m >= 63 ? ~0ull : (2ull << m) - 1));
 }
 
-__global__ void __launch_bounds__(128) tree_rows_kernel(TreeArgs a) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int row = blockIdx.x * 4 + warp, lg = blockIdx.y, s = blockIdx.z;
-    const TreeSpan sp = tree_span(a, s, threadIdx.x == 0);
-    __shared__ float qs[4][kTreeD];
-    const int m = row / a.r;
-    if (row >= a.rows || m >= sp.n_q) return;
-    const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
-    for (int d = lane; d < kTreeD; d += 32) qs[warp][d] = __bfloat162float(a.q[orow * kTreeD + d]);
-    __syncwarp();
-    const unsigned long long bits = a.mask ? a.mask[(size_t)s * a.M + m] : (m >= 63 ? ~0ull : (2ull << m) - 1);
-    const int end = sp.n_view + (a.tail_k ? sp.n_tail + sp.n_q : 0);
-    float top = -INFINITY, z = 0.0f, o[4] = {};
-    for (int t0 = 0; t0 < end; t0 += 32) {
-        const int t = t0 + lane, j = t - sp.n_view - sp.n_tail;
-        const bool sees = t < end && (j < 0 || ((bits >> j) & 1));
-        const __nv_bfloat16 *kr = nullptr, *vr = nullptr;
-        if (sees) {
-            if (t >= sp.n_view) { const size_t at = tail_row(a, s, lg, t - sp.n_view); kr = a.tail_k + at; vr = a.tail_v + at; }
-            else if (a.view_k) { const size_t at = view_row(a, s, lg, t); kr = a.view_k + at; vr = a.view_v + at; }
-            else { kr = a.pages + page_row(a, s, lg, t, false); vr = a.pages + page_row(a, s, lg, t, true); }
+// columns [c0, c0 + 32) of a tail tile that a row sees: committed tokens, then its drafted ones
+__device__ __forceinline__ uint32_t tail_word(int c0, int n_tail, unsigned long long bits) {
+    const int d = n_tail - c0;                       // column of drafted token 0
+    const uint32_t committed = d >= 32 ? 0xffffffffu : d <= 0 ? 0u : (1u << d) - 1u;
+    const uint32_t drafted = d >= 32 || d <= -64 ? 0u : d >= 0 ? (uint32_t)(bits << d) : (uint32_t)(bits >> -d);
+    return committed | drafted;
+}
+
+// CTA that holds tile x of the line: tiles [total c / n, total (c + 1) / n) are CTA c's
+__device__ __forceinline__ int tile_owner(long long x, long long total, int n) { return (int)(((x + 1) * n - 1) / total); }
+
+// a role's walk over the CTA's segments
+struct TreeWalk {
+    long long pos, end, base;     // next tile on the line, the CTA's end, first tile of session s
+    int s, lg, rg, head, t0, t1;  // the segment: tiles [t0, t1) of head `head`
+    TreeSpan sp;
+    __device__ __forceinline__ bool next(const TreeArgs& a, int groups) {
+        if (pos >= end) return false;
+        const int heads = a.L * a.G * groups;
+        sp = tree_span(a, s, false);
+        while (base + (long long)sp.tiles * heads <= pos) {
+            base += (long long)sp.tiles * heads;
+            sp = tree_span(a, ++s, false);
         }
-        float x = -INFINITY;
-        if (sees) {
-            x = 0.0f;
-            for (int d = 0; d < kTreeD; ++d) x += qs[warp][d] * __bfloat162float(kr[d]);
-            x *= a.scale;
-        }
-        float mx = x;
-        for (int w = 16; w; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-        const float nt = fmaxf(top, mx), ref = nt > -INFINITY ? nt : 0.0f;
-        const float corr = expf(top - ref), p = expf(x - ref);
-        float sum = p;
-        for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-        z = z * corr + sum;
-        top = nt;
-        for (int i = 0; i < 4; ++i) o[i] *= corr;
-        for (int u = 0; u < 32; ++u) {
-            const float pu = __shfl_sync(0xffffffffu, p, u);
-            const __nv_bfloat16* vu = (const __nv_bfloat16*)__shfl_sync(0xffffffffu, (unsigned long long)vr, u);
-            if (!vu) continue;                    // not visible: its value is not touched
-            for (int i = 0; i < 4; ++i) o[i] += pu * __bfloat162float(vu[lane + 32 * i]);
-        }
+        const int at = (int)((pos - base) / sp.tiles);
+        lg = at / groups;
+        rg = at % groups;
+        head = s * heads + at;
+        t0 = (int)(pos - base - (long long)at * sp.tiles);
+        t1 = (int)min((long long)sp.tiles, t0 + (end - pos));
+        pos += t1 - t0;
+        return true;
     }
-    for (int i = 0; i < 4; ++i) a.out[orow * kTreeD + lane + 32 * i] = __float2bfloat16(z == 0.0f ? 0.0f : o[i] / z);
-    if (lane == 0) a.lse[orow] = z == 0.0f ? -INFINITY : top + logf(z);
+};
+
+template <int QT, bool PAGED, bool MASS>
+__global__ void __launch_bounds__(kTreeThreads, 1)
+tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                  const __grid_constant__ CUtensorMap map_tk, const __grid_constant__ CUtensorMap map_tv,
+                  const __grid_constant__ TreeWork w) {
+    constexpr int RING = QT == 1 ? kTreeRing1 : kTreeRing2;
+    extern __shared__ unsigned char smem_dyn[];
+    __shared__ uint64_t full[RING], empty[RING], q_full, s_full[2], p_full[2], pv_done[2], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ long long plan_begin, plan_end, plan_base;
+    __shared__ int plan_s;
+    const TreeArgs& a = w.a;
+    unsigned char* smem_q = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+    unsigned char* ring = smem_q + (size_t)QT * kTreeSlot;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int LG = a.L * a.G;
+
+    if (tid == 0) {
+        for (int i = 0; i < RING; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&pv_done[i], 1); }
+        ptx::mbar_init(&q_full, 8);
+        ptx::mbar_init(&drained, 1);
+        ptx::fence_mbar_init();
+    }
+    if (warp == 1) {
+        t5::tmem_alloc(&tmem_slot, 512);
+        t5::tmem_relinquish();
+    }
+    pdl_wait();        // everything earlier in the stream is complete and visible from here on
+    pdl_trigger();
+    if (warp == 0) {
+        // the CTA's part of the line, and the session it starts in
+        long long sum = 0;
+        for (int s = lane; s < a.ns; s += 32) sum += tree_span(a, s, blockIdx.x == 0).tiles;
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        const int heads = LG * w.row_groups;
+        const long long total = sum * heads;
+        const int n = (int)min((long long)gridDim.x, total);
+        const bool idle = (int)blockIdx.x >= n;
+        const long long begin = idle ? 0 : total * blockIdx.x / n, end = idle ? 0 : total * (blockIdx.x + 1) / n;
+        long long before = 0;
+        for (int s0 = 0; s0 < a.ns; s0 += 32) {
+            const int s = s0 + lane;
+            const long long mine = s < a.ns ? (long long)tree_span(a, s, false).tiles * heads : 0;
+            long long incl = mine;
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += up;
+            }
+            const long long lo = before + incl - mine;
+            if (begin >= lo && begin < lo + mine) { plan_s = s; plan_base = lo; }
+            if (blockIdx.x == 0 && s < a.ns) w.start[s] = lo;
+            before += __shfl_sync(0xffffffffu, incl, 31);
+            if (blockIdx.x != 0 && (idle || before > begin)) break;
+        }
+        if (lane == 0) { plan_begin = begin; plan_end = end; if (blockIdx.x == 0) w.start[a.ns] = total; }
+    }
+    t5::fence_before();
+    __syncthreads();
+    t5::fence_after();
+    const uint32_t tmem = tmem_slot;
+    TreeWalk walk;
+    walk.pos = plan_begin; walk.end = plan_end; walk.base = plan_base; walk.s = plan_s;
+
+    // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
+    // every role still reaches its end.
+    bool ok = true;
+    if (warp == 0) {
+        // ------------------------------------------------ TMA: K and V of every tile, in turn, through the ring
+        int n = 0;                                            // loads so far
+        auto slot_free = [&]() {
+            if (ok && n >= RING) ok = ptx::mbar_wait(&empty[n % RING], (uint32_t)(((n / RING) & 1) ^ 1));
+            ok = __all_sync(0xffffffffu, ok);
+        };
+        const int box = PAGED ? min(a.B, 64) : 64;            // tokens per copy
+        const int boxes = kTreeTile / box;
+        while (walk.next(a, w.row_groups)) {
+            const int n_box = (walk.sp.n_view + box - 1) / box;           // copies that hold view tokens
+            const int b_end = min(n_box, min(walk.t1, walk.sp.view_tiles) * boxes);
+            const int NB = PAGED ? a.nblocks_dev[a.session_first + walk.s] : 0;
+            // page of the block that copy b reads: two dependent loads, 32 copies at a time and a batch ahead
+            auto lookup = [&](int b) -> int {
+                if (!PAGED || b >= b_end) return -1;
+                const int id = a.sel_ids[(size_t)walk.s * a.sel_stride + (int)((long long)b * box / a.B)];
+                int pg = -1;
+                if (id >= 0 && id < NB) pg = a.tables[(size_t)(a.session_first + walk.s) * a.max_bps + id];
+                if (pg < 0 || pg >= a.max_blocks) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); pg = 0; }
+                return pg;                                    // a flagged id reads page 0; the status word reports it
+            };
+            int b0 = walk.t0 * boxes, page = lookup(b0 + lane), page_next = lookup(b0 + 32 + lane);
+            for (int t = walk.t0; t < walk.t1; ++t) {
+                const bool in_view = t < walk.sp.view_tiles;
+                const int tt = (t - walk.sp.view_tiles) * kTreeTile;      // first tail row of a tail tile
+                const int live = in_view ? min(boxes, b_end - t * boxes) : min(2, (walk.sp.n_tail + walk.sp.n_q - tt + 63) / 64);
+                const uint32_t bytes = (uint32_t)live * (uint32_t)(in_view ? box : 64) * 256u;
+                if (PAGED && in_view && t * boxes >= b0 + 32) {
+                    b0 += 32;
+                    page = page_next;
+                    page_next = lookup(b0 + 32 + lane);
+                }
+                // in a view tile of the pages the lane that looked a copy's page up issues it, else lanes 0 and 1
+                const int u = PAGED && in_view ? b0 + lane - t * boxes : lane;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv, ++n) {
+                    slot_free();
+                    const int st = n % RING;
+                    if (ok && lane == 0) ptx::mbar_expect_tx(&full[st], bytes);
+                    __syncwarp();
+                    if (ok && u >= 0 && u < live) {
+                        unsigned char* dst = ring + (size_t)st * kTreeSlot;
+                        if (!in_view) {
+                            const CUtensorMap* m = kv ? &map_tv : &map_tk;
+                            const int row = walk.s * a.tail_cap + tt + u * 64;
+                            ptx::tma_load_3d(dst + u * 64 * 128, m, 0, walk.lg, row, &full[st]);
+                            ptx::tma_load_3d(dst + kTreeHalf + u * 64 * 128, m, 64, walk.lg, row, &full[st]);
+                        } else if (PAGED) {
+                            // pages [page][K | V][LG] tiles of B rows of 256 B
+                            const int z = (page * 2 + kv) * LG + walk.lg, y = (int)(((long long)t * kTreeTile + u * box) % a.B);
+                            ptx::tma_load_3d(dst + u * box * 128, &map_k, 0, y, z, &full[st]);
+                            ptx::tma_load_3d(dst + kTreeHalf + u * box * 128, &map_k, 64, y, z, &full[st]);
+                        } else {
+                            const CUtensorMap* m = kv ? &map_v : &map_k;
+                            const int z = walk.s * LG + walk.lg, y = t * kTreeTile + u * 64;
+                            ptx::tma_load_3d(dst + u * 64 * 128, m, 0, y, z, &full[st]);
+                            ptx::tma_load_3d(dst + kTreeHalf + u * 64 * 128, m, 64, y, z, &full[st]);
+                        }
+                    }
+                    if (!ok) --n;                             // not issued
+                }
+            }
+        }
+        // the copies still in flight land before the CTA gives its shared memory back
+        for (int i = max(0, n - RING); i < n; ++i) ok = ptx::mbar_wait(&full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
+        if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA
+        const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
+        int tiles = 0, seg = 0, cnt[2] = {0, 0};              // tiles before this segment; units so far per slot
+        auto wait = [&](uint64_t* bar, int phase) {
+            if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1));
+            ok = __all_sync(0xffffffffu, ok);
+        };
+        while (walk.next(a, w.row_groups)) {
+            const int units = (walk.t1 - walk.t0) * QT;       // (tile, row tile) or tiles: unit u belongs to slot u & 1
+            wait(&q_full, seg);
+            for (int u = 0; u <= units; ++u) {
+                if (u < units) {
+                    const int x = u & 1, k = 2 * (tiles + (QT == 1 ? u : u >> 1)), st = k % RING;
+                    if (QT == 1 || x == 0) wait(&full[st], k / RING);
+                    if (cnt[x] > 0) wait(&pv_done[x], cnt[x] - 1);            // P lies where S goes
+                    if (ok && lane == 0) {
+                        t5::fence_after();
+                        const uint32_t al = q_lo + (QT == 2 ? (uint32_t)x * (kTreeSlot >> 4) : 0u), bl = ring_lo + (uint32_t)st * (kTreeSlot >> 4);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint32_t o = (uint32_t)(i >> 2) * (kTreeHalf >> 4) + (uint32_t)(i & 3) * 2u;
+                            t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kTreeIdescS, i > 0 ? 1u : 0u);
+                        }
+                        t5::commit(&s_full[x]);
+                        if (QT == 1 || x == 1) t5::commit(&empty[st]);
+                    }
+                    ++cnt[x];
+                }
+                if (u > 0) {
+                    const int pu = u - 1, x = pu & 1, v = 2 * (tiles + (QT == 1 ? pu : pu >> 1)) + 1, st = v % RING;
+                    // cnt[x] already counts the next unit of this slot only if u belongs to it, which it never does (u - 1 and u differ)
+                    if (QT == 1 || x == 0) wait(&full[st], v / RING);
+                    wait(&p_full[x], cnt[x] - 1);
+                    if (ok && lane == 0) {
+                        t5::fence_after();
+                        const uint32_t bl = (ring_lo + (uint32_t)st * (kTreeSlot >> 4)) | (kTreeVStep << 16);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)i * 8u,
+                                            t5::make_desc(bl + (uint32_t)i * (2048u >> 4)), kTreeIdescO, pu > 1 || i > 0 ? 1u : 0u);
+                        t5::commit(&pv_done[x]);
+                        if (QT == 1 || x == 1) t5::commit(&empty[st]);
+                    }
+                }
+            }
+            tiles += walk.t1 - walk.t0;
+            ++seg;
+        }
+        if (lane == 0) t5::commit(&drained);                  // MMAs in flight end before the tensor memory is given back
+        ok = ptx::mbar_wait(&drained, 0u) && ok;
+        if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
+    } else {
+        // ------------------------------------------------ rows: a thread is TMEM lane 32 (warp & 3) + lane of slot x
+        const int x = (warp - 2) >> 2, gt = (tid - 64) & 127;               // slot; thread of the slot's 128
+        const int row_in = (warp & 3) * 32 + lane;                           // row of the row tile
+        const uint32_t s_addr = tmem + (uint32_t)x * 256u + ((uint32_t)((warp & 3) * 32) << 16), o_addr = s_addr + 128u;
+        const float scale2 = a.scale * 1.4426950408889634f;
+        int tiles = 0, cnt = 0;
+        auto wait = [&](uint64_t* bar, int phase) {
+            if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1));
+            ok = __all_sync(0xffffffffu, ok);
+        };
+        while (walk.next(a, w.row_groups)) {
+            const TreeSpan sp = walk.sp;
+            const int l = walk.lg / a.G, g = walk.lg % a.G;
+            const int rows = sp.n_q * a.r, row0 = walk.rg * QT * kTreeRows;   // live rows of the head; the group's first
+            // both slots are done with the last segment's Q before it is replaced
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            for (int i = tid - 64; i < QT * kTreeRows * 16; i += 256) {
+                const int rr = i >> 4, c = i & 15, row = row0 + rr;
+                uint4 val = make_uint4(0u, 0u, 0u, 0u);
+                if (row < rows)
+                    val = *reinterpret_cast<const uint4*>(a.q + ((((size_t)walk.s * a.M + row / a.r) * a.L + l) * a.H + (size_t)g * a.r + row % a.r) * kTreeD + c * 8);
+                *reinterpret_cast<uint4*>(smem_q + (size_t)(rr >> 7) * kTreeSlot + (size_t)(c >> 3) * kTreeHalf + (rr & 127) * 128 + (((c & 7) ^ (rr & 7)) << 4)) = val;
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&q_full);
+
+            const int row = row0 + (QT == 2 ? x * kTreeRows : 0) + row_in;
+            const bool warp_live = row - lane < rows;                         // any row of this warp is real
+            const unsigned long long bits = row < rows ? tree_bits(a, walk.s, row / a.r, sp.n_q) : 0ull;
+            float ref = -INFINITY, sum = 0.0f;
+            bool cleared = false;
+            const int n_units = QT == 1 ? (walk.t1 - walk.t0 + 1 - x) >> 1 : walk.t1 - walk.t0;
+            for (int j = 0; j < n_units; ++j) {
+                const int ti = QT == 1 ? 2 * j + x : j, t = walk.t0 + ti;
+                const bool in_view = t < sp.view_tiles;
+                const int c0 = (in_view ? t : t - sp.view_tiles) * kTreeTile;             // first token of the tile in view or tail
+                const int n_valid = min(kTreeTile, (in_view ? sp.n_view : sp.n_tail + sp.n_q) - c0);
+                wait(&s_full[x], cnt);
+                if ((n_valid < kTreeTile || !in_view) && (QT == 1 || x == 0)) {
+                    // values nobody sees become zero; drafted values that are not finite too (the merge adds them)
+                    const int v = 2 * (tiles + ti) + 1, st = v % RING;
+                    wait(&full[st], v / RING);
+                    unsigned char* vt = ring + (size_t)st * kTreeSlot;
+                    const int first = in_view ? n_valid : min(max(sp.n_tail - c0, 0), n_valid);
+                    for (int i = first * 16 + gt; i < kTreeTile * 16; i += 128) {
+                        const int rr = i >> 4, c = i & 15;
+                        uint4* p = reinterpret_cast<uint4*>(vt + (size_t)(c >> 3) * kTreeHalf + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
+                        uint4 val = make_uint4(0u, 0u, 0u, 0u);
+                        bool put = true;
+                        if (rr < n_valid) {
+                            val = *p;
+                            put = false;
+                            uint32_t* e = reinterpret_cast<uint32_t*>(&val);
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) {
+                                if ((e[h] & 0x00007f80u) == 0x00007f80u) { e[h] &= 0xffff0000u; put = true; }
+                                if ((e[h] & 0x7f800000u) == 0x7f800000u) { e[h] &= 0x0000ffffu; put = true; }
+                            }
+                            cleared |= put;
+                        }
+                        if (put) *p = val;
+                    }
+                    ptx::fence_proxy_async_smem();
+                }
+                if (warp_live) {
+                    t5::fence_after();
+                    // two sweeps over the 128 logits, 32 columns at a time: the maximum, then the weights.  (Held in registers in
+                    // between they spill; a second read of tensor memory is cheaper.)
+                    const bool masked = n_valid < kTreeTile || !in_view;
+                    uint32_t word[4];
+                    if (masked) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int left = n_valid - 32 * c;
+                            word[c] = in_view ? (left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u)
+                                              : tail_word(c0 + 32 * c, sp.n_tail, bits);
+                        }
+                    }
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t sv[32];
+                        t5::ld32_issue(s_addr + 32u * c, sv);
+                        t5::ld_wait(sv);
+                        if (MASS && in_view && row < rows) {
+                            float* lp = w.logits + (((size_t)walk.s * LG + walk.lg) * a.rows + row) * a.cap + c0 + 32 * c;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                if (32 * c + i < n_valid)
+                                    *reinterpret_cast<float4*>(lp + i) =
+                                        make_float4(__uint_as_float(sv[i]) * scale2, __uint_as_float(sv[i + 1]) * scale2,
+                                                    __uint_as_float(sv[i + 2]) * scale2, __uint_as_float(sv[i + 3]) * scale2);
+                        }
+                        if (masked) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!((word[c] >> i) & 1u)) sv[i] = 0xff800000u;
+                        }
+                        float mc[8];                              // a tree of three-input maxima
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            mc[i] = fmaxf(f2::max3(__uint_as_float(sv[4 * i]), __uint_as_float(sv[4 * i + 1]), __uint_as_float(sv[4 * i + 2])), __uint_as_float(sv[4 * i + 3]));
+                        mx = f2::max3(mx, f2::max3(f2::max3(mc[0], mc[1], mc[2]), mc[3], mc[4]), f2::max3(mc[5], mc[6], mc[7]));
+                    }
+                    const float m2 = mx * scale2;
+                    const bool moves = m2 > ref + kTreeSlack;                 // true for the first finite logit: ref is -inf
+                    if (__any_sync(0xffffffffu, moves)) {
+                        const float to = moves ? m2 : ref, corr = moves ? t5::ex2(ref - to) : 1.0f;
+                        if (j > 0) {
+                            // the last product into O is complete: S was issued after it
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t ov[32];
+                                t5::ld32_issue(o_addr + 32u * c, ov);
+                                t5::ld_wait(ov);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
+                                t5::st32(o_addr + 32u * c, ov);
+                            }
+                        }
+                        sum *= corr;
+                        ref = to;
+                    }
+                    const float use = ref > -INFINITY ? ref : 0.0f;           // nothing seen yet: every weight is exp2(-inf) = 0
+                    const uint64_t sc2 = f2::pk(scale2, scale2), nm2 = f2::pk(-use, -use);
+                    uint64_t acc0 = f2::pk(0.0f, 0.0f), acc1 = acc0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t sv[32], pk[16];
+                        t5::ld32_issue(s_addr + 32u * c, sv);
+                        t5::ld_wait(sv);
+                        if (masked) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!((word[c] >> i) & 1u)) sv[i] = 0xff800000u;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            float p0, p1;
+                            f2::unpk(f2::fma(f2::pk(sv[i], sv[i + 1]), sc2, nm2), p0, p1);
+                            p0 = t5::ex2(p0);
+                            p1 = t5::ex2(p1);
+                            if (i & 2) acc1 = f2::add(acc1, f2::pk(p0, p1)); else acc0 = f2::add(acc0, f2::pk(p0, p1));
+                            pk[i >> 1] = ptx::pack_bf16x2(p0, p1);
+                        }
+                        // columns [16 c, 16 c + 16): logits of chunks that have been read
+                        t5::st16(s_addr + 16u * c, pk);
+                    }
+                    float a0, a1, a2, a3;
+                    f2::unpk(acc0, a0, a1);
+                    f2::unpk(acc1, a2, a3);
+                    sum += (a0 + a1) + (a2 + a3);
+                    t5::st_wait();
+                    t5::fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&p_full[x]);
+                ++cnt;
+            }
+            // the segment's sums
+            const size_t seg = (size_t)blockIdx.x + walk.head;
+            if (n_units > 0) wait(&pv_done[x], cnt - 1);
+            if (warp_live) {
+                t5::fence_after();
+                const size_t at = (seg * 2 + x) * w.rows_slot + row_in;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t ov[32];
+                    t5::ld32_issue(o_addr + 32u * c, ov);
+                    t5::ld_wait(ov);
+                    if (row < rows && n_units > 0) {
+                        uint4* dst = reinterpret_cast<uint4*>(w.part_o + at * kTreeD + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) dst[i] = make_uint4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
+                    }
+                }
+                if (row < rows) w.part_ml[at] = make_float2(ref, sum);
+                t5::fence_before();
+            }
+            cleared = __any_sync(0xffffffffu, cleared);
+            if (lane == 0) reinterpret_cast<unsigned char*>(w.part_nf + seg)[warp - 2] = cleared ? 1 : 0;
+            tiles += walk.t1 - walk.t0;
+        }
+        if (!ok && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
+    }
+    t5::fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        t5::fence_after();
+        t5::tmem_dealloc(tmem, 512);
+    }
 }
 
-__global__ void __launch_bounds__(128) tree_mass_kernel(TreeArgs a) {
-    const int t = blockIdx.x * 128 + threadIdx.x, lg = blockIdx.y, s = blockIdx.z;
+// Joins the segments of one query row in the order of the line; a thread per dimension.
+__global__ void __launch_bounds__(kTreeD)
+tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
+    pdl_wait();
+    pdl_trigger();
+    const TreeArgs& a = w.a;
+    const int LG = a.L * a.G, row = blockIdx.x, hz = blockIdx.y, s = hz / LG, lg = hz % LG, col = threadIdx.x;
     const TreeSpan sp = tree_span(a, s, false);
-    if (t >= sp.n_view) return;
-    const __nv_bfloat16* kr = a.view_k + view_row(a, s, lg, t);
-    float w = 0.0f;
-    for (int row = 0; row < sp.n_q * a.r; ++row) {
-        const size_t orow = (((size_t)s * a.M + row / a.r) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
-        float x = 0.0f;
-        for (int d = 0; d < kTreeD; ++d) x += __bfloat162float(a.q[orow * kTreeD + d]) * __bfloat162float(kr[d]);
-        w += expf(x * a.scale - a.lse[orow]);
+    const int m = row / a.r;
+    if (m >= sp.n_q) return;
+    const int in_group = w.row_tiles * kTreeRows, rg = row / in_group, rr = row % in_group;
+    const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
+    float top = -INFINITY, z = 0.0f, acc = 0.0f;
+    unsigned long long nf = 0;
+    if (sp.tiles > 0) {
+        const long long total = w.start[a.ns], first = w.start[s] + ((long long)lg * w.row_groups + rg) * sp.tiles;
+        const int n = (int)min((long long)n_ctas, total);
+        const int c0 = tile_owner(first, total, n), c1 = tile_owner(first + sp.tiles - 1, total, n);
+        const size_t head = ((size_t)s * LG + lg) * w.row_groups + rg;
+        const int per = w.row_tiles == 1 ? 2 : 1;                         // one row tile: both slots hold a share of every row
+        const int parts = (c1 - c0 + 1) * per;
+        auto where = [&](int i) { return ((c0 + i / per + head) * 2 + (per == 2 ? i % 2 : rr >> 7)) * w.rows_slot + (rr & 127); };
+        for (int i = 0; i < parts; ++i) top = fmaxf(top, w.part_ml[where(i)].x);
+        for (int i = 0; i < parts; i += 4) {
+            float2 ml[4];
+            float po[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const size_t at = where(min(i + u, parts - 1));
+                ml[u] = w.part_ml[at];
+                po[u] = w.part_o[at * kTreeD + col];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u < parts && (ml[u].x > -INFINITY || ml[u].y != 0.0f)) {    // a share without a visible token holds no sums
+                    const float f = t5::ex2(ml[u].x - top);
+                    acc += f * po[u];
+                    z += f * ml[u].y;
+                }
+        }
+        for (int c = c0; c <= c1; ++c) nf |= w.part_nf[c + head];
     }
-    float* mp = a.mass + ((size_t)s * a.L * a.G + lg) * a.cap + t;
-    *mp = a.decay * *mp + w;
+    const bool none = z == 0.0f;
+    float out = none ? 0.0f : acc / z;
+    if (nf) {
+        // drafted values that are not finite were left out: they reach the rows that see them here
+        const unsigned long long bits = tree_bits(a, s, m, sp.n_q);
+        for (int j = 0; j < sp.n_q; ++j)
+            if ((bits >> j) & 1) {
+                const float v = __bfloat162float(a.tail_v[(((size_t)s * a.tail_cap + sp.n_tail + j) * LG + lg) * kTreeD + col]);
+                if (!isfinite(v)) out += v;
+            }
+    }
+    a.out[orow * kTreeD + col] = __float2bfloat16(out);
+    const float lse2 = none ? -INFINITY : top + log2f(z);
+    if (col == 0) {
+        a.lse[orow] = lse2 * 0.6931471805599453f;
+        if (w.lse2) w.lse2[(size_t)hz * a.rows + row] = lse2;
+    }
+}
+
+// mass = decay mass + sum over the rows of exp2(logit - lse): the logits that the attention left, four tokens a thread.
+__global__ void __launch_bounds__(128)
+tree_mass_kernel(const __grid_constant__ TreeWork w) {
+    pdl_wait();
+    pdl_trigger();
+    const TreeArgs& a = w.a;
+    const int hz = blockIdx.y, s = hz / (a.L * a.G);
+    const TreeSpan sp = tree_span(a, s, false);
+    const int t = (blockIdx.x * 128 + threadIdx.x) * 4;
+    if (t >= sp.n_view) return;                          // n_view is a multiple of 16
+    const int rows = sp.n_q * a.r;
+    const float* lp = w.logits + (size_t)hz * a.rows * a.cap + t;
+    const float* zp = w.lse2 + (size_t)hz * a.rows;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int row = 0; row < rows; ++row) {
+        const float4 v = *reinterpret_cast<const float4*>(lp + (size_t)row * a.cap);
+        const float z = zp[row];
+        sum.x += t5::ex2(v.x - z); sum.y += t5::ex2(v.y - z); sum.z += t5::ex2(v.z - z); sum.w += t5::ex2(v.w - z);
+    }
+    float4* mp = reinterpret_cast<float4*>(a.mass + (size_t)hz * a.cap + t);
+    const float4 m = *mp;
+    *mp = make_float4(fmaf(a.decay, m.x, sum.x), fmaf(a.decay, m.y, sum.y), fmaf(a.decay, m.z, sum.z), fmaf(a.decay, m.w, sum.w));
+}
+
+// sizes and places inside the workspace; base null: sizes alone
+static size_t plan_tree(const kvmem_pool_config_t& c, int n_sessions, int M, int mass_cap, char* base, TreeWork* w) {
+    const int rows = M * (c.n_q_heads / c.n_kv_heads);
+    w->row_tiles = rows <= kTreeRows ? 1 : 2;
+    w->row_groups = (rows + w->row_tiles * kTreeRows - 1) / (w->row_tiles * kTreeRows);
+    w->rows_slot = std::min(rows, kTreeRows);
+    const size_t heads = (size_t)n_sessions * c.n_layers * c.n_kv_heads, segs = heads * w->row_groups + kSMs;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return base ? base + at : nullptr; };
+    w->part_o = (float*)take(segs * 2 * w->rows_slot * kTreeD * sizeof(float));
+    w->part_ml = (float2*)take(segs * 2 * w->rows_slot * sizeof(float2));
+    w->part_nf = (unsigned long long*)take(segs * 8);
+    w->start = (long long*)take(((size_t)n_sessions + 1) * 8);
+    w->lse2 = mass_cap ? (float*)take(heads * rows * sizeof(float)) : nullptr;
+    w->logits = mass_cap ? (float*)take(heads * rows * mass_cap * sizeof(float)) : nullptr;
+    return off;
 }
 
 size_t tree_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int mass_cap_tokens) {
-    (void)c; (void)n_sessions; (void)n_q_tokens; (void)mass_cap_tokens;
-    return 256;
+    TreeWork w;
+    return plan_tree(c, n_sessions, n_q_tokens, mass_cap_tokens, nullptr, &w);
+}
+
+// [outer][rows][128 dims] bf16, boxes of 64 dims x box_rows x 1, 128-byte swizzle; tail: [tokens][heads][128] with boxes of 64 tokens
+static bool tree_map(CUtensorMap* map, const __nv_bfloat16* p, cuuint64_t d1, cuuint64_t d2, cuuint32_t box1, cuuint32_t box2) {
+    static PFN_cuTensorMapEncodeTiled_v12000 enc = [] {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr) : nullptr;
+    }();
+    if (!enc) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)kTreeD, d1, d2};
+    cuuint64_t strides[2] = {(cuuint64_t)kTreeD * 2, d1 * kTreeD * 2};
+    cuuint32_t box[3] = {64, box1, box2}, step[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int QT, bool PAGED, bool MASS>
+static cudaError_t launch_split(const kvmem_pool& p, int grid, cudaStream_t st, const CUtensorMap (&m)[4], const TreeWork& w) {
+    static PerDeviceOnce done;
+    if (done.pending(p.cfg.device)) {
+        const cudaError_t e = cudaFuncSetAttribute(tree_split_kernel<QT, PAGED, MASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTreeSmem);
+        if (e != cudaSuccess) return e;
+        done.mark(p.cfg.device);
+    }
+    return launch_pdl(tree_split_kernel<QT, PAGED, MASS>, dim3((unsigned)grid), dim3(kTreeThreads), kTreeSmem, st, m[0], m[1], m[2], m[3], w);
 }
 
 cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace, cudaStream_t st) {
-    (void)p; (void)workspace;
-    tree_rows_kernel<<<dim3((a.rows + 3) / 4, a.L * a.G, a.ns), 128, 0, st>>>(a);
-    if (a.mass) tree_mass_kernel<<<dim3((a.cap + 127) / 128, a.L * a.G, a.ns), 128, 0, st>>>(a);
-    return cudaGetLastError();
+    const int LG = a.L * a.G;
+    TreeWork w{};
+    plan_tree(p.cfg, a.ns, a.M, a.mass ? a.cap : 0, (char*)workspace, &w);
+    w.a = a;
+    CUtensorMap m[4];
+    const bool paged = a.view_k == nullptr;
+    bool made = paged ? tree_map(&m[0], a.pages, (cuuint64_t)a.B, (cuuint64_t)a.max_blocks * 2 * LG, (cuuint32_t)std::min(a.B, 64), 1)
+                      : tree_map(&m[0], a.view_k, (cuuint64_t)a.cap, (cuuint64_t)a.ns * LG, 64, 1) &&
+                            tree_map(&m[1], a.view_v, (cuuint64_t)a.cap, (cuuint64_t)a.ns * LG, 64, 1);
+    if (paged) m[1] = m[0];
+    if (a.tail_k)
+        made = made && tree_map(&m[2], a.tail_k, (cuuint64_t)LG, (cuuint64_t)a.ns * a.tail_cap, 1, 64) &&
+               tree_map(&m[3], a.tail_v, (cuuint64_t)LG, (cuuint64_t)a.ns * a.tail_cap, 1, 64);
+    else m[2] = m[3] = m[0];
+    if (!made) return cudaErrorInvalidValue;
+    const long long most = (long long)a.ns * LG * w.row_groups * ((a.cap + kTreeTile - 1) / kTreeTile + (a.tail_cap + kTreeTile - 1) / kTreeTile);
+    const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), most);
+    cudaError_t e;
+    if (a.mass) e = launch_split<1, false, true>(p, grid, st, m, w);            // at most 64 rows
+    else if (paged) e = w.row_tiles == 1 ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);
+    else e = w.row_tiles == 1 ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(tree_merge_kernel, dim3((unsigned)a.rows, (unsigned)(a.ns * LG)), dim3(kTreeD), 0, st, w, grid);
+    if (e != cudaSuccess || !a.mass) return e;
+    return launch_pdl(tree_mass_kernel, dim3((unsigned)((a.cap + 511) / 512), (unsigned)(a.ns * LG)), dim3(128), 0, st, w);
 }
 
 }  // namespace kvmem

@@ -507,7 +507,7 @@ tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
     pdl_wait();
     pdl_trigger();
     const TreeArgs& a = w.a;
-    const int LG = a.L * a.G, row = blockIdx.x, hz = blockIdx.y, s = hz / LG, lg = hz % LG, col = threadIdx.x;
+    const int LG = a.L * a.G, row = blockIdx.y, hz = blockIdx.x, s = hz / LG, lg = hz % LG, col = threadIdx.x;
     const TreeSpan sp = tree_span(a, s, false);
     const int m = row / a.r;
     if (m >= sp.n_q) return;
@@ -568,9 +568,9 @@ tree_mass_kernel(const __grid_constant__ TreeWork w) {
     pdl_wait();
     pdl_trigger();
     const TreeArgs& a = w.a;
-    const int hz = blockIdx.y, s = hz / (a.L * a.G);
+    const int hz = blockIdx.x, s = hz / (a.L * a.G);
     const TreeSpan sp = tree_span(a, s, false);
-    const int t = (blockIdx.x * 128 + threadIdx.x) * 4;
+    const int t = (blockIdx.y * 128 + threadIdx.x) * 4;
     if (t >= sp.n_view) return;                          // n_view is a multiple of 16
     const int rows = sp.n_q * a.r;
     const float* lp = w.logits + (size_t)hz * a.rows * a.cap + t;
@@ -659,9 +659,9 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     else if (paged) e = w.row_tiles == 1 ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);
     else e = w.row_tiles == 1 ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(tree_merge_kernel, dim3((unsigned)a.rows, (unsigned)(a.ns * LG)), dim3(kTreeD), 0, st, w, grid);
+    e = launch_pdl(tree_merge_kernel, dim3((unsigned)(a.ns * LG), (unsigned)a.rows), dim3(kTreeD), 0, st, w, grid);
     if (e != cudaSuccess || !a.mass) return e;
-    return launch_pdl(tree_mass_kernel, dim3((unsigned)((a.cap + 511) / 512), (unsigned)(a.ns * LG)), dim3(128), 0, st, w);
+    return launch_pdl(tree_mass_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.cap + 511) / 512)), dim3(128), 0, st, w);
 }
 
 }  // namespace kvmem

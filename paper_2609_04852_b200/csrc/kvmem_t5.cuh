@@ -22,6 +22,14 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// true in one lane of a converged warp, always the same one.  (Unlike lane == 0 it leaves the operands of what it guards
+// warp-uniform for the compiler, so that an MMA's descriptors need no move between register files.)
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 // D[tmem] (+)= A[smem] * B[smem]^T, bf16 inputs, fp32 accumulate, one CTA
 __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -48,6 +56,15 @@ __device__ __forceinline__ void ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
         : "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
 // wait for the loads issued so far; the registers go through the wait, so that no use of them can move in front of it
 __device__ __forceinline__ void ld_wait(uint32_t (&r)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -58,23 +75,19 @@ __device__ __forceinline__ void ld_wait(uint32_t (&r)[32]) {
                  :
                  : "memory");
 }
+__device__ __forceinline__ void ld_wait(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
         "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
-        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
-        "r"(r[31])
         : "memory");
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -130,11 +143,39 @@ __device__ __forceinline__ uint64_t add(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+// NaN if any operand is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 }  // namespace f2
+
+// 2^x for a pair, on the FMA and integer pipes: the share of the exponentials that the special-function
+// unit (16 results per clock and SM) is spared.  x = n + f with n the nearest
+// integer and |f| <= 1/2; 2^f by a degree-4 polynomial (relative error below 3e-6), 2^n by adding n to
+// the exponent field.  Arguments below -125 (including -inf) return about 2^-125 instead of 0, which
+// is immaterial next to weights that sum to one per query row.
+__device__ __forceinline__ uint64_t ex2_poly2(uint64_t x2) {
+    float x0, x1;
+    f2::unpk(x2, x0, x1);
+    const uint64_t x = f2::pk(fmaxf(x0, -125.0f), fmaxf(x1, -125.0f));
+    const uint64_t t = f2::add(x, f2::pk(12582912.0f, 12582912.0f));         // 1.5 * 2^23: n sits in the low mantissa bits
+    const uint64_t n = f2::add(t, f2::pk(-12582912.0f, -12582912.0f));
+    const uint64_t f = f2::fma(n, f2::pk(-1.0f, -1.0f), x);                   // exact
+    uint64_t p = f2::fma(f2::pk(0.009570100344717503f, 0.009570100344717503f), f, f2::pk(0.05591785907745361f, 0.05591785907745361f));
+    p = f2::fma(p, f, f2::pk(0.240247443318367f, 0.240247443318367f));
+    p = f2::fma(p, f, f2::pk(0.6931217908859253f, 0.6931217908859253f));
+    p = f2::fma(p, f, f2::pk(0.9999992847442627f, 0.9999992847442627f));
+    uint32_t p0, p1, t0, t1;
+    f2::unpk(p, p0, p1);
+    f2::unpk(t, t0, t1);
+    return f2::pk(p0 + (t0 << 23), p1 + (t1 << 23));
+}
 
 }  // namespace kvmem

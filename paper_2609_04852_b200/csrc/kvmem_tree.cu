@@ -39,10 +39,10 @@ constexpr int kTreeTile = 128;                    // tokens per tile
 constexpr int kTreeHalf = kTreeTile * 128;        // bytes of one 64-dim half of a 128-row operand tile (16 KiB)
 constexpr int kTreeSlot = 2 * kTreeHalf;          // a K, V or Q tile
 constexpr int kTreeRows = 128;                    // rows of a row tile: TMEM lanes
-constexpr int kTreeThreads = 64 + 256;            // TMA warp, MMA warp, two groups of four row warps
+constexpr int kTreeThreads = 64 + 512;            // TMA warp, MMA warp, sixteen row warps
+constexpr int kTreePoly = 4;                      // every n-th pair of exponentials off the special-function unit (0: none)
 constexpr int kTreeRing1 = 6, kTreeRing2 = 5;     // ring slots beside one or two Q tiles: 224 KiB in all
 constexpr float kTreeSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
-constexpr size_t kTreeSmem = (size_t)(1 + kTreeRing1) * kTreeSlot + 1024;
 static_assert(1 + kTreeRing1 == 2 + kTreeRing2, "both forms take the same shared memory");
 constexpr uint32_t kTreeIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
 constexpr uint32_t kTreeIdescO = kTreeIdescS | (1u << 16);                                        // B with dims contiguous (V as it lies)
@@ -58,7 +58,7 @@ struct TreeWork {
     int row_tiles, row_groups, rows_slot;   // row tiles per CTA (1, 2), groups of them per head, rows stored per slot
     float* part_o;                // [segment][slot][rows_slot][128]
     float2* part_ml;              // [segment][slot][rows_slot]: (reference, sum of weights), log2 domain
-    unsigned long long* part_nf;  // [segment]: a byte per row warp, set where it cleared a drafted value that is not finite
+    ulonglong2* part_nf;          // [segment]: a byte per row warp, set where it cleared a drafted value that is not finite
     long long* start;             // [ns + 1]: tiles of the sessions before, in head units; filled by CTA 0
     float* lse2;                  // [ns][LG][rows]: log-sum-exp in the log2 domain (weights only)
     float* logits;                // [ns][LG][rows][cap]: scaled logits, log2 domain (weights only)
@@ -120,32 +120,63 @@ struct TreeWalk {
     }
 };
 
+// 32 logits of a row to weights exp2(x scale2 - ref), bf16 pairs in pk; their fp32 sum goes to acc0 + acc1
+template <int POLY>
+__device__ __forceinline__ void tree_weights(const uint32_t (&sv)[32], uint64_t sc2, uint64_t nm2, uint64_t& acc0, uint64_t& acc1, uint32_t (&pk)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        uint64_t e = f2::fma(f2::pk(sv[2 * i], sv[2 * i + 1]), sc2, nm2);
+        float p0, p1;
+        if (POLY > 0 && i % (POLY > 0 ? POLY : 1) == POLY - 1) e = ex2_poly2(e);
+        else {
+            f2::unpk(e, p0, p1);
+            e = f2::pk(t5::ex2(p0), t5::ex2(p1));
+        }
+        f2::unpk(e, p0, p1);
+        if (i & 1) acc1 = f2::add(acc1, e); else acc0 = f2::add(acc0, e);
+        pk[i] = ptx::pack_bf16x2(p0, p1);
+    }
+}
+
+struct TreeShared {
+    uint64_t full[kTreeRing1], empty[kTreeRing1], q_full, s_full[2], p_full[2], o_done[2], drained;
+    long long plan_begin, plan_end, plan_base;
+    int plan_s;
+    uint32_t tmem;
+    float half_max[2][2][kTreeRows];      // [slot][half of the columns]: exchanged between the two threads of a row
+};
+// Nothing static beside it: the dynamic part then starts where shared memory does, on the 1,024 bytes that the swizzle needs
+// (checked), and all 227 KB are in use.
+constexpr size_t kTreeSmem = (size_t)(1 + kTreeRing1) * kTreeSlot + sizeof(TreeShared);
+static_assert(kTreeSmem <= 232448, "227 KB of shared memory per CTA");
+
 template <int QT, bool PAGED, bool MASS>
 __global__ void __launch_bounds__(kTreeThreads, 1)
 tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CUtensorMap map_tk, const __grid_constant__ CUtensorMap map_tv,
                   const __grid_constant__ TreeWork w) {
     constexpr int RING = QT == 1 ? kTreeRing1 : kTreeRing2;
-    extern __shared__ unsigned char smem_dyn[];
-    __shared__ uint64_t full[RING], empty[RING], q_full, s_full[2], p_full[2], pv_done[2], drained;
-    __shared__ uint32_t tmem_slot;
-    __shared__ long long plan_begin, plan_end, plan_base;
-    __shared__ int plan_s;
+    extern __shared__ __align__(1024) unsigned char smem_q[];      // Q tiles, the ring, then the small things
     const TreeArgs& a = w.a;
-    unsigned char* smem_q = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
     unsigned char* ring = smem_q + (size_t)QT * kTreeSlot;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    TreeShared& sh = *reinterpret_cast<TreeShared*>(smem_q + (size_t)(1 + kTreeRing1) * kTreeSlot);
+    uint64_t *full = sh.full, *empty = sh.empty, *s_full = sh.s_full, *p_full = sh.p_full, *o_done = sh.o_done;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int LG = a.L * a.G;
 
+    if (ptx::smem_u32(smem_q) & 1023u) {          // never: see TreeShared
+        if (tid == 0) atomicExch(a.status, (int)KVMEM_E_UNSUPPORTED);
+        return;
+    }
     if (tid == 0) {
         for (int i = 0; i < RING; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&pv_done[i], 1); }
-        ptx::mbar_init(&q_full, 8);
-        ptx::mbar_init(&drained, 1);
+        for (int i = 0; i < 2; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 8); ptx::mbar_init(&o_done[i], 1); }
+        ptx::mbar_init(&sh.q_full, 16);
+        ptx::mbar_init(&sh.drained, 1);
         ptx::fence_mbar_init();
     }
     if (warp == 1) {
-        t5::tmem_alloc(&tmem_slot, 512);
+        t5::tmem_alloc(&sh.tmem, 512);
         t5::tmem_relinquish();
     }
     pdl_wait();        // everything earlier in the stream is complete and visible from here on
@@ -170,19 +201,19 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 if (lane >= d) incl += up;
             }
             const long long lo = before + incl - mine;
-            if (begin >= lo && begin < lo + mine) { plan_s = s; plan_base = lo; }
+            if (begin >= lo && begin < lo + mine) { sh.plan_s = s; sh.plan_base = lo; }
             if (blockIdx.x == 0 && s < a.ns) w.start[s] = lo;
             before += __shfl_sync(0xffffffffu, incl, 31);
             if (blockIdx.x != 0 && (idle || before > begin)) break;
         }
-        if (lane == 0) { plan_begin = begin; plan_end = end; if (blockIdx.x == 0) w.start[a.ns] = total; }
+        if (lane == 0) { sh.plan_begin = begin; sh.plan_end = end; if (blockIdx.x == 0) w.start[a.ns] = total; }
     }
     t5::fence_before();
     __syncthreads();
     t5::fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = sh.tmem;
     TreeWalk walk;
-    walk.pos = plan_begin; walk.end = plan_end; walk.base = plan_base; walk.s = plan_s;
+    walk.pos = sh.plan_begin; walk.end = sh.plan_end; walk.base = sh.plan_base; walk.s = sh.plan_s;
 
     // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
     // every role still reaches its end.
@@ -255,85 +286,100 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         for (int i = max(0, n - RING); i < n; ++i) ok = ptx::mbar_wait(&full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
         if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
     } else if (warp == 1) {
-        // ------------------------------------------------ MMA
-        const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
-        int tiles = 0, seg = 0, cnt[2] = {0, 0};              // tiles before this segment; units so far per slot
-        auto wait = [&](uint64_t* bar, int phase) {
-            if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1));
-            ok = __all_sync(0xffffffffu, ok);
-        };
-        while (walk.next(a, w.row_groups)) {
-            const int units = (walk.t1 - walk.t0) * QT;       // (tile, row tile) or tiles: unit u belongs to slot u & 1
-            wait(&q_full, seg);
-            for (int u = 0; u <= units; ++u) {
-                if (u < units) {
-                    const int x = u & 1, k = 2 * (tiles + (QT == 1 ? u : u >> 1)), st = k % RING;
-                    if (QT == 1 || x == 0) wait(&full[st], k / RING);
-                    if (cnt[x] > 0) wait(&pv_done[x], cnt[x] - 1);            // P lies where S goes
-                    if (ok && lane == 0) {
-                        t5::fence_after();
-                        const uint32_t al = q_lo + (QT == 2 ? (uint32_t)x * (kTreeSlot >> 4) : 0u), bl = ring_lo + (uint32_t)st * (kTreeSlot >> 4);
+        // ------------------------------------------------ MMA: one thread
+        // Order: S(0) S(1) | O(0) S(2) | O(1) S(3) | ...: a slot's next logits are issued right behind the product that reads its
+        // weights, in whose place they go.  MMAs that one thread issues run in order, so there is nothing to wait for.
+        if (t5::elect()) {
+            const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
+            int tiles = 0, seg = 0, cnt[2] = {0, 0};          // tiles before this segment; units so far per slot
+            auto wait = [&](uint64_t* bar, int phase) { if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1)); };
+            auto keys_in = [&](int u) {                       // the key tile of unit u has landed
+                const int k = 2 * (tiles + (QT == 1 ? u : u >> 1));
+                if (QT == 1 || (u & 1) == 0) wait(&full[k % RING], k / RING);
+            };
+            auto logits = [&](int u) {                        // S of unit u: slot u & 1
+                const int x = u & 1, k = 2 * (tiles + (QT == 1 ? u : u >> 1)), st = k % RING;
+                if (!ok) return;
+                t5::fence_after();
+                const uint32_t al = q_lo + (QT == 2 ? (uint32_t)x * (kTreeSlot >> 4) : 0u), bl = ring_lo + (uint32_t)st * (kTreeSlot >> 4);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const uint32_t o = (uint32_t)(i >> 2) * (kTreeHalf >> 4) + (uint32_t)(i & 3) * 2u;
-                            t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kTreeIdescS, i > 0 ? 1u : 0u);
-                        }
-                        t5::commit(&s_full[x]);
-                        if (QT == 1 || x == 1) t5::commit(&empty[st]);
-                    }
-                    ++cnt[x];
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t o = (uint32_t)(i >> 2) * (kTreeHalf >> 4) + (uint32_t)(i & 3) * 2u;
+                    t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kTreeIdescS, i > 0 ? 1u : 0u);
                 }
-                if (u > 0) {
-                    const int pu = u - 1, x = pu & 1, v = 2 * (tiles + (QT == 1 ? pu : pu >> 1)) + 1, st = v % RING;
-                    // cnt[x] already counts the next unit of this slot only if u belongs to it, which it never does (u - 1 and u differ)
+                t5::commit(&s_full[x]);
+                if (QT == 1 || x == 1) t5::commit(&empty[st]);
+            };
+            while (walk.next(a, w.row_groups)) {
+                const int units = (walk.t1 - walk.t0) * QT;   // (tile, row tile) or tiles
+                wait(&sh.q_full, seg);
+                keys_in(0);
+                logits(0);
+                if (units > 1) { keys_in(1); logits(1); }
+                for (int u = 0; u < units; ++u) {
+                    const int x = u & 1, v = 2 * (tiles + (QT == 1 ? u : u >> 1)) + 1, st = v % RING;
                     if (QT == 1 || x == 0) wait(&full[st], v / RING);
-                    wait(&p_full[x], cnt[x] - 1);
-                    if (ok && lane == 0) {
+                    if (u + 2 < units) keys_in(u + 2);        // ahead of the weights, which come last
+                    wait(&p_full[x], cnt[x]++);
+                    if (ok) {
                         t5::fence_after();
                         const uint32_t bl = (ring_lo + (uint32_t)st * (kTreeSlot >> 4)) | (kTreeVStep << 16);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)i * 8u,
-                                            t5::make_desc(bl + (uint32_t)i * (2048u >> 4)), kTreeIdescO, pu > 1 || i > 0 ? 1u : 0u);
-                        t5::commit(&pv_done[x]);
+                            t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)((i >> 2) * 64 + (i & 3) * 8),
+                                            t5::make_desc(bl + (uint32_t)i * (2048u >> 4)), kTreeIdescO, u > 1 || i > 0 ? 1u : 0u);
+                        if (u + 2 >= units) t5::commit(&o_done[x]);
                         if (QT == 1 || x == 1) t5::commit(&empty[st]);
                     }
+                    if (u + 2 < units) logits(u + 2);
                 }
+                tiles += walk.t1 - walk.t0;
+                ++seg;
             }
-            tiles += walk.t1 - walk.t0;
-            ++seg;
+            t5::commit(&sh.drained);                             // MMAs in flight end before the tensor memory is given back
+            ok = ptx::mbar_wait(&sh.drained, 0u) && ok;
+            if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
         }
-        if (lane == 0) t5::commit(&drained);                  // MMAs in flight end before the tensor memory is given back
-        ok = ptx::mbar_wait(&drained, 0u) && ok;
-        if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
     } else {
-        // ------------------------------------------------ rows: a thread is TMEM lane 32 (warp & 3) + lane of slot x
-        const int x = (warp - 2) >> 2, gt = (tid - 64) & 127;               // slot; thread of the slot's 128
+        // ------------------------------------------------ rows: two threads a row, each with half of a tile's columns
+        // Warps 2 .. 17: TMEM lanes 32 (warp & 3) + lane; groups of four warps are slot 0 columns 0 - 63, 64 - 127, slot 1 likewise.
+        const int group = (warp - 2) >> 2, x = group >> 1, hh = group & 1, gt = (tid - 64) & 255;      // gt: thread of the slot's 256
         const int row_in = (warp & 3) * 32 + lane;                           // row of the row tile
-        const uint32_t s_addr = tmem + (uint32_t)x * 256u + ((uint32_t)((warp & 3) * 32) << 16), o_addr = s_addr + 128u;
+        const uint32_t lanes = tmem + (uint32_t)x * 256u + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_addr = lanes + 64u * hh, o_addr = lanes + 128u + 64u * hh;
         const float scale2 = a.scale * 1.4426950408889634f;
-        int tiles = 0, cnt = 0;
+        int tiles = 0, cnt = 0, done = 0;                   // tiles before this segment; units and finished segments of the slot
         auto wait = [&](uint64_t* bar, int phase) {
             if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1));
             ok = __all_sync(0xffffffffu, ok);
         };
+        // the two warps that share the slot's rows 32 (warp & 3) ..
+        auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(2 + x * 4 + (warp & 3)) : "memory"); };
         while (walk.next(a, w.row_groups)) {
             const TreeSpan sp = walk.sp;
             const int l = walk.lg / a.G, g = walk.lg % a.G;
             const int rows = sp.n_q * a.r, row0 = walk.rg * QT * kTreeRows;   // live rows of the head; the group's first
-            // both slots are done with the last segment's Q before it is replaced
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            for (int i = tid - 64; i < QT * kTreeRows * 16; i += 256) {
-                const int rr = i >> 4, c = i & 15, row = row0 + rr;
-                uint4 val = make_uint4(0u, 0u, 0u, 0u);
-                if (row < rows)
-                    val = *reinterpret_cast<const uint4*>(a.q + ((((size_t)walk.s * a.M + row / a.r) * a.L + l) * a.H + (size_t)g * a.r + row % a.r) * kTreeD + c * 8);
-                *reinterpret_cast<uint4*>(smem_q + (size_t)(rr >> 7) * kTreeSlot + (size_t)(c >> 3) * kTreeHalf + (rr & 127) * 128 + (((c & 7) ^ (rr & 7)) << 4)) = val;
+            {
+                // Q: all loads first, then, once both slots are done with the last segment's, the stores
+                uint4 val[4 * QT];
+                const int c = tid & 15;
+#pragma unroll
+                for (int i = 0; i < 4 * QT; ++i) {
+                    const int row = row0 + ((tid - 64) >> 4) + 32 * i;
+                    val[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (row < rows)
+                        val[i] = *reinterpret_cast<const uint4*>(a.q + ((((size_t)walk.s * a.M + row / a.r) * a.L + l) * a.H + (size_t)g * a.r + row % a.r) * kTreeD + c * 8);
+                }
+                asm volatile("bar.sync 1, 512;" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < 4 * QT; ++i) {
+                    const int rr = ((tid - 64) >> 4) + 32 * i;
+                    *reinterpret_cast<uint4*>(smem_q + (size_t)(rr >> 7) * kTreeSlot + (size_t)(c >> 3) * kTreeHalf + (rr & 127) * 128 + (((c & 7) ^ (rr & 7)) << 4)) = val[i];
+                }
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.q_full);
             }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&q_full);
-
             const int row = row0 + (QT == 2 ? x * kTreeRows : 0) + row_in;
             const bool warp_live = row - lane < rows;                         // any row of this warp is real
             const unsigned long long bits = row < rows ? tree_bits(a, walk.s, row / a.r, sp.n_q) : 0ull;
@@ -345,14 +391,14 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const bool in_view = t < sp.view_tiles;
                 const int c0 = (in_view ? t : t - sp.view_tiles) * kTreeTile;             // first token of the tile in view or tail
                 const int n_valid = min(kTreeTile, (in_view ? sp.n_view : sp.n_tail + sp.n_q) - c0);
-                wait(&s_full[x], cnt);
-                if ((n_valid < kTreeTile || !in_view) && (QT == 1 || x == 0)) {
+                const bool masked = n_valid < kTreeTile || !in_view;
+                if (masked && (QT == 1 || x == 0)) {
                     // values nobody sees become zero; drafted values that are not finite too (the merge adds them)
                     const int v = 2 * (tiles + ti) + 1, st = v % RING;
                     wait(&full[st], v / RING);
                     unsigned char* vt = ring + (size_t)st * kTreeSlot;
                     const int first = in_view ? n_valid : min(max(sp.n_tail - c0, 0), n_valid);
-                    for (int i = first * 16 + gt; i < kTreeTile * 16; i += 128) {
+                    for (int i = first * 16 + gt; i < kTreeTile * 16; i += 256) {
                         const int rr = i >> 4, c = i & 15;
                         uint4* p = reinterpret_cast<uint4*>(vt + (size_t)(c >> 3) * kTreeHalf + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
                         uint4 val = make_uint4(0u, 0u, 0u, 0u);
@@ -372,89 +418,88 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     }
                     ptx::fence_proxy_async_smem();
                 }
+                wait(&s_full[x], cnt);
                 if (warp_live) {
                     t5::fence_after();
-                    // two sweeps over the 128 logits, 32 columns at a time: the maximum, then the weights.  (Held in registers in
-                    // between they spill; a second read of tensor memory is cheaper.)
-                    const bool masked = n_valid < kTreeTile || !in_view;
-                    uint32_t word[4];
+                    // Two sweeps over the thread's 64 logits, 32 at a time: the maximum, then the weights.  (All 64 held in between cost
+                    // registers that spill, and a spill is slow here: shared memory leaves the L1 no room for it.)
+                    uint32_t word[2] = {0xffffffffu, 0xffffffffu};
                     if (masked) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int left = n_valid - 32 * c;
+                        for (int c = 0; c < 2; ++c) {
+                            const int left = n_valid - 64 * hh - 32 * c;
                             word[c] = in_view ? (left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u)
-                                              : tail_word(c0 + 32 * c, sp.n_tail, bits);
+                                              : tail_word(c0 + 64 * hh + 32 * c, sp.n_tail, bits);
                         }
                     }
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t sv[32];
+                    auto logits = [&](int c, uint32_t (&sv)[32]) {
                         t5::ld32_issue(s_addr + 32u * c, sv);
                         t5::ld_wait(sv);
-                        if (MASS && in_view && row < rows) {
-                            float* lp = w.logits + (((size_t)walk.s * LG + walk.lg) * a.rows + row) * a.cap + c0 + 32 * c;
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4)
-                                if (32 * c + i < n_valid)
-                                    *reinterpret_cast<float4*>(lp + i) =
-                                        make_float4(__uint_as_float(sv[i]) * scale2, __uint_as_float(sv[i + 1]) * scale2,
-                                                    __uint_as_float(sv[i + 2]) * scale2, __uint_as_float(sv[i + 3]) * scale2);
-                        }
                         if (masked) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 if (!((word[c] >> i) & 1u)) sv[i] = 0xff800000u;
                         }
-                        float mc[8];                              // a tree of three-input maxima
+                    };
+                    float m2 = -INFINITY;                         // the row's largest logit in this tile, NaN if one is
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            mc[i] = fmaxf(f2::max3(__uint_as_float(sv[4 * i]), __uint_as_float(sv[4 * i + 1]), __uint_as_float(sv[4 * i + 2])), __uint_as_float(sv[4 * i + 3]));
-                        mx = f2::max3(mx, f2::max3(f2::max3(mc[0], mc[1], mc[2]), mc[3], mc[4]), f2::max3(mc[5], mc[6], mc[7]));
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t sv[32];
+                        logits(c, sv);
+                        if (MASS && in_view && row < rows) {
+                            float* lp = w.logits + (((size_t)walk.s * LG + walk.lg) * a.rows + row) * a.cap + c0 + 64 * hh + 32 * c;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                if (64 * hh + 32 * c + i < n_valid)
+                                    *reinterpret_cast<float4*>(lp + i) =
+                                        make_float4(__uint_as_float(sv[i]) * scale2, __uint_as_float(sv[i + 1]) * scale2,
+                                                    __uint_as_float(sv[i + 2]) * scale2, __uint_as_float(sv[i + 3]) * scale2);
+                        }
+                        float m[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t* e = &sv[i * 8];
+                            m[i] = f2::max3_nan(f2::max3_nan(__uint_as_float(e[0]), __uint_as_float(e[1]), __uint_as_float(e[2])),
+                                                f2::max3_nan(__uint_as_float(e[3]), __uint_as_float(e[4]), __uint_as_float(e[5])),
+                                                f2::max3_nan(__uint_as_float(e[6]), __uint_as_float(e[7]), __uint_as_float(e[7])));
+                        }
+                        m2 = f2::max3_nan(f2::max3_nan(m[0], m[1], m[2]), m[3], m2);
                     }
-                    const float m2 = mx * scale2;
-                    const bool moves = m2 > ref + kTreeSlack;                 // true for the first finite logit: ref is -inf
+                    sh.half_max[x][hh][row_in] = m2;
+                    pair_sync();
+                    m2 = scale2 * f2::max3_nan(m2, sh.half_max[x][hh ^ 1][row_in], m2);
+                    // true for the first logit that is not -inf (ref is), and for a NaN
+                    const bool moves = !(m2 <= ref + kTreeSlack) && m2 != -INFINITY;
                     if (__any_sync(0xffffffffu, moves)) {
                         const float to = moves ? m2 : ref, corr = moves ? t5::ex2(ref - to) : 1.0f;
                         if (j > 0) {
-                            // the last product into O is complete: S was issued after it
+                            // the last product into O is complete: this tile's logits were issued after it
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
-                                uint32_t ov[32];
-                                t5::ld32_issue(o_addr + 32u * c, ov);
+                                uint32_t ov[16];
+                                t5::ld16_issue(o_addr + 16u * c, ov);
                                 t5::ld_wait(ov);
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
-                                t5::st32(o_addr + 32u * c, ov);
+                                for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
+                                t5::st16(o_addr + 16u * c, ov);
                             }
                         }
                         sum *= corr;
                         ref = to;
                     }
-                    const float use = ref > -INFINITY ? ref : 0.0f;           // nothing seen yet: every weight is exp2(-inf) = 0
+                    const bool unseen = ref == -INFINITY;         // nothing seen yet: every weight is exp2(-inf) = 0
+                    const float use = unseen ? 0.0f : ref;
                     const uint64_t sc2 = f2::pk(scale2, scale2), nm2 = f2::pk(-use, -use);
                     uint64_t acc0 = f2::pk(0.0f, 0.0f), acc1 = acc0;
+                    // the polynomial has no zero and no NaN: where a weight may have to be either, the special-function unit alone
+                    const bool exact = masked || __any_sync(0xffffffffu, unseen);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < 2; ++c) {
                         uint32_t sv[32], pk[16];
-                        t5::ld32_issue(s_addr + 32u * c, sv);
-                        t5::ld_wait(sv);
-                        if (masked) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (!((word[c] >> i) & 1u)) sv[i] = 0xff800000u;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            float p0, p1;
-                            f2::unpk(f2::fma(f2::pk(sv[i], sv[i + 1]), sc2, nm2), p0, p1);
-                            p0 = t5::ex2(p0);
-                            p1 = t5::ex2(p1);
-                            if (i & 2) acc1 = f2::add(acc1, f2::pk(p0, p1)); else acc0 = f2::add(acc0, f2::pk(p0, p1));
-                            pk[i >> 1] = ptx::pack_bf16x2(p0, p1);
-                        }
-                        // columns [16 c, 16 c + 16): logits of chunks that have been read
-                        t5::st16(s_addr + 16u * c, pk);
+                        logits(c, sv);
+                        if (exact) tree_weights<0>(sv, sc2, nm2, acc0, acc1, pk);
+                        else tree_weights<kTreePoly>(sv, sc2, nm2, acc0, acc1, pk);
+                        t5::st16(s_addr + 16u * c, pk);           // over logits that this thread has read
                     }
                     float a0, a1, a2, a3;
                     f2::unpk(acc0, a0, a1);
@@ -469,22 +514,24 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
             // the segment's sums
             const size_t seg = (size_t)blockIdx.x + walk.head;
-            if (n_units > 0) wait(&pv_done[x], cnt - 1);
+            if (n_units > 0) wait(&o_done[x], done++);
             if (warp_live) {
                 t5::fence_after();
                 const size_t at = (seg * 2 + x) * w.rows_slot + row_in;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t ov[32];
                     t5::ld32_issue(o_addr + 32u * c, ov);
                     t5::ld_wait(ov);
                     if (row < rows && n_units > 0) {
-                        uint4* dst = reinterpret_cast<uint4*>(w.part_o + at * kTreeD + 32 * c);
+                        uint4* dst = reinterpret_cast<uint4*>(w.part_o + at * kTreeD + 64 * hh + 32 * c);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) dst[i] = make_uint4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
                     }
                 }
-                if (row < rows) w.part_ml[at] = make_float2(ref, sum);
+                if (hh == 1) sh.half_max[x][1][row_in] = sum;
+                pair_sync();
+                if (hh == 0 && row < rows) w.part_ml[at] = make_float2(ref, sum + sh.half_max[x][1][row_in]);
                 t5::fence_before();
             }
             cleared = __any_sync(0xffffffffu, cleared);
@@ -513,35 +560,48 @@ tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
     if (m >= sp.n_q) return;
     const int in_group = w.row_tiles * kTreeRows, rg = row / in_group, rr = row % in_group;
     const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
-    float top = -INFINITY, z = 0.0f, acc = 0.0f;
-    unsigned long long nf = 0;
+    const int lane = col & 31;
+    float z = 0.0f, acc = 0.0f, top = -INFINITY;
+    bool nf = false;
     if (sp.tiles > 0) {
         const long long total = w.start[a.ns], first = w.start[s] + ((long long)lg * w.row_groups + rg) * sp.tiles;
         const int n = (int)min((long long)n_ctas, total);
         const int c0 = tile_owner(first, total, n), c1 = tile_owner(first + sp.tiles - 1, total, n);
-        const size_t head = ((size_t)s * LG + lg) * w.row_groups + rg;
-        const int per = w.row_tiles == 1 ? 2 : 1;                         // one row tile: both slots hold a share of every row
-        const int parts = (c1 - c0 + 1) * per;
-        auto where = [&](int i) { return ((c0 + i / per + head) * 2 + (per == 2 ? i % 2 : rr >> 7)) * w.rows_slot + (rr & 127); };
-        for (int i = 0; i < parts; ++i) top = fmaxf(top, w.part_ml[where(i)].x);
-        for (int i = 0; i < parts; i += 4) {
-            float2 ml[4];
-            float po[4];
+        const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
+        // one row tile: both slots hold a share of every row; two: slot rr / 128 does
+        const int per = w.row_tiles == 1 ? 2 : 1, parts = (c1 - c0 + 1) * per;
+        const size_t at0 = (seg * 2 + (per == 1 ? rr >> 7 : 0)) * w.rows_slot + (rr & 127), step = (size_t)(3 - per) * w.rows_slot;
+        // every warp takes the statistics of 32 shares at a time, a lane each, and rescales what it has when the maximum grows
+        for (int i0 = 0; i0 < parts; i0 += 32) {
+            const int left = min(32, parts - i0);
+            const float2 ml = lane < left ? w.part_ml[at0 + (size_t)(i0 + lane) * step] : make_float2(-INFINITY, 0.0f);
+            float mx = ml.x;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const size_t at = where(min(i + u, parts - 1));
-                ml[u] = w.part_ml[at];
-                po[u] = w.part_o[at * kTreeD + col];
-            }
+            for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+            const float to = fmaxf(top, mx);
+            const bool holds = ml.x > -INFINITY || ml.y != 0.0f;         // a share without a visible token holds no sums
+            const float f = holds ? t5::ex2(ml.x - to) : 0.0f, back = top > -INFINITY ? t5::ex2(top - to) : 1.0f;
+            acc *= back;
+            z *= back;
+            top = to;
+            const uint32_t live = __ballot_sync(0xffffffffu, holds);
+            for (int u0 = 0; u0 < left; u0 += 8) {
+                float po[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (i + u < parts && (ml[u].x > -INFINITY || ml[u].y != 0.0f)) {    // a share without a visible token holds no sums
-                    const float f = t5::ex2(ml[u].x - top);
-                    acc += f * po[u];
-                    z += f * ml[u].y;
+                for (int u = 0; u < 8; ++u) po[u] = (live >> min(u0 + u, 31)) & 1u && u0 + u < left ? w.part_o[(at0 + (size_t)(i0 + u0 + u) * step) * kTreeD + col] : 0.0f;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int src = min(u0 + u, 31);
+                    const float fu = __shfl_sync(0xffffffffu, f, src), lu = __shfl_sync(0xffffffffu, ml.y, src);
+                    if (u0 + u < left && ((live >> src) & 1u)) {
+                        acc += fu * po[u];
+                        z += fu * lu;
+                    }
                 }
+            }
         }
-        for (int c = c0; c <= c1; ++c) nf |= w.part_nf[c + head];
+        for (int c = lane; c <= c1 - c0; c += 32) nf |= (w.part_nf[seg + c].x | w.part_nf[seg + c].y) != 0;
+        nf = __any_sync(0xffffffffu, nf);
     }
     const bool none = z == 0.0f;
     float out = none ? 0.0f : acc / z;
@@ -597,7 +657,7 @@ static size_t plan_tree(const kvmem_pool_config_t& c, int n_sessions, int M, int
     auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return base ? base + at : nullptr; };
     w->part_o = (float*)take(segs * 2 * w->rows_slot * kTreeD * sizeof(float));
     w->part_ml = (float2*)take(segs * 2 * w->rows_slot * sizeof(float2));
-    w->part_nf = (unsigned long long*)take(segs * 8);
+    w->part_nf = (ulonglong2*)take(segs * sizeof(ulonglong2));
     w->start = (long long*)take(((size_t)n_sessions + 1) * 8);
     w->lse2 = mass_cap ? (float*)take(heads * rows * sizeof(float)) : nullptr;
     w->logits = mass_cap ? (float*)take(heads * rows * mass_cap * sizeof(float)) : nullptr;

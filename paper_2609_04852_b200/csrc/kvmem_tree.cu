@@ -51,15 +51,22 @@ constexpr uint32_t kTreeVStep = (uint32_t)kTreeHalf >> 4;      // leading offset
 struct TreeSpan {
     int n_view, n_tail, n_q;      // view tokens, committed tail tokens, drafted tokens of the session
     int view_tiles, tiles;        // tiles of the view, tiles of view and tail
+    int groups;                   // row groups per KV head: up to two row tiles each
+};
+
+// what the merge needs to know of a session; entry ns holds the total in `start`
+struct TreeInfo {
+    long long start;              // first tile of the session on the line
+    int tiles, groups, n_q, n_tail;
 };
 
 struct TreeWork {
     TreeArgs a;
-    int row_tiles, row_groups, rows_slot;   // row tiles per CTA (1, 2), groups of them per head, rows stored per slot
+    int row_groups, rows_slot;    // most row groups a head can have, rows stored per slot
     float* part_o;                // [segment][slot][rows_slot][128]
     float2* part_ml;              // [segment][slot][rows_slot]: (reference, sum of weights), log2 domain
     ulonglong2* part_nf;          // [segment]: a byte per row warp, set where it cleared a drafted value that is not finite
-    long long* start;             // [ns + 1]: tiles of the sessions before, in head units; filled by CTA 0
+    TreeInfo* info;               // [ns + 1], filled by CTA 0
     float* lse2;                  // [ns][LG][rows]: log-sum-exp in the log2 domain (weights only)
     float* logits;                // [ns][LG][rows][cap]: scaled logits, log2 domain (weights only)
 };
@@ -75,6 +82,7 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& a, int s, bool rep
         if (report && t.n_tail != n) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
     }
     t.view_tiles = (t.n_view + kTreeTile - 1) / kTreeTile;
+    t.groups = (t.n_q * a.r + 2 * kTreeRows - 1) / (2 * kTreeRows);
     t.tiles = t.n_q > 0 ? t.view_tiles + (a.tail_k ? (t.n_tail + t.n_q + kTreeTile - 1) / kTreeTile : 0) : 0;
     return t;
 }
@@ -93,26 +101,34 @@ __device__ __forceinline__ uint32_t tail_word(int c0, int n_tail, unsigned long 
     return committed | drafted;
 }
 
+// row tiles of row group rg when the session has `rows` live rows: with one, the slots take tiles in turn
+__device__ __forceinline__ int tree_row_tiles(int rows, int rg) { return rows - rg * 2 * kTreeRows > kTreeRows ? 2 : 1; }
+
 // CTA that holds tile x of the line: tiles [total c / n, total (c + 1) / n) are CTA c's
-__device__ __forceinline__ int tile_owner(long long x, long long total, int n) { return (int)(((x + 1) * n - 1) / total); }
+__device__ __forceinline__ int tile_owner(long long x, long long total, int n) {
+    const unsigned long long num = (unsigned long long)(x + 1) * n - 1;
+    return num < (1ull << 32) ? (int)((unsigned)num / (unsigned)total) : (int)(num / (unsigned long long)total);
+}
 
 // a role's walk over the CTA's segments
 struct TreeWalk {
     long long pos, end, base;     // next tile on the line, the CTA's end, first tile of session s
-    int s, lg, rg, head, t0, t1;  // the segment: tiles [t0, t1) of head `head`
+    int s, lg, rg, head, t0, t1;  // the segment: tiles [t0, t1) of head `head` (a row group of a KV head)
+    int qt;                       // its row tiles
     TreeSpan sp;
-    __device__ __forceinline__ bool next(const TreeArgs& a, int groups) {
+    __device__ __forceinline__ bool next(const TreeArgs& a, int most_groups) {
         if (pos >= end) return false;
-        const int heads = a.L * a.G * groups;
+        const int LG = a.L * a.G;
         sp = tree_span(a, s, false);
-        while (base + (long long)sp.tiles * heads <= pos) {
-            base += (long long)sp.tiles * heads;
+        while (base + (long long)sp.tiles * sp.groups * LG <= pos) {
+            base += (long long)sp.tiles * sp.groups * LG;
             sp = tree_span(a, ++s, false);
         }
         const int at = (int)((pos - base) / sp.tiles);
-        lg = at / groups;
-        rg = at % groups;
-        head = s * heads + at;
+        lg = at / sp.groups;
+        rg = at % sp.groups;
+        head = (s * LG + lg) * most_groups + rg;
+        qt = tree_row_tiles(sp.n_q * a.r, rg);
         t0 = (int)(pos - base - (long long)at * sp.tiles);
         t1 = (int)min((long long)sp.tiles, t0 + (end - pos));
         pos += t1 - t0;
@@ -184,17 +200,21 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (warp == 0) {
         // the CTA's part of the line, and the session it starts in
         long long sum = 0;
-        for (int s = lane; s < a.ns; s += 32) sum += tree_span(a, s, blockIdx.x == 0).tiles;
+        for (int s = lane; s < a.ns; s += 32) {
+            const TreeSpan sp = tree_span(a, s, blockIdx.x == 0);
+            sum += (long long)sp.tiles * sp.groups;
+        }
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        const int heads = LG * w.row_groups;
-        const long long total = sum * heads;
+        const long long total = sum * LG;
         const int n = (int)min((long long)gridDim.x, total);
         const bool idle = (int)blockIdx.x >= n;
         const long long begin = idle ? 0 : total * blockIdx.x / n, end = idle ? 0 : total * (blockIdx.x + 1) / n;
         long long before = 0;
         for (int s0 = 0; s0 < a.ns; s0 += 32) {
             const int s = s0 + lane;
-            const long long mine = s < a.ns ? (long long)tree_span(a, s, false).tiles * heads : 0;
+            TreeSpan sp{};
+            if (s < a.ns) sp = tree_span(a, s, false);
+            const long long mine = (long long)sp.tiles * sp.groups * LG;
             long long incl = mine;
             for (int d = 1; d < 32; d <<= 1) {
                 const long long up = __shfl_up_sync(0xffffffffu, incl, d);
@@ -202,11 +222,11 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
             const long long lo = before + incl - mine;
             if (begin >= lo && begin < lo + mine) { sh.plan_s = s; sh.plan_base = lo; }
-            if (blockIdx.x == 0 && s < a.ns) w.start[s] = lo;
+            if (blockIdx.x == 0 && s < a.ns) w.info[s] = TreeInfo{lo, sp.tiles, sp.groups, sp.n_q, sp.n_tail};
             before += __shfl_sync(0xffffffffu, incl, 31);
             if (blockIdx.x != 0 && (idle || before > begin)) break;
         }
-        if (lane == 0) { sh.plan_begin = begin; sh.plan_end = end; if (blockIdx.x == 0) w.start[a.ns] = total; }
+        if (lane == 0) { sh.plan_begin = begin; sh.plan_end = end; if (blockIdx.x == 0) w.info[a.ns].start = total; }
     }
     t5::fence_before();
     __syncthreads();
@@ -293,32 +313,34 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
             int tiles = 0, seg = 0, cnt[2] = {0, 0};          // tiles before this segment; units so far per slot
             auto wait = [&](uint64_t* bar, int phase) { if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1)); };
+            bool two = false;                                 // two row tiles: units are (tile, row tile), else tiles
             auto keys_in = [&](int u) {                       // the key tile of unit u has landed
-                const int k = 2 * (tiles + (QT == 1 ? u : u >> 1));
-                if (QT == 1 || (u & 1) == 0) wait(&full[k % RING], k / RING);
+                const int k = 2 * (tiles + (two ? u >> 1 : u));
+                if (!two || (u & 1) == 0) wait(&full[k % RING], k / RING);
             };
             auto logits = [&](int u) {                        // S of unit u: slot u & 1
-                const int x = u & 1, k = 2 * (tiles + (QT == 1 ? u : u >> 1)), st = k % RING;
+                const int x = u & 1, k = 2 * (tiles + (two ? u >> 1 : u)), st = k % RING;
                 if (!ok) return;
                 t5::fence_after();
-                const uint32_t al = q_lo + (QT == 2 ? (uint32_t)x * (kTreeSlot >> 4) : 0u), bl = ring_lo + (uint32_t)st * (kTreeSlot >> 4);
+                const uint32_t al = q_lo + (two ? (uint32_t)x * (kTreeSlot >> 4) : 0u), bl = ring_lo + (uint32_t)st * (kTreeSlot >> 4);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t o = (uint32_t)(i >> 2) * (kTreeHalf >> 4) + (uint32_t)(i & 3) * 2u;
                     t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kTreeIdescS, i > 0 ? 1u : 0u);
                 }
                 t5::commit(&s_full[x]);
-                if (QT == 1 || x == 1) t5::commit(&empty[st]);
+                if (!two || x == 1) t5::commit(&empty[st]);
             };
             while (walk.next(a, w.row_groups)) {
-                const int units = (walk.t1 - walk.t0) * QT;   // (tile, row tile) or tiles
+                two = QT == 2 && walk.qt == 2;
+                const int units = (walk.t1 - walk.t0) * (two ? 2 : 1);
                 wait(&sh.q_full, seg);
                 keys_in(0);
                 logits(0);
                 if (units > 1) { keys_in(1); logits(1); }
                 for (int u = 0; u < units; ++u) {
-                    const int x = u & 1, v = 2 * (tiles + (QT == 1 ? u : u >> 1)) + 1, st = v % RING;
-                    if (QT == 1 || x == 0) wait(&full[st], v / RING);
+                    const int x = u & 1, v = 2 * (tiles + (two ? u >> 1 : u)) + 1, st = v % RING;
+                    if (!two || x == 0) wait(&full[st], v / RING);
                     if (u + 2 < units) keys_in(u + 2);        // ahead of the weights, which come last
                     wait(&p_full[x], cnt[x]++);
                     if (ok) {
@@ -329,7 +351,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)((i >> 2) * 64 + (i & 3) * 8),
                                             t5::make_desc(bl + (uint32_t)i * (2048u >> 4)), kTreeIdescO, u > 1 || i > 0 ? 1u : 0u);
                         if (u + 2 >= units) t5::commit(&o_done[x]);
-                        if (QT == 1 || x == 1) t5::commit(&empty[st]);
+                        if (!two || x == 1) t5::commit(&empty[st]);
                     }
                     if (u + 2 < units) logits(u + 2);
                 }
@@ -358,7 +380,8 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         while (walk.next(a, w.row_groups)) {
             const TreeSpan sp = walk.sp;
             const int l = walk.lg / a.G, g = walk.lg % a.G;
-            const int rows = sp.n_q * a.r, row0 = walk.rg * QT * kTreeRows;   // live rows of the head; the group's first
+            const int rows = sp.n_q * a.r, row0 = walk.rg * 2 * kTreeRows;    // live rows of the head; the group's first
+            const bool two = QT == 2 && walk.qt == 2;
             {
                 // Q: all loads first, then, once both slots are done with the last segment's, the stores
                 uint4 val[4 * QT];
@@ -380,19 +403,19 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&sh.q_full);
             }
-            const int row = row0 + (QT == 2 ? x * kTreeRows : 0) + row_in;
+            const int row = row0 + (two ? x * kTreeRows : 0) + row_in;
             const bool warp_live = row - lane < rows;                         // any row of this warp is real
             const unsigned long long bits = row < rows ? tree_bits(a, walk.s, row / a.r, sp.n_q) : 0ull;
             float ref = -INFINITY, sum = 0.0f;
             bool cleared = false;
-            const int n_units = QT == 1 ? (walk.t1 - walk.t0 + 1 - x) >> 1 : walk.t1 - walk.t0;
+            const int n_units = two ? walk.t1 - walk.t0 : (walk.t1 - walk.t0 + 1 - x) >> 1;
             for (int j = 0; j < n_units; ++j) {
-                const int ti = QT == 1 ? 2 * j + x : j, t = walk.t0 + ti;
+                const int ti = two ? j : 2 * j + x, t = walk.t0 + ti;
                 const bool in_view = t < sp.view_tiles;
                 const int c0 = (in_view ? t : t - sp.view_tiles) * kTreeTile;             // first token of the tile in view or tail
                 const int n_valid = min(kTreeTile, (in_view ? sp.n_view : sp.n_tail + sp.n_q) - c0);
                 const bool masked = n_valid < kTreeTile || !in_view;
-                if (masked && (QT == 1 || x == 0)) {
+                if (masked && (!two || x == 0)) {
                     // values nobody sees become zero; drafted values that are not finite too (the merge adds them)
                     const int v = 2 * (tiles + ti) + 1, st = v % RING;
                     wait(&full[st], v / RING);
@@ -555,21 +578,23 @@ tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
     pdl_trigger();
     const TreeArgs& a = w.a;
     const int LG = a.L * a.G, row = blockIdx.y, hz = blockIdx.x, s = hz / LG, lg = hz % LG, col = threadIdx.x;
-    const TreeSpan sp = tree_span(a, s, false);
+    const TreeInfo in = w.info[s];
+    const long long total = w.info[a.ns].start;
     const int m = row / a.r;
-    if (m >= sp.n_q) return;
-    const int in_group = w.row_tiles * kTreeRows, rg = row / in_group, rr = row % in_group;
+    if (m >= in.n_q) return;
+    const int rg = row / (2 * kTreeRows), rr = row % (2 * kTreeRows);
     const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
     const int lane = col & 31;
     float z = 0.0f, acc = 0.0f, top = -INFINITY;
     bool nf = false;
-    if (sp.tiles > 0) {
-        const long long total = w.start[a.ns], first = w.start[s] + ((long long)lg * w.row_groups + rg) * sp.tiles;
+    if (in.tiles > 0) {
+        const long long first = in.start + ((long long)lg * in.groups + rg) * in.tiles;
         const int n = (int)min((long long)n_ctas, total);
-        const int c0 = tile_owner(first, total, n), c1 = tile_owner(first + sp.tiles - 1, total, n);
+        const int c0 = tile_owner(first, total, n), c1 = tile_owner(first + in.tiles - 1, total, n);
         const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
+        for (int c = lane; c <= c1 - c0; c += 32) { const ulonglong2 f = w.part_nf[seg + c]; nf |= (f.x | f.y) != 0; }
         // one row tile: both slots hold a share of every row; two: slot rr / 128 does
-        const int per = w.row_tiles == 1 ? 2 : 1, parts = (c1 - c0 + 1) * per;
+        const int per = tree_row_tiles(in.n_q * a.r, rg) == 1 ? 2 : 1, parts = (c1 - c0 + 1) * per;
         const size_t at0 = (seg * 2 + (per == 1 ? rr >> 7 : 0)) * w.rows_slot + (rr & 127), step = (size_t)(3 - per) * w.rows_slot;
         // every warp takes the statistics of 32 shares at a time, a lane each, and rescales what it has when the maximum grows
         for (int i0 = 0; i0 < parts; i0 += 32) {
@@ -585,32 +610,30 @@ tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
             z *= back;
             top = to;
             const uint32_t live = __ballot_sync(0xffffffffu, holds);
-            for (int u0 = 0; u0 < left; u0 += 8) {
-                float po[8];
+            for (int u0 = 0; u0 < left; u0 += 16) {
+                float po[16];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) po[u] = (live >> min(u0 + u, 31)) & 1u && u0 + u < left ? w.part_o[(at0 + (size_t)(i0 + u0 + u) * step) * kTreeD + col] : 0.0f;
+                for (int u = 0; u < 16; ++u) po[u] = (live >> (u0 + u)) & 1u ? w.part_o[(at0 + (size_t)(i0 + u0 + u) * step) * kTreeD + col] : 0.0f;
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int src = min(u0 + u, 31);
-                    const float fu = __shfl_sync(0xffffffffu, f, src), lu = __shfl_sync(0xffffffffu, ml.y, src);
-                    if (u0 + u < left && ((live >> src) & 1u)) {
+                for (int u = 0; u < 16; ++u) {
+                    const float fu = __shfl_sync(0xffffffffu, f, u0 + u), lu = __shfl_sync(0xffffffffu, ml.y, u0 + u);
+                    if ((live >> (u0 + u)) & 1u) {
                         acc += fu * po[u];
                         z += fu * lu;
                     }
                 }
             }
         }
-        for (int c = lane; c <= c1 - c0; c += 32) nf |= (w.part_nf[seg + c].x | w.part_nf[seg + c].y) != 0;
         nf = __any_sync(0xffffffffu, nf);
     }
     const bool none = z == 0.0f;
     float out = none ? 0.0f : acc / z;
     if (nf) {
         // drafted values that are not finite were left out: they reach the rows that see them here
-        const unsigned long long bits = tree_bits(a, s, m, sp.n_q);
-        for (int j = 0; j < sp.n_q; ++j)
+        const unsigned long long bits = tree_bits(a, s, m, in.n_q);
+        for (int j = 0; j < in.n_q; ++j)
             if ((bits >> j) & 1) {
-                const float v = __bfloat162float(a.tail_v[(((size_t)s * a.tail_cap + sp.n_tail + j) * LG + lg) * kTreeD + col]);
+                const float v = __bfloat162float(a.tail_v[(((size_t)s * a.tail_cap + in.n_tail + j) * LG + lg) * kTreeD + col]);
                 if (!isfinite(v)) out += v;
             }
     }
@@ -649,8 +672,7 @@ tree_mass_kernel(const __grid_constant__ TreeWork w) {
 // sizes and places inside the workspace; base null: sizes alone
 static size_t plan_tree(const kvmem_pool_config_t& c, int n_sessions, int M, int mass_cap, char* base, TreeWork* w) {
     const int rows = M * (c.n_q_heads / c.n_kv_heads);
-    w->row_tiles = rows <= kTreeRows ? 1 : 2;
-    w->row_groups = (rows + w->row_tiles * kTreeRows - 1) / (w->row_tiles * kTreeRows);
+    w->row_groups = (rows + 2 * kTreeRows - 1) / (2 * kTreeRows);
     w->rows_slot = std::min(rows, kTreeRows);
     const size_t heads = (size_t)n_sessions * c.n_layers * c.n_kv_heads, segs = heads * w->row_groups + kSMs;
     size_t off = 0;
@@ -658,7 +680,7 @@ static size_t plan_tree(const kvmem_pool_config_t& c, int n_sessions, int M, int
     w->part_o = (float*)take(segs * 2 * w->rows_slot * kTreeD * sizeof(float));
     w->part_ml = (float2*)take(segs * 2 * w->rows_slot * sizeof(float2));
     w->part_nf = (ulonglong2*)take(segs * sizeof(ulonglong2));
-    w->start = (long long*)take(((size_t)n_sessions + 1) * 8);
+    w->info = (TreeInfo*)take(((size_t)n_sessions + 1) * sizeof(TreeInfo));
     w->lse2 = mass_cap ? (float*)take(heads * rows * sizeof(float)) : nullptr;
     w->logits = mass_cap ? (float*)take(heads * rows * mass_cap * sizeof(float)) : nullptr;
     return off;
@@ -716,8 +738,8 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), most);
     cudaError_t e;
     if (a.mass) e = launch_split<1, false, true>(p, grid, st, m, w);            // at most 64 rows
-    else if (paged) e = w.row_tiles == 1 ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);
-    else e = w.row_tiles == 1 ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
+    else if (paged) e = a.rows <= kTreeRows ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);
+    else e = a.rows <= kTreeRows ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
     if (e != cudaSuccess) return e;
     e = launch_pdl(tree_merge_kernel, dim3((unsigned)(a.ns * LG), (unsigned)a.rows), dim3(kTreeD), 0, st, w, grid);
     if (e != cudaSuccess || !a.mass) return e;

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import List, Optional, Sequence, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -231,8 +231,10 @@ class Pool:
         self._host_ws: Optional[torch.Tensor] = None
         self._host_staging: Optional[torch.Tensor] = None
         self._staging: Optional[torch.Tensor] = None
-        self._decode_ws: Optional[torch.Tensor] = None
+        self._dims = (n_layers, n_q_heads, n_kv_heads, head_dim)
+        self._decode_ws: Optional[Tuple[int, int]] = None              # pointer and bytes of the newest
         self._decode_ws_all: List[torch.Tensor] = []
+        self._decode_need: Dict[tuple, int] = {}
 
     # ---- lifetime
     def close(self) -> None:
@@ -418,47 +420,56 @@ class Pool:
                                           ws.data_ptr(), ws.numel(), _stream()))
 
     # ---- decode over a view: drafted tokens, accumulated weights, eviction
+    # These calls run once per decoded token, on views that may take a few microseconds: their checks are kept short.
     def _place(self, name: str, t: torch.Tensor, dtype, shape) -> int:
         """Pointer of a contiguous tensor of this dtype and shape on the pool's device; ValueError for any other."""
-        if not t.is_cuda or t.device != self.device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {self.device}, got "
                              f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (strided)'}")
         return t.data_ptr()
 
-    def _decode_workspace(self, need: int, workspace: Optional[torch.Tensor]) -> Tuple[int, int]:
-        if need == 0:
-            raise KvmemError(E_INVALID, self.lib.kvmem_last_error().decode())
+    def _decode_workspace(self, sizer, key, workspace: Optional[torch.Tensor]) -> Tuple[int, int]:
+        """sizer(cfg, *key) bytes: the caller's tensor, or the pool's own."""
         if workspace is not None:
             return self._place("workspace", workspace, torch.uint8, (workspace.numel(),)), workspace.numel()
-        if self._decode_ws is None or self._decode_ws.numel() < need:
+        need = self._decode_need.get((sizer.__name__, key))
+        if need is None:
+            need = sizer(C.byref(self.cfg), *key)
+            if need == 0:
+                raise KvmemError(E_INVALID, self.lib.kvmem_last_error().decode())
+            self._decode_need[(sizer.__name__, key)] = need
+        if self._decode_ws is None or self._decode_ws[1] < need:
             # a captured graph may still replay on a smaller one, so those are kept; each is at least twice the one before
-            size = need if self._decode_ws is None else max(need, 2 * self._decode_ws.numel())
+            size = need if self._decode_ws is None else max(need, 2 * self._decode_ws[1])
             self._decode_ws_all.append(torch.empty(size, dtype=torch.uint8, device=self.device))
-            self._decode_ws = self._decode_ws_all[-1]
-        return self._decode_ws.data_ptr(), self._decode_ws.numel()
+            self._decode_ws = (self._decode_ws_all[-1].data_ptr(), size)
+        return self._decode_ws
 
     def _decode_common(self, q, n_sel, tail, out, lse, n_q):
-        c = self.cfg
+        L, H, G, d = self._dims
         if q.dim() != 5:
             raise ValueError("q: expected [n_sessions][n_q_tokens][L][H][d]")
-        ns, M = q.shape[:2]
-        shape = (ns, M, c.n_layers, c.n_q_heads, c.head_dim)
-        qp = self._place("q", q, torch.bfloat16, shape)
-        np_ = self._place("n_sel", n_sel, torch.int32, (ns,))
-        op, lp = self._place("out", out, torch.bfloat16, shape), self._place("lse", lse, torch.float32, shape[:4])
-        nq = None if n_q is None else self._place("n_q", n_q, torch.int32, (ns,))
+        ns, M = q.shape[0], q.shape[1]
+        shape, place = (ns, M, L, H, d), self._place
+        qp = place("q", q, torch.bfloat16, shape)
+        np_ = place("n_sel", n_sel, torch.int32, (ns,))
+        op, lp = place("out", out, torch.bfloat16, shape), place("lse", lse, torch.float32, shape[:4])
+        nq = None if n_q is None else place("n_q", n_q, torch.int32, (ns,))
         tp = None
         if tail is not None:
             cap = tail.k.shape[1] if tail.k.dim() == 5 else -1
-            ts = (ns, cap, c.n_layers, c.n_kv_heads, c.head_dim)
-            tp = C.byref(TailStruct(self._place("tail.k", tail.k, torch.bfloat16, ts), self._place("tail.v", tail.v, torch.bfloat16, ts),
-                                    cap, self._place("tail.n_tokens", tail.n_tokens, torch.int32, (ns,))))
+            ts = (ns, cap, L, G, d)
+            tp = C.byref(TailStruct(place("tail.k", tail.k, torch.bfloat16, ts), place("tail.v", tail.v, torch.bfloat16, ts),
+                                    cap, place("tail.n_tokens", tail.n_tokens, torch.int32, (ns,))))
         return ns, M, qp, np_, tp, op, lp, nq
 
     def _view_of(self, name: str, view: View, ns: int) -> Tuple[int, int, int]:
-        c = self.cfg
-        shape = (ns, c.n_layers, c.n_kv_heads, view.cap_tokens, c.head_dim)
-        return self._place(name + ".k", view.k, torch.bfloat16, shape), self._place(name + ".v", view.v, torch.bfloat16, shape), view.cap_tokens
+        L, _, G, d = self._dims
+        shape = (ns, L, G, view.cap_tokens, d)
+        return self._place(name, view.k, torch.bfloat16, shape), self._place(name, view.v, torch.bfloat16, shape), view.cap_tokens
+
+    def _raw_stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def view_tree_attend(self, q: torch.Tensor, view: View, n_sel: torch.Tensor, tail: Optional[Tail], out: torch.Tensor,
                          lse: torch.Tensor, mask: Optional[torch.Tensor] = None, n_q: Optional[torch.Tensor] = None,
@@ -470,8 +481,8 @@ class Pool:
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         vk, vv, cap = self._view_of("view", view, ns)
         mp = None if mask is None else self._place("mask", mask, torch.int64, (ns, M))
-        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes(C.byref(self.cfg), ns, M), workspace)
-        _check(self.lib.kvmem_view_tree_attend(self.handle, ns, qp, M, nq, mp, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, _stream()))
+        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace)
+        _check(self.lib.kvmem_view_tree_attend(self.handle, ns, qp, M, nq, mp, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, self._raw_stream()))
 
     def paged_tree_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, tail: Optional[Tail],
                           out: torch.Tensor, lse: torch.Tensor, mask: Optional[torch.Tensor] = None,
@@ -481,22 +492,22 @@ class Pool:
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         sp = self._place("sel_ids", sel_ids, torch.int32, (ns, sel_ids.shape[-1]))
         mp = None if mask is None else self._place("mask", mask, torch.int64, (ns, M))
-        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes(C.byref(self.cfg), ns, M), workspace)
+        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace)
         _check(self.lib.kvmem_paged_tree_attend(self.handle, session_first, ns, qp, M, nq, mp, sp, sel_ids.shape[-1], np_, tp,
-                                                scale, op, lp, wp, wn, _stream()))
+                                                scale, op, lp, wp, wn, self._raw_stream()))
 
     def view_attend_mass(self, q: torch.Tensor, view: View, n_sel: torch.Tensor, mass: torch.Tensor, out: torch.Tensor,
                          lse: torch.Tensor, tail: Optional[Tail] = None, n_q: Optional[torch.Tensor] = None, decay: float = 1.0,
                          scale: float = 0.0, workspace: Optional[torch.Tensor] = None) -> None:
         """view_tree_attend for a chain that also sets mass fp32 [n_sessions][L][G][cap_tokens] to decay * mass + the
         attention weight of each view token, summed over the query rows of its KV head (n_q_tokens * H/G <= 64)."""
-        c = self.cfg
+        L, _, G, _ = self._dims
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         vk, vv, cap = self._view_of("view", view, ns)
-        ap = self._place("mass", mass, torch.float32, (ns, c.n_layers, c.n_kv_heads, cap))
-        wp, wn = self._decode_workspace(self.lib.kvmem_mass_workspace_bytes(C.byref(self.cfg), ns, M, cap), workspace)
+        ap = self._place("mass", mass, torch.float32, (ns, L, G, cap))
+        wp, wn = self._decode_workspace(self.lib.kvmem_mass_workspace_bytes, (ns, M, cap), workspace)
         _check(self.lib.kvmem_view_attend_mass(self.handle, ns, qp, M, nq, vk, vv, cap, np_, tp, scale, ap, decay, op, lp, wp, wn,
-                                               _stream()))
+                                               self._raw_stream()))
 
     def view_evict(self, view: View, n_sel: torch.Tensor, mass: torch.Tensor, dst: View, n_sel_out: torch.Tensor,
                    dst_mass: torch.Tensor, kept: Optional[torch.Tensor] = None, keep_blocks: Optional[int] = None,
@@ -504,18 +515,19 @@ class Pool:
         """Keep the keep_blocks (default: dst's capacity) * block_tokens tokens of each KV head with the largest mass,
         the first n_sink_tokens and last n_recent_tokens among them, and move them in order to dst; n_sel_out int32
         [n_sessions] receives dst's lengths in blocks, kept int32 [n_sessions][L][G][keep_blocks * B] the tokens' places."""
-        c = self.cfg
+        L, _, G, _ = self._dims
+        B = self.cfg.block_tokens
         ns = n_sel.shape[0]
-        keep = dst.cap_tokens // c.block_tokens if keep_blocks is None else keep_blocks
+        keep = dst.cap_tokens // B if keep_blocks is None else keep_blocks
         vk, vv, cap = self._view_of("view", view, ns)
         dk, dv, dcap = self._view_of("dst", dst, ns)
-        heads = (ns, c.n_layers, c.n_kv_heads)
+        heads = (ns, L, G)
         ap, dp = self._place("mass", mass, torch.float32, (*heads, cap)), self._place("dst_mass", dst_mass, torch.float32, (*heads, dcap))
-        kp = None if kept is None else self._place("kept", kept, torch.int32, (*heads, keep * c.block_tokens))
+        kp = None if kept is None else self._place("kept", kept, torch.int32, (*heads, keep * B))
         np_, no = self._place("n_sel", n_sel, torch.int32, (ns,)), self._place("n_sel_out", n_sel_out, torch.int32, (ns,))
-        wp, wn = self._decode_workspace(self.lib.kvmem_evict_workspace_bytes(C.byref(self.cfg), ns, keep), workspace)
+        wp, wn = self._decode_workspace(self.lib.kvmem_evict_workspace_bytes, (ns, keep), workspace)
         _check(self.lib.kvmem_view_evict(self.handle, ns, vk, vv, cap, np_, ap, keep, n_sink_tokens, n_recent_tokens, dk, dv, dcap,
-                                         dp, kp, no, wp, wn, _stream()))
+                                         dp, kp, no, wp, wn, self._raw_stream()))
 
     def materialize_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, view: View,
                            out: torch.Tensor, lse: torch.Tensor, scale: float = 0.0, session_first: int = 0) -> None:

@@ -156,26 +156,4 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 }  // namespace f2
 
-// 2^x for a pair, on the FMA and integer pipes: the share of the exponentials that the special-function
-// unit (16 results per clock and SM) is spared.  x = n + f with n the nearest
-// integer and |f| <= 1/2; 2^f by a degree-4 polynomial (relative error below 3e-6), 2^n by adding n to
-// the exponent field.  Arguments below -125 (including -inf) return about 2^-125 instead of 0, which
-// is immaterial next to weights that sum to one per query row.
-__device__ __forceinline__ uint64_t ex2_poly2(uint64_t x2) {
-    float x0, x1;
-    f2::unpk(x2, x0, x1);
-    const uint64_t x = f2::pk(fmaxf(x0, -125.0f), fmaxf(x1, -125.0f));
-    const uint64_t t = f2::add(x, f2::pk(12582912.0f, 12582912.0f));         // 1.5 * 2^23: n sits in the low mantissa bits
-    const uint64_t n = f2::add(t, f2::pk(-12582912.0f, -12582912.0f));
-    const uint64_t f = f2::fma(n, f2::pk(-1.0f, -1.0f), x);                   // exact
-    uint64_t p = f2::fma(f2::pk(0.009570100344717503f, 0.009570100344717503f), f, f2::pk(0.05591785907745361f, 0.05591785907745361f));
-    p = f2::fma(p, f, f2::pk(0.240247443318367f, 0.240247443318367f));
-    p = f2::fma(p, f, f2::pk(0.6931217908859253f, 0.6931217908859253f));
-    p = f2::fma(p, f, f2::pk(0.9999992847442627f, 0.9999992847442627f));
-    uint32_t p0, p1, t0, t1;
-    f2::unpk(p, p0, p1);
-    f2::unpk(t, t0, t1);
-    return f2::pk(p0 + (t0 << 23), p1 + (t1 << 23));
-}
-
 }  // namespace kvmem

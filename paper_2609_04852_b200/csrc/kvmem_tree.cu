@@ -5,12 +5,12 @@
 // The query rows of a KV head (drafted tokens x query heads that share it) are the rows of one or two 128-row tiles, the
 // tokens come in tiles of 128: view tiles first, then tail tiles (committed and drafted tokens).  Per tile
 //     S = Q K^T   tcgen05.mma, both operands in shared memory, 128 x 128 fp32 accumulators in tensor memory
-//     P = exp2(S scale log2e - ref)   a thread per row: one TMEM lane, so maximum and sum need no shuffles
+//     P = exp2(S scale log2e - ref)   two threads per row (TMEM lane), each with half of the columns: no shuffles
 //     O += P V    tcgen05.mma, P as bf16 in tensor memory (in the place of S), V from shared memory
 // Two slots (S, P and O each: 2 x 256 columns, all of tensor memory) keep the tensor pipe and the special-function unit
 // busy in turn: with up to 128 rows the slots take tiles alternately and are merged at the end like two splits; with more
-// rows slot w is row tile w and both read the same K and V tile.  One warp fetches tiles with TMA (128-byte swizzle) into a
-// ring of 32 KiB slots, one issues the MMAs, eight hold the rows.
+// rows slot w is row tile w and both read the same K and V tile.  Two warps fetch tiles with TMA (128-byte swizzle), one the
+// keys and one the values, into a ring of 32 KiB slots, one thread issues the MMAs, sixteen warps hold the rows.
 //
 // ref is a running maximum that moves only when a row's logits pass it by 8 (in powers of two): O is then rescaled in
 // tensor memory.  Until then the weights may reach 2^8, which costs neither fp32 nor bf16 any precision.
@@ -39,8 +39,8 @@ constexpr int kTreeTile = 128;                    // tokens per tile
 constexpr int kTreeHalf = kTreeTile * 128;        // bytes of one 64-dim half of a 128-row operand tile (16 KiB)
 constexpr int kTreeSlot = 2 * kTreeHalf;          // a K, V or Q tile
 constexpr int kTreeRows = 128;                    // rows of a row tile: TMEM lanes
-constexpr int kTreeThreads = 64 + 512;            // TMA warp, MMA warp, sixteen row warps
-constexpr int kTreePoly = 4;                      // every n-th pair of exponentials off the special-function unit (0: none)
+constexpr int kTreeThreads = 32 * 19;              // key and value TMA warps, MMA warp, sixteen row warps
+constexpr int kTreeVWarp = 18;
 constexpr int kTreeRing1 = 6, kTreeRing2 = 5;     // ring slots beside one or two Q tiles: 224 KiB in all
 constexpr float kTreeSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
 static_assert(1 + kTreeRing1 == 2 + kTreeRing2, "both forms take the same shared memory");
@@ -110,6 +110,22 @@ __device__ __forceinline__ int tile_owner(long long x, long long total, int n) {
     return num < (1ull << 32) ? (int)((unsigned)num / (unsigned)total) : (int)(num / (unsigned long long)total);
 }
 
+// Waits for up to three phases (null: none), asked together; the last is the one that is waited for longest.
+__device__ __forceinline__ bool wait_step(uint64_t* b0, int ph0, uint64_t* b1, int ph1, uint64_t* b2, int ph2) {
+    uint64_t t0 = 0;
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+        const bool k0 = b0 == nullptr || ptx::mbar_test_wait(b0, (uint32_t)ph0), k1 = b1 == nullptr || ptx::mbar_test_wait(b1, (uint32_t)ph1);
+        const bool k2 = ptx::mbar_try_wait(b2, (uint32_t)ph2);
+        if (k0 & k1 & k2) return true;
+        if ((i & 255u) == 255u) {
+            const uint64_t now = ptx::globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > kWaitLimitNs) return false;
+        }
+    }
+    return false;
+}
+
 // a role's walk over the CTA's segments
 struct TreeWalk {
     long long pos, end, base;     // next tile on the line, the CTA's end, first tile of session s
@@ -136,20 +152,16 @@ struct TreeWalk {
     }
 };
 
-// 32 logits of a row to weights exp2(x scale2 - ref), bf16 pairs in pk; their fp32 sum goes to acc0 + acc1
-template <int POLY>
+// 32 logits of a row to weights exp2(x scale2 - ref), bf16 pairs in pk; their fp32 sum goes to acc0 + acc1.  (A quarter of the
+// exponentials as a polynomial on the FMA pipe, as chunked scoring has it, gains nothing: the unit waits for the MMAs.)
 __device__ __forceinline__ void tree_weights(const uint32_t (&sv)[32], uint64_t sc2, uint64_t nm2, uint64_t& acc0, uint64_t& acc1, uint32_t (&pk)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        uint64_t e = f2::fma(f2::pk(sv[2 * i], sv[2 * i + 1]), sc2, nm2);
         float p0, p1;
-        if (POLY > 0 && i % (POLY > 0 ? POLY : 1) == POLY - 1) e = ex2_poly2(e);
-        else {
-            f2::unpk(e, p0, p1);
-            e = f2::pk(t5::ex2(p0), t5::ex2(p1));
-        }
-        f2::unpk(e, p0, p1);
-        if (i & 1) acc1 = f2::add(acc1, e); else acc0 = f2::add(acc0, e);
+        f2::unpk(f2::fma(f2::pk(sv[2 * i], sv[2 * i + 1]), sc2, nm2), p0, p1);
+        p0 = t5::ex2(p0);
+        p1 = t5::ex2(p1);
+        if (i & 1) acc1 = f2::add(acc1, f2::pk(p0, p1)); else acc0 = f2::add(acc0, f2::pk(p0, p1));
         pk[i] = ptx::pack_bf16x2(p0, p1);
     }
 }
@@ -191,6 +203,11 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         ptx::mbar_init(&sh.drained, 1);
         ptx::fence_mbar_init();
     }
+    if (tid == 32 * kTreeVWarp) {
+        ptx::prefetch_tensormap(&map_k);
+        if (!PAGED) ptx::prefetch_tensormap(&map_v);
+        if (a.tail_k) { ptx::prefetch_tensormap(&map_tk); ptx::prefetch_tensormap(&map_tv); }
+    }
     if (warp == 1) {
         t5::tmem_alloc(&sh.tmem, 512);
         t5::tmem_relinquish();
@@ -228,25 +245,30 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
         if (lane == 0) { sh.plan_begin = begin; sh.plan_end = end; if (blockIdx.x == 0) w.info[a.ns].start = total; }
     }
+    // warp 0 has what it needs and goes on; the others wait for the plan and the tensor memory
     t5::fence_before();
-    __syncthreads();
+    if (warp == 0) {
+        __syncwarp();
+        asm volatile("bar.arrive 10, %0;" ::"n"(kTreeThreads) : "memory");
+    } else {
+        asm volatile("bar.sync 10, %0;" ::"n"(kTreeThreads) : "memory");
+    }
     t5::fence_after();
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = warp == 0 ? 0u : sh.tmem;
     TreeWalk walk;
     walk.pos = sh.plan_begin; walk.end = sh.plan_end; walk.base = sh.plan_base; walk.s = sh.plan_s;
 
     // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
     // every role still reaches its end.
     bool ok = true;
-    if (warp == 0) {
-        // ------------------------------------------------ TMA: K and V of every tile, in turn, through the ring
-        int n = 0;                                            // loads so far
-        auto slot_free = [&]() {
-            if (ok && n >= RING) ok = ptx::mbar_wait(&empty[n % RING], (uint32_t)(((n / RING) & 1) ^ 1));
-            ok = __all_sync(0xffffffffu, ok);
-        };
+    if (warp == 0 || warp == kTreeVWarp) {
+        // ------------------------------------------------ TMA: warp 0 the keys, the last warp the values, each with every second
+        // load of the ring
+        const int kv = warp == 0 ? 0 : 1;
+        const CUtensorMap *map_in = PAGED || kv == 0 ? &map_k : &map_v, *map_tail = kv ? &map_tv : &map_tk;
+        int n = kv;                                           // next load
         const int box = PAGED ? min(a.B, 64) : 64;            // tokens per copy
-        const int boxes = kTreeTile / box;
+        const int boxes = kTreeTile / box, per_block = PAGED ? max(a.B / 64, 1) : 1;     // copies per tile, per block
         while (walk.next(a, w.row_groups)) {
             const int n_box = (walk.sp.n_view + box - 1) / box;           // copies that hold view tokens
             const int b_end = min(n_box, min(walk.t1, walk.sp.view_tiles) * boxes);
@@ -254,18 +276,18 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             // page of the block that copy b reads: two dependent loads, 32 copies at a time and a batch ahead
             auto lookup = [&](int b) -> int {
                 if (!PAGED || b >= b_end) return -1;
-                const int id = a.sel_ids[(size_t)walk.s * a.sel_stride + (int)((long long)b * box / a.B)];
+                const int id = a.sel_ids[(size_t)walk.s * a.sel_stride + (per_block == 1 ? b : b / per_block)];
                 int pg = -1;
                 if (id >= 0 && id < NB) pg = a.tables[(size_t)(a.session_first + walk.s) * a.max_bps + id];
                 if (pg < 0 || pg >= a.max_blocks) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); pg = 0; }
                 return pg;                                    // a flagged id reads page 0; the status word reports it
             };
             int b0 = walk.t0 * boxes, page = lookup(b0 + lane), page_next = lookup(b0 + 32 + lane);
-            for (int t = walk.t0; t < walk.t1; ++t) {
+            const int z_view = walk.s * LG + walk.lg, row_tail = walk.s * a.tail_cap;
+            for (int t = walk.t0; t < walk.t1; ++t, n += 2) {
                 const bool in_view = t < walk.sp.view_tiles;
                 const int tt = (t - walk.sp.view_tiles) * kTreeTile;      // first tail row of a tail tile
                 const int live = in_view ? min(boxes, b_end - t * boxes) : min(2, (walk.sp.n_tail + walk.sp.n_q - tt + 63) / 64);
-                const uint32_t bytes = (uint32_t)live * (uint32_t)(in_view ? box : 64) * 256u;
                 if (PAGED && in_view && t * boxes >= b0 + 32) {
                     b0 += 32;
                     page = page_next;
@@ -273,37 +295,30 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 }
                 // in a view tile of the pages the lane that looked a copy's page up issues it, else lanes 0 and 1
                 const int u = PAGED && in_view ? b0 + lane - t * boxes : lane;
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv, ++n) {
-                    slot_free();
-                    const int st = n % RING;
-                    if (ok && lane == 0) ptx::mbar_expect_tx(&full[st], bytes);
-                    __syncwarp();
-                    if (ok && u >= 0 && u < live) {
-                        unsigned char* dst = ring + (size_t)st * kTreeSlot;
-                        if (!in_view) {
-                            const CUtensorMap* m = kv ? &map_tv : &map_tk;
-                            const int row = walk.s * a.tail_cap + tt + u * 64;
-                            ptx::tma_load_3d(dst + u * 64 * 128, m, 0, walk.lg, row, &full[st]);
-                            ptx::tma_load_3d(dst + kTreeHalf + u * 64 * 128, m, 64, walk.lg, row, &full[st]);
-                        } else if (PAGED) {
-                            // pages [page][K | V][LG] tiles of B rows of 256 B
-                            const int z = (page * 2 + kv) * LG + walk.lg, y = (int)(((long long)t * kTreeTile + u * box) % a.B);
-                            ptx::tma_load_3d(dst + u * box * 128, &map_k, 0, y, z, &full[st]);
-                            ptx::tma_load_3d(dst + kTreeHalf + u * box * 128, &map_k, 64, y, z, &full[st]);
-                        } else {
-                            const CUtensorMap* m = kv ? &map_v : &map_k;
-                            const int z = walk.s * LG + walk.lg, y = t * kTreeTile + u * 64;
-                            ptx::tma_load_3d(dst + u * 64 * 128, m, 0, y, z, &full[st]);
-                            ptx::tma_load_3d(dst + kTreeHalf + u * 64 * 128, m, 64, y, z, &full[st]);
-                        }
+                const int st = n % RING;
+                if (ok && n >= RING) ok = ptx::mbar_wait(&empty[st], (uint32_t)(((n / RING) & 1) ^ 1));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == 0) ptx::mbar_expect_tx(&full[st], (uint32_t)live * (uint32_t)(in_view ? box : 64) * 256u);
+                __syncwarp();
+                if (u >= 0 && u < live) {
+                    unsigned char* dst = ring + (size_t)st * kTreeSlot + u * (in_view ? box : 64) * 128;
+                    if (!in_view) {
+                        ptx::tma_load_3d(dst, map_tail, 0, walk.lg, row_tail + tt + u * 64, &full[st]);
+                        ptx::tma_load_3d(dst + kTreeHalf, map_tail, 64, walk.lg, row_tail + tt + u * 64, &full[st]);
+                    } else {
+                        // pages: [page][K | V][LG] tiles of B rows of 256 B
+                        const int y = PAGED ? (per_block == 1 ? 0 : (b0 + lane) % per_block * 64) : t * kTreeTile + u * 64;
+                        const int z = PAGED ? (page * 2 + kv) * LG + walk.lg : z_view;
+                        ptx::tma_load_3d(dst, map_in, 0, y, z, &full[st]);
+                        ptx::tma_load_3d(dst + kTreeHalf, map_in, 64, y, z, &full[st]);
                     }
-                    if (!ok) --n;                             // not issued
                 }
             }
+            if (!ok) break;
         }
         // the copies still in flight land before the CTA gives its shared memory back
-        for (int i = max(0, n - RING); i < n; ++i) ok = ptx::mbar_wait(&full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
+        for (int i = max(kv, n - (RING & ~1)); i < n; i += 2) ok = ptx::mbar_wait(&full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
         if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
     } else if (warp == 1) {
         // ------------------------------------------------ MMA: one thread
@@ -311,51 +326,54 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         // weights, in whose place they go.  MMAs that one thread issues run in order, so there is nothing to wait for.
         if (t5::elect()) {
             const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
-            int tiles = 0, seg = 0, cnt[2] = {0, 0};          // tiles before this segment; units so far per slot
-            auto wait = [&](uint64_t* bar, int phase) { if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1)); };
+            // Scalar code between the MMAs is latency: ring places move by addition, and the barriers of a step are asked together.
+            struct Place {
+                int st, ph;
+                __device__ __forceinline__ void next() { st += 2; if (st >= RING) { st -= RING; ph ^= 1; } }
+            } kp{0, 0}, vp{1, 0};                             // next key tile, next value tile
+            int seg = 0, p_ph[2] = {0, 0};
             bool two = false;                                 // two row tiles: units are (tile, row tile), else tiles
-            auto keys_in = [&](int u) {                       // the key tile of unit u has landed
-                const int k = 2 * (tiles + (two ? u >> 1 : u));
-                if (!two || (u & 1) == 0) wait(&full[k % RING], k / RING);
-            };
-            auto logits = [&](int u) {                        // S of unit u: slot u & 1
-                const int x = u & 1, k = 2 * (tiles + (two ? u >> 1 : u)), st = k % RING;
-                if (!ok) return;
-                t5::fence_after();
-                const uint32_t al = q_lo + (two ? (uint32_t)x * (kTreeSlot >> 4) : 0u), bl = ring_lo + (uint32_t)st * (kTreeSlot >> 4);
+            auto logits = [&](int x) {                        // S of slot x from the key tile at kp
+                if (ok) {
+                    t5::fence_after();
+                    const uint32_t al = q_lo + (two ? (uint32_t)x * (kTreeSlot >> 4) : 0u), bl = ring_lo + (uint32_t)kp.st * (kTreeSlot >> 4);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t o = (uint32_t)(i >> 2) * (kTreeHalf >> 4) + (uint32_t)(i & 3) * 2u;
-                    t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kTreeIdescS, i > 0 ? 1u : 0u);
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t o = (uint32_t)(i >> 2) * (kTreeHalf >> 4) + (uint32_t)(i & 3) * 2u;
+                        t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kTreeIdescS, i > 0 ? 1u : 0u);
+                    }
+                    t5::commit(&s_full[x]);
+                    if (!two || x == 1) t5::commit(&empty[kp.st]);
                 }
-                t5::commit(&s_full[x]);
-                if (!two || x == 1) t5::commit(&empty[st]);
+                if (!two || x == 1) kp.next();
             };
             while (walk.next(a, w.row_groups)) {
                 two = QT == 2 && walk.qt == 2;
                 const int units = (walk.t1 - walk.t0) * (two ? 2 : 1);
-                wait(&sh.q_full, seg);
-                keys_in(0);
+                if (ok) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)(seg & 1)) && ptx::mbar_wait(&full[kp.st], (uint32_t)kp.ph);
                 logits(0);
-                if (units > 1) { keys_in(1); logits(1); }
+                if (units > 1) {
+                    if (ok && !two) ok = ptx::mbar_wait(&full[kp.st], (uint32_t)kp.ph);
+                    logits(1);
+                }
                 for (int u = 0; u < units; ++u) {
-                    const int x = u & 1, v = 2 * (tiles + (two ? u >> 1 : u)) + 1, st = v % RING;
-                    if (!two || x == 0) wait(&full[st], v / RING);
-                    if (u + 2 < units) keys_in(u + 2);        // ahead of the weights, which come last
-                    wait(&p_full[x], cnt[x]++);
+                    const int x = u & 1;
+                    const bool more = u + 2 < units, fresh = !two || x == 0;           // fresh: this slot meets the tiles first
+                    if (ok) ok = wait_step(fresh ? &full[vp.st] : nullptr, vp.ph, more && fresh ? &full[kp.st] : nullptr, kp.ph, &p_full[x], p_ph[x]);
+                    p_ph[x] ^= 1;
                     if (ok) {
                         t5::fence_after();
-                        const uint32_t bl = (ring_lo + (uint32_t)st * (kTreeSlot >> 4)) | (kTreeVStep << 16);
+                        const uint32_t bl = (ring_lo + (uint32_t)vp.st * (kTreeSlot >> 4)) | (kTreeVStep << 16);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)((i >> 2) * 64 + (i & 3) * 8),
                                             t5::make_desc(bl + (uint32_t)i * (2048u >> 4)), kTreeIdescO, u > 1 || i > 0 ? 1u : 0u);
-                        if (u + 2 >= units) t5::commit(&o_done[x]);
-                        if (!two || x == 1) t5::commit(&empty[st]);
+                        if (!more) t5::commit(&o_done[x]);
+                        if (!two || x == 1) t5::commit(&empty[vp.st]);
                     }
-                    if (u + 2 < units) logits(u + 2);
+                    if (!two || x == 1) vp.next();
+                    if (more) logits(x);
                 }
-                tiles += walk.t1 - walk.t0;
                 ++seg;
             }
             t5::commit(&sh.drained);                             // MMAs in flight end before the tensor memory is given back
@@ -446,26 +464,28 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     t5::fence_after();
                     // Two sweeps over the thread's 64 logits, 32 at a time: the maximum, then the weights.  (All 64 held in between cost
                     // registers that spill, and a spill is slow here: shared memory leaves the L1 no room for it.)
-                    uint32_t word[2] = {0xffffffffu, 0xffffffffu};
+                    uint32_t word0 = 0xffffffffu, word1 = 0xffffffffu;        // visible columns, 32 each
                     if (masked) {
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
+                        auto word = [&](int c) {
                             const int left = n_valid - 64 * hh - 32 * c;
-                            word[c] = in_view ? (left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u)
-                                              : tail_word(c0 + 64 * hh + 32 * c, sp.n_tail, bits);
-                        }
+                            return in_view ? (left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u) : tail_word(c0 + 64 * hh + 32 * c, sp.n_tail, bits);
+                        };
+                        word0 = word(0);
+                        word1 = word(1);
                     }
                     auto logits = [&](int c, uint32_t (&sv)[32]) {
                         t5::ld32_issue(s_addr + 32u * c, sv);
                         t5::ld_wait(sv);
                         if (masked) {
+                            const uint32_t word = c == 0 ? word0 : word1;
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (!((word[c] >> i) & 1u)) sv[i] = 0xff800000u;
+                                if (!((word >> i) & 1u)) sv[i] = 0xff800000u;
                         }
                     };
+                    // (Loops, not unrolled: the first pass through fresh code costs more than the loops do.)
                     float m2 = -INFINITY;                         // the row's largest logit in this tile, NaN if one is
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 2; ++c) {
                         uint32_t sv[32];
                         logits(c, sv);
@@ -497,7 +517,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         const float to = moves ? m2 : ref, corr = moves ? t5::ex2(ref - to) : 1.0f;
                         if (j > 0) {
                             // the last product into O is complete: this tile's logits were issued after it
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < 4; ++c) {
                                 uint32_t ov[16];
                                 t5::ld16_issue(o_addr + 16u * c, ov);
@@ -514,14 +534,11 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     const float use = unseen ? 0.0f : ref;
                     const uint64_t sc2 = f2::pk(scale2, scale2), nm2 = f2::pk(-use, -use);
                     uint64_t acc0 = f2::pk(0.0f, 0.0f), acc1 = acc0;
-                    // the polynomial has no zero and no NaN: where a weight may have to be either, the special-function unit alone
-                    const bool exact = masked || __any_sync(0xffffffffu, unseen);
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 2; ++c) {
                         uint32_t sv[32], pk[16];
                         logits(c, sv);
-                        if (exact) tree_weights<0>(sv, sc2, nm2, acc0, acc1, pk);
-                        else tree_weights<kTreePoly>(sv, sc2, nm2, acc0, acc1, pk);
+                        tree_weights(sv, sc2, nm2, acc0, acc1, pk);
                         t5::st16(s_addr + 16u * c, pk);           // over logits that this thread has read
                     }
                     float a0, a1, a2, a3;
@@ -541,15 +558,30 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             if (warp_live) {
                 t5::fence_after();
                 const size_t at = (seg * 2 + x) * w.rows_slot + row_in;
+                if (n_units > 0) {
+                    // 16 columns at a time through 2 KB of this warp in the Q tiles, which no MMA reads any more, so that four
+                    // lanes write 64 consecutive bytes of a row (a lane with 16 bytes of a row of its own takes four times as
+                    // many cycles of the store path)
+                    float4* stage = reinterpret_cast<float4*>(smem_q + (warp - 2) * 2048);
+                    const int n_live = min(32, rows - (row - lane));
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t ov[32];
-                    t5::ld32_issue(o_addr + 32u * c, ov);
-                    t5::ld_wait(ov);
-                    if (row < rows && n_units > 0) {
-                        uint4* dst = reinterpret_cast<uint4*>(w.part_o + at * kTreeD + 64 * hh + 32 * c);
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t ov[16];
+                        t5::ld16_issue(o_addr + 16u * c, ov);
+                        t5::ld_wait(ov);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) dst[i] = make_uint4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
+                        for (int i = 0; i < 4; ++i)
+                            stage[lane * 4 + (i ^ ((lane >> 1) & 3))] = make_float4(__uint_as_float(ov[4 * i]), __uint_as_float(ov[4 * i + 1]),
+                                                                                     __uint_as_float(ov[4 * i + 2]), __uint_as_float(ov[4 * i + 3]));
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int rr = i * 8 + (lane >> 2);
+                            if (rr < n_live)
+                                *reinterpret_cast<float4*>(w.part_o + (at - lane + rr) * kTreeD + 64 * hh + 16 * c + 4 * (lane & 3)) =
+                                    stage[rr * 4 + ((lane & 3) ^ ((rr >> 1) & 3))];
+                        }
+                        __syncwarp();
                     }
                 }
                 if (hh == 1) sh.half_max[x][1][row_in] = sum;
@@ -571,32 +603,35 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
 }
 
-// Joins the segments of one query row in the order of the line; a thread per dimension.
-__global__ void __launch_bounds__(kTreeD)
+// Joins the segments of one query row in the order of the line: a warp per row, four dimensions a lane.  Bound by the latency
+// of a few dependent reads, so the shares' sums are requested sixteen at a time.
+constexpr int kMergeRows = 8;
+__global__ void __launch_bounds__(32 * kMergeRows)
 tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
     pdl_wait();
     pdl_trigger();
     const TreeArgs& a = w.a;
-    const int LG = a.L * a.G, row = blockIdx.y, hz = blockIdx.x, s = hz / LG, lg = hz % LG, col = threadIdx.x;
+    const int LG = a.L * a.G, hz = blockIdx.x, s = hz / LG, lg = hz % LG, lane = threadIdx.x & 31;
+    const int row = blockIdx.y * kMergeRows + (threadIdx.x >> 5);
     const TreeInfo in = w.info[s];
     const long long total = w.info[a.ns].start;
     const int m = row / a.r;
     if (m >= in.n_q) return;
     const int rg = row / (2 * kTreeRows), rr = row % (2 * kTreeRows);
-    const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
-    const int lane = col & 31;
-    float z = 0.0f, acc = 0.0f, top = -INFINITY;
+    float z = 0.0f, top = -INFINITY;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     bool nf = false;
     if (in.tiles > 0) {
         const long long first = in.start + ((long long)lg * in.groups + rg) * in.tiles;
         const int n = (int)min((long long)n_ctas, total);
         const int c0 = tile_owner(first, total, n), c1 = tile_owner(first + in.tiles - 1, total, n);
         const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
-        for (int c = lane; c <= c1 - c0; c += 32) { const ulonglong2 f = w.part_nf[seg + c]; nf |= (f.x | f.y) != 0; }
         // one row tile: both slots hold a share of every row; two: slot rr / 128 does
         const int per = tree_row_tiles(in.n_q * a.r, rg) == 1 ? 2 : 1, parts = (c1 - c0 + 1) * per;
         const size_t at0 = (seg * 2 + (per == 1 ? rr >> 7 : 0)) * w.rows_slot + (rr & 127), step = (size_t)(3 - per) * w.rows_slot;
-        // every warp takes the statistics of 32 shares at a time, a lane each, and rescales what it has when the maximum grows
+        const float4* po = reinterpret_cast<const float4*>(w.part_o + at0 * kTreeD) + lane;
+        for (int c = lane; c <= c1 - c0; c += 32) { const ulonglong2 f = w.part_nf[seg + c]; nf |= (f.x | f.y) != 0; }
+        // the statistics of 32 shares at a time, a lane each; what there is is rescaled when the maximum grows
         for (int i0 = 0; i0 < parts; i0 += 32) {
             const int left = min(32, parts - i0);
             const float2 ml = lane < left ? w.part_ml[at0 + (size_t)(i0 + lane) * step] : make_float2(-INFINITY, 0.0f);
@@ -606,40 +641,47 @@ tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
             const float to = fmaxf(top, mx);
             const bool holds = ml.x > -INFINITY || ml.y != 0.0f;         // a share without a visible token holds no sums
             const float f = holds ? t5::ex2(ml.x - to) : 0.0f, back = top > -INFINITY ? t5::ex2(top - to) : 1.0f;
-            acc *= back;
-            z *= back;
+            float zi = holds ? f * ml.y : 0.0f;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) zi += __shfl_xor_sync(0xffffffffu, zi, d);
+            acc.x *= back; acc.y *= back; acc.z *= back; acc.w *= back;
+            z = z * back + zi;
             top = to;
             const uint32_t live = __ballot_sync(0xffffffffu, holds);
             for (int u0 = 0; u0 < left; u0 += 16) {
-                float po[16];
+                float4 v[16];
 #pragma unroll
-                for (int u = 0; u < 16; ++u) po[u] = (live >> (u0 + u)) & 1u ? w.part_o[(at0 + (size_t)(i0 + u0 + u) * step) * kTreeD + col] : 0.0f;
+                for (int u = 0; u < 16; ++u)
+                    if ((live >> (u0 + u)) & 1u) v[u] = po[(size_t)(i0 + u0 + u) * step * (kTreeD / 4)];
 #pragma unroll
                 for (int u = 0; u < 16; ++u) {
-                    const float fu = __shfl_sync(0xffffffffu, f, u0 + u), lu = __shfl_sync(0xffffffffu, ml.y, u0 + u);
-                    if ((live >> (u0 + u)) & 1u) {
-                        acc += fu * po[u];
-                        z += fu * lu;
-                    }
+                    const float fu = __shfl_sync(0xffffffffu, f, u0 + u);
+                    if ((live >> (u0 + u)) & 1u) { acc.x += fu * v[u].x; acc.y += fu * v[u].y; acc.z += fu * v[u].z; acc.w += fu * v[u].w; }
                 }
             }
         }
         nf = __any_sync(0xffffffffu, nf);
     }
+    const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
     const bool none = z == 0.0f;
-    float out = none ? 0.0f : acc / z;
+    float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (!none) { out[0] = acc.x / z; out[1] = acc.y / z; out[2] = acc.z / z; out[3] = acc.w / z; }
     if (nf) {
         // drafted values that are not finite were left out: they reach the rows that see them here
         const unsigned long long bits = tree_bits(a, s, m, in.n_q);
         for (int j = 0; j < in.n_q; ++j)
             if ((bits >> j) & 1) {
-                const float v = __bfloat162float(a.tail_v[(((size_t)s * a.tail_cap + in.n_tail + j) * LG + lg) * kTreeD + col]);
-                if (!isfinite(v)) out += v;
+                const __nv_bfloat16* vr = a.tail_v + (((size_t)s * a.tail_cap + in.n_tail + j) * LG + lg) * kTreeD + 4 * lane;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v = __bfloat162float(vr[i]);
+                    if (!isfinite(v)) out[i] += v;
+                }
             }
     }
-    a.out[orow * kTreeD + col] = __float2bfloat16(out);
+    *reinterpret_cast<uint2*>(a.out + orow * kTreeD + 4 * lane) = make_uint2(ptx::pack_bf16x2(out[0], out[1]), ptx::pack_bf16x2(out[2], out[3]));
     const float lse2 = none ? -INFINITY : top + log2f(z);
-    if (col == 0) {
+    if (lane == 0) {
         a.lse[orow] = lse2 * 0.6931471805599453f;
         if (w.lse2) w.lse2[(size_t)hz * a.rows + row] = lse2;
     }
@@ -741,7 +783,7 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     else if (paged) e = a.rows <= kTreeRows ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);
     else e = a.rows <= kTreeRows ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(tree_merge_kernel, dim3((unsigned)(a.ns * LG), (unsigned)a.rows), dim3(kTreeD), 0, st, w, grid);
+    e = launch_pdl(tree_merge_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + kMergeRows - 1) / kMergeRows)), dim3(32 * kMergeRows), 0, st, w, grid);
     if (e != cudaSuccess || !a.mass) return e;
     return launch_pdl(tree_mass_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.cap + 511) / 512)), dim3(128), 0, st, w);
 }

@@ -42,6 +42,7 @@ constexpr int kTreeRows = 128;                    // rows of a row tile: TMEM la
 constexpr int kTreeThreads = 32 * 19;              // key and value TMA warps, MMA warp, sixteen row warps
 constexpr int kTreeVWarp = 18;
 constexpr int kTreeRing1 = 6, kTreeRing2 = 5;     // ring slots beside one or two Q tiles: 224 KiB in all
+constexpr int kTreeSwitch = 3;                    // what going on to another head costs a CTA, in tiles
 constexpr float kTreeSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
 static_assert(1 + kTreeRing1 == 2 + kTreeRing2, "both forms take the same shared memory");
 constexpr uint32_t kTreeIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
@@ -54,7 +55,7 @@ struct TreeSpan {
     int groups;                   // row groups per KV head: up to two row tiles each
 };
 
-// what the merge needs to know of a session; entry ns holds the total in `start`
+// what the merge needs to know of a session; entry ns holds the line's tiles in `start` and the CTAs that share it in `tiles`
 struct TreeInfo {
     long long start;              // first tile of the session on the line
     int tiles, groups, n_q, n_tail;
@@ -216,14 +217,30 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     pdl_trigger();
     if (warp == 0) {
         // the CTA's part of the line, and the session it starts in
-        long long sum = 0;
+        long long sum = 0, lo_t = INT32_MAX, hi_t = 0;        // tiles of a KV head, over the sessions
         for (int s = lane; s < a.ns; s += 32) {
             const TreeSpan sp = tree_span(a, s, blockIdx.x == 0);
-            sum += (long long)sp.tiles * sp.groups;
+            const long long t = (long long)sp.tiles * sp.groups;
+            sum += t;
+            lo_t = min(lo_t, t);
+            hi_t = max(hi_t, t);
         }
-        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            lo_t = min(lo_t, __shfl_xor_sync(0xffffffffu, lo_t, d));
+            hi_t = max(hi_t, __shfl_xor_sync(0xffffffffu, hi_t, d));
+        }
         const long long total = sum * LG;
-        const int n = (int)min((long long)gridDim.x, total);
+        int n = (int)min((long long)gridDim.x, total);
+        // Heads of one length: with the largest multiple of their number of CTAs no CTA has parts of two heads, which costs a few
+        // SMs but saves the switch (about three tiles' time); the better of the two.
+        const long long n_heads = (long long)a.ns * LG * w.row_groups;
+        if (lo_t == hi_t && n_heads <= gridDim.x && hi_t > 0) {
+            const long long tiles = hi_t / w.row_groups;      // of one row group
+            const int per_head = (int)min((long long)(gridDim.x / (int)n_heads), tiles);
+            if ((tiles + per_head - 1) / per_head <= (total + n - 1) / n + kTreeSwitch) n = per_head * (int)n_heads;
+        }
         const bool idle = (int)blockIdx.x >= n;
         const long long begin = idle ? 0 : total * blockIdx.x / n, end = idle ? 0 : total * (blockIdx.x + 1) / n;
         long long before = 0;
@@ -233,9 +250,12 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             if (s < a.ns) sp = tree_span(a, s, false);
             const long long mine = (long long)sp.tiles * sp.groups * LG;
             long long incl = mine;
-            for (int d = 1; d < 32; d <<= 1) {
-                const long long up = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += up;
+            if (a.ns > 1) {
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+                    if (lane >= d) incl += up;
+                }
             }
             const long long lo = before + incl - mine;
             if (begin >= lo && begin < lo + mine) { sh.plan_s = s; sh.plan_base = lo; }
@@ -243,7 +263,11 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             before += __shfl_sync(0xffffffffu, incl, 31);
             if (blockIdx.x != 0 && (idle || before > begin)) break;
         }
-        if (lane == 0) { sh.plan_begin = begin; sh.plan_end = end; if (blockIdx.x == 0) w.info[a.ns].start = total; }
+        if (lane == 0) {
+            sh.plan_begin = begin;
+            sh.plan_end = end;
+            if (blockIdx.x == 0) w.info[a.ns] = TreeInfo{total, n, 0, 0, 0};
+        }
     }
     // warp 0 has what it needs and goes on; the others wait for the plan and the tensor memory
     t5::fence_before();
@@ -266,6 +290,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         // load of the ring
         const int kv = warp == 0 ? 0 : 1;
         const CUtensorMap *map_in = PAGED || kv == 0 ? &map_k : &map_v, *map_tail = kv ? &map_tv : &map_tk;
+        const uint64_t once = ptx::l2_evict_first();          // keys and values make room for the partial sums: 41 -> 38 us at 32,768 tokens
         int n = kv;                                           // next load
         const int box = PAGED ? min(a.B, 64) : 64;            // tokens per copy
         const int boxes = kTreeTile / box, per_block = PAGED ? max(a.B / 64, 1) : 1;     // copies per tile, per block
@@ -310,8 +335,8 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         // pages: [page][K | V][LG] tiles of B rows of 256 B
                         const int y = PAGED ? (per_block == 1 ? 0 : (b0 + lane) % per_block * 64) : t * kTreeTile + u * 64;
                         const int z = PAGED ? (page * 2 + kv) * LG + walk.lg : z_view;
-                        ptx::tma_load_3d(dst, map_in, 0, y, z, &full[st]);
-                        ptx::tma_load_3d(dst + kTreeHalf, map_in, 64, y, z, &full[st]);
+                        ptx::tma_load_3d_hint(dst, map_in, 0, y, z, &full[st], once);
+                        ptx::tma_load_3d_hint(dst + kTreeHalf, map_in, 64, y, z, &full[st], once);
                     }
                 }
             }
@@ -607,14 +632,13 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 // of a few dependent reads, so the shares' sums are requested sixteen at a time.
 constexpr int kMergeRows = 8;
 __global__ void __launch_bounds__(32 * kMergeRows)
-tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
+tree_merge_kernel(const __grid_constant__ TreeWork w) {
     pdl_wait();
     pdl_trigger();
     const TreeArgs& a = w.a;
     const int LG = a.L * a.G, hz = blockIdx.x, s = hz / LG, lg = hz % LG, lane = threadIdx.x & 31;
     const int row = blockIdx.y * kMergeRows + (threadIdx.x >> 5);
-    const TreeInfo in = w.info[s];
-    const long long total = w.info[a.ns].start;
+    const TreeInfo in = w.info[s], line = w.info[a.ns];
     const int m = row / a.r;
     if (m >= in.n_q) return;
     const int rg = row / (2 * kTreeRows), rr = row % (2 * kTreeRows);
@@ -623,42 +647,53 @@ tree_merge_kernel(const __grid_constant__ TreeWork w, int n_ctas) {
     bool nf = false;
     if (in.tiles > 0) {
         const long long first = in.start + ((long long)lg * in.groups + rg) * in.tiles;
-        const int n = (int)min((long long)n_ctas, total);
-        const int c0 = tile_owner(first, total, n), c1 = tile_owner(first + in.tiles - 1, total, n);
+        const int c0 = tile_owner(first, line.start, line.tiles), c1 = tile_owner(first + in.tiles - 1, line.start, line.tiles);
         const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
         // one row tile: both slots hold a share of every row; two: slot rr / 128 does
         const int per = tree_row_tiles(in.n_q * a.r, rg) == 1 ? 2 : 1, parts = (c1 - c0 + 1) * per;
         const size_t at0 = (seg * 2 + (per == 1 ? rr >> 7 : 0)) * w.rows_slot + (rr & 127), step = (size_t)(3 - per) * w.rows_slot;
         const float4* po = reinterpret_cast<const float4*>(w.part_o + at0 * kTreeD) + lane;
         for (int c = lane; c <= c1 - c0; c += 32) { const ulonglong2 f = w.part_nf[seg + c]; nf |= (f.x | f.y) != 0; }
-        // the statistics of 32 shares at a time, a lane each; what there is is rescaled when the maximum grows
-        for (int i0 = 0; i0 < parts; i0 += 32) {
-            const int left = min(32, parts - i0);
-            const float2 ml = lane < left ? w.part_ml[at0 + (size_t)(i0 + lane) * step] : make_float2(-INFINITY, 0.0f);
-            float mx = ml.x;
+        // the statistics of 64 shares at a time, two a lane; what there is is rescaled when the maximum grows
+        for (int i0 = 0; i0 < parts; i0 += 64) {
+            const int left = min(64, parts - i0);
+            float2 ml[2];
+            bool holds[2];                                    // a share without a visible token holds no sums
+            float f[2], zi = 0.0f, mx = -INFINITY;
+            uint32_t live[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                ml[e] = 32 * e + lane < left ? w.part_ml[at0 + (size_t)(i0 + 32 * e + lane) * step] : make_float2(-INFINITY, 0.0f);
+                holds[e] = ml[e].x > -INFINITY || ml[e].y != 0.0f;
+                live[e] = __ballot_sync(0xffffffffu, holds[e]);
+                mx = fmaxf(mx, ml[e].x);
+            }
 #pragma unroll
             for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-            const float to = fmaxf(top, mx);
-            const bool holds = ml.x > -INFINITY || ml.y != 0.0f;         // a share without a visible token holds no sums
-            const float f = holds ? t5::ex2(ml.x - to) : 0.0f, back = top > -INFINITY ? t5::ex2(top - to) : 1.0f;
-            float zi = holds ? f * ml.y : 0.0f;
+            const float to = fmaxf(top, mx), back = top > -INFINITY ? t5::ex2(top - to) : 1.0f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                f[e] = holds[e] ? t5::ex2(ml[e].x - to) : 0.0f;
+                if (holds[e]) zi += f[e] * ml[e].y;
+            }
 #pragma unroll
             for (int d = 16; d; d >>= 1) zi += __shfl_xor_sync(0xffffffffu, zi, d);
             acc.x *= back; acc.y *= back; acc.z *= back; acc.w *= back;
             z = z * back + zi;
             top = to;
-            const uint32_t live = __ballot_sync(0xffffffffu, holds);
-            for (int u0 = 0; u0 < left; u0 += 16) {
-                float4 v[16];
 #pragma unroll
-                for (int u = 0; u < 16; ++u)
-                    if ((live >> (u0 + u)) & 1u) v[u] = po[(size_t)(i0 + u0 + u) * step * (kTreeD / 4)];
+            for (int e = 0; e < 2; ++e)
+                for (int u0 = 0; u0 < min(32, left - 32 * e); u0 += 16) {
+                    float4 v[16];
 #pragma unroll
-                for (int u = 0; u < 16; ++u) {
-                    const float fu = __shfl_sync(0xffffffffu, f, u0 + u);
-                    if ((live >> (u0 + u)) & 1u) { acc.x += fu * v[u].x; acc.y += fu * v[u].y; acc.z += fu * v[u].z; acc.w += fu * v[u].w; }
+                    for (int u = 0; u < 16; ++u)
+                        if ((live[e] >> (u0 + u)) & 1u) v[u] = po[(size_t)(i0 + 32 * e + u0 + u) * step * (kTreeD / 4)];
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) {
+                        const float fu = __shfl_sync(0xffffffffu, f[e], u0 + u);
+                        if ((live[e] >> (u0 + u)) & 1u) { acc.x += fu * v[u].x; acc.y += fu * v[u].y; acc.z += fu * v[u].z; acc.w += fu * v[u].w; }
+                    }
                 }
-            }
         }
         nf = __any_sync(0xffffffffu, nf);
     }
@@ -783,7 +818,7 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     else if (paged) e = a.rows <= kTreeRows ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);
     else e = a.rows <= kTreeRows ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(tree_merge_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + kMergeRows - 1) / kMergeRows)), dim3(32 * kMergeRows), 0, st, w, grid);
+    e = launch_pdl(tree_merge_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + kMergeRows - 1) / kMergeRows)), dim3(32 * kMergeRows), 0, st, w);
     if (e != cudaSuccess || !a.mass) return e;
     return launch_pdl(tree_mass_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.cap + 511) / 512)), dim3(128), 0, st, w);
 }

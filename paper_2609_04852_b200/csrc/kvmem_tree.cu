@@ -458,8 +458,11 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const int c0 = (in_view ? t : t - sp.view_tiles) * kTreeTile;             // first token of the tile in view or tail
                 const int n_valid = min(kTreeTile, (in_view ? sp.n_view : sp.n_tail + sp.n_q) - c0);
                 const bool masked = n_valid < kTreeTile || !in_view;
+                wait(&s_full[x], cnt);
                 if (masked && (!two || x == 0)) {
-                    // values nobody sees become zero; drafted values that are not finite too (the merge adds them)
+                    // Values nobody sees become zero; drafted values that are not finite too (the merge adds them).  Only now: the tile
+                    // that was in this ring slot before has landed for certain once these logits are there, and a wait for a phase
+                    // two ahead of the barrier's would be over at once.
                     const int v = 2 * (tiles + ti) + 1, st = v % RING;
                     wait(&full[st], v / RING);
                     unsigned char* vt = ring + (size_t)st * kTreeSlot;
@@ -484,7 +487,6 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     }
                     ptx::fence_proxy_async_smem();
                 }
-                wait(&s_full[x], cnt);
                 if (warp_live) {
                     t5::fence_after();
                     // Two sweeps over the thread's 64 logits, 32 at a time: the maximum, then the weights.  (All 64 held in between cost

@@ -189,6 +189,38 @@ def test_tree_attention_matches_the_definition(i, paged):
     c.check()
 
 
+# Many tiles per CTA, segments that begin and end anywhere, ragged ends behind full tiles: (the ring of tiles has wrapped
+# around several times when a masked tile comes up)
+LONG = [
+    dict(ns=4, L=2, H=16, G=4, lens=(300, 77, 129, 255), M=12, n_q=(12, 5, 9, 1), tails=(90, 3, 40, 200)),     # 48 rows per KV head
+    dict(ns=3, H=32, G=8, lens=(501, 33, 250), M=16, B=32, tails=(50, 129, 0)),                                   # 64 rows
+    dict(ns=3, H=16, G=2, lens=(400, 1, 222), M=31, n_q=(31, 31, 10), B=48, tails=(700, 5, 64)),               # 248 and 80 rows
+    dict(ns=2, H=16, G=2, lens=(300, 299), M=33, n_q=(33, 32), tails=(600, 100), mask="all"),                  # 264 and 256 rows
+    dict(ns=8, H=32, G=8, lens=(200, 52, 73, 95, 116, 137, 158, 0), M=4, tails=(33, 3, 7, 11, 14, 18, 22, 29), mask="chain"),
+    dict(ns=1, H=4, G=1, lens=(3001,), M=7, B=16, tails=(1000,)),                                                 # one head on all SMs
+]
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("i", range(len(LONG)))
+def test_long_and_ragged_views(i, paged):
+    if paged and LONG[i].get("B", 64) == 48:
+        pytest.skip("a block size the pages do not take")
+    c = Case(paged=paged, seed=200 + i, **LONG[i])
+    for _ in range(3):
+        c.out.fill_(77.0); c.lse.fill_(55.0)
+        c.call()
+        c.check()
+
+
+@pytest.mark.parametrize("i", [1, 4])
+def test_weights_over_long_and_ragged_views(i):
+    c = Case(seed=230 + i, **{**LONG[i], "mask": "chain", "M": 4})
+    c.mass = c.guards.empty((c.ns, c.L, c.G, c.capb * c.B), torch.float32)
+    c.call(decay=0.5)
+    c.check(0.5, torch.zeros_like(c.mass))
+
+
 @pytest.mark.parametrize("B,lens", [(48, (5,)), (80, (3,)), (240, (2,)), (256, (2,)), (192, (3,)), (112, (1,))])
 def test_block_sizes_of_the_view(B, lens):
     c = Case(B=B, lens=lens, seed=B)

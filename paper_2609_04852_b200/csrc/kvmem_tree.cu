@@ -15,8 +15,9 @@
 // ref is a running maximum that moves only when a row's logits pass it by 8 (in powers of two): O is then rescaled in
 // tensor memory.  Until then the weights may reach 2^8, which costs neither fp32 nor bf16 any precision.
 //
-// Work: the tiles of all (session, KV head, row group) lie on one line, cut into as many equal parts as there are CTAs
-// (one per SM), so that sessions of any lengths keep all SMs busy to the end.  A CTA's share of one head is a segment;
+// Work: the tiles of all (session, KV head, row group) lie on one line, with a lead of three tiles' time ahead of each head for
+// the switch, cut into as many equal parts as there are CTAs (one per SM), so that sessions of any lengths keep all SMs busy
+// to the end.  A CTA's share of one head is a segment;
 // each leaves unnormalised sums, row references and row sums, and tree_merge_kernel joins a head's segments in order: the
 // result depends on the sizes alone, not on timing.  Lengths are read on the device.
 //
@@ -55,10 +56,10 @@ struct TreeSpan {
     int groups;                   // row groups per KV head: up to two row tiles each
 };
 
-// what the merge needs to know of a session; entry ns holds the line's tiles in `start` and the CTAs that share it in `tiles`
+// What the merge needs to know of a session: where it starts on the line, its tiles, row groups, drafted and committed tokens.
+// Entry ns: the line's length, the CTAs that share it, a head's lead.
 struct TreeInfo {
-    long long start;              // first tile of the session on the line
-    int tiles, groups, n_q, n_tail;
+    int start, tiles, groups, n_q, n_tail;
 };
 
 struct TreeWork {
@@ -105,10 +106,17 @@ __device__ __forceinline__ uint32_t tail_word(int c0, int n_tail, unsigned long 
 // row tiles of row group rg when the session has `rows` live rows: with one, the slots take tiles in turn
 __device__ __forceinline__ int tree_row_tiles(int rows, int rg) { return rows - rg * 2 * kTreeRows > kTreeRows ? 2 : 1; }
 
-// CTA that holds tile x of the line: tiles [total c / n, total (c + 1) / n) are CTA c's
-__device__ __forceinline__ int tile_owner(long long x, long long total, int n) {
-    const unsigned long long num = (unsigned long long)(x + 1) * n - 1;
-    return num < (1ull << 32) ? (int)((unsigned)num / (unsigned)total) : (int)(num / (unsigned long long)total);
+// The line: per (session, KV head, row group) `lead` units that stand for what going on to another head costs a CTA, and a unit
+// per tile; CTA c of n has units [total c / n, total (c + 1) / n).  The host refuses calls that could pass 2^30 units.
+constexpr int kTreeMostTiles = 1 << 30;
+// x * m / d; the product fits 32 bits in any call that fits the memory, and a division of 64 bits takes several times as long
+__device__ __forceinline__ int mul_div(int x, int m, int d) {
+    const unsigned long long p = (unsigned long long)x * (unsigned)m;
+    return p < (1ull << 32) ? (int)((unsigned)p / (unsigned)d) : (int)(p / (unsigned)d);
+}
+__device__ __forceinline__ int line_owner(int x, int total, int n) {
+    const unsigned long long p = (unsigned long long)(x + 1) * (unsigned)n - 1u;
+    return p < (1ull << 32) ? (int)((unsigned)p / (unsigned)total) : (int)(p / (unsigned)total);
 }
 
 // Waits for up to three phases (null: none), asked together; the last is the one that is waited for longest.
@@ -129,27 +137,32 @@ __device__ __forceinline__ bool wait_step(uint64_t* b0, int ph0, uint64_t* b1, i
 
 // a role's walk over the CTA's segments
 struct TreeWalk {
-    long long pos, end, base;     // next tile on the line, the CTA's end, first tile of session s
+    int pos, end, base, lead;     // next unit of the line, the CTA's end, first unit of session s
     int s, lg, rg, head, t0, t1;  // the segment: tiles [t0, t1) of head `head` (a row group of a KV head)
     int qt;                       // its row tiles
     TreeSpan sp;
     __device__ __forceinline__ bool next(const TreeArgs& a, int most_groups) {
-        if (pos >= end) return false;
         const int LG = a.L * a.G;
-        sp = tree_span(a, s, false);
-        while (base + (long long)sp.tiles * sp.groups * LG <= pos) {
-            base += (long long)sp.tiles * sp.groups * LG;
-            sp = tree_span(a, ++s, false);
+        while (pos < end) {
+            sp = tree_span(a, s, false);
+            while (true) {
+                const int units = sp.tiles ? (sp.tiles + lead) * sp.groups * LG : 0;
+                if (base + units > pos) break;
+                base += units;
+                sp = tree_span(a, ++s, false);
+            }
+            const int per = sp.tiles + lead, at = (pos - base) / per, from = base + at * per + lead;   // unit of the head's first tile
+            t0 = max(pos - from, 0);
+            t1 = min(sp.tiles, end - from);
+            pos = min(end, from + sp.tiles);
+            if (t0 >= t1) continue;                       // nothing but the head's lead
+            lg = at / sp.groups;
+            rg = at % sp.groups;
+            head = (s * LG + lg) * most_groups + rg;
+            qt = tree_row_tiles(sp.n_q * a.r, rg);
+            return true;
         }
-        const int at = (int)((pos - base) / sp.tiles);
-        lg = at / sp.groups;
-        rg = at % sp.groups;
-        head = (s * LG + lg) * most_groups + rg;
-        qt = tree_row_tiles(sp.n_q * a.r, rg);
-        t0 = (int)(pos - base - (long long)at * sp.tiles);
-        t1 = (int)min((long long)sp.tiles, t0 + (end - pos));
-        pos += t1 - t0;
-        return true;
+        return false;
     }
 };
 
@@ -169,8 +182,7 @@ __device__ __forceinline__ void tree_weights(const uint32_t (&sv)[32], uint64_t 
 
 struct TreeShared {
     uint64_t full[kTreeRing1], empty[kTreeRing1], q_full, s_full[2], p_full[2], o_done[2], drained;
-    long long plan_begin, plan_end, plan_base;
-    int plan_s;
+    int plan_begin, plan_end, plan_base, plan_s, plan_lead;
     uint32_t tmem;
     float half_max[2][2][kTreeRows];      // [slot][half of the columns]: exchanged between the two threads of a row
 };
@@ -217,47 +229,50 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     pdl_trigger();
     if (warp == 0) {
         // the CTA's part of the line, and the session it starts in
-        long long sum = 0, lo_t = INT32_MAX, hi_t = 0;        // tiles of a KV head, over the sessions
+        int sum = 0, live = 0, lo_t = INT32_MAX, hi_t = 0;    // tiles and heads of one KV head, over the sessions
         for (int s = lane; s < a.ns; s += 32) {
             const TreeSpan sp = tree_span(a, s, blockIdx.x == 0);
-            const long long t = (long long)sp.tiles * sp.groups;
-            sum += t;
-            lo_t = min(lo_t, t);
-            hi_t = max(hi_t, t);
+            const int heads = sp.tiles ? sp.groups : 0;
+            sum += sp.tiles * heads;
+            live += heads;
+            lo_t = min(lo_t, sp.tiles);
+            hi_t = max(hi_t, sp.tiles);
         }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            lo_t = min(lo_t, __shfl_xor_sync(0xffffffffu, lo_t, d));
-            hi_t = max(hi_t, __shfl_xor_sync(0xffffffffu, hi_t, d));
+        if (a.ns > 1) {
+            sum = __reduce_add_sync(0xffffffffu, sum);
+            live = __reduce_add_sync(0xffffffffu, live);
+            lo_t = __reduce_min_sync(0xffffffffu, lo_t);
+            hi_t = __reduce_max_sync(0xffffffffu, hi_t);
+        } else {
+            sum = __shfl_sync(0xffffffffu, sum, 0); live = __shfl_sync(0xffffffffu, live, 0);
+            lo_t = __shfl_sync(0xffffffffu, lo_t, 0); hi_t = __shfl_sync(0xffffffffu, hi_t, 0);
         }
-        const long long total = sum * LG;
-        int n = (int)min((long long)gridDim.x, total);
-        // Heads of one length: with the largest multiple of their number of CTAs no CTA has parts of two heads, which costs a few
-        // SMs but saves the switch (about three tiles' time); the better of the two.
-        const long long n_heads = (long long)a.ns * LG * w.row_groups;
-        if (lo_t == hi_t && n_heads <= gridDim.x && hi_t > 0) {
-            const long long tiles = hi_t / w.row_groups;      // of one row group
-            const int per_head = (int)min((long long)(gridDim.x / (int)n_heads), tiles);
-            if ((tiles + per_head - 1) / per_head <= (total + n - 1) / n + kTreeSwitch) n = per_head * (int)n_heads;
+        const int heads = live * LG, tiles = sum * LG;
+        int lead = heads > 1 ? kTreeSwitch : 0, n = min((int)gridDim.x, tiles);
+        // Heads of one length: with a multiple of their number of CTAs none has parts of two heads.  That costs a few SMs and saves
+        // the switches; the better of the two.
+        if (lo_t == hi_t && heads > 0 && heads <= gridDim.x) {
+            const int per_head = min((int)gridDim.x / heads, hi_t);
+            if ((hi_t + per_head - 1) / per_head <= (tiles + n - 1) / n + kTreeSwitch) { n = per_head * heads; lead = 0; }
         }
+        const int total = tiles + heads * lead;
         const bool idle = (int)blockIdx.x >= n;
-        const long long begin = idle ? 0 : total * blockIdx.x / n, end = idle ? 0 : total * (blockIdx.x + 1) / n;
-        long long before = 0;
+        const int begin = idle ? 0 : mul_div(total, blockIdx.x, n), end = idle ? 0 : mul_div(total, blockIdx.x + 1, n);
+        int before = 0;
         for (int s0 = 0; s0 < a.ns; s0 += 32) {
             const int s = s0 + lane;
             TreeSpan sp{};
             if (s < a.ns) sp = tree_span(a, s, false);
-            const long long mine = (long long)sp.tiles * sp.groups * LG;
-            long long incl = mine;
+            const int mine = sp.tiles ? (sp.tiles + lead) * sp.groups * LG : 0;
+            int incl = mine;
             if (a.ns > 1) {
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
-                    const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+                    const int up = __shfl_up_sync(0xffffffffu, incl, d);
                     if (lane >= d) incl += up;
                 }
             }
-            const long long lo = before + incl - mine;
+            const int lo = before + incl - mine;
             if (begin >= lo && begin < lo + mine) { sh.plan_s = s; sh.plan_base = lo; }
             if (blockIdx.x == 0 && s < a.ns) w.info[s] = TreeInfo{lo, sp.tiles, sp.groups, sp.n_q, sp.n_tail};
             before += __shfl_sync(0xffffffffu, incl, 31);
@@ -266,7 +281,8 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if (lane == 0) {
             sh.plan_begin = begin;
             sh.plan_end = end;
-            if (blockIdx.x == 0) w.info[a.ns] = TreeInfo{total, n, 0, 0, 0};
+            sh.plan_lead = lead;
+            if (blockIdx.x == 0) w.info[a.ns] = TreeInfo{total, n, lead, 0, 0};
         }
     }
     // warp 0 has what it needs and goes on; the others wait for the plan and the tensor memory
@@ -280,7 +296,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     t5::fence_after();
     const uint32_t tmem = warp == 0 ? 0u : sh.tmem;
     TreeWalk walk;
-    walk.pos = sh.plan_begin; walk.end = sh.plan_end; walk.base = sh.plan_base; walk.s = sh.plan_s;
+    walk.pos = sh.plan_begin; walk.end = sh.plan_end; walk.base = sh.plan_base; walk.s = sh.plan_s; walk.lead = sh.plan_lead;
 
     // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
     // every role still reaches its end.
@@ -457,7 +473,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const bool in_view = t < sp.view_tiles;
                 const int c0 = (in_view ? t : t - sp.view_tiles) * kTreeTile;             // first token of the tile in view or tail
                 const int n_valid = min(kTreeTile, (in_view ? sp.n_view : sp.n_tail + sp.n_q) - c0);
-                const bool masked = n_valid < kTreeTile || !in_view;
+                const bool masked = n_valid < kTreeTile || (!in_view && c0 + kTreeTile > sp.n_tail);      // any column that some row does not see
                 wait(&s_full[x], cnt);
                 if (masked && (!two || x == 0)) {
                     // Values nobody sees become zero; drafted values that are not finite too (the merge adds them).  Only now: the tile
@@ -648,8 +664,8 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     bool nf = false;
     if (in.tiles > 0) {
-        const long long first = in.start + ((long long)lg * in.groups + rg) * in.tiles;
-        const int c0 = tile_owner(first, line.start, line.tiles), c1 = tile_owner(first + in.tiles - 1, line.start, line.tiles);
+        const int first = in.start + (lg * in.groups + rg) * (in.tiles + line.groups) + line.groups;
+        const int c0 = line_owner(first, line.start, line.tiles), c1 = line_owner(first + in.tiles - 1, line.start, line.tiles);
         const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
         // one row tile: both slots hold a share of every row; two: slot rr / 128 does
         const int per = tree_row_tiles(in.n_q * a.r, rg) == 1 ? 2 : 1, parts = (c1 - c0 + 1) * per;
@@ -814,6 +830,7 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     else m[2] = m[3] = m[0];
     if (!made) return cudaErrorInvalidValue;
     const long long most = (long long)a.ns * LG * w.row_groups * ((a.cap + kTreeTile - 1) / kTreeTile + (a.tail_cap + kTreeTile - 1) / kTreeTile);
+    if (most + (long long)a.ns * LG * w.row_groups * kTreeSwitch >= kTreeMostTiles) return cudaErrorInvalidConfiguration;
     const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), most);
     cudaError_t e;
     if (a.mass) e = launch_split<1, false, true>(p, grid, st, m, w);            // at most 64 rows

@@ -42,10 +42,12 @@ constexpr int kTreeSlot = 2 * kTreeHalf;          // a K, V or Q tile
 constexpr int kTreeRows = 128;                    // rows of a row tile: TMEM lanes
 constexpr int kTreeThreads = 32 * 19;              // key and value TMA warps, MMA warp, sixteen row warps
 constexpr int kTreeVWarp = 18;
-constexpr int kTreeRing1 = 6, kTreeRing2 = 5;     // ring slots beside one or two Q tiles: 224 KiB in all
+// Ring slots, K and V tiles in turn: two tiles of each per SM, 18.5 MiB over the 148.  There is room for six slots beside one Q
+// tile, but more requests than HBM's latency asks for only lengthen its queues: eight sessions of 65,536 tokens take 176 us
+// with four slots and 181 with six, 262,144 tokens with weights 237 and 250, 32,768 tokens 37.7 with either.
+constexpr int kTreeRing = 4;
 constexpr int kTreeSwitch = 3;                    // what going on to another head costs a CTA, in tiles
 constexpr float kTreeSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
-static_assert(1 + kTreeRing1 == 2 + kTreeRing2, "both forms take the same shared memory");
 constexpr uint32_t kTreeIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
 constexpr uint32_t kTreeIdescO = kTreeIdescS | (1u << 16);                                        // B with dims contiguous (V as it lies)
 constexpr uint32_t kTreeVStep = (uint32_t)kTreeHalf >> 4;      // leading offset of V's descriptor: from dims 0..63 to 64..127
@@ -181,26 +183,25 @@ __device__ __forceinline__ void tree_weights(const uint32_t (&sv)[32], uint64_t 
 }
 
 struct TreeShared {
-    uint64_t full[kTreeRing1], empty[kTreeRing1], q_full, s_full[2], p_full[2], o_done[2], drained;
+    uint64_t full[kTreeRing], empty[kTreeRing], q_full, s_full[2], p_full[2], o_done[2], drained;
     int plan_begin, plan_end, plan_base, plan_s, plan_lead;
     uint32_t tmem;
     float half_max[2][2][kTreeRows];      // [slot][half of the columns]: exchanged between the two threads of a row
 };
 // Nothing static beside it: the dynamic part then starts where shared memory does, on the 1,024 bytes that the swizzle needs
-// (checked), and all 227 KB are in use.
-constexpr size_t kTreeSmem = (size_t)(1 + kTreeRing1) * kTreeSlot + sizeof(TreeShared);
-static_assert(kTreeSmem <= 232448, "227 KB of shared memory per CTA");
+// (checked).
+constexpr size_t tree_smem(int q_tiles) { return (size_t)(q_tiles + kTreeRing) * kTreeSlot + sizeof(TreeShared); }
 
 template <int QT, bool PAGED, bool MASS>
 __global__ void __launch_bounds__(kTreeThreads, 1)
 tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CUtensorMap map_tk, const __grid_constant__ CUtensorMap map_tv,
                   const __grid_constant__ TreeWork w) {
-    constexpr int RING = QT == 1 ? kTreeRing1 : kTreeRing2;
+    constexpr int RING = kTreeRing;
     extern __shared__ __align__(1024) unsigned char smem_q[];      // Q tiles, the ring, then the small things
     const TreeArgs& a = w.a;
     unsigned char* ring = smem_q + (size_t)QT * kTreeSlot;
-    TreeShared& sh = *reinterpret_cast<TreeShared*>(smem_q + (size_t)(1 + kTreeRing1) * kTreeSlot);
+    TreeShared& sh = *reinterpret_cast<TreeShared*>(ring + (size_t)RING * kTreeSlot);
     uint64_t *full = sh.full, *empty = sh.empty, *s_full = sh.s_full, *p_full = sh.p_full, *o_done = sh.o_done;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int LG = a.L * a.G;
@@ -359,7 +360,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             if (!ok) break;
         }
         // the copies still in flight land before the CTA gives its shared memory back
-        for (int i = max(kv, n - (RING & ~1)); i < n; i += 2) ok = ptx::mbar_wait(&full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
+        for (int i = max(kv, n - RING); i < n; i += 2) ok = ptx::mbar_wait(&full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
         if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
     } else if (warp == 1) {
         // ------------------------------------------------ MMA: one thread
@@ -806,11 +807,11 @@ template <int QT, bool PAGED, bool MASS>
 static cudaError_t launch_split(const kvmem_pool& p, int grid, cudaStream_t st, const CUtensorMap (&m)[4], const TreeWork& w) {
     static PerDeviceOnce done;
     if (done.pending(p.cfg.device)) {
-        const cudaError_t e = cudaFuncSetAttribute(tree_split_kernel<QT, PAGED, MASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTreeSmem);
+        const cudaError_t e = cudaFuncSetAttribute(tree_split_kernel<QT, PAGED, MASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tree_smem(QT));
         if (e != cudaSuccess) return e;
         done.mark(p.cfg.device);
     }
-    return launch_pdl(tree_split_kernel<QT, PAGED, MASS>, dim3((unsigned)grid), dim3(kTreeThreads), kTreeSmem, st, m[0], m[1], m[2], m[3], w);
+    return launch_pdl(tree_split_kernel<QT, PAGED, MASS>, dim3((unsigned)grid), dim3(kTreeThreads), tree_smem(QT), st, m[0], m[1], m[2], m[3], w);
 }
 
 cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace, cudaStream_t st) {

@@ -647,24 +647,31 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
 }
 
-// Joins the segments of one query row in the order of the line: a warp per row, four dimensions a lane.  Bound by the latency
-// of a few dependent reads, so the shares' sums are requested sixteen at a time.
-constexpr int kMergeRows = 8;
-__global__ void __launch_bounds__(32 * kMergeRows)
+// Joins the segments of one query row in the order of the line, four dimensions a lane.  Bound by latency: a round of dependent
+// reads costs some 2 us here, so a warp requests the sums of sixteen shares together.  WARPS = 4: four warps a row, each with
+// sixteen of 64 shares, where all rows are resident at a time that way (one CTA an SM): 13.7 us a call at 2,048 tokens and 32
+// rows per KV head against 15.7; WARPS = 1 where there are more rows: 7.6 us against 28 for 2,048 of them.
+constexpr int kMergeThreads = 256;
+constexpr int kMergeWideRows = kSMs * kMergeThreads / 128;            // rows up to which a row gets four warps
+template <int WARPS>
+__global__ void __launch_bounds__(kMergeThreads, WARPS == 1 ? 2 : 1)
 tree_merge_kernel(const __grid_constant__ TreeWork w) {
+    constexpr int ROWS = kMergeThreads / 32 / WARPS;
+    __shared__ float4 sums[ROWS][WARPS][32];
     pdl_wait();
     pdl_trigger();
     const TreeArgs& a = w.a;
     const int LG = a.L * a.G, hz = blockIdx.x, s = hz / LG, lg = hz % LG, lane = threadIdx.x & 31;
-    const int row = blockIdx.y * kMergeRows + (threadIdx.x >> 5);
+    const int quarter = (threadIdx.x >> 5) % WARPS, mine = (threadIdx.x >> 5) / WARPS;
+    const int row = blockIdx.y * ROWS + mine;
     const TreeInfo in = w.info[s], line = w.info[a.ns];
     const int m = row / a.r;
-    if (m >= in.n_q) return;
+    const bool there = m < in.n_q;
     const int rg = row / (2 * kTreeRows), rr = row % (2 * kTreeRows);
     float z = 0.0f, top = -INFINITY;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     bool nf = false;
-    if (in.tiles > 0) {
+    if (there && in.tiles > 0) {
         const int first = in.start + (lg * in.groups + rg) * (in.tiles + line.groups) + line.groups;
         const int c0 = line_owner(first, line.start, line.tiles), c1 = line_owner(first + in.tiles - 1, line.start, line.tiles);
         const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
@@ -700,21 +707,35 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
             acc.x *= back; acc.y *= back; acc.z *= back; acc.w *= back;
             z = z * back + zi;
             top = to;
+            // sixteen at a time: all of them, or this warp's
+#pragma unroll 1
+            for (int b = WARPS == 1 ? 0 : quarter; b < (WARPS == 1 ? (left + 15) / 16 : quarter + 1); ++b) {
+                const uint32_t here = ((b & 2) ? live[1] : live[0]) >> (16 * (b & 1));
+                const float fb = (b & 2) ? f[1] : f[0];
+                float4 v[16];
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                for (int u0 = 0; u0 < min(32, left - 32 * e); u0 += 16) {
-                    float4 v[16];
+                for (int u = 0; u < 16; ++u)
+                    if ((here >> u) & 1u) v[u] = po[(size_t)(i0 + 16 * b + u) * step * (kTreeD / 4)];
 #pragma unroll
-                    for (int u = 0; u < 16; ++u)
-                        if ((live[e] >> (u0 + u)) & 1u) v[u] = po[(size_t)(i0 + 32 * e + u0 + u) * step * (kTreeD / 4)];
-#pragma unroll
-                    for (int u = 0; u < 16; ++u) {
-                        const float fu = __shfl_sync(0xffffffffu, f[e], u0 + u);
-                        if ((live[e] >> (u0 + u)) & 1u) { acc.x += fu * v[u].x; acc.y += fu * v[u].y; acc.z += fu * v[u].z; acc.w += fu * v[u].w; }
-                    }
+                for (int u = 0; u < 16; ++u) {
+                    const float fu = __shfl_sync(0xffffffffu, fb, 16 * (b & 1) + u);
+                    if ((here >> u) & 1u) { acc.x += fu * v[u].x; acc.y += fu * v[u].y; acc.z += fu * v[u].z; acc.w += fu * v[u].w; }
                 }
+            }
         }
         nf = __any_sync(0xffffffffu, nf);
+    }
+    if (WARPS > 1) {
+        sums[mine][quarter][lane] = acc;
+        __syncthreads();
+    }
+    if (quarter > 0 || !there) return;
+    if (WARPS > 1) {
+        const float4 b1 = sums[mine][1 % WARPS][lane], b2 = sums[mine][2 % WARPS][lane], b3 = sums[mine][3 % WARPS][lane];
+        acc.x = (acc.x + b1.x) + (b2.x + b3.x);
+        acc.y = (acc.y + b1.y) + (b2.y + b3.y);
+        acc.z = (acc.z + b1.z) + (b2.z + b3.z);
+        acc.w = (acc.w + b1.w) + (b2.w + b3.w);
     }
     const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
     const bool none = z == 0.0f;
@@ -838,7 +859,9 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     else if (paged) e = a.rows <= kTreeRows ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);
     else e = a.rows <= kTreeRows ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(tree_merge_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + kMergeRows - 1) / kMergeRows)), dim3(32 * kMergeRows), 0, st, w);
+    const long long all_rows = (long long)a.ns * LG * a.rows;
+    if (all_rows <= kMergeWideRows) e = launch_pdl(tree_merge_kernel<4>, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + 1) / 2)), dim3(kMergeThreads), 0, st, w);
+    else e = launch_pdl(tree_merge_kernel<1>, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + 7) / 8)), dim3(kMergeThreads), 0, st, w);
     if (e != cudaSuccess || !a.mass) return e;
     return launch_pdl(tree_mass_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.cap + 511) / 512)), dim3(128), 0, st, w);
 }

@@ -231,6 +231,7 @@ class Pool:
         self._host_ws: Optional[torch.Tensor] = None
         self._host_staging: Optional[torch.Tensor] = None
         self._staging: Optional[torch.Tensor] = None
+        self._index = device
         self._dims = (n_layers, n_q_heads, n_kv_heads, head_dim)
         self._decode_ws: Optional[Tuple[int, int]] = None              # pointer and bytes of the newest
         self._decode_ws_all: List[torch.Tensor] = []
@@ -423,7 +424,7 @@ class Pool:
     # These calls run once per decoded token, on views that may take a few microseconds: their checks are kept short.
     def _place(self, name: str, t: torch.Tensor, dtype, shape) -> int:
         """Pointer of a contiguous tensor of this dtype and shape on the pool's device; ValueError for any other."""
-        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {self.device}, got "
                              f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (strided)'}")
         return t.data_ptr()
@@ -469,7 +470,7 @@ class Pool:
         return self._place(name, view.k, torch.bfloat16, shape), self._place(name, view.v, torch.bfloat16, shape), view.cap_tokens
 
     def _raw_stream(self) -> int:
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
+        return torch._C._cuda_getCurrentRawStream(self._index)
 
     def view_tree_attend(self, q: torch.Tensor, view: View, n_sel: torch.Tensor, tail: Optional[Tail], out: torch.Tensor,
                          lse: torch.Tensor, mask: Optional[torch.Tensor] = None, n_q: Optional[torch.Tensor] = None,

@@ -571,8 +571,10 @@ typedef struct {
  * kvmem_view_tree_attend reads a materialised view (any block size the pool accepts); kvmem_paged_tree_attend reads the
  * selected blocks' pages through the block table in the order of sel_ids (block sizes that divide 64 tokens or are a
  * multiple of it), as kvmem_paged_attend does, with its rule for ids out of range.  Built for head_dim 128.  HBM traffic:
- * one read of the view up to 256 query rows (n_q_tokens * H/G) per KV head, one per 256 rows above.
+ * one read of the view up to 256 query rows (n_q_tokens * H/G) per KV head, one per 256 rows above.  The result does not
+ * depend on timing: the same bits from run to run.
  * An n_tokens[s] outside [0, cap_tokens - n_q[s]] is clamped to it and reported as KVMEM_E_DEVICE_RANGE.
+ * A call is limited to 2^30 tiles of 128 tokens over all sessions, layers and KV heads, and to 65,536 query rows per KV head.
  * Errors: KVMEM_E_INVALID (pointers, sizes, n_q_tokens, tail too short), KVMEM_E_UNSUPPORTED, KVMEM_E_CAPACITY (workspace),
  * KVMEM_E_STATE (an FP8 repository, paged form). */
 size_t kvmem_tree_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens);
@@ -596,7 +598,8 @@ int kvmem_paged_tree_attend(kvmem_pool_t* pool, int32_t session_first, int32_t n
  * were.  The weights are those of the whole softmax, tail included.
  *   mass   DEVICE fp32 [n_sessions][L][G][view_cap_tokens]; decay finite and non-negative (1: plain sum)
  *   workspace  DEVICE, kvmem_mass_workspace_bytes(), 256-byte aligned
- * n_q_tokens * (H/G) <= 64.  Other arguments and errors as above. */
+ * n_q_tokens * (H/G) <= 64 and view_cap_tokens <= 2^24 (KVMEM_E_UNSUPPORTED otherwise).  The workspace holds the logits of all
+ * query rows: 4 bytes per row, KV head and token of the view's capacity.  Other arguments and errors as above. */
 size_t kvmem_mass_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens,
                                   int32_t view_cap_tokens);
 int kvmem_view_attend_mass(kvmem_pool_t* pool, int32_t n_sessions, const void* q /*DEVICE*/, int32_t n_q_tokens,

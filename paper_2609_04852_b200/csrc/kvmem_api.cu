@@ -1108,6 +1108,7 @@ static int tree_common(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32
     }
     if (n_q_tokens < 1 || n_q_tokens > kMaxDrafted) { set_error("n_q_tokens must be in [1, %d]", kMaxDrafted); return KVMEM_E_INVALID; }
     if (p->cfg.head_dim != 128) { set_error("attention kernel is built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
+    if ((int64_t)n_q_tokens * p->geo.r > 65536) { set_error("n_q_tokens * (H/G) = %lld exceeds 65536 rows per KV head", (long long)n_q_tokens * p->geo.r); return KVMEM_E_UNSUPPORTED; }
     if (!(scale >= 0.0f) || !std::isfinite(scale)) { set_error("scale must be finite and non-negative (0 selects 1/sqrt(d))"); return KVMEM_E_INVALID; }
     if (tail) {
         if (!tail->k || !tail->v || !tail->n_tokens || !aligned(tail->k, 16) || !aligned(tail->v, 16)) {
@@ -1198,6 +1199,7 @@ int kvmem_view_attend_mass(kvmem_pool_t* p, int32_t n_sessions, const void* q, i
     if (!mass || !aligned(mass, 16)) { set_error("kvmem_view_attend_mass: mass must be a 16-byte aligned device pointer"); return KVMEM_E_INVALID; }
     if (!(decay >= 0.0f) || !std::isfinite(decay)) { set_error("decay must be finite and non-negative"); return KVMEM_E_INVALID; }
     if (a.rows > 64) { set_error("n_q_tokens * (H/G) = %d exceeds 64 rows per call", a.rows); return KVMEM_E_UNSUPPORTED; }
+    if (view_cap_tokens > (1 << 24)) { set_error("views of more than 2^24 tokens are not supported"); return KVMEM_E_UNSUPPORTED; }
     const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, view_cap_tokens);
     if (workspace_bytes < need) { set_error("weight workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
     a.mass = mass; a.decay = decay;

@@ -231,6 +231,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (warp == 0) {
         // the CTA's part of the line, and the session it starts in
         int sum = 0, live = 0, lo_t = INT32_MAX, hi_t = 0;    // tiles and heads of one KV head, over the sessions
+#pragma unroll 4
         for (int s = lane; s < a.ns; s += 32) {
             const TreeSpan sp = tree_span(a, s, blockIdx.x == 0);
             const int heads = sp.tiles ? sp.groups : 0;

@@ -213,6 +213,29 @@ def test_long_and_ragged_views(i, paged):
         c.check()
 
 
+@pytest.mark.parametrize("mass", [False, True])
+def test_many_sessions(mass):
+    """More sessions than a warp has lanes, most of them short, some empty, some without a drafted token."""
+    ns = 101
+    c = Case(ns=ns, H=8, G=2, B=16, lens=[(7 * s) % 23 if s % 5 else 0 for s in range(ns)], M=3, n_q=[s % 4 for s in range(ns)],
+             tails=[(11 * s) % 41 for s in range(ns)], mask="chain" if mass else "tree", seed=9, cap_blocks=23)
+    before = None
+    if mass:
+        c.mass = c.guards.empty((ns, 1, 2, c.capb * c.B), torch.float32, fill=0.25)
+        before = c.mass.clone()
+    c.call(**({"decay": 0.5} if mass else {}))
+    c.check(0.5, before)
+
+
+def test_the_same_bits_from_run_to_run():
+    c = Case(seed=3, **LONG[0])
+    c.call()
+    first = (c.out.clone(), c.lse.clone())
+    for _ in range(10):
+        c.call()
+    assert torch.equal(c.out, first[0]) and torch.equal(c.lse, first[1])
+
+
 @pytest.mark.parametrize("i", [1, 4])
 def test_weights_over_long_and_ragged_views(i):
     c = Case(seed=230 + i, **{**LONG[i], "mask": "chain", "M": 4})

@@ -598,7 +598,7 @@ int kvmem_paged_tree_attend(kvmem_pool_t* pool, int32_t session_first, int32_t n
  * were.  The weights are those of the whole softmax, tail included.
  *   mass   DEVICE fp32 [n_sessions][L][G][view_cap_tokens]; decay finite and non-negative (1: plain sum)
  *   workspace  DEVICE, kvmem_mass_workspace_bytes(), 256-byte aligned
- * n_q_tokens * (H/G) <= 64 and view_cap_tokens <= 2^24 (KVMEM_E_UNSUPPORTED otherwise).  The workspace holds the logits of all
+ * n_q_tokens * (H/G) <= 64 and view_cap_tokens <= 2^23 (KVMEM_E_UNSUPPORTED otherwise).  The workspace holds the logits of all
  * query rows: 4 bytes per row, KV head and token of the view's capacity.  Other arguments and errors as above. */
 size_t kvmem_mass_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens,
                                   int32_t view_cap_tokens);

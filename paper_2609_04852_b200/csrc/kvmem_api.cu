@@ -1199,7 +1199,7 @@ int kvmem_view_attend_mass(kvmem_pool_t* p, int32_t n_sessions, const void* q, i
     if (!mass || !aligned(mass, 16)) { set_error("kvmem_view_attend_mass: mass must be a 16-byte aligned device pointer"); return KVMEM_E_INVALID; }
     if (!(decay >= 0.0f) || !std::isfinite(decay)) { set_error("decay must be finite and non-negative"); return KVMEM_E_INVALID; }
     if (a.rows > 64) { set_error("n_q_tokens * (H/G) = %d exceeds 64 rows per call", a.rows); return KVMEM_E_UNSUPPORTED; }
-    if (view_cap_tokens > (1 << 24)) { set_error("views of more than 2^24 tokens are not supported"); return KVMEM_E_UNSUPPORTED; }
+    if (view_cap_tokens > (1 << 23)) { set_error("views of more than 2^23 tokens are not supported"); return KVMEM_E_UNSUPPORTED; }
     const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, view_cap_tokens);
     if (workspace_bytes < need) { set_error("weight workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
     a.mass = mass; a.decay = decay;

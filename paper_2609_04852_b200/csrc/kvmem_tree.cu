@@ -648,31 +648,31 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
 }
 
-// Joins the segments of one query row in the order of the line, four dimensions a lane.  Bound by latency: a round of dependent
-// reads costs some 2 us here, so a warp requests the sums of sixteen shares together.  WARPS = 4: four warps a row, each with
-// sixteen of 64 shares, where all rows are resident at a time that way (one CTA an SM): 13.7 us a call at 2,048 tokens and 32
-// rows per KV head against 15.7; WARPS = 1 where there are more rows: 7.6 us against 28 for 2,048 of them.
+// Joins the segments of one query row in the order of the line, four dimensions a lane.  Bound by latency (a round of dependent
+// reads costs some 2 us here), so a row gets WARPS warps, each with a run of its shares, as far as all rows are then resident
+// at a time (one CTA an SM), and a warp requests sixteen sums together.  Four warps against one, a call at 2,048 tokens and 32
+// rows per KV head: 13.7 us against 15.7; at 2,048 rows in all the merge alone takes 28 us with four and 7.6 with one.
 constexpr int kMergeThreads = 256;
-constexpr int kMergeWideRows = kSMs * kMergeThreads / 128;            // rows up to which a row gets four warps
 template <int WARPS>
 __global__ void __launch_bounds__(kMergeThreads, WARPS == 1 ? 2 : 1)
 tree_merge_kernel(const __grid_constant__ TreeWork w) {
     constexpr int ROWS = kMergeThreads / 32 / WARPS;
     __shared__ float4 sums[ROWS][WARPS][32];
+    __shared__ float2 stats[ROWS][WARPS];
     pdl_wait();
     pdl_trigger();
     const TreeArgs& a = w.a;
     const int LG = a.L * a.G, hz = blockIdx.x, s = hz / LG, lg = hz % LG, lane = threadIdx.x & 31;
-    const int quarter = (threadIdx.x >> 5) % WARPS, mine = (threadIdx.x >> 5) / WARPS;
+    const int part = (threadIdx.x >> 5) % WARPS, mine = (threadIdx.x >> 5) / WARPS;
     const int row = blockIdx.y * ROWS + mine;
     const TreeInfo in = w.info[s], line = w.info[a.ns];
     const int m = row / a.r;
     const bool there = m < in.n_q;
-    const int rg = row / (2 * kTreeRows), rr = row % (2 * kTreeRows);
     float z = 0.0f, top = -INFINITY;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     bool nf = false;
     if (there && in.tiles > 0) {
+        const int rg = row / (2 * kTreeRows), rr = row % (2 * kTreeRows);
         const int first = in.start + (lg * in.groups + rg) * (in.tiles + line.groups) + line.groups;
         const int c0 = line_owner(first, line.start, line.tiles), c1 = line_owner(first + in.tiles - 1, line.start, line.tiles);
         const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
@@ -681,62 +681,60 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
         const size_t at0 = (seg * 2 + (per == 1 ? rr >> 7 : 0)) * w.rows_slot + (rr & 127), step = (size_t)(3 - per) * w.rows_slot;
         const float4* po = reinterpret_cast<const float4*>(w.part_o + at0 * kTreeD) + lane;
         for (int c = lane; c <= c1 - c0; c += 32) { const ulonglong2 f = w.part_nf[seg + c]; nf |= (f.x | f.y) != 0; }
-        // the statistics of 64 shares at a time, two a lane; what there is is rescaled when the maximum grows
-        for (int i0 = 0; i0 < parts; i0 += 64) {
-            const int left = min(64, parts - i0);
-            float2 ml[2];
-            bool holds[2];                                    // a share without a visible token holds no sums
-            float f[2], zi = 0.0f, mx = -INFINITY;
-            uint32_t live[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                ml[e] = 32 * e + lane < left ? w.part_ml[at0 + (size_t)(i0 + 32 * e + lane) * step] : make_float2(-INFINITY, 0.0f);
-                holds[e] = ml[e].x > -INFINITY || ml[e].y != 0.0f;
-                live[e] = __ballot_sync(0xffffffffu, holds[e]);
-                mx = fmaxf(mx, ml[e].x);
-            }
+        // the statistics of 32 shares at a time, a lane each; what there is is rescaled when the maximum grows
+        const int last = (int)((long long)parts * (part + 1) / WARPS);
+        for (int i0 = (int)((long long)parts * part / WARPS); i0 < last; i0 += 32) {
+            const int left = min(32, last - i0);
+            const float2 ml = lane < left ? w.part_ml[at0 + (size_t)(i0 + lane) * step] : make_float2(-INFINITY, 0.0f);
+            const bool holds = ml.x > -INFINITY || ml.y != 0.0f;          // a share without a visible token holds no sums
+            const uint32_t live = __ballot_sync(0xffffffffu, holds);
+            float mx = ml.x;
 #pragma unroll
             for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
             const float to = fmaxf(top, mx), back = top > -INFINITY ? t5::ex2(top - to) : 1.0f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                f[e] = holds[e] ? t5::ex2(ml[e].x - to) : 0.0f;
-                if (holds[e]) zi += f[e] * ml[e].y;
-            }
+            const float f = holds ? t5::ex2(ml.x - to) : 0.0f;
+            float zi = holds ? f * ml.y : 0.0f;
 #pragma unroll
             for (int d = 16; d; d >>= 1) zi += __shfl_xor_sync(0xffffffffu, zi, d);
             acc.x *= back; acc.y *= back; acc.z *= back; acc.w *= back;
             z = z * back + zi;
             top = to;
-            // sixteen at a time: all of them, or this warp's
 #pragma unroll 1
-            for (int b = WARPS == 1 ? 0 : quarter; b < (WARPS == 1 ? (left + 15) / 16 : quarter + 1); ++b) {
-                const uint32_t here = ((b & 2) ? live[1] : live[0]) >> (16 * (b & 1));
-                const float fb = (b & 2) ? f[1] : f[0];
+            for (int u0 = 0; u0 < left; u0 += 16) {
                 float4 v[16];
 #pragma unroll
                 for (int u = 0; u < 16; ++u)
-                    if ((here >> u) & 1u) v[u] = po[(size_t)(i0 + 16 * b + u) * step * (kTreeD / 4)];
+                    if ((live >> (u0 + u)) & 1u) v[u] = po[(size_t)(i0 + u0 + u) * step * (kTreeD / 4)];
 #pragma unroll
                 for (int u = 0; u < 16; ++u) {
-                    const float fu = __shfl_sync(0xffffffffu, fb, 16 * (b & 1) + u);
-                    if ((here >> u) & 1u) { acc.x += fu * v[u].x; acc.y += fu * v[u].y; acc.z += fu * v[u].z; acc.w += fu * v[u].w; }
+                    const float fu = __shfl_sync(0xffffffffu, f, u0 + u);
+                    if ((live >> (u0 + u)) & 1u) { acc.x += fu * v[u].x; acc.y += fu * v[u].y; acc.z += fu * v[u].z; acc.w += fu * v[u].w; }
                 }
             }
         }
         nf = __any_sync(0xffffffffu, nf);
     }
     if (WARPS > 1) {
-        sums[mine][quarter][lane] = acc;
+        sums[mine][part][lane] = acc;
+        if (lane == 0) stats[mine][part] = make_float2(top, z);
         __syncthreads();
     }
-    if (quarter > 0 || !there) return;
+    if (part > 0 || !there) return;
     if (WARPS > 1) {
-        const float4 b1 = sums[mine][1 % WARPS][lane], b2 = sums[mine][2 % WARPS][lane], b3 = sums[mine][3 % WARPS][lane];
-        acc.x = (acc.x + b1.x) + (b2.x + b3.x);
-        acc.y = (acc.y + b1.y) + (b2.y + b3.y);
-        acc.z = (acc.z + b1.z) + (b2.z + b3.z);
-        acc.w = (acc.w + b1.w) + (b2.w + b3.w);
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) top = fmaxf(top, stats[mine][i].x);
+        z = 0.0f;
+        acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) {
+            const float2 st = stats[mine][i];
+            if (st.x > -INFINITY || st.y != 0.0f) {
+                const float f = t5::ex2(st.x - top);
+                const float4 v = sums[mine][i][lane];
+                z += f * st.y;
+                acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+            }
+        }
     }
     const size_t orow = (((size_t)s * a.M + m) * a.L + lg / a.G) * a.H + (size_t)(lg % a.G) * a.r + row % a.r;
     const bool none = z == 0.0f;
@@ -763,28 +761,57 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
     }
 }
 
-// mass = decay mass + sum over the rows of exp2(logit - lse): the logits that the attention left, four tokens a thread.
-__global__ void __launch_bounds__(128)
+// mass = decay mass + sum over the rows of exp2(logit - lse), from the logits that the attention left.  A warp takes 256 tokens,
+// eight a lane, and four to eight of the rows, so that a thread has eight loads in flight; `split` warps (1, 2, 4, 8) share out
+// the rows of their tokens and a block's warps cover WARPS / split runs of tokens.  (One row a warp: 19 us instead of 13 for 64
+// heads of 65,536 tokens and four rows; all rows in one warp: 17 us more for 64 rows of 20,000 tokens.)
+constexpr int kMassTokens = 256;
+template <int split, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS)
 tree_mass_kernel(const __grid_constant__ TreeWork w) {
+    __shared__ float4 sums[WARPS][2][32];
     pdl_wait();
     pdl_trigger();
     const TreeArgs& a = w.a;
-    const int hz = blockIdx.x, s = hz / (a.L * a.G);
+    const int hz = blockIdx.x, s = hz / (a.L * a.G), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const TreeSpan sp = tree_span(a, s, false);
-    const int t = (blockIdx.y * 128 + threadIdx.x) * 4;
-    if (t >= sp.n_view) return;                          // n_view is a multiple of 16
-    const int rows = sp.n_q * a.r;
-    const float* lp = w.logits + (size_t)hz * a.rows * a.cap + t;
-    const float* zp = w.lse2 + (size_t)hz * a.rows;
-    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int row = 0; row < rows; ++row) {
-        const float4 v = *reinterpret_cast<const float4*>(lp + (size_t)row * a.cap);
-        const float z = zp[row];
-        sum.x += t5::ex2(v.x - z); sum.y += t5::ex2(v.y - z); sum.z += t5::ex2(v.z - z); sum.w += t5::ex2(v.w - z);
+    const int block0 = blockIdx.y * (kMassTokens * (WARPS / split));
+    if (block0 >= sp.n_view) return;
+    const int rows = sp.n_q * a.r, part = warp % split, t0 = block0 + warp / split * kMassTokens + 4 * lane;
+    float4* mp = reinterpret_cast<float4*>(a.mass + (size_t)hz * a.cap + t0);
+    float4 sum[2], m[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        sum[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (part == 0 && t0 + 128 * e < sp.n_view) m[e] = mp[32 * e];       // n_view is a multiple of 16
     }
-    float4* mp = reinterpret_cast<float4*>(a.mass + (size_t)hz * a.cap + t);
-    const float4 m = *mp;
-    *mp = make_float4(fmaf(a.decay, m.x, sum.x), fmaf(a.decay, m.y, sum.y), fmaf(a.decay, m.z, sum.z), fmaf(a.decay, m.w, sum.w));
+#pragma unroll 4
+    for (int row = part; row < rows; row += split) {
+        const float4* lp = reinterpret_cast<const float4*>(w.logits + ((size_t)hz * a.rows + row) * a.cap + t0);
+        const float z = w.lse2[(size_t)hz * a.rows + row];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (t0 + 128 * e < sp.n_view) {
+                const float4 v = __ldcs(lp + 32 * e);
+                sum[e].x += t5::ex2(v.x - z); sum[e].y += t5::ex2(v.y - z); sum[e].z += t5::ex2(v.z - z); sum[e].w += t5::ex2(v.w - z);
+            }
+    }
+    if (split > 1) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) sums[warp][e][lane] = sum[e];
+        __syncthreads();
+        if (part > 0) return;
+        for (int i = 1; i < split; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float4 v = sums[warp + i][e][lane];
+                sum[e].x += v.x; sum[e].y += v.y; sum[e].z += v.z; sum[e].w += v.w;
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (t0 + 128 * e < sp.n_view)
+            mp[32 * e] = make_float4(fmaf(a.decay, m[e].x, sum[e].x), fmaf(a.decay, m[e].y, sum[e].y), fmaf(a.decay, m[e].z, sum[e].z), fmaf(a.decay, m[e].w, sum[e].w));
 }
 
 // sizes and places inside the workspace; base null: sizes alone
@@ -861,10 +888,20 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     else e = a.rows <= kTreeRows ? launch_split<1, false, false>(p, grid, st, m, w) : launch_split<2, false, false>(p, grid, st, m, w);
     if (e != cudaSuccess) return e;
     const long long all_rows = (long long)a.ns * LG * a.rows;
-    if (all_rows <= kMergeWideRows) e = launch_pdl(tree_merge_kernel<4>, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + 1) / 2)), dim3(kMergeThreads), 0, st, w);
-    else e = launch_pdl(tree_merge_kernel<1>, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + 7) / 8)), dim3(kMergeThreads), 0, st, w);
+    auto merge = [&](auto kernel, int rows) {
+        return launch_pdl(kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.rows + rows - 1) / rows)), dim3(kMergeThreads), 0, st, w);
+    };
+    e = all_rows <= kSMs ? merge(tree_merge_kernel<8>, 1) : all_rows <= 2 * kSMs ? merge(tree_merge_kernel<4>, 2)
+      : all_rows <= 4 * kSMs ? merge(tree_merge_kernel<2>, 4) : merge(tree_merge_kernel<1>, 8);
     if (e != cudaSuccess || !a.mass) return e;
-    return launch_pdl(tree_mass_kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.cap + 511) / 512)), dim3(128), 0, st, w);
+    auto weights = [&](auto kernel, int tokens, int warps) {
+        return launch_pdl(kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.cap + tokens - 1) / tokens)), dim3(32 * warps), 0, st, w);
+    };
+    // few rows and enough tokens to fill the SMs in long runs: whole warps on tokens; else the rows are shared out (5.3 -> 3.3 us at
+    // 2,048 tokens)
+    const bool many = (long long)a.ns * LG * (a.cap / (8 * kMassTokens)) >= 2 * kSMs;
+    return many && a.rows <= 4 ? weights(tree_mass_kernel<1, 8>, 8 * kMassTokens, 8) : many && a.rows <= 8 ? weights(tree_mass_kernel<2, 8>, 4 * kMassTokens, 8)
+         : a.rows <= 16 ? weights(tree_mass_kernel<4, 4>, kMassTokens, 4) : weights(tree_mass_kernel<8, 8>, kMassTokens, 8);
 }
 
 }  // namespace kvmem

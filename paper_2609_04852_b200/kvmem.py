@@ -157,6 +157,14 @@ def _dev(t: torch.Tensor, dtype=None) -> int:
     return t.data_ptr()
 
 
+def _place(name: str, t: torch.Tensor, dtype, shape: tuple, device: int) -> int:
+    """Pointer of a contiguous tensor of this dtype and shape on this device; ValueError for any other."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on cuda:{device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (strided)'}")
+    return t.data_ptr()
+
+
 class HostStep:
     """kvmem_recall_step_host with its arguments checked and marshalled once; see Pool.host_step."""
 
@@ -422,17 +430,10 @@ class Pool:
 
     # ---- decode over a view: drafted tokens, accumulated weights, eviction
     # These calls run once per decoded token, on views that may take a few microseconds: their checks are kept short.
-    def _place(self, name: str, t: torch.Tensor, dtype, shape) -> int:
-        """Pointer of a contiguous tensor of this dtype and shape on the pool's device; ValueError for any other."""
-        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {self.device}, got "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (strided)'}")
-        return t.data_ptr()
-
     def _decode_workspace(self, sizer, key, workspace: Optional[torch.Tensor]) -> Tuple[int, int]:
         """sizer(cfg, *key) bytes: the caller's tensor, or the pool's own."""
         if workspace is not None:
-            return self._place("workspace", workspace, torch.uint8, (workspace.numel(),)), workspace.numel()
+            return _place("workspace", workspace, torch.uint8, (workspace.numel(),), self._index), workspace.numel()
         need = self._decode_need.get((sizer.__name__, key))
         if need is None:
             need = sizer(C.byref(self.cfg), *key)
@@ -448,26 +449,29 @@ class Pool:
 
     def _decode_common(self, q, n_sel, tail, out, lse, n_q):
         L, H, G, d = self._dims
+        dev, bf16, i32 = self._index, torch.bfloat16, torch.int32
         if q.dim() != 5:
             raise ValueError("q: expected [n_sessions][n_q_tokens][L][H][d]")
-        ns, M = q.shape[0], q.shape[1]
-        shape, place = (ns, M, L, H, d), self._place
-        qp = place("q", q, torch.bfloat16, shape)
-        np_ = place("n_sel", n_sel, torch.int32, (ns,))
-        op, lp = place("out", out, torch.bfloat16, shape), place("lse", lse, torch.float32, shape[:4])
-        nq = None if n_q is None else place("n_q", n_q, torch.int32, (ns,))
+        ns, M, _, _, _ = q.shape
+        shape, per_session = (ns, M, L, H, d), (ns,)
+        qp = _place("q", q, bf16, shape, dev)
+        np_ = _place("n_sel", n_sel, i32, per_session, dev)
+        op, lp = _place("out", out, bf16, shape, dev), _place("lse", lse, torch.float32, (ns, M, L, H), dev)
+        nq = None if n_q is None else _place("n_q", n_q, i32, per_session, dev)
         tp = None
         if tail is not None:
-            cap = tail.k.shape[1] if tail.k.dim() == 5 else -1
+            tk = tail.k
+            cap = tk.shape[1] if tk.dim() == 5 else -1
             ts = (ns, cap, L, G, d)
-            tp = C.byref(TailStruct(place("tail.k", tail.k, torch.bfloat16, ts), place("tail.v", tail.v, torch.bfloat16, ts),
-                                    cap, place("tail.n_tokens", tail.n_tokens, torch.int32, (ns,))))
+            tp = TailStruct(_place("tail.k", tk, bf16, ts, dev), _place("tail.v", tail.v, bf16, ts, dev), cap,
+                            _place("tail.n_tokens", tail.n_tokens, i32, per_session, dev))
         return ns, M, qp, np_, tp, op, lp, nq
 
     def _view_of(self, name: str, view: View, ns: int) -> Tuple[int, int, int]:
         L, _, G, d = self._dims
-        shape = (ns, L, G, view.cap_tokens, d)
-        return self._place(name, view.k, torch.bfloat16, shape), self._place(name, view.v, torch.bfloat16, shape), view.cap_tokens
+        cap = view.cap_tokens
+        shape = (ns, L, G, cap, d)
+        return _place(name, view.k, torch.bfloat16, shape, self._index), _place(name, view.v, torch.bfloat16, shape, self._index), cap
 
     def _raw_stream(self) -> int:
         return torch._C._cuda_getCurrentRawStream(self._index)
@@ -481,7 +485,7 @@ class Pool:
         streams, other captured graphs) need a workspace each (kvmem_tree_workspace_bytes); None: the pool's own."""
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         vk, vv, cap = self._view_of("view", view, ns)
-        mp = None if mask is None else self._place("mask", mask, torch.int64, (ns, M))
+        mp = None if mask is None else _place("mask", mask, torch.int64, (ns, M), self._index)
         wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace)
         _check(self.lib.kvmem_view_tree_attend(self.handle, ns, qp, M, nq, mp, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, self._raw_stream()))
 
@@ -491,8 +495,8 @@ class Pool:
                           workspace: Optional[torch.Tensor] = None) -> None:
         """view_tree_attend straight over the selected blocks' pages: sel_ids int32 [n_sessions][stride]."""
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
-        sp = self._place("sel_ids", sel_ids, torch.int32, (ns, sel_ids.shape[-1]))
-        mp = None if mask is None else self._place("mask", mask, torch.int64, (ns, M))
+        sp = _place("sel_ids", sel_ids, torch.int32, (ns, sel_ids.shape[-1]), self._index)
+        mp = None if mask is None else _place("mask", mask, torch.int64, (ns, M), self._index)
         wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace)
         _check(self.lib.kvmem_paged_tree_attend(self.handle, session_first, ns, qp, M, nq, mp, sp, sel_ids.shape[-1], np_, tp,
                                                 scale, op, lp, wp, wn, self._raw_stream()))
@@ -505,7 +509,7 @@ class Pool:
         L, _, G, _ = self._dims
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         vk, vv, cap = self._view_of("view", view, ns)
-        ap = self._place("mass", mass, torch.float32, (ns, L, G, cap))
+        ap = _place("mass", mass, torch.float32, (ns, L, G, cap), self._index)
         wp, wn = self._decode_workspace(self.lib.kvmem_mass_workspace_bytes, (ns, M, cap), workspace)
         _check(self.lib.kvmem_view_attend_mass(self.handle, ns, qp, M, nq, vk, vv, cap, np_, tp, scale, ap, decay, op, lp, wp, wn,
                                                self._raw_stream()))
@@ -523,9 +527,9 @@ class Pool:
         vk, vv, cap = self._view_of("view", view, ns)
         dk, dv, dcap = self._view_of("dst", dst, ns)
         heads = (ns, L, G)
-        ap, dp = self._place("mass", mass, torch.float32, (*heads, cap)), self._place("dst_mass", dst_mass, torch.float32, (*heads, dcap))
-        kp = None if kept is None else self._place("kept", kept, torch.int32, (*heads, keep * B))
-        np_, no = self._place("n_sel", n_sel, torch.int32, (ns,)), self._place("n_sel_out", n_sel_out, torch.int32, (ns,))
+        ap, dp = _place("mass", mass, torch.float32, (*heads, cap), self._index), _place("dst_mass", dst_mass, torch.float32, (*heads, dcap), self._index)
+        kp = None if kept is None else _place("kept", kept, torch.int32, (*heads, keep * B), self._index)
+        np_, no = _place("n_sel", n_sel, torch.int32, (ns,), self._index), _place("n_sel_out", n_sel_out, torch.int32, (ns,), self._index)
         wp, wn = self._decode_workspace(self.lib.kvmem_evict_workspace_bytes, (ns, keep), workspace)
         _check(self.lib.kvmem_view_evict(self.handle, ns, vk, vv, cap, np_, ap, keep, n_sink_tokens, n_recent_tokens, dk, dv, dcap,
                                          dp, kp, no, wp, wn, self._raw_stream()))

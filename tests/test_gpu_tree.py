@@ -178,6 +178,8 @@ GEOMETRIES = [
     dict(ns=2, lens=(20, 3), M=12, B=128, tails=(61, 127)),
     dict(lens=(6,), M=4, B=64, tails=(300,), mask="all"),
     dict(lens=(30,), M=8, B=64, scale=0.02),
+    dict(M=64, H=64, G=1, lens=(2,)),                                  # 4,096 rows on one KV head: sixteen row groups
+    dict(M=1, H=128, G=1, lens=(9,), mask="chain"),                    # a single token, 128 heads on a KV head
 ]
 
 
@@ -367,6 +369,92 @@ def test_an_id_out_of_range_is_reported(bad):
     torch.cuda.synchronize()
     assert c.pool.device_status() == kvmem.E_DEVICE_RANGE
     c.guards.check()
+
+
+def test_ids_may_repeat_and_come_in_any_order():
+    """The selected blocks are read in the order of sel_ids; a block that is named twice counts twice."""
+    c = Case(ns=2, lens=(7, 5), B=32, M=4, paged=True, seed=14)
+    c.sel[0, :7] = torch.tensor([6, 0, 6, 3, 1, 0, 6], dtype=torch.int32)
+    c.sel[1, :5] = torch.tensor([4, 4, 4, 4, 2], dtype=torch.int32)
+    hist = c.hk.shape[1] // c.B
+    at = c.sel.long().clamp(max=hist - 1).view(2, c.capb, 1, 1, 1, 1).expand(2, c.capb, c.B, c.L, c.G, D)
+    c.k, c.v = (x.view(2, hist, c.B, c.L, c.G, D).gather(1, at).view(2, c.capb * c.B, c.L, c.G, D).permute(0, 2, 3, 1, 4)
+                for x in (c.hk, c.hv))
+    c.call()
+    c.check()
+
+
+def test_some_of_a_pools_sessions():
+    c = Case(ns=4, lens=(3, 9, 0, 6), M=5, paged=True, seed=15, n_q=(5, 2, 4, 5))
+    whole_out, whole_lse = torch.full_like(c.out, 77.0), torch.full_like(c.lse, 55.0)
+    c.call()
+    whole_out.copy_(c.out); whole_lse.copy_(c.lse)
+    part = slice(1, 3)
+    out, lse = torch.full_like(c.out[part].contiguous(), 77.0), torch.full_like(c.lse[part].contiguous(), 55.0)
+    c.pool.paged_tree_attend(c.q[part].contiguous(), c.sel[part].contiguous(), c.n_sel[part].contiguous(),
+                             Tail(c.tk[part].contiguous(), c.tv[part].contiguous(), c.nt_dev[part].contiguous()), out, lse,
+                             mask=c.mask[part].contiguous(), n_q=c.nq_dev[part].contiguous(), session_first=1)
+    torch.cuda.synchronize()
+    # other cuts of the line, other roundings of the same sums: within the roundings of the weights and the result
+    assert bool(((out.float() - whole_out[part].float()).abs() <= 2.0 ** -6 * whole_out[part].float().abs() + 1e-3).all())
+    assert bool(((lse - whole_lse[part]).abs() <= 1e-4)[lse > -math.inf].all())
+
+
+def test_with_plain_launches():
+    from paper_2609_04852_b200 import set_option
+    c = Case(seed=16, **LONG[0])
+    c.call()
+    torch.cuda.synchronize()
+    first = c.out.clone()
+    set_option("pdl", 0)
+    try:
+        c.out.fill_(77.0); c.lse.fill_(55.0)
+        c.call()
+        c.check()
+    finally:
+        set_option("pdl", 1)
+    assert torch.equal(c.out, first)
+
+
+def test_a_first_call_may_be_captured():
+    """A process whose first calls are captured: nothing they need is set up by an eager call before."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2609_04852_b200 import Pool, Tail, View
+pool = Pool(1, 8, 2, 128, 64, 1, 1, 1, 0)
+g = torch.Generator(device="cuda").manual_seed(1)
+rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)
+def buffers(M):
+    return rnd(1, M, 1, 8, 128), torch.zeros(1, M, 1, 8, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, M, 1, 8, device="cuda")
+view, n = View(rnd(1, 1, 2, 640, 128), rnd(1, 1, 2, 640, 128), 640), torch.tensor([9], dtype=torch.int32, device="cuda")
+tail = Tail(rnd(1, 80, 1, 2, 128), rnd(1, 80, 1, 2, 128), torch.tensor([5], dtype=torch.int32, device="cuda"))
+mass, dm = torch.zeros(1, 1, 2, 640, device="cuda"), torch.zeros(1, 1, 2, 256, device="cuda")
+dst, nd = View(torch.zeros(1, 1, 2, 256, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 1, 2, 256, 128, dtype=torch.bfloat16, device="cuda"), 256), torch.zeros(1, dtype=torch.int32, device="cuda")
+few, many, one = buffers(3), buffers(64), buffers(1)
+def all_calls():
+    pool.view_tree_attend(few[0], view, n, tail, few[1], few[2])
+    pool.view_tree_attend(many[0], view, n, tail, many[1], many[2])
+    pool.view_attend_mass(one[0], view, n, mass, one[1], one[2], tail=tail, decay=0.0)
+    pool.view_evict(view, n, mass, dst, nd, dm, n_sink_tokens=3)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    all_calls()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (few[1], many[1], one[1], mass, dst.k, dm, nd)]
+assert pool.device_status() == 0 and nd.item() == 4 and float(mass.sum()) > 0 and all(float(t.float().abs().sum()) > 0 for t in got)
+all_calls()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (few[1], many[1], one[1], mass, dst.k, dm, nd)))
+print("same")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0 and "same" in done.stdout, done.stderr[-2000:]
 
 
 MASS = [

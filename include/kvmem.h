@@ -574,7 +574,8 @@ typedef struct {
  * one read of the view up to 256 query rows (n_q_tokens * H/G) per KV head, one per 256 rows above.  The result does not
  * depend on timing: the same bits from run to run.
  * An n_tokens[s] outside [0, cap_tokens - n_q[s]] is clamped to it and reported as KVMEM_E_DEVICE_RANGE.
- * A call is limited to 2^30 tiles of 128 tokens over all sessions, layers and KV heads, and to 65,536 query rows per KV head.
+ * A call is limited to 2^30 tiles of 128 tokens over all sessions, layers and KV heads (2^29 with more than 128 query rows per
+ * KV head, counted per 256 rows), and to 65,536 query rows per KV head.
  * Errors: KVMEM_E_INVALID (pointers, sizes, n_q_tokens, tail too short), KVMEM_E_UNSUPPORTED, KVMEM_E_CAPACITY (workspace),
  * KVMEM_E_STATE (an FP8 repository, paged form). */
 size_t kvmem_tree_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens);

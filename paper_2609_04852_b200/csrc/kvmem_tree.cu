@@ -46,7 +46,6 @@ constexpr int kTreeVWarp = 18;
 // tile, but more requests than HBM's latency asks for only lengthen its queues: eight sessions of 65,536 tokens take 176 us
 // with four slots and 181 with six, 262,144 tokens with weights 237 and 250, 32,768 tokens 37.7 with either.
 constexpr int kTreeRing = 4;
-constexpr int kTreeSwitch = 3;                    // what going on to another head costs a CTA, in tiles
 constexpr float kTreeSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
 constexpr uint32_t kTreeIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
 constexpr uint32_t kTreeIdescO = kTreeIdescS | (1u << 16);                                        // B with dims contiguous (V as it lies)
@@ -108,9 +107,25 @@ __device__ __forceinline__ uint32_t tail_word(int c0, int n_tail, unsigned long 
 // row tiles of row group rg when the session has `rows` live rows: with one, the slots take tiles in turn
 __device__ __forceinline__ int tree_row_tiles(int rows, int rg) { return rows - rg * 2 * kTreeRows > kTreeRows ? 2 : 1; }
 
-// The line: per (session, KV head, row group) `lead` units that stand for what going on to another head costs a CTA, and a unit
-// per tile; CTA c of n has units [total c / n, total (c + 1) / n).  The host refuses calls that could pass 2^30 units.
-constexpr int kTreeMostTiles = 1 << 30;
+// The line: per (session, KV head, row group) `lead` units that stand for what going on to another head costs a CTA, and units for
+// its tiles; CTA c of n has the tiles that begin in units [total c / n, total (c + 1) / n).  A tile is one unit; in a call
+// where heads may have two row tiles (wide: more than 128 rows) one with two is two, and a part is two units or more, so that no
+// CTA between two others of a head is left without a tile of it.  (All tiles alike: 53 us instead of 49 for rows of 256 + 8, 64
+// instead of 55 for 256 + 128, 24,864 tokens, 8 heads; the longer walk costs calls of 192 or 256 rows 1.5 to 5 %.)  The host refuses
+// calls that could pass 2^30 units.
+constexpr int kTreeMostUnits = 1 << 30;
+constexpr __host__ __device__ int tree_lead(bool wide) { return wide ? 8 : 3; }
+constexpr __host__ __device__ int tree_most(bool wide) { return wide ? 2 : 1; }     // units of a tile at most
+struct TreeCosts {
+    int shift;         // log2 of the units of a tile of the last row group; the ones before it have two row tiles
+    int full, head;    // units of a row group before the last, of the KV head
+    __device__ __forceinline__ TreeCosts(const TreeSpan& sp, int r, int lead) {
+        shift = tree_row_tiles(sp.n_q * r, sp.groups - 1) - 1;
+        full = 2 * sp.tiles + lead;
+        head = (sp.groups - 1) * full + (sp.tiles << shift) + lead;
+    }
+};
+
 // x * m / d; the product fits 32 bits in any call that fits the memory, and a division of 64 bits takes several times as long
 __device__ __forceinline__ int mul_div(int x, int m, int d) {
     const unsigned long long p = (unsigned long long)x * (unsigned)m;
@@ -143,25 +158,37 @@ struct TreeWalk {
     int s, lg, rg, head, t0, t1;  // the segment: tiles [t0, t1) of head `head` (a row group of a KV head)
     int qt;                       // its row tiles
     TreeSpan sp;
+    template <bool WIDE>
     __device__ __forceinline__ bool next(const TreeArgs& a, int most_groups) {
         const int LG = a.L * a.G;
         while (pos < end) {
             sp = tree_span(a, s, false);
             while (true) {
-                const int units = sp.tiles ? (sp.tiles + lead) * sp.groups * LG : 0;
+                const int units = sp.tiles ? (WIDE ? TreeCosts(sp, a.r, lead).head : sp.tiles + lead) * LG : 0;
                 if (base + units > pos) break;
                 base += units;
                 sp = tree_span(a, ++s, false);
             }
-            const int per = sp.tiles + lead, at = (pos - base) / per, from = base + at * per + lead;   // unit of the head's first tile
-            t0 = max(pos - from, 0);
-            t1 = min(sp.tiles, end - from);
-            pos = min(end, from + sp.tiles);
-            if (t0 >= t1) continue;                       // nothing but the head's lead
-            lg = at / sp.groups;
-            rg = at % sp.groups;
+            int from, shift = 0;                              // unit of the row group's first tile; a tile is 2^shift units
+            rg = 0;
+            if (WIDE) {
+                const TreeCosts u(sp, a.r, lead);
+                lg = (pos - base) / u.head;
+                from = base + lg * u.head;
+                if (sp.groups > 1) rg = min((pos - from) / u.full, sp.groups - 1);
+                shift = rg == sp.groups - 1 ? u.shift : 1;
+                from += rg * u.full + lead;
+            } else {
+                lg = (pos - base) / (sp.tiles + lead);
+                from = base + lg * (sp.tiles + lead) + lead;
+            }
+            const int up = (1 << shift) - 1;
+            t0 = (max(pos - from, 0) + up) >> shift;
+            t1 = min(sp.tiles, WIDE ? (max(end - from, 0) + up) >> shift : end - from);
+            pos = min(end, from + (sp.tiles << shift));
+            if (t0 >= t1) continue;                           // nothing but the head's lead
             head = (s * LG + lg) * most_groups + rg;
-            qt = tree_row_tiles(sp.n_q * a.r, rg);
+            qt = shift + 1;
             return true;
         }
         return false;
@@ -230,15 +257,23 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     pdl_trigger();
     if (warp == 0) {
         // the CTA's part of the line, and the session it starts in
-        int sum = 0, live = 0, lo_t = INT32_MAX, hi_t = 0;    // tiles and heads of one KV head, over the sessions
+        constexpr bool WIDE = QT == 2;
+        int sum = 0, live = 0, lo_t = INT32_MAX, hi_t = 0;    // one KV head of all sessions: units of tiles, row groups; units of a row group
 #pragma unroll 4
         for (int s = lane; s < a.ns; s += 32) {
             const TreeSpan sp = tree_span(a, s, blockIdx.x == 0);
             const int heads = sp.tiles ? sp.groups : 0;
-            sum += sp.tiles * heads;
+            if (WIDE) {
+                const TreeCosts u(sp, a.r, 0);
+                sum += heads ? u.head : 0;
+                lo_t = min(lo_t, sp.tiles << u.shift);
+                hi_t = max(hi_t, heads > 1 ? u.full : sp.tiles << u.shift);
+            } else {
+                sum += sp.tiles * heads;
+                lo_t = min(lo_t, sp.tiles);
+                hi_t = max(hi_t, sp.tiles);
+            }
             live += heads;
-            lo_t = min(lo_t, sp.tiles);
-            hi_t = max(hi_t, sp.tiles);
         }
         if (a.ns > 1) {
             sum = __reduce_add_sync(0xffffffffu, sum);
@@ -250,12 +285,12 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             lo_t = __shfl_sync(0xffffffffu, lo_t, 0); hi_t = __shfl_sync(0xffffffffu, hi_t, 0);
         }
         const int heads = live * LG, tiles = sum * LG;
-        int lead = heads > 1 ? kTreeSwitch : 0, n = min((int)gridDim.x, tiles);
+        int lead = heads > 1 ? tree_lead(WIDE) : 0, n = min((int)gridDim.x, (tiles + tree_most(WIDE) - 1) / tree_most(WIDE));
         // Heads of one length: with a multiple of their number of CTAs none has parts of two heads.  That costs a few SMs and saves
         // the switches; the better of the two.
         if (lo_t == hi_t && heads > 0 && heads <= gridDim.x) {
-            const int per_head = min((int)gridDim.x / heads, hi_t);
-            if ((hi_t + per_head - 1) / per_head <= (tiles + n - 1) / n + kTreeSwitch) { n = per_head * heads; lead = 0; }
+            const int per_head = min((int)gridDim.x / heads, max(hi_t / tree_most(WIDE), 1));
+            if ((hi_t + per_head - 1) / per_head <= (tiles + n - 1) / n + tree_lead(WIDE)) { n = per_head * heads; lead = 0; }
         }
         const int total = tiles + heads * lead;
         const bool idle = (int)blockIdx.x >= n;
@@ -265,7 +300,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const int s = s0 + lane;
             TreeSpan sp{};
             if (s < a.ns) sp = tree_span(a, s, false);
-            const int mine = sp.tiles ? (sp.tiles + lead) * sp.groups * LG : 0;
+            const int mine = sp.tiles ? (WIDE ? TreeCosts(sp, a.r, lead).head : sp.tiles + lead) * LG : 0;
             int incl = mine;
             if (a.ns > 1) {
 #pragma unroll
@@ -312,7 +347,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         int n = kv;                                           // next load
         const int box = PAGED ? min(a.B, 64) : 64;            // tokens per copy
         const int boxes = kTreeTile / box, per_block = PAGED ? max(a.B / 64, 1) : 1;     // copies per tile, per block
-        while (walk.next(a, w.row_groups)) {
+        while (walk.next<(QT == 2)>(a, w.row_groups)) {
             const int n_box = (walk.sp.n_view + box - 1) / box;           // copies that hold view tokens
             const int b_end = min(n_box, min(walk.t1, walk.sp.view_tiles) * boxes);
             const int NB = PAGED ? a.nblocks_dev[a.session_first + walk.s] : 0;
@@ -390,7 +425,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 }
                 if (!two || x == 1) kp.next();
             };
-            while (walk.next(a, w.row_groups)) {
+            while (walk.next<(QT == 2)>(a, w.row_groups)) {
                 two = QT == 2 && walk.qt == 2;
                 const int units = (walk.t1 - walk.t0) * (two ? 2 : 1);
                 if (ok) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)(seg & 1)) && ptx::mbar_wait(&full[kp.st], (uint32_t)kp.ph);
@@ -438,7 +473,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         };
         // the two warps that share the slot's rows 32 (warp & 3) ..
         auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(2 + x * 4 + (warp & 3)) : "memory"); };
-        while (walk.next(a, w.row_groups)) {
+        while (walk.next<(QT == 2)>(a, w.row_groups)) {
             const TreeSpan sp = walk.sp;
             const int l = walk.lg / a.G, g = walk.lg % a.G;
             const int rows = sp.n_q * a.r, row0 = walk.rg * 2 * kTreeRows;    // live rows of the head; the group's first
@@ -673,8 +708,14 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
     bool nf = false;
     if (there && in.tiles > 0) {
         const int rg = row / (2 * kTreeRows), rr = row % (2 * kTreeRows);
-        const int first = in.start + (lg * in.groups + rg) * (in.tiles + line.groups) + line.groups;
-        const int c0 = line_owner(first, line.start, line.tiles), c1 = line_owner(first + in.tiles - 1, line.start, line.tiles);
+        int first = in.start + lg * (in.tiles + line.groups) + line.groups, shift = 0;
+        if (a.rows > kTreeRows) {
+            const TreeCosts u(TreeSpan{0, 0, in.n_q, 0, in.tiles, in.groups}, a.r, line.groups);
+            first = in.start + lg * u.head + rg * u.full + line.groups;
+            shift = rg == in.groups - 1 ? u.shift : 1;
+        }
+        const int last_tile = first + ((in.tiles - 1) << shift);
+        const int c0 = line_owner(first, line.start, line.tiles), c1 = line_owner(last_tile, line.start, line.tiles);
         const size_t seg = ((size_t)s * LG + lg) * w.row_groups + rg + c0;
         // one row tile: both slots hold a share of every row; two: slot rr / 128 does
         const int per = tree_row_tiles(in.n_q * a.r, rg) == 1 ? 2 : 1, parts = (c1 - c0 + 1) * per;
@@ -880,7 +921,8 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     else m[2] = m[3] = m[0];
     if (!made) return cudaErrorInvalidValue;
     const long long most = (long long)a.ns * LG * w.row_groups * ((a.cap + kTreeTile - 1) / kTreeTile + (a.tail_cap + kTreeTile - 1) / kTreeTile);
-    if (most + (long long)a.ns * LG * w.row_groups * kTreeSwitch >= kTreeMostTiles) return cudaErrorInvalidConfiguration;
+    const bool wide = a.rows > kTreeRows;
+    if (most * tree_most(wide) + (long long)a.ns * LG * w.row_groups * tree_lead(wide) >= kTreeMostUnits) return cudaErrorInvalidConfiguration;
     const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), most);
     cudaError_t e;
     if (a.mass) e = launch_split<1, false, true>(p, grid, st, m, w);            // at most 64 rows

@@ -15,7 +15,7 @@
 // ref is a running maximum that moves only when a row's logits pass it by 8 (in powers of two): O is then rescaled in
 // tensor memory.  Until then the weights may reach 2^8, which costs neither fp32 nor bf16 any precision.
 //
-// Work: the tiles of all (session, KV head, row group) lie on one line, with a lead of three tiles' time ahead of each head for
+// Work: the tiles of all (session, KV head, row group) lie on one line, with a lead of a few tiles' time ahead of each head for
 // the switch, cut into as many equal parts as there are CTAs (one per SM), so that sessions of any lengths keep all SMs busy
 // to the end.  A CTA's share of one head is a segment;
 // each leaves unnormalised sums, row references and row sums, and tree_merge_kernel joins a head's segments in order: the
@@ -116,6 +116,7 @@ __device__ __forceinline__ int tree_row_tiles(int rows, int rg) { return rows - 
 constexpr int kTreeMostUnits = 1 << 30;
 constexpr __host__ __device__ int tree_lead(bool wide) { return wide ? 8 : 3; }
 constexpr __host__ __device__ int tree_most(bool wide) { return wide ? 2 : 1; }     // units of a tile at most
+// of a session, in a wide call
 struct TreeCosts {
     int shift;         // log2 of the units of a tile of the last row group; the ones before it have two row tiles
     int full, head;    // units of a row group before the last, of the KV head

@@ -200,6 +200,8 @@ LONG = [
     dict(ns=2, H=16, G=2, lens=(300, 299), M=33, n_q=(33, 32), tails=(600, 100), mask="all"),                  # 264 and 256 rows
     dict(ns=8, H=32, G=8, lens=(200, 52, 73, 95, 116, 137, 158, 0), M=4, tails=(33, 3, 7, 11, 14, 18, 22, 29), mask="chain"),
     dict(ns=1, H=4, G=1, lens=(3001,), M=7, B=16, tails=(1000,)),                                                 # one head on all SMs
+    dict(ns=4, H=16, G=2, lens=(100, 3, 57, 9), M=48, n_q=(48, 17, 16, 0), tails=(500, 0, 30, 4)),                # 384, 136, 128, 0 rows
+    dict(ns=2, H=16, G=2, lens=(0, 1), M=64, n_q=(64, 33), tails=(0, 70)),                                       # 512 and 264, few tiles
 ]
 
 

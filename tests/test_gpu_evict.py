@@ -123,6 +123,30 @@ def test_lengths_out_of_range_are_clamped_and_the_length_may_be_updated_in_place
     c.check()
 
 
+def test_with_plain_launches():
+    c = Case(ns=2, lens=(70, 9), keep=8, kind="ties", sink=3, seed=12)
+    kvmem.set_option("pdl", 0)
+    try:
+        c.call()
+        c.check()
+    finally:
+        kvmem.set_option("pdl", 1)
+
+
+def test_two_streams_with_their_own_workspaces():
+    cases = [Case(lens=(130,), keep=40, kind=kind, recent=5, seed=20 + i) for i, kind in enumerate(("heavy", "ties"))]
+    need = [c.pool.lib.kvmem_evict_workspace_bytes(kvmem.C.byref(c.pool.cfg), c.ns, c.keep) for c in cases]
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in need]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, w, st in zip(cases, ws, streams):
+            with torch.cuda.stream(st):
+                c.call(workspace=w, kept=None)
+    for c in cases:
+        c.check(kept_written=False)
+
+
 def test_captured_eviction_follows_the_device():
     c = Case(ns=2, lens=(9, 4), keep=3, recent=20, seed=9)
     c.call()

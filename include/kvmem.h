@@ -553,8 +553,8 @@ typedef struct {
  *     visible(i) = the T view tokens, the committed tail tokens, and each drafted token j < n_q[s] whose bit j is set in
  *                  mask[s][i]
  *     out = softmax over visible(i) of (q_i . k * scale), times v          lse = ln sum over visible(i) of exp(q_i . k * scale)
- * A token that sees nothing gets out = 0 and lse = -inf.  A token that is not visible to i does not reach i's result,
- * whatever its key and value hold (infinities and NaN included).
+ * A token that sees nothing, or nothing but logits of -inf, gets out = 0 and lse = -inf.  A token that is not visible to i
+ * does not reach i's result, whatever its key and value hold (infinities and NaN included).
  *   q        DEVICE bf16 [n_sessions][n_q_tokens][L][H][d], n_q_tokens in [1, 64]
  *   n_q      DEVICE int32 [n_sessions] drafted tokens of each session (clamped to [0, n_q_tokens]); NULL: n_q_tokens each.
  *            out and lse of the tokens behind n_q[s] are left as they were
@@ -596,7 +596,8 @@ int kvmem_paged_tree_attend(kvmem_pool_t* pool, int32_t session_first, int32_t n
  *     mass[s][l][g][t] = decay * mass[s][l][g][t] + sum over tokens i < n_q[s] and the heads h of KV head g of
  *                        exp(q_i . k_t * scale - lse[s][i][l][h])                     for t < T
  * (fp32 throughout, a fixed order of addition: the same bits from run to run).  Entries at T and above are left as they
- * were.  The weights are those of the whole softmax, tail included.
+ * were.  The weights are those of the whole softmax, tail included.  A query row whose lse is -inf adds nothing; one with a
+ * logit of NaN makes the weights of its head's view tokens NaN.
  *   mass   DEVICE fp32 [n_sessions][L][G][view_cap_tokens]; decay finite and non-negative (1: plain sum)
  *   workspace  DEVICE, kvmem_mass_workspace_bytes(), 256-byte aligned
  * n_q_tokens * (H/G) <= 64 and view_cap_tokens <= 2^23 (KVMEM_E_UNSUPPORTED otherwise).  The workspace holds the logits of all

@@ -70,7 +70,7 @@ struct TreeWork {
     float2* part_ml;              // [segment][slot][rows_slot]: (reference, sum of weights), log2 domain
     ulonglong2* part_nf;          // [segment]: a byte per row warp, set where it cleared a drafted value that is not finite
     TreeInfo* info;               // [ns + 1], filled by CTA 0
-    float* lse2;                  // [ns][LG][rows]: log-sum-exp in the log2 domain (weights only)
+    float* lse2;                  // [ns][LG][rows]: log-sum-exp in the log2 domain, +inf where it is -inf (weights only)
     float* logits;                // [ns][LG][rows][cap]: scaled logits, log2 domain (weights only)
 };
 
@@ -782,7 +782,7 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
     const bool none = z == 0.0f;
     float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (!none) { out[0] = acc.x / z; out[1] = acc.y / z; out[2] = acc.z / z; out[3] = acc.w / z; }
-    if (nf) {
+    if (nf && !none) {
         // drafted values that are not finite were left out: they reach the rows that see them here
         const unsigned long long bits = tree_bits(a, s, m, in.n_q);
         for (int j = 0; j < in.n_q; ++j)
@@ -799,7 +799,8 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
     const float lse2 = none ? -INFINITY : top + log2f(z);
     if (lane == 0) {
         a.lse[orow] = lse2 * 0.6931471805599453f;
-        if (w.lse2) w.lse2[(size_t)hz * a.rows + row] = lse2;
+        // a row without any weight adds none to its tokens: exp2(x - inf) = 0 there, where -inf - -inf would be NaN
+        if (w.lse2) w.lse2[(size_t)hz * a.rows + row] = none ? INFINITY : lse2;
     }
 }
 

@@ -1,0 +1,118 @@
+"""Decode over a view at the edges of its definitions: infinities and NaN in the call that accumulates weights."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_tree import Case
+
+pytestmark = pytest.mark.gpu
+
+
+def weights_case(mass_seed=5, **kw):
+    c = Case(mask="chain", **kw)
+    c.mass = c.guards.empty((c.ns, c.L, c.G, c.capb * c.B), torch.float32)
+    c.mass.copy_(torch.rand(c.mass.shape, generator=torch.Generator().manual_seed(mass_seed)))
+    return c
+
+
+RAGGED = dict(ns=2, L=2, lens=(3, 20), M=2, tails=(4, 0), seed=71)
+
+
+@pytest.mark.parametrize("decay", [1.0, 0.5])
+def test_rows_whose_logits_are_all_minus_infinity_add_nothing_to_the_weights(decay):
+    """Everything that the rows of one KV head see has a key of -inf in a dimension where the queries are positive: out = 0
+    (a drafted value that is not finite included), lse = -inf and the weights only decay; every other head is what it is
+    without that.  The next step's weights are ordinary."""
+    c, clean = weights_case(**RAGGED), weights_case(**RAGGED)
+    s, l, g, r = 0, 1, 1, c.H // c.G
+    heads = slice(g * r, (g + 1) * r)
+    for x in (c, clean):
+        x.q[s, :, l, heads, 5] = 1.5
+    before, finite = c.mass.clone(), (c.k[s, l, g, :, 5].clone(), c.tk[s, :, l, g, 5].clone(), c.tv[s, c.tails[s], l, g, 9].clone())
+    c.k[s, l, g, :, 5] = -math.inf
+    c.tk[s, :, l, g, 5] = -math.inf
+    c.tv[s, c.tails[s], l, g, 9] = math.inf
+    c.call(decay=decay)
+    clean.call(decay=decay)
+    torch.cuda.synchronize()
+    assert bool((c.out[s, :, l, heads] == 0).all()) and bool((c.lse[s, :, l, heads] == -math.inf).all())
+    T = c.lens[s] * c.B
+    want = before[s, l, g].clone()
+    want[:T] *= decay
+    assert torch.equal(c.mass[s, l, g], want)
+    for name in ("out", "lse", "mass"):
+        a, b = getattr(c, name).clone(), getattr(clean, name).clone()
+        for x in (a, b):
+            (x[s, l, g] if name == "mass" else x[s, :, l, heads]).zero_()
+        assert torch.equal(a, b), name
+    c.k[s, l, g, :, 5], c.tk[s, :, l, g, 5], c.tv[s, c.tails[s], l, g, 9] = finite
+    before = c.mass.clone()
+    c.call(decay=decay)
+    c.check(decay, before)
+
+
+def test_a_token_whose_logits_are_minus_infinity_keeps_its_weight():
+    """One view token with such a key: its weight only decays, the others' are those of a softmax without it (decay 0.5,
+    exact for the token; the others against the plain values of the remaining tokens, in 64 bits)."""
+    c = weights_case(lens=(5,), M=2, tails=(3,), seed=72)
+    c.q[:, :, :, :, 5] = 0.5
+    c.k[:, :, :, 17, 5] = -math.inf
+    before = c.mass.clone()
+    c.call(decay=0.5)
+    torch.cuda.synchronize()
+    assert torch.equal(c.mass[:, :, :, 17], 0.5 * before[:, :, :, 17])
+    T, r = 5 * c.B, c.H // c.G
+    rest = [t for t in range(T) if t != 17]
+    for g in range(c.G):
+        K = torch.cat([c.k[0, 0, g, rest], c.tk[0, :3 + c.M, 0, g]]).double()
+        w = torch.zeros(T - 1, dtype=torch.float64, device="cuda")
+        mag = 0.0
+        for i in range(c.M):
+            Ki = K[:T - 1 + 3 + i + 1]
+            q = c.q[0, i, 0, g * r:(g + 1) * r].double()
+            w += ((q @ Ki.T) / math.sqrt(128)).softmax(1)[:, :T - 1].sum(0)
+            mag = max(mag, ((q.abs() @ Ki.abs().T) / math.sqrt(128)).max().item())
+        want = 0.5 * before[0, 0, g, rest].double() + w
+        # the bounds of test_gpu_tree.py: a logit is off by 128 * 2^-23 of its terms' magnitudes, twice (its own and the log-sum-exp's)
+        tol = w * (2 * 128 * 2.0 ** -23 * mag + 2.0 ** -13 + 2.0 ** -20) + want * 2.0 ** -22
+        assert bool(((c.mass[0, 0, g, rest].double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_nothing_masked_reaches_the_weights(value):
+    """Keys and values behind the view's end and behind the tail, and values of drafted tokens, are not in any weight."""
+    kw = dict(ns=2, lens=(3, 5), B=32, M=4, n_q=(4, 2), tails=(9, 2), seed=73)
+    c, clean = weights_case(**kw), weights_case(**kw)
+    for s in range(2):
+        c.k[s, :, :, c.lens[s] * c.B:] = value
+        c.v[s, :, :, c.lens[s] * c.B:] = value
+        end = c.tails[s] + c.n_q[s]
+        c.tk[s, end:] = value
+        c.tv[s, end:] = value
+        c.tv[s, end - 1, :, :, 7] = value                        # a value that only the last drafted token sees
+    c.call(decay=0.5)
+    clean.call(decay=0.5)
+    torch.cuda.synchronize()
+    assert torch.equal(c.mass, clean.mass)
+    for s in range(2):
+        last = c.n_q[s] - 1
+        assert torch.equal(c.lse[s], clean.lse[s]) and torch.equal(c.out[s, :last], clean.out[s, :last])
+    c.guards.check()
+
+
+def test_a_logit_that_is_not_a_number_stays_with_its_head():
+    """A NaN among the keys of one KV head makes its rows and the weights of its tokens NaN, as the definition does, and
+    touches nothing behind the view's end and no other head."""
+    c, clean = weights_case(**RAGGED), weights_case(**RAGGED)
+    s, l, g, r = 1, 0, 1, c.H // c.G
+    c.k[s, l, g, 130, 3] = math.nan
+    c.call(decay=0.5)
+    clean.call(decay=0.5)
+    torch.cuda.synchronize()
+    T = c.lens[s] * c.B
+    assert bool(c.mass[s, l, g, :T].isnan().all()) and bool(c.out[s, :, l, g * r:(g + 1) * r].isnan().all())
+    assert torch.equal(c.mass[s, l, g, T:], clean.mass[s, l, g, T:])
+    c.mass[s, l, g] = clean.mass[s, l, g]
+    assert torch.equal(c.mass, clean.mass)
+    c.guards.check()

@@ -574,10 +574,12 @@ typedef struct {
  * one read of the view up to 256 query rows (n_q_tokens * H/G) per KV head, one per 256 rows above.  The result does not
  * depend on timing: the same bits from run to run.
  * An n_tokens[s] outside [0, cap_tokens - n_q[s]] is clamped to it and reported as KVMEM_E_DEVICE_RANGE.
- * A call is limited to 2^30 tiles of 128 tokens over all sessions, layers and KV heads (2^29 with more than 128 query rows per
- * KV head, counted per 256 rows), and to 65,536 query rows per KV head.
- * Errors: KVMEM_E_INVALID (pointers, sizes, n_q_tokens, tail too short), KVMEM_E_UNSUPPORTED, KVMEM_E_CAPACITY (workspace),
- * KVMEM_E_STATE (an FP8 repository, paged form). */
+ * A call is limited to 65,536 query rows per KV head, and to fewer than 2^30 units over all sessions, layers and KV heads, counted
+ * from the capacities: per KV head one unit for each 128 tokens of the view (or of sel_stride blocks) and of the tail, either rounded
+ * up, and 3 more; with more than 128 query rows per KV head two for each 128 tokens and 8 more, for every 256 rows.
+ * Errors: KVMEM_E_INVALID (pointers, sizes, n_q_tokens, tail too short), KVMEM_E_UNSUPPORTED (limits, head_dim, block size),
+ * KVMEM_E_CAPACITY (workspace), KVMEM_E_STATE (an FP8 repository, paged form).  The workspace sizes here and below are 0, with
+ * kvmem_last_error set, for what their calls refuse whatever else they are given. */
 size_t kvmem_tree_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens);
 int kvmem_view_tree_attend(kvmem_pool_t* pool, int32_t n_sessions, const void* q /*DEVICE*/, int32_t n_q_tokens,
                            const int32_t* n_q /*DEVICE, may be NULL*/, const uint64_t* mask /*DEVICE, may be NULL*/,
@@ -623,7 +625,9 @@ int kvmem_view_attend_mass(kvmem_pool_t* pool, int32_t n_sessions, const void* q
  *   kept          DEVICE int32 [n_sessions][L][G][C] receives the kept tokens' places in the old view, or NULL
  *   n_sel_out     DEVICE int32 [n_sessions]; may be n_sel itself
  *   workspace     DEVICE, kvmem_evict_workspace_bytes(), 256-byte aligned
- * Errors: KVMEM_E_INVALID, KVMEM_E_CAPACITY, KVMEM_E_UNSUPPORTED (head_dim other than 128). */
+ * A call is limited to 2^28 - 1 KV heads over all sessions and layers, and to 2^31 - 1 pieces of 64 kept tokens over them, counted
+ * from min(C, view_cap_tokens).
+ * Errors: KVMEM_E_INVALID, KVMEM_E_CAPACITY, KVMEM_E_UNSUPPORTED (these limits, head_dim other than 128). */
 size_t kvmem_evict_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t keep_blocks);
 int kvmem_view_evict(kvmem_pool_t* pool, int32_t n_sessions, const void* view_k /*DEVICE*/, const void* view_v /*DEVICE*/,
                      int32_t view_cap_tokens, const int32_t* n_sel /*DEVICE*/, const float* mass /*DEVICE*/,

@@ -1079,12 +1079,33 @@ static bool overlap(const void* p, size_t n, const void* q, size_t m) {
     return a < b + m && b < a + n;
 }
 
+// What the attention calls refuse for its size alone, and their workspace sizes with them.  weights: the call that accumulates
+// them; view_cap_tokens 0: a view of any length.  KVMEM_OK, or the status with its message set.
+static int tree_sizes(const kvmem_pool_config_t& c, int32_t n_sessions, int32_t n_q_tokens, bool weights, int32_t view_cap_tokens) {
+    if (n_sessions < 1 || n_sessions > 65535) { set_error("n_sessions must be in [1, 65535]"); return KVMEM_E_INVALID; }
+    if (n_q_tokens < 1 || n_q_tokens > kMaxDrafted) { set_error("n_q_tokens must be in [1, %d]", kMaxDrafted); return KVMEM_E_INVALID; }
+    if (view_cap_tokens && (view_cap_tokens < c.block_tokens || view_cap_tokens % c.block_tokens != 0)) {
+        set_error("view_cap_tokens must be a positive multiple of block_tokens");
+        return KVMEM_E_INVALID;
+    }
+    if (c.head_dim != 128) { set_error("the attention kernel is built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
+    const long long rows = (long long)n_q_tokens * (c.n_q_heads / c.n_kv_heads), most = weights ? 64 : 65536;
+    if (rows > most) { set_error("n_q_tokens * (H/G) = %lld exceeds %lld rows per KV head", rows, most); return KVMEM_E_UNSUPPORTED; }
+    if (weights && view_cap_tokens > (1 << 23)) { set_error("views of more than 2^23 tokens are not supported"); return KVMEM_E_UNSUPPORTED; }
+    return KVMEM_OK;
+}
+
+static int line_fits(const kvmem_pool_config_t& c, int32_t n_sessions, int32_t n_q_tokens, int32_t cap_tokens, int32_t tail_cap_tokens) {
+    if (tree_line_fits(c, n_sessions, n_q_tokens, cap_tokens, tail_cap_tokens)) return KVMEM_OK;
+    set_error("%d sessions of up to %d + %d tokens are more than 2^30 units of a line of tiles", n_sessions, cap_tokens, tail_cap_tokens);
+    return KVMEM_E_UNSUPPORTED;
+}
+
 static size_t tree_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t n_q_tokens, int32_t mass_cap, const char* who) {
     const char* why = "";
-    if (!cfg || !config_valid(*cfg, &why) || n_sessions < 1 || n_sessions > 65535 || n_q_tokens < 1 || n_q_tokens > kMaxDrafted || mass_cap < 0) {
-        set_error("invalid arguments to %s", who);
-        return 0;
-    }
+    if (!cfg || !config_valid(*cfg, &why)) { set_error("invalid arguments to %s", who); return 0; }
+    if (tree_sizes(*cfg, n_sessions, n_q_tokens, mass_cap > 0, mass_cap) != KVMEM_OK ||
+        line_fits(*cfg, n_sessions, n_q_tokens, mass_cap ? mass_cap : cfg->block_tokens, 0) != KVMEM_OK) return 0;
     return tree_workspace_bytes(*cfg, n_sessions, n_q_tokens, mass_cap);
 }
 
@@ -1100,15 +1121,11 @@ size_t kvmem_mass_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sess
 // what the three attention calls check alike; fills the arguments that do not depend on where the keys live
 static int tree_common(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32_t n_q_tokens, const int32_t* n_q,
                        const uint64_t* mask, const int32_t* n_sel, const kvmem_tail_t* tail, float scale, void* out, float* lse,
-                       const void* workspace, const char* who, TreeArgs* a) {
-    if (n_sessions < 1 || n_sessions > 65535) { set_error("n_sessions must be in [1, 65535]"); return KVMEM_E_INVALID; }
-    if (!q || !n_sel || !out || !lse || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256)) {
+                       const char* who, TreeArgs* a) {
+    if (!q || !n_sel || !out || !lse || !aligned(q, 16) || !aligned(out, 16)) {
         set_error("%s: null or misaligned pointer", who);
         return KVMEM_E_INVALID;
     }
-    if (n_q_tokens < 1 || n_q_tokens > kMaxDrafted) { set_error("n_q_tokens must be in [1, %d]", kMaxDrafted); return KVMEM_E_INVALID; }
-    if (p->cfg.head_dim != 128) { set_error("attention kernel is built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
-    if ((int64_t)n_q_tokens * p->geo.r > 65536) { set_error("n_q_tokens * (H/G) = %lld exceeds 65536 rows per KV head", (long long)n_q_tokens * p->geo.r); return KVMEM_E_UNSUPPORTED; }
     if (!(scale >= 0.0f) || !std::isfinite(scale)) { set_error("scale must be finite and non-negative (0 selects 1/sqrt(d))"); return KVMEM_E_INVALID; }
     if (tail) {
         if (!tail->k || !tail->v || !tail->n_tokens || !aligned(tail->k, 16) || !aligned(tail->v, 16)) {
@@ -1133,16 +1150,24 @@ static int tree_common(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32
     return KVMEM_OK;
 }
 
-static int tree_view(kvmem_pool_t* p, const void* view_k, const void* view_v, int32_t view_cap_tokens, const char* who, TreeArgs* a) {
+static int tree_view(const void* view_k, const void* view_v, int32_t view_cap_tokens, const char* who, TreeArgs* a) {
     if (!view_k || !view_v || !aligned(view_k, 128) || !aligned(view_v, 128)) {
         set_error("%s: null or misaligned pointer (views need 128-byte alignment)", who);
         return KVMEM_E_INVALID;
     }
-    if (view_cap_tokens < p->cfg.block_tokens || view_cap_tokens % p->cfg.block_tokens != 0) {
-        set_error("view_cap_tokens must be a positive multiple of block_tokens");
-        return KVMEM_E_INVALID;
-    }
     a->view_k = (const __nv_bfloat16*)view_k; a->view_v = (const __nv_bfloat16*)view_v; a->cap = view_cap_tokens;
+    return KVMEM_OK;
+}
+
+// limits of the whole call, the workspace, the launches
+static int tree_run(kvmem_pool_t* p, const TreeArgs& a, void* workspace, size_t workspace_bytes, void* stream, const char* who) {
+    const int rc = line_fits(p->cfg, a.ns, a.M, a.cap, a.tail_cap);
+    if (rc != KVMEM_OK) return rc;
+    if (!workspace || !aligned(workspace, 256)) { set_error("%s: null or misaligned workspace", who); return KVMEM_E_INVALID; }
+    const size_t need = tree_workspace_bytes(p->cfg, a.ns, a.M, a.mass ? a.cap : 0);
+    if (workspace_bytes < need) { set_error("%s: the workspace holds %zu bytes, %zu needed", who, workspace_bytes, need); return KVMEM_E_CAPACITY; }
+    const cudaError_t e = launch_tree(*p, a, workspace, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(who, e);
     return KVMEM_OK;
 }
 
@@ -1150,16 +1175,13 @@ int kvmem_view_tree_attend(kvmem_pool_t* p, int32_t n_sessions, const void* q, i
                            const uint64_t* mask, const void* view_k, const void* view_v, int32_t view_cap_tokens,
                            const int32_t* n_sel, const kvmem_tail_t* tail, float scale, void* out, float* lse, void* workspace,
                            size_t workspace_bytes, void* stream) {
+    const char* who = "kvmem_view_tree_attend";
     if (!pool_live(p)) return KVMEM_E_STATE;
     TreeArgs a{};
-    int rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, mask, n_sel, tail, scale, out, lse, workspace, "kvmem_view_tree_attend", &a);
-    if (rc == KVMEM_OK) rc = tree_view(p, view_k, view_v, view_cap_tokens, "kvmem_view_tree_attend", &a);
-    if (rc != KVMEM_OK) return rc;
-    const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, 0);
-    if (workspace_bytes < need) { set_error("tree workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
-    cudaError_t e = launch_tree(*p, a, workspace, (cudaStream_t)stream);
-    if (e != cudaSuccess) return cuda_fail("tree attention kernel launch", e);
-    return KVMEM_OK;
+    int rc = tree_sizes(p->cfg, n_sessions, n_q_tokens, false, view_cap_tokens ? view_cap_tokens : -1);
+    if (rc == KVMEM_OK) rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, mask, n_sel, tail, scale, out, lse, who, &a);
+    if (rc == KVMEM_OK) rc = tree_view(view_k, view_v, view_cap_tokens, who, &a);
+    return rc == KVMEM_OK ? tree_run(p, a, workspace, workspace_bytes, stream, who) : rc;
 }
 
 int kvmem_paged_tree_attend(kvmem_pool_t* p, int32_t session_first, int32_t n_sessions, const void* q, int32_t n_q_tokens,
@@ -1169,51 +1191,55 @@ int kvmem_paged_tree_attend(kvmem_pool_t* p, int32_t session_first, int32_t n_se
     if (!pool_live(p)) return KVMEM_E_STATE;
     if (!sessions_ok(p, session_first, n_sessions)) return KVMEM_E_INVALID;
     if (!pages_are(p, false, "kvmem_paged_tree_attend")) return KVMEM_E_STATE;
+    const char* who = "kvmem_paged_tree_attend";
     TreeArgs a{};
-    const int rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, mask, n_sel, tail, scale, out, lse, workspace, "kvmem_paged_tree_attend", &a);
+    int rc = tree_sizes(p->cfg, n_sessions, n_q_tokens, false, 0);
+    if (rc == KVMEM_OK) rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, mask, n_sel, tail, scale, out, lse, who, &a);
     if (rc != KVMEM_OK) return rc;
-    if (!paged_block_size_ok(p, false, "kvmem_paged_tree_attend")) return KVMEM_E_UNSUPPORTED;
+    if (!paged_block_size_ok(p, false, who)) return KVMEM_E_UNSUPPORTED;
     if (!sel_ids || sel_stride < 1 || (int64_t)sel_stride * p->cfg.block_tokens > INT32_MAX - 256) {
         set_error("kvmem_paged_tree_attend: sel_ids is null, or sel_stride is not positive or too long");
         return KVMEM_E_INVALID;
     }
-    const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, 0);
-    if (workspace_bytes < need) { set_error("tree workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
     a.sel_ids = sel_ids; a.sel_stride = sel_stride; a.cap = sel_stride * p->cfg.block_tokens;
     a.pages = p->pages; a.tables = p->tables; a.nblocks_dev = p->nblocks_dev; a.session_first = session_first;
     a.max_bps = p->geo.max_bps; a.max_blocks = p->geo.max_blocks;
-    cudaError_t e = launch_tree(*p, a, workspace, (cudaStream_t)stream);
-    if (e != cudaSuccess) return cuda_fail("paged tree attention kernel launch", e);
-    return KVMEM_OK;
+    return tree_run(p, a, workspace, workspace_bytes, stream, who);
 }
 
 int kvmem_view_attend_mass(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32_t n_q_tokens, const int32_t* n_q,
                            const void* view_k, const void* view_v, int32_t view_cap_tokens, const int32_t* n_sel,
                            const kvmem_tail_t* tail, float scale, float* mass, float decay, void* out, float* lse,
                            void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "kvmem_view_attend_mass";
     if (!pool_live(p)) return KVMEM_E_STATE;
     TreeArgs a{};
-    int rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, nullptr, n_sel, tail, scale, out, lse, workspace, "kvmem_view_attend_mass", &a);
-    if (rc == KVMEM_OK) rc = tree_view(p, view_k, view_v, view_cap_tokens, "kvmem_view_attend_mass", &a);
+    int rc = tree_sizes(p->cfg, n_sessions, n_q_tokens, true, view_cap_tokens ? view_cap_tokens : -1);
+    if (rc == KVMEM_OK) rc = tree_common(p, n_sessions, q, n_q_tokens, n_q, nullptr, n_sel, tail, scale, out, lse, who, &a);
+    if (rc == KVMEM_OK) rc = tree_view(view_k, view_v, view_cap_tokens, who, &a);
     if (rc != KVMEM_OK) return rc;
     if (!mass || !aligned(mass, 16)) { set_error("kvmem_view_attend_mass: mass must be a 16-byte aligned device pointer"); return KVMEM_E_INVALID; }
     if (!(decay >= 0.0f) || !std::isfinite(decay)) { set_error("decay must be finite and non-negative"); return KVMEM_E_INVALID; }
-    if (a.rows > 64) { set_error("n_q_tokens * (H/G) = %d exceeds 64 rows per call", a.rows); return KVMEM_E_UNSUPPORTED; }
-    if (view_cap_tokens > (1 << 23)) { set_error("views of more than 2^23 tokens are not supported"); return KVMEM_E_UNSUPPORTED; }
-    const size_t need = tree_workspace_bytes(p->cfg, n_sessions, n_q_tokens, view_cap_tokens);
-    if (workspace_bytes < need) { set_error("weight workspace holds %zu bytes, %zu needed", workspace_bytes, need); return KVMEM_E_CAPACITY; }
     a.mass = mass; a.decay = decay;
-    cudaError_t e = launch_tree(*p, a, workspace, (cudaStream_t)stream);
-    if (e != cudaSuccess) return cuda_fail("attention with weights kernel launch", e);
+    return tree_run(p, a, workspace, workspace_bytes, stream, who);
+}
+
+// What the eviction refuses for its size alone, and its workspace size with it; view_cap_tokens 0: a view of any length
+static int evict_sizes(const kvmem_pool_config_t& c, int32_t n_sessions, int32_t keep_blocks, int32_t view_cap_tokens) {
+    if (n_sessions < 1 || n_sessions > 65535) { set_error("n_sessions must be in [1, 65535]"); return KVMEM_E_INVALID; }
+    if (keep_blocks < 1 || (int64_t)keep_blocks * c.block_tokens > INT32_MAX) { set_error("keep_blocks must be positive and keep_blocks * block_tokens below 2^31"); return KVMEM_E_INVALID; }
+    if (c.head_dim != 128) { set_error("the eviction kernels are built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
+    if (!evict_grid_fits(c, n_sessions, keep_blocks, view_cap_tokens)) {
+        set_error("%d sessions with %d blocks kept are more than 2^31 pieces of 64 tokens, or 2^28 KV heads", n_sessions, keep_blocks);
+        return KVMEM_E_UNSUPPORTED;
+    }
     return KVMEM_OK;
 }
 
 size_t kvmem_evict_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t keep_blocks) {
     const char* why = "";
-    if (!cfg || !config_valid(*cfg, &why) || n_sessions < 1 || n_sessions > 65535 || keep_blocks < 1) {
-        set_error("invalid arguments to kvmem_evict_workspace_bytes");
-        return 0;
-    }
+    if (!cfg || !config_valid(*cfg, &why)) { set_error("invalid arguments to kvmem_evict_workspace_bytes"); return 0; }
+    if (evict_sizes(*cfg, n_sessions, keep_blocks, 0) != KVMEM_OK) return 0;
     return evict_workspace_bytes(*cfg, n_sessions, keep_blocks);
 }
 
@@ -1222,19 +1248,17 @@ int kvmem_view_evict(kvmem_pool_t* p, int32_t n_sessions, const void* view_k, co
                      void* dst_k, void* dst_v, int32_t dst_cap_tokens, float* dst_mass, int32_t* kept, int32_t* n_sel_out,
                      void* workspace, size_t workspace_bytes, void* stream) {
     if (!pool_live(p)) return KVMEM_E_STATE;
-    if (n_sessions < 1 || n_sessions > 65535) { set_error("n_sessions must be in [1, 65535]"); return KVMEM_E_INVALID; }
+    const int B = p->cfg.block_tokens;
+    if (view_cap_tokens < B || view_cap_tokens % B != 0) { set_error("view_cap_tokens must be a positive multiple of block_tokens"); return KVMEM_E_INVALID; }
+    const int rc = evict_sizes(p->cfg, n_sessions, keep_blocks, view_cap_tokens);
+    if (rc != KVMEM_OK) return rc;
     if (!view_k || !view_v || !n_sel || !mass || !dst_k || !dst_v || !dst_mass || !n_sel_out || !workspace || !aligned(view_k, 128) ||
         !aligned(view_v, 128) || !aligned(dst_k, 128) || !aligned(dst_v, 128) || !aligned(mass, 16) || !aligned(dst_mass, 16) ||
         !aligned(workspace, 256)) {
         set_error("kvmem_view_evict: null or misaligned pointer (views need 128-byte alignment)");
         return KVMEM_E_INVALID;
     }
-    if (p->cfg.head_dim != 128) { set_error("the eviction kernels are built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
-    const int B = p->cfg.block_tokens;
-    if (view_cap_tokens < B || view_cap_tokens % B != 0 || keep_blocks < 1 || (int64_t)keep_blocks * B > dst_cap_tokens) {
-        set_error("view_cap_tokens must be a positive multiple of block_tokens and the destination hold keep_blocks >= 1 blocks");
-        return KVMEM_E_INVALID;
-    }
+    if ((int64_t)keep_blocks * B > dst_cap_tokens) { set_error("the destination holds %d tokens, %d blocks are to be kept", dst_cap_tokens, keep_blocks); return KVMEM_E_INVALID; }
     if (n_sink_tokens < 0 || n_recent_tokens < 0) { set_error("n_sink_tokens and n_recent_tokens must not be negative"); return KVMEM_E_INVALID; }
     const size_t heads = (size_t)n_sessions * p->geo.L * p->geo.G;
     const size_t src_b = heads * view_cap_tokens * 256, dst_b = heads * dst_cap_tokens * 256;

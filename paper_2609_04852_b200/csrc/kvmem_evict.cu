@@ -251,6 +251,15 @@ size_t evict_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int k
            align_up((size_t)n_sessions * c.n_layers * c.n_kv_heads * keep_blocks * c.block_tokens * 4, 256);
 }
 
+// CTAs of the gather per head
+static long long evict_chunks(long long keep_tokens, int cap) { return (std::min<long long>(keep_tokens, cap) + kEvRows - 1) / kEvRows; }
+
+bool evict_grid_fits(const kvmem_pool_config_t& c, int n_sessions, int keep_blocks, int cap_tokens) {
+    const long long heads = (long long)n_sessions * c.n_layers * c.n_kv_heads;
+    const long long chunks = cap_tokens ? evict_chunks((long long)keep_blocks * c.block_tokens, cap_tokens) : 1;
+    return heads <= INT32_MAX / 8 && heads * chunks <= INT32_MAX;              // eight CTAs a head at most in the selection
+}
+
 template <int CL>
 static cudaError_t launch_select(const kvmem_pool& p, const EvictArgs& a, int32_t* ids, int2* lengths, cudaStream_t st) {
     static PerDeviceOnce done;
@@ -280,15 +289,13 @@ cudaError_t launch_evict(const kvmem_pool& p, const EvictArgs& a, void* workspac
     int2* lengths = (int2*)workspace;
     int32_t* ids = a.kept ? a.kept : (int32_t*)((char*)workspace + align_up((size_t)a.ns * sizeof(int2), 256));
     const long long heads = (long long)a.ns * a.LG;
-    const long long chunks64 = (std::min<long long>((long long)a.keep * a.B, a.cap) + kEvRows - 1) / kEvRows;
-    if (heads * chunks64 > INT32_MAX || heads * 8 > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const int chunks = (int)evict_chunks((long long)a.keep * a.B, a.cap);
     // CTAs per head: from 2,048 tokens a CTA up, at most 8 (a portable cluster), and no more than fill the SMs once
     int cluster = 1;
     while (cluster < 8 && (long long)cluster * 2048 < a.cap && heads * cluster * 2 <= p.sm_count) cluster *= 2;
     cudaError_t e = cluster == 1 ? launch_select<1>(p, a, ids, lengths, st) : cluster == 2 ? launch_select<2>(p, a, ids, lengths, st)
                   : cluster == 4 ? launch_select<4>(p, a, ids, lengths, st) : launch_select<8>(p, a, ids, lengths, st);
     if (e != cudaSuccess) return e;
-    const int chunks = (int)chunks64;
     return launch_pdl(evict_gather_kernel, dim3((unsigned)heads * (unsigned)chunks), dim3(256), 0, st, a, (const int32_t*)ids, (const int2*)lengths, chunks);
 }
 

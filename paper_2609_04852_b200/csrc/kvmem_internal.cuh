@@ -264,6 +264,7 @@ struct TreeArgs {
     float scale, decay;
 };
 size_t tree_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int mass_cap_tokens);
+bool tree_line_fits(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int cap_tokens, int tail_cap_tokens);   // launch_tree's limit
 cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace, cudaStream_t st);
 
 struct EvictArgs {
@@ -277,6 +278,7 @@ struct EvictArgs {
     int ns, LG, B, cap, dst_cap, keep, n_sink, n_recent;
 };
 size_t evict_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int keep_blocks);
+bool evict_grid_fits(const kvmem_pool_config_t& c, int n_sessions, int keep_blocks, int cap_tokens);   // launch_evict's limit; cap 0: one piece a head
 cudaError_t launch_evict(const kvmem_pool& p, const EvictArgs& a, void* workspace, cudaStream_t st);
 
 }  // namespace kvmem

@@ -112,7 +112,7 @@ __device__ __forceinline__ int tree_row_tiles(int rows, int rg) { return rows - 
 // where heads may have two row tiles (wide: more than 128 rows) one with two is two, and a part is two units or more, so that no
 // CTA between two others of a head is left without a tile of it.  (All tiles alike: 53 us instead of 49 for rows of 256 + 8, 64
 // instead of 55 for 256 + 128, 24,864 tokens, 8 heads; the longer walk costs calls of 192 or 256 rows 1.5 to 5 %.)  The host refuses
-// calls that could pass 2^30 units.
+// calls that could pass 2^30 units (tree_line_fits).
 constexpr int kTreeMostUnits = 1 << 30;
 constexpr __host__ __device__ int tree_lead(bool wide) { return wide ? 8 : 3; }
 constexpr __host__ __device__ int tree_most(bool wide) { return wide ? 2 : 1; }     // units of a tile at most
@@ -879,6 +879,16 @@ size_t tree_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int n_
     return plan_tree(c, n_sessions, n_q_tokens, mass_cap_tokens, nullptr, &w);
 }
 
+// most tiles of a row group, counted from the capacities
+static long long tree_tiles(int cap, int tail_cap) { return ((long long)cap + kTreeTile - 1) / kTreeTile + ((long long)tail_cap + kTreeTile - 1) / kTreeTile; }
+
+bool tree_line_fits(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int cap_tokens, int tail_cap_tokens) {
+    const long long rows = (long long)n_q_tokens * (c.n_q_heads / c.n_kv_heads);
+    const long long groups = (long long)n_sessions * c.n_layers * c.n_kv_heads * ((rows + 2 * kTreeRows - 1) / (2 * kTreeRows));
+    const bool wide = rows > kTreeRows;
+    return groups < kTreeMostUnits && groups * (tree_tiles(cap_tokens, tail_cap_tokens) * tree_most(wide) + tree_lead(wide)) < kTreeMostUnits;
+}
+
 // [outer][rows][128 dims] bf16, boxes of 64 dims x box_rows x 1, 128-byte swizzle; tail: [tokens][heads][128] with boxes of 64 tokens
 static bool tree_map(CUtensorMap* map, const __nv_bfloat16* p, cuuint64_t d1, cuuint64_t d2, cuuint32_t box1, cuuint32_t box2) {
     static PFN_cuTensorMapEncodeTiled_v12000 enc = [] {
@@ -922,10 +932,7 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
                tree_map(&m[3], a.tail_v, (cuuint64_t)LG, (cuuint64_t)a.ns * a.tail_cap, 1, 64);
     else m[2] = m[3] = m[0];
     if (!made) return cudaErrorInvalidValue;
-    const long long most = (long long)a.ns * LG * w.row_groups * ((a.cap + kTreeTile - 1) / kTreeTile + (a.tail_cap + kTreeTile - 1) / kTreeTile);
-    const bool wide = a.rows > kTreeRows;
-    if (most * tree_most(wide) + (long long)a.ns * LG * w.row_groups * tree_lead(wide) >= kTreeMostUnits) return cudaErrorInvalidConfiguration;
-    const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), most);
+    const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), (long long)a.ns * LG * w.row_groups * tree_tiles(a.cap, a.tail_cap));
     cudaError_t e;
     if (a.mass) e = launch_split<1, false, true>(p, grid, st, m, w);            // at most 64 rows
     else if (paged) e = a.rows <= kTreeRows ? launch_split<1, true, false>(p, grid, st, m, w) : launch_split<2, true, false>(p, grid, st, m, w);

@@ -430,15 +430,16 @@ class Pool:
 
     # ---- decode over a view: drafted tokens, accumulated weights, eviction
     # These calls run once per decoded token, on views that may take a few microseconds: their checks are kept short.
-    def _decode_workspace(self, sizer, key, workspace: Optional[torch.Tensor]) -> Tuple[int, int]:
-        """sizer(cfg, *key) bytes: the caller's tensor, or the pool's own."""
+    def _decode_workspace(self, sizer, key, workspace: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+        """sizer(cfg, *key) bytes: the caller's tensor, or the pool's own.  A size that has none goes to the call without a
+        workspace: it is refused there, with its own status."""
         if workspace is not None:
             return _place("workspace", workspace, torch.uint8, (workspace.numel(),), self._index), workspace.numel()
         need = self._decode_need.get((sizer.__name__, key))
         if need is None:
             need = sizer(C.byref(self.cfg), *key)
             if need == 0:
-                raise KvmemError(E_INVALID, self.lib.kvmem_last_error().decode())
+                return None, 0
             self._decode_need[(sizer.__name__, key)] = need
         if self._decode_ws is None or self._decode_ws[1] < need:
             # a captured graph may still replay on a smaller one, so those are kept; each is at least twice the one before

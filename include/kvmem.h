@@ -660,6 +660,11 @@ int kvmem_device_status(kvmem_pool_t* pool, int32_t* status /*HOST*/, void* stre
  *   waited_ns  DEVICE uint64, may be NULL: receives the time the wait lasted, in nanoseconds */
 int kvmem_selftest_wait_timeout(kvmem_pool_t* pool, uint32_t limit_us, uint64_t* waited_ns /*DEVICE*/, void* stream);
 
+/* The same for the wait of the tree attention's MMA thread, which asks up to three barriers together: barrier unmet (0 .. 2) of
+ * the three is never arrived at, the other two are complete.  Arguments, status and effects as above.  (No counterpart.) */
+int kvmem_selftest_joint_wait_timeout(kvmem_pool_t* pool, int32_t unmet, uint32_t limit_us, uint64_t* waited_ns /*DEVICE*/,
+                                      void* stream);
+
 /* Process-wide implementation switches used to compare kernel variants; "gather_mode" and "score_mode"
  * never change results, "chunk_poly" moves scores by a few 1e-6 relative.  (No counterpart in the paper.)  "gather_mode": 1 = bulk asynchronous copies through shared memory
  * (default), 0 = 128-bit load/store copy.  "score_mode" (decode-sized queries): 1 = dot products on the

@@ -72,6 +72,26 @@ __device__ __forceinline__ bool mbar_wait_limited(uint64_t* bar, uint32_t parity
 }
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) { return mbar_wait_limited(bar, parity, kWaitLimitNs); }
 
+// Same bound, for up to three phases (null: none) that are asked together, for one thread; the last is the one that is waited
+// for longest.
+__device__ __forceinline__ bool mbar_wait_joint_limited(uint64_t* b0, int ph0, uint64_t* b1, int ph1, uint64_t* b2, int ph2, uint64_t limit_ns) {
+    uint64_t t0 = 0;
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+        const bool k0 = b0 == nullptr || mbar_test_wait(b0, (uint32_t)ph0), k1 = b1 == nullptr || mbar_test_wait(b1, (uint32_t)ph1);
+        const bool k2 = mbar_try_wait(b2, (uint32_t)ph2);
+        if (k0 & k1 & k2) return true;
+        if ((i & 255u) == 255u) {
+            const uint64_t now = globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > limit_ns) return false;
+        }
+    }
+    return false;
+}
+__device__ __forceinline__ bool mbar_wait_joint(uint64_t* b0, int ph0, uint64_t* b1, int ph1, uint64_t* b2, int ph2) {
+    return mbar_wait_joint_limited(b0, ph0, b1, ph1, b2, ph2, kWaitLimitNs);
+}
+
 // Same bound, for waits that are expected to be long (a control warp waiting for the warps that do the
 // arithmetic): every attempt may stay suspended in hardware for up to kSuspendNs, so the waiting warp
 // issues almost no instructions and leaves the issue slots and the shared-memory pipe to the others.

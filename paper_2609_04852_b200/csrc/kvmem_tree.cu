@@ -137,22 +137,6 @@ __device__ __forceinline__ int line_owner(int x, int total, int n) {
     return p < (1ull << 32) ? (int)((unsigned)p / (unsigned)total) : (int)(p / (unsigned)total);
 }
 
-// Waits for up to three phases (null: none), asked together; the last is the one that is waited for longest.
-__device__ __forceinline__ bool wait_step(uint64_t* b0, int ph0, uint64_t* b1, int ph1, uint64_t* b2, int ph2) {
-    uint64_t t0 = 0;
-    for (uint32_t i = 0; i < kSpinLimit; ++i) {
-        const bool k0 = b0 == nullptr || ptx::mbar_test_wait(b0, (uint32_t)ph0), k1 = b1 == nullptr || ptx::mbar_test_wait(b1, (uint32_t)ph1);
-        const bool k2 = ptx::mbar_try_wait(b2, (uint32_t)ph2);
-        if (k0 & k1 & k2) return true;
-        if ((i & 255u) == 255u) {
-            const uint64_t now = ptx::globaltimer_ns();
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > kWaitLimitNs) return false;
-        }
-    }
-    return false;
-}
-
 // a role's walk over the CTA's segments
 struct TreeWalk {
     int pos, end, base, lead;     // next unit of the line, the CTA's end, first unit of session s
@@ -438,7 +422,7 @@ tree_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 for (int u = 0; u < units; ++u) {
                     const int x = u & 1;
                     const bool more = u + 2 < units, fresh = !two || x == 0;           // fresh: this slot meets the tiles first
-                    if (ok) ok = wait_step(fresh ? &full[vp.st] : nullptr, vp.ph, more && fresh ? &full[kp.st] : nullptr, kp.ph, &p_full[x], p_ph[x]);
+                    if (ok) ok = ptx::mbar_wait_joint(fresh ? &full[vp.st] : nullptr, vp.ph, more && fresh ? &full[kp.st] : nullptr, kp.ph, &p_full[x], p_ph[x]);
                     p_ph[x] ^= 1;
                     if (ok) {
                         t5::fence_after();

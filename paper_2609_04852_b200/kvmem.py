@@ -105,6 +105,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "kvmem_view_attend_fp8": (C.c_int, [vp, i32, vp, i32, vp, vp, i32, vp, f32, f32, f32, vp, vp, vp, sz, vp]),
         "kvmem_view_attend_static": (C.c_int, [vp, i32, vp, i32, vp, vp, i32, vp, f32, vp, vp, vp]),
         "kvmem_selftest_wait_timeout": (C.c_int, [vp, C.c_uint32, vp, vp]),
+        "kvmem_selftest_joint_wait_timeout": (C.c_int, [vp, i32, C.c_uint32, vp, vp]),
         "kvmem_tree_workspace_bytes": (sz, [cfgp, i32, i32]),
         "kvmem_mass_workspace_bytes": (sz, [cfgp, i32, i32, i32]),
         "kvmem_evict_workspace_bytes": (sz, [cfgp, i32, i32]),
@@ -135,7 +136,7 @@ EXPORTED = ("kvmem_pool_bytes", "kvmem_budget_blocks", "kvmem_select_workspace_b
             "kvmem_view_cache_reset", "kvmem_view_cache_update", "kvmem_view_cache_attend", "kvmem_paged_attend_rope", "kvmem_topk", "kvmem_score_host_workspace_bytes",
             "kvmem_score_host_staging_bytes", "kvmem_score_host_index", "kvmem_materialize_fp8", "kvmem_view_attend_fp8",
             "kvmem_materialize_attend_rope", "kvmem_paged_attend_fp8", "kvmem_materialize_attend_fp8",
-            "kvmem_paged_attend_fp8_rope", "kvmem_selftest_wait_timeout", "kvmem_materialize_delta",
+            "kvmem_paged_attend_fp8_rope", "kvmem_selftest_wait_timeout", "kvmem_selftest_joint_wait_timeout", "kvmem_materialize_delta",
             "kvmem_materialize_fp8_rope", "kvmem_tree_workspace_bytes", "kvmem_view_tree_attend", "kvmem_paged_tree_attend",
             "kvmem_mass_workspace_bytes", "kvmem_view_attend_mass", "kvmem_evict_workspace_bytes", "kvmem_view_evict")
 
@@ -717,6 +718,12 @@ class Pool:
         The status word then holds E_TIMEOUT until device_status() reads it."""
         waited = torch.zeros(1, dtype=torch.int64, device=self.device)
         _check(self.lib.kvmem_selftest_wait_timeout(self.handle, limit_us, waited.data_ptr(), _stream()))
+        return int(waited.item())
+
+    def selftest_joint_wait_timeout(self, unmet: int, limit_us: int = 1000) -> int:
+        """The same for the wait that asks three barriers together; barrier `unmet` (0 .. 2) is the one nobody arrives at."""
+        waited = torch.zeros(1, dtype=torch.int64, device=self.device)
+        _check(self.lib.kvmem_selftest_joint_wait_timeout(self.handle, unmet, limit_us, waited.data_ptr(), _stream()))
         return int(waited.item())
 
     def device_status(self) -> int:

@@ -1,9 +1,12 @@
-"""Decode over a view at the edges of its definitions: infinities and NaN in the call that accumulates weights."""
+"""Decode over a view at the edges of its definitions: infinities and NaN in the call that accumulates weights, a wait of its
+kernel that runs out."""
 import math
 
 import pytest
 import torch
 
+from paper_2609_04852_b200 import KvmemError
+from paper_2609_04852_b200 import kvmem
 from test_gpu_tree import Case
 
 pytestmark = pytest.mark.gpu
@@ -116,3 +119,27 @@ def test_a_logit_that_is_not_a_number_stays_with_its_head():
     c.mass[s, l, g] = clean.mass[s, l, g]
     assert torch.equal(c.mass, clean.mass)
     c.guards.check()
+
+
+@pytest.mark.parametrize("unmet", [0, 1, 2])
+def test_a_joint_wait_that_runs_out_sets_the_status_word_and_leaves_the_pool_usable(unmet):
+    """The MMA thread's wait for three barriers, one of which nobody arrives at: with a limit of 2 ms it gives up, whichever
+    of the three it is, reports KVMEM_E_TIMEOUT and returns; a call on the same pool is then right."""
+    c = Case(lens=(5,), M=40, seed=80)                           # 160 rows per KV head: two row tiles, all three barriers in use
+    assert c.pool.device_status() == 0
+    waited = c.pool.selftest_joint_wait_timeout(unmet, 2000)
+    assert 2_000_000 <= waited < 500_000_000, f"the wait lasted {waited} ns"
+    assert c.pool.device_status() == kvmem.E_TIMEOUT
+    assert c.pool.device_status() == 0
+    c.call()
+    c.check()
+
+
+def test_the_joint_waits_refusals():
+    c = Case(lens=(1,), M=1)
+    for unmet, limit_us in ((-1, 1000), (3, 1000), (0, 0), (0, 100001)):
+        with pytest.raises(KvmemError) as e:
+            c.pool.selftest_joint_wait_timeout(unmet, limit_us)
+        assert e.value.status == kvmem.E_INVALID
+    assert c.pool.lib.kvmem_selftest_joint_wait_timeout(None, 0, 1000, None, None) == kvmem.E_STATE
+    assert c.pool.device_status() == 0

@@ -242,15 +242,21 @@ class Pool:
         self._staging: Optional[torch.Tensor] = None
         self._index = device
         self._dims = (n_layers, n_q_heads, n_kv_heads, head_dim)
-        self._decode_ws: Optional[Tuple[int, int]] = None              # pointer and bytes of the newest
-        self._decode_ws_all: List[torch.Tensor] = []
+        self._decode_ws: Optional[torch.Tensor] = None
+        self._decode_at: Tuple[int, int] = (0, 0)                      # its pointer and bytes
+        self._decode_stream = 0                                        # the stream it was made on
+        self._decode_pinned = False                                    # a captured graph or another stream may still write it
+        self._decode_kept: List[torch.Tensor] = []                     # smaller ones of which that holds
         self._decode_need: Dict[tuple, int] = {}
 
     # ---- lifetime
     def close(self) -> None:
+        """The work of this pool must be over, and no captured graph of it is replayed any more: its workspaces are given back."""
         if self.handle:
             self.lib.kvmem_pool_destroy(self.handle)
             self.handle = C.c_void_p()
+            self._decode_ws, self._decode_at, self._decode_pinned = None, (0, 0), False
+            self._decode_kept.clear()
 
     def __del__(self):
         try:
@@ -431,7 +437,7 @@ class Pool:
 
     # ---- decode over a view: drafted tokens, accumulated weights, eviction
     # These calls run once per decoded token, on views that may take a few microseconds: their checks are kept short.
-    def _decode_workspace(self, sizer, key, workspace: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+    def _decode_workspace(self, sizer, key, workspace: Optional[torch.Tensor], stream: int) -> Tuple[Optional[int], int]:
         """sizer(cfg, *key) bytes: the caller's tensor, or the pool's own.  A size that has none goes to the call without a
         workspace: it is refused there, with its own status."""
         if workspace is not None:
@@ -442,12 +448,23 @@ class Pool:
             if need == 0:
                 return None, 0
             self._decode_need[(sizer.__name__, key)] = need
-        if self._decode_ws is None or self._decode_ws[1] < need:
-            # a captured graph may still replay on a smaller one, so those are kept; each is at least twice the one before
-            size = need if self._decode_ws is None else max(need, 2 * self._decode_ws[1])
-            self._decode_ws_all.append(torch.empty(size, dtype=torch.uint8, device=self.device))
-            self._decode_ws = (self._decode_ws_all[-1].data_ptr(), size)
-        return self._decode_ws
+        if self._decode_at[1] < need:
+            self._grow_decode_workspace(need, stream)
+        if not self._decode_pinned and (stream != self._decode_stream or torch._C._cuda_isCurrentStreamCapturing()):
+            self._decode_pinned = True
+        return self._decode_at
+
+    def _grow_decode_workspace(self, need: int, stream: int) -> None:
+        # One that only calls of its own stream used goes back to the allocator, which hands it out in that stream's order.  One that a
+        # captured graph replays on or another stream used is kept; small ones then at least double, so that what is kept stays little.
+        size = need
+        if self._decode_pinned:
+            self._decode_kept.append(self._decode_ws)
+            if 2 * self._decode_at[1] <= 64 << 20:
+                size = max(need, 2 * self._decode_at[1])
+        self._decode_ws, self._decode_at, self._decode_pinned = None, (0, 0), False
+        ws = torch.empty(size, dtype=torch.uint8, device=self.device)
+        self._decode_ws, self._decode_at, self._decode_stream = ws, (ws.data_ptr(), size), stream
 
     def _decode_common(self, q, n_sel, tail, out, lse, n_q):
         L, H, G, d = self._dims
@@ -488,8 +505,9 @@ class Pool:
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         vk, vv, cap = self._view_of("view", view, ns)
         mp = None if mask is None else _place("mask", mask, torch.int64, (ns, M), self._index)
-        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace)
-        _check(self.lib.kvmem_view_tree_attend(self.handle, ns, qp, M, nq, mp, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, self._raw_stream()))
+        st = self._raw_stream()
+        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace, st)
+        _check(self.lib.kvmem_view_tree_attend(self.handle, ns, qp, M, nq, mp, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, st))
 
     def paged_tree_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, tail: Optional[Tail],
                           out: torch.Tensor, lse: torch.Tensor, mask: Optional[torch.Tensor] = None,
@@ -499,9 +517,10 @@ class Pool:
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         sp = _place("sel_ids", sel_ids, torch.int32, (ns, sel_ids.shape[-1]), self._index)
         mp = None if mask is None else _place("mask", mask, torch.int64, (ns, M), self._index)
-        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace)
+        st = self._raw_stream()
+        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace, st)
         _check(self.lib.kvmem_paged_tree_attend(self.handle, session_first, ns, qp, M, nq, mp, sp, sel_ids.shape[-1], np_, tp,
-                                                scale, op, lp, wp, wn, self._raw_stream()))
+                                                scale, op, lp, wp, wn, st))
 
     def view_attend_mass(self, q: torch.Tensor, view: View, n_sel: torch.Tensor, mass: torch.Tensor, out: torch.Tensor,
                          lse: torch.Tensor, tail: Optional[Tail] = None, n_q: Optional[torch.Tensor] = None, decay: float = 1.0,
@@ -512,9 +531,10 @@ class Pool:
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         vk, vv, cap = self._view_of("view", view, ns)
         ap = _place("mass", mass, torch.float32, (ns, L, G, cap), self._index)
-        wp, wn = self._decode_workspace(self.lib.kvmem_mass_workspace_bytes, (ns, M, cap), workspace)
+        st = self._raw_stream()
+        wp, wn = self._decode_workspace(self.lib.kvmem_mass_workspace_bytes, (ns, M, cap), workspace, st)
         _check(self.lib.kvmem_view_attend_mass(self.handle, ns, qp, M, nq, vk, vv, cap, np_, tp, scale, ap, decay, op, lp, wp, wn,
-                                               self._raw_stream()))
+                                               st))
 
     def view_evict(self, view: View, n_sel: torch.Tensor, mass: torch.Tensor, dst: View, n_sel_out: torch.Tensor,
                    dst_mass: torch.Tensor, kept: Optional[torch.Tensor] = None, keep_blocks: Optional[int] = None,
@@ -532,9 +552,10 @@ class Pool:
         ap, dp = _place("mass", mass, torch.float32, (*heads, cap), self._index), _place("dst_mass", dst_mass, torch.float32, (*heads, dcap), self._index)
         kp = None if kept is None else _place("kept", kept, torch.int32, (*heads, keep * B), self._index)
         np_, no = _place("n_sel", n_sel, torch.int32, (ns,), self._index), _place("n_sel_out", n_sel_out, torch.int32, (ns,), self._index)
-        wp, wn = self._decode_workspace(self.lib.kvmem_evict_workspace_bytes, (ns, keep), workspace)
+        st = self._raw_stream()
+        wp, wn = self._decode_workspace(self.lib.kvmem_evict_workspace_bytes, (ns, keep), workspace, st)
         _check(self.lib.kvmem_view_evict(self.handle, ns, vk, vv, cap, np_, ap, keep, n_sink_tokens, n_recent_tokens, dk, dv, dcap,
-                                         dp, kp, no, wp, wn, self._raw_stream()))
+                                         dp, kp, no, wp, wn, st))
 
     def materialize_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, view: View,
                            out: torch.Tensor, lse: torch.Tensor, scale: float = 0.0, session_first: int = 0) -> None:

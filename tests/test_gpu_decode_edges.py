@@ -1,5 +1,6 @@
 """Decode over a view at the edges of its definitions: infinities and NaN in the call that accumulates weights, a wait of its
-kernel that runs out."""
+kernel that runs out, the pool's own workspace."""
+import gc
 import math
 
 import pytest
@@ -143,3 +144,99 @@ def test_the_joint_waits_refusals():
         assert e.value.status == kvmem.E_INVALID
     assert c.pool.lib.kvmem_selftest_joint_wait_timeout(None, 0, 1000, None, None) == kvmem.E_STATE
     assert c.pool.device_status() == 0
+
+
+# ---- the pool's own workspace
+
+def held():
+    """Bytes of all live tensors (as asked for, whatever blocks they came out of)."""
+    return torch.cuda.memory_stats()["requested_bytes.all.current"]
+
+
+def own_bytes(c):
+    lib, cfg = c.pool.lib, kvmem.C.byref(c.pool.cfg)
+    if c.mass is None:
+        return lib.kvmem_tree_workspace_bytes(cfg, c.ns, c.M)
+    return lib.kvmem_mass_workspace_bytes(cfg, c.ns, c.M, c.capb * c.B)
+
+
+def three_sizes():
+    """Three calls of one pool whose workspaces hold some 83, 157 and 158 MB."""
+    cases = [weights_case(lens=(3,), M=16, cap_blocks=blocks, seed=90 + i) for i, blocks in enumerate((2225, 4500, 4525))]
+    for c in cases[1:]:
+        c.pool = cases[0].pool
+    gc.collect()
+    return cases
+
+
+def test_a_workspace_that_grows_gives_the_smaller_one_back():
+    cases = three_sizes()
+    sizes = [own_bytes(c) for c in cases]
+    assert 64 << 20 < sizes[0] < sizes[1] < sizes[2] < 1.02 * sizes[1]
+    base = held()
+    for c, size in zip(cases, sizes):
+        before = c.mass.clone()
+        c.call(decay=0.5)
+        del before
+        assert held() - base == size
+    cases[0].call()                                              # a smaller call takes the larger workspace
+    assert held() - base == sizes[2]
+    cases[0].pool.close()
+    assert held() == base
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("why", ["captured", "other stream"])
+def test_a_workspace_that_may_still_be_written_is_kept(why):
+    """One that a captured graph replays on, or that a call on another stream than its own used, outlives the growth: memory
+    handed out afterwards is not written by a replay.  close() gives all of it back."""
+    cases = three_sizes()
+    sizes = [own_bytes(c) for c in cases]
+    small = cases[0]
+    small.call(decay=0.0)
+    torch.cuda.synchronize()
+    first, graph = (small.out.clone(), small.lse.clone()), None
+    if why == "captured":
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            small.call(decay=0.0)
+    else:
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            small.call(decay=0.0)
+        torch.cuda.synchronize()
+    base = held() - sizes[0]
+    cases[1].call(decay=0.0)
+    assert held() - base == sizes[0] + sizes[1]
+    if graph is not None:
+        others = [torch.full((sizes[0],), 0xA5, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        small.out.zero_()
+        small.lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(small.out, first[0]) and torch.equal(small.lse, first[1])
+        assert all(bool((o == 0xA5).all()) for o in others)
+        del others
+    cases[2].call(decay=0.0)                                     # the second was only used on its own stream: given back
+    assert held() - base == sizes[0] + sizes[2]
+    small.pool.close()
+    assert held() - base == 0
+    torch.cuda.synchronize()
+
+
+def test_small_workspaces_that_are_kept_double():
+    """Graphs captured at growing sizes: what is kept stays within twice the largest."""
+    cases = [Case(lens=(2,), M=M, seed=M) for M in (1, 2, 3, 5, 8, 13, 21, 34, 64)]
+    for c in cases[1:]:
+        c.pool = cases[0].pool
+    gc.collect()
+    start, graphs = held(), []
+    for c in cases:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.call()
+        graphs.append(g)
+    assert held() - start <= 4 * own_bytes(cases[-1])      # the newest: at most twice; the ones before: as much
+    for c, g in zip(cases, graphs):
+        g.replay()
+        c.check()

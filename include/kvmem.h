@@ -570,7 +570,10 @@ typedef struct {
  *            on the GPU (two streams, two captured graphs) need one each
  * kvmem_view_tree_attend reads a materialised view (any block size the pool accepts); kvmem_paged_tree_attend reads the
  * selected blocks' pages through the block table in the order of sel_ids (block sizes that divide 64 tokens or are a
- * multiple of it), as kvmem_paged_attend does, with its rule for ids out of range.  Built for head_dim 128.  HBM traffic:
+ * multiple of it), as kvmem_paged_attend does, with its rule for ids out of range.  Its keys are the stored ones, as they lie, in one
+ * softmax with the tail's: on a pool with rotary support these are raw keys without a position, so position-consistent decode
+ * (queries and tail at the positions behind the view) materialises first (kvmem_materialize_rope, then kvmem_view_tree_attend); with
+ * rope_in_block_keys, whose keys carry angles of their own, the paged form is refused.  Built for head_dim 128.  HBM traffic:
  * one read of the view up to 256 query rows (n_q_tokens * H/G) per KV head, one per 256 rows above.  The result does not
  * depend on timing: the same bits from run to run.
  * An n_tokens[s] outside [0, cap_tokens - n_q[s]] is clamped to it and reported as KVMEM_E_DEVICE_RANGE.
@@ -578,7 +581,7 @@ typedef struct {
  * from the capacities: per KV head one unit for each 128 tokens of the view (or of sel_stride blocks) and of the tail, either rounded
  * up, and 3 more; with more than 128 query rows per KV head two for each 128 tokens and 8 more, for every 256 rows.
  * Errors: KVMEM_E_INVALID (pointers, sizes, n_q_tokens, tail too short), KVMEM_E_UNSUPPORTED (limits, head_dim, block size),
- * KVMEM_E_CAPACITY (workspace), KVMEM_E_STATE (an FP8 repository, paged form).  The workspace sizes here and below are 0, with
+ * KVMEM_E_CAPACITY (workspace), KVMEM_E_STATE (paged form: an FP8 repository, in-block-rotated keys).  The workspace sizes here and below are 0, with
  * kvmem_last_error set, for what their calls refuse whatever else they are given. */
 size_t kvmem_tree_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens);
 int kvmem_view_tree_attend(kvmem_pool_t* pool, int32_t n_sessions, const void* q /*DEVICE*/, int32_t n_q_tokens,

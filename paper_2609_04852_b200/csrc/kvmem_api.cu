@@ -1191,6 +1191,10 @@ int kvmem_paged_tree_attend(kvmem_pool_t* p, int32_t session_first, int32_t n_se
     if (!pool_live(p)) return KVMEM_E_STATE;
     if (!sessions_ok(p, session_first, n_sessions)) return KVMEM_E_INVALID;
     if (!pages_are(p, false, "kvmem_paged_tree_attend")) return KVMEM_E_STATE;
+    if (p->cfg.rope_in_block_keys) {
+        set_error("kvmem_paged_tree_attend has no positions for keys rotated by their offset in the block: kvmem_materialize_rope and kvmem_view_tree_attend");
+        return KVMEM_E_STATE;
+    }
     const char* who = "kvmem_paged_tree_attend";
     TreeArgs a{};
     int rc = tree_sizes(p->cfg, n_sessions, n_q_tokens, false, 0);

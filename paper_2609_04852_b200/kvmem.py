@@ -513,7 +513,8 @@ class Pool:
                           out: torch.Tensor, lse: torch.Tensor, mask: Optional[torch.Tensor] = None,
                           n_q: Optional[torch.Tensor] = None, scale: float = 0.0, session_first: int = 0,
                           workspace: Optional[torch.Tensor] = None) -> None:
-        """view_tree_attend straight over the selected blocks' pages: sel_ids int32 [n_sessions][stride]."""
+        """view_tree_attend straight over the selected blocks' pages: sel_ids int32 [n_sessions][stride].  Stored keys as they lie: where
+        keys carry positions, materialize_rope and view_tree_attend (a pool with rope_in_block_keys is refused)."""
         ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
         sp = _place("sel_ids", sel_ids, torch.int32, (ns, sel_ids.shape[-1]), self._index)
         mp = None if mask is None else _place("mask", mask, torch.int64, (ns, M), self._index)

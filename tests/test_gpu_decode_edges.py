@@ -1,12 +1,12 @@
 """Decode over a view at the edges of its definitions: infinities and NaN in the call that accumulates weights, a wait of its
-kernel that runs out, the pool's own workspace."""
+kernel that runs out, the pool's own workspace, pools with rotary support."""
 import gc
 import math
 
 import pytest
 import torch
 
-from paper_2609_04852_b200 import KvmemError
+from paper_2609_04852_b200 import KvmemError, Pool
 from paper_2609_04852_b200 import kvmem
 from test_gpu_tree import Case
 
@@ -240,3 +240,59 @@ def test_small_workspaces_that_are_kept_double():
     for c, g in zip(cases, graphs):
         g.replay()
         c.check()
+
+
+# ---- pools with rotary support
+
+def rotary_pool(c, in_block):
+    """c's history in a pool whose pages hold raw keys, or keys rotated by their offset in the block."""
+    pool = Pool(c.L, c.H, c.G, 128, c.B, c.ns, c.ns * c.hk.shape[1] // c.B, c.hk.shape[1] // c.B, 0, 2048, 1e6, rope_in_block_keys=in_block)
+    for s in range(c.ns):
+        pool.append_blocks(s, c.hk[s], c.hv[s])
+    return pool
+
+
+def test_pages_of_raw_keys_are_read_as_they_lie():
+    c, plain = (Case(ns=2, L=2, lens=(5, 3), M=6, tails=(9, 70), paged=True, seed=100) for _ in range(2))
+    c.pool = rotary_pool(c, False)
+    c.call()
+    plain.call()
+    c.check()
+    assert torch.equal(c.out, plain.out) and torch.equal(c.lse, plain.lse)
+
+
+def test_pages_of_keys_rotated_in_their_block_are_refused():
+    """No position makes their angles those of one view: they are materialised first."""
+    c = Case(ns=2, lens=(5, 3), M=6, paged=True, seed=101)
+    c.pool = rotary_pool(c, True)
+    with pytest.raises(KvmemError) as e:
+        c.call()
+    assert e.value.status == kvmem.E_STATE and "materialize_rope" in str(e.value)
+    torch.cuda.synchronize()
+    assert bool((c.out == 77.0).all()) and bool((c.lse == 55.0).all())
+
+
+@pytest.mark.parametrize("in_block", [False, True])
+def test_position_consistent_decode_materialises_first(in_block):
+    """Drafted tokens at the positions behind a rotated view: the view's keys are those of compact positions, tail and
+    queries carry their own, and the result is the attention over them."""
+    c = Case(ns=2, L=2, lens=(5, 3), M=6, tails=(9, 70), paged=True, seed=102)
+    pool = rotary_pool(c, in_block)
+    view = pool.new_view(c.ns, c.capb * c.B)
+    pool.materialize_rope(c.sel, c.n_sel, view)
+    raw = c.k
+    for s in range(c.ns):
+        T, end = c.lens[s] * c.B, c.tcap
+        pos = torch.arange(T, dtype=torch.int32, device="cuda")
+        want = pool.rope_rotate(raw[s, :, :, :T].permute(2, 0, 1, 3).reshape(T, c.L * c.G, 128).contiguous(), pos).view(T, c.L, c.G, 128)
+        got = view.k[s, :, :, :T].permute(2, 0, 1, 3).float()
+        # in-block keys are rounded once more, 2^-8 of each of the two elements that a rotation mixes, and both results once (2^-8):
+        # four times 2^-8 of the head's largest element
+        assert bool(((got - want.float()).abs() <= (2.0 ** -7 * want.float().abs().amax(3, keepdim=True) * 2 if in_block else 0.0)).all())
+        tpos = torch.arange(T, T + end, dtype=torch.int32, device="cuda")
+        c.tk[s] = pool.rope_rotate(c.tk[s].reshape(end, c.L * c.G, 128).contiguous(), tpos).view(end, c.L, c.G, 128)
+        qpos = T + c.tails[s] + torch.arange(c.M, dtype=torch.int32, device="cuda")
+        c.q[s] = pool.rope_rotate(c.q[s].reshape(c.M, c.L * c.H, 128).contiguous(), qpos).view(c.M, c.L, c.H, 128)
+    c.k, c.v, c.pool, c.paged = view.k, view.v, pool, False
+    c.call()
+    c.check()

@@ -1,5 +1,5 @@
-"""Decode over a view at the edges of its definitions: infinities and NaN in the call that accumulates weights, a wait of its
-kernel that runs out, the pool's own workspace, pools with rotary support."""
+"""Decode over a view at the edges of its definitions: infinities and NaN in the call that accumulates weights, both sides of
+each choice of its last kernel, a wait of the attention kernel that runs out, the pool's own workspace, pools with rotary support."""
 import gc
 import math
 
@@ -120,6 +120,24 @@ def test_a_logit_that_is_not_a_number_stays_with_its_head():
     c.mass[s, l, g] = clean.mass[s, l, g]
     assert torch.equal(c.mass, clean.mass)
     c.guards.check()
+
+
+# Which kernel sums the weights: with 296 runs of 2,048 tokens of capacity over all heads (64 heads: 10,240 tokens) or more, up to 4
+# rows are one warp's (2,048 tokens a block), up to 8 two warps' (1,024 tokens a block); up to 16 rows, and fewer below those
+# capacities, are four warps' (256 tokens a block), more rows eight warps'.  Block sizes of 16 tokens, lengths on either side of
+# the blocks' ends, an empty view, a full one, sessions with fewer drafted tokens than the call's.
+SUMS = [(M, H, cap) for cap in (640, 639, 645) for M, H in ((1, 32), (2, 32), (3, 8), (5, 8), (1, 8), (7, 8))] + [(3, 32, 640), (8, 40, 640)]
+
+
+@pytest.mark.parametrize("decay", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("M,H,cap", SUMS)
+def test_each_kernel_that_sums_the_weights(M, H, cap, decay):
+    lens = (cap, 0, 64, 63, 129, 321, 638, 1)
+    c = weights_case(mass_seed=M, ns=8, H=H, G=8, B=16, lens=lens, M=M, n_q=[M, M, M, max(M - 1, 0), M, 1, M, (M + 1) // 2],
+                     tails=(0, 5, 130, 0, 1, 64, 17, 2), cap_blocks=cap, seed=300 + M)
+    before = c.mass.clone()
+    c.call(decay=decay)
+    c.check(decay, before)
 
 
 @pytest.mark.parametrize("unmet", [0, 1, 2])

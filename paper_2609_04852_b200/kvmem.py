@@ -150,6 +150,9 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None)      # torch.cuda.is_current_stream_capturing; a build without CUDA has none
+
+
 def _dev(t: torch.Tensor, dtype=None) -> int:
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("expected a contiguous CUDA tensor")
@@ -437,20 +440,21 @@ class Pool:
 
     # ---- decode over a view: drafted tokens, accumulated weights, eviction
     # These calls run once per decoded token, on views that may take a few microseconds: their checks are kept short.
-    def _decode_workspace(self, sizer, key, workspace: Optional[torch.Tensor], stream: int) -> Tuple[Optional[int], int]:
-        """sizer(cfg, *key) bytes: the caller's tensor, or the pool's own.  A size that has none goes to the call without a
-        workspace: it is refused there, with its own status."""
+    def _decode_workspace(self, workspace: Optional[torch.Tensor], stream: int, *key) -> Tuple[Optional[int], int]:
+        """The caller's tensor, or the pool's own of kvmem_<key[0]>_workspace_bytes(cfg, *key[1:]) bytes.  A size that has none goes to
+        the call without a workspace: it is refused there, with its own status."""
         if workspace is not None:
             return _place("workspace", workspace, torch.uint8, (workspace.numel(),), self._index), workspace.numel()
-        need = self._decode_need.get((sizer.__name__, key))
+        need = self._decode_need.get(key)
         if need is None:
-            need = sizer(C.byref(self.cfg), *key)
+            need = getattr(self.lib, f"kvmem_{key[0]}_workspace_bytes")(C.byref(self.cfg), *key[1:])
             if need == 0:
                 return None, 0
-            self._decode_need[(sizer.__name__, key)] = need
+            self._decode_need[key] = need
         if self._decode_at[1] < need:
             self._grow_decode_workspace(need, stream)
-        if not self._decode_pinned and (stream != self._decode_stream or torch._C._cuda_isCurrentStreamCapturing()):
+        # (the default stream, 0, cannot be captured: calls on it need not ask)
+        if not self._decode_pinned and (stream != self._decode_stream or (stream != 0 and _capturing())):
             self._decode_pinned = True
         return self._decode_at
 
@@ -506,7 +510,7 @@ class Pool:
         vk, vv, cap = self._view_of("view", view, ns)
         mp = None if mask is None else _place("mask", mask, torch.int64, (ns, M), self._index)
         st = self._raw_stream()
-        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace, st)
+        wp, wn = self._decode_workspace(workspace, st, "tree", ns, M)
         _check(self.lib.kvmem_view_tree_attend(self.handle, ns, qp, M, nq, mp, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, st))
 
     def paged_tree_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, tail: Optional[Tail],
@@ -519,7 +523,7 @@ class Pool:
         sp = _place("sel_ids", sel_ids, torch.int32, (ns, sel_ids.shape[-1]), self._index)
         mp = None if mask is None else _place("mask", mask, torch.int64, (ns, M), self._index)
         st = self._raw_stream()
-        wp, wn = self._decode_workspace(self.lib.kvmem_tree_workspace_bytes, (ns, M), workspace, st)
+        wp, wn = self._decode_workspace(workspace, st, "tree", ns, M)
         _check(self.lib.kvmem_paged_tree_attend(self.handle, session_first, ns, qp, M, nq, mp, sp, sel_ids.shape[-1], np_, tp,
                                                 scale, op, lp, wp, wn, st))
 
@@ -533,7 +537,7 @@ class Pool:
         vk, vv, cap = self._view_of("view", view, ns)
         ap = _place("mass", mass, torch.float32, (ns, L, G, cap), self._index)
         st = self._raw_stream()
-        wp, wn = self._decode_workspace(self.lib.kvmem_mass_workspace_bytes, (ns, M, cap), workspace, st)
+        wp, wn = self._decode_workspace(workspace, st, "mass", ns, M, cap)
         _check(self.lib.kvmem_view_attend_mass(self.handle, ns, qp, M, nq, vk, vv, cap, np_, tp, scale, ap, decay, op, lp, wp, wn,
                                                st))
 
@@ -554,7 +558,7 @@ class Pool:
         kp = None if kept is None else _place("kept", kept, torch.int32, (*heads, keep * B), self._index)
         np_, no = _place("n_sel", n_sel, torch.int32, (ns,), self._index), _place("n_sel_out", n_sel_out, torch.int32, (ns,), self._index)
         st = self._raw_stream()
-        wp, wn = self._decode_workspace(self.lib.kvmem_evict_workspace_bytes, (ns, keep), workspace, st)
+        wp, wn = self._decode_workspace(workspace, st, "evict", ns, keep)
         _check(self.lib.kvmem_view_evict(self.handle, ns, vk, vv, cap, np_, ap, keep, n_sink_tokens, n_recent_tokens, dk, dv, dcap,
                                          dp, kp, no, wp, wn, st))
 

@@ -204,25 +204,26 @@ def test_a_workspace_that_grows_gives_the_smaller_one_back():
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("why", ["captured", "other stream"])
+@pytest.mark.parametrize("why", ["captured", "captured on its stream", "other stream"])
 def test_a_workspace_that_may_still_be_written_is_kept(why):
     """One that a captured graph replays on, or that a call on another stream than its own used, outlives the growth: memory
     handed out afterwards is not written by a replay.  close() gives all of it back."""
     cases = three_sizes()
     sizes = [own_bytes(c) for c in cases]
-    small = cases[0]
-    small.call(decay=0.0)
+    small, side, graph = cases[0], torch.cuda.Stream(), None
     torch.cuda.synchronize()
-    first, graph = (small.out.clone(), small.lse.clone()), None
-    if why == "captured":
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            small.call(decay=0.0)
-    else:
-        side = torch.cuda.Stream()
+    with torch.cuda.stream(side if why == "captured on its stream" else torch.cuda.current_stream()):
+        small.call(decay=0.0)
+    torch.cuda.synchronize()
+    first = (small.out.clone(), small.lse.clone())
+    if why == "other stream":
         with torch.cuda.stream(side):
             small.call(decay=0.0)
-        torch.cuda.synchronize()
+    else:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            small.call(decay=0.0)
+    torch.cuda.synchronize()
     base = held() - sizes[0]
     cases[1].call(decay=0.0)
     assert held() - base == sizes[0] + sizes[1]

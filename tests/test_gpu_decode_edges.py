@@ -8,6 +8,7 @@ import torch
 
 from paper_2609_04852_b200 import KvmemError, Pool
 from paper_2609_04852_b200 import kvmem
+from test_gpu_evict import Case as EvictCase
 from test_gpu_tree import Case
 
 pytestmark = pytest.mark.gpu
@@ -162,6 +163,56 @@ def test_the_joint_waits_refusals():
         assert e.value.status == kvmem.E_INVALID
     assert c.pool.lib.kvmem_selftest_joint_wait_timeout(None, 0, 1000, None, None) == kvmem.E_STATE
     assert c.pool.device_status() == 0
+
+
+# ---- sizes at the ends of the ranges
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("kw", [
+    dict(M=64, H=1024, G=1, lens=(2,), B=32, tails=(9,)),                          # 65,536 rows on one KV head: 256 row groups
+    dict(M=1, H=3, G=3, lens=(1,), B=16, tails=(0,), cap_blocks=1, tail_cap=1),   # a capacity below one copy's 64 rows, one tail row
+    dict(M=5, H=4, G=2, ns=3, lens=(1, 1, 0), B=16, tails=(11, 0, 3), cap_blocks=1, tail_cap=16),
+    dict(M=2, H=2, G=1, lens=(0,), tails=(70001,)),                                # everything in the tail
+], ids=["65536 rows", "one row", "one block", "long tail"])
+def test_smallest_and_largest(paged, kw):
+    c = Case(paged=paged, seed=110, extra=0, **kw)
+    c.call()
+    c.check()
+
+
+def test_thousands_of_sessions():
+    """4,999 sessions, a few tokens each, some empty; every 97th is compared, and all of them must be written or left."""
+    ns = 4999
+    c = Case(ns=ns, H=2, G=1, B=16, lens=[(5 * s) % 3 for s in range(ns)], M=2, n_q=[s % 3 for s in range(ns)],
+             tails=[(7 * s) % 4 for s in range(ns)], mask="chain", seed=111, cap_blocks=2)
+    c.mass = c.guards.empty((ns, 1, 1, c.capb * c.B), torch.float32, fill=0.25)
+    c.call(decay=0.5)
+    torch.cuda.synchronize()
+    live = torch.arange(2).view(1, 2) < c.nq_dev.cpu().view(ns, 1)
+    assert torch.equal((c.lse != 55.0).all(3).all(2).cpu(), live)
+    for s in range(0, ns, 97):
+        one = c.n_q[s]
+        if one == 0:
+            assert bool((c.mass[s, 0, 0, :c.lens[s] * 16] == 0.125).all())
+            continue
+        p, T, ref, absv, lse, dx = c.reference(s, 0)
+        got = c.out[s, :one, 0].reshape(one * 2, 128).double()
+        assert bool(((got - ref).abs() <= (2.0 ** -8 + 2.0 ** -14 + 2 * dx) * absv * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-30).all())
+        w = p[:, :T].sum(0)
+        want = 0.125 + w
+        assert bool(((c.mass[s, 0, 0, :T].double() - want).abs() <= w * (2 * dx + 2.0 ** -13 + 2.0 ** -20) + want * 2.0 ** -22).all())
+        assert bool((c.mass[s, 0, 0, T:] == 0.25).all())
+    c.guards.check()
+
+
+@pytest.mark.parametrize("kind", ["heavy", "ties", "zero"])
+def test_eviction_by_one_cta_of_more_tokens_than_it_holds(kind):
+    """160 heads, a CTA each, two sessions of more than the 36,864 tokens whose weights fit its shared memory; a destination
+    whose capacity is no multiple of anything."""
+    lens = [580, 0, 3, 601, 1, 0, 2, 9, 5, 1]
+    c = EvictCase(ns=10, G=16, B=64, lens=lens, keep=99, sink=5, recent=130, kind=kind, seed=112, dst_cap=99 * 64 + 5)
+    c.call()
+    c.check()
 
 
 # ---- the pool's own workspace

@@ -98,8 +98,8 @@ static bool pool_live(const kvmem_pool* p) {
 }
 
 static bool sessions_ok(const kvmem_pool* p, int first, int n) {
-    if (first < 0 || n < 1 || first + n > p->cfg.max_sessions) {
-        set_error("sessions [%d, %d) outside [0, %d)", first, first + n, p->cfg.max_sessions);
+    if (first < 0 || n < 1 || first > p->cfg.max_sessions - n) {
+        set_error("sessions [%d, %lld) outside [0, %d)", first, (long long)first + n, p->cfg.max_sessions);
         return false;
     }
     return true;

@@ -104,3 +104,18 @@ def test_python_calls_report_the_calls_own_status():
             pool.view_evict(view, n, mass, kvmem.View(torch.zeros_like(view.k), torch.zeros_like(view.k), 64), n.clone(), torch.zeros_like(mass),
                             keep_blocks=0 if d == 128 else 1)
         assert e.value.status == (kvmem.E_INVALID if d == 128 else kvmem.E_UNSUPPORTED)
+
+
+@pytest.mark.gpu
+def test_session_ranges_whose_end_passes_32_bits_are_refused():
+    pool = Pool(1, 8, 2, 128, 64, 4, 4, 4, 0)
+    lib, last = pool.lib, (1 << 31) - 1
+    dev = torch.device("cuda", 0)
+    big, n = torch.zeros(1 << 20, dtype=torch.uint8, device=dev), torch.zeros(4, dtype=torch.int32, device=dev)
+    p, z, stream = big.data_ptr(), n.data_ptr(), torch.cuda.current_stream().cuda_stream
+    for first, ns in ((last, 1), (last, 4), (1, last), (last, last), (4, 1), (1, 4), (-1, 1), (0, 0), (0, -1)):
+        assert lib.kvmem_paged_tree_attend(pool.handle, first, ns, p, 1, z, None, z, 1, z, None, 0.0, p, p, p, 1 << 20, stream) == kvmem.E_INVALID, (first, ns)
+    assert lib.kvmem_session_blocks(pool.handle, last) == kvmem.E_INVALID and lib.kvmem_session_reset(pool.handle, last, stream) == kvmem.E_INVALID
+    assert lib.kvmem_session_blocks(pool.handle, 3) == 0
+    torch.cuda.synchronize()
+    assert bool((big == 0).all())

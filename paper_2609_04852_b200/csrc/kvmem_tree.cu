@@ -43,8 +43,9 @@ constexpr int kTreeRows = 128;                    // rows of a row tile: TMEM la
 constexpr int kTreeThreads = 32 * 19;              // key and value TMA warps, MMA warp, sixteen row warps
 constexpr int kTreeVWarp = 18;
 // Ring slots, K and V tiles in turn: two tiles of each per SM, 18.5 MiB over the 148.  There is room for six slots beside one Q
-// tile, but more requests than HBM's latency asks for only lengthen its queues: eight sessions of 65,536 tokens take 176 us
-// with four slots and 181 with six, 262,144 tokens with weights 237 and 250, 32,768 tokens 37.7 with either.
+// tile, but more requests than HBM's latency asks for only lengthen its queues: eight sessions of up to 65,536 tokens take 177 us
+// with four slots and 184 with six, 262,144 tokens with the weights of 16 rows 225 and 240, 32,768 tokens 34.6 and 35.2 (SM clock at
+// 1,965 MHz; under the power limit 192 and 191, 234 and 245, 34.9 and 35.4).
 constexpr int kTreeRing = 4;
 constexpr float kTreeSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
 constexpr uint32_t kTreeIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
@@ -111,8 +112,11 @@ __device__ __forceinline__ int tree_row_tiles(int rows, int rg) { return rows - 
 // its tiles; CTA c of n has the tiles that begin in units [total c / n, total (c + 1) / n).  A tile is one unit; in a call
 // where heads may have two row tiles (wide: more than 128 rows) one with two is two, and a part is two units or more, so that no
 // CTA between two others of a head is left without a tile of it.  (All tiles alike: 53 us instead of 49 for rows of 256 + 8, 64
-// instead of 55 for 256 + 128, 24,864 tokens, 8 heads; the longer walk costs calls of 192 or 256 rows 1.5 to 5 %.)  The host refuses
-// calls that could pass 2^30 units (tree_line_fits).
+// instead of 55 for 256 + 128, 24,864 tokens, 8 heads; the longer walk costs calls of 192 or 256 rows 1.5 to 5 %.)  The leads, in
+// us: eight ragged sessions of up to 24,896 tokens, 8 heads, take 75.5, 72.1, 71.9, 72.4 with a lead of 1, 2, 3, 5 at 4 rows and 82.3,
+// 80.1, 77.9, 76.5 at 48; two sessions of 24,896 and 19,264, 2 layers, 4 heads (wide) 60.9, 58.8, 57.9, 57.4 with 3, 5, 8, 12 at 136
+// rows, 67.3, 65.3, 63.8, 63.3 at 192, 69.7, 68.0, 66.7, 64.9 at 256, and the same within the noise of some 5 % at 264 to 512.
+// The host refuses calls that could pass 2^30 units (tree_line_fits).
 constexpr int kTreeMostUnits = 1 << 30;
 constexpr __host__ __device__ int tree_lead(bool wide) { return wide ? 8 : 3; }
 constexpr __host__ __device__ int tree_most(bool wide) { return wide ? 2 : 1; }     // units of a tile at most
@@ -790,8 +794,11 @@ tree_merge_kernel(const __grid_constant__ TreeWork w) {
 
 // mass = decay mass + sum over the rows of exp2(logit - lse), from the logits that the attention left.  A warp takes 256 tokens,
 // eight a lane, and four to eight of the rows, so that a thread has eight loads in flight; `split` warps (1, 2, 4, 8) share out
-// the rows of their tokens and a block's warps cover WARPS / split runs of tokens.  (One row a warp: 19 us instead of 13 for 64
-// heads of 65,536 tokens and four rows; all rows in one warp: 17 us more for 64 rows of 20,000 tokens.)
+// the rows of their tokens and a block's warps cover WARPS / split runs of tokens.  Whole calls (attention, merge, weights) with
+// 1, 2, 4, 8 warps to a row set, in us: 64 heads of 10,240 tokens 64.6, 65.3, 65.7, 68.6 at one row, 69.5, 67.9, 67.9, 70.6 at 4,
+// 72.1, 69.3, 69.2, 71.3 at 8, 79.8, 76.0, 74.3, 76.2 at 16, 115, 106, 102, 104 at 32, 214, 187, 176, 177 at 64; 8 heads of 262,144
+// tokens 184, 184, 187, 193 at 4 rows, 202, 199, 200, 207 at 8, 239, 231, 231, 237 at 16, 308, 298, 296, 300 at 32, 541, 503, 492,
+// 500 at 64.
 constexpr int kMassTokens = 256;
 template <int split, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS)
@@ -932,8 +939,8 @@ cudaError_t launch_tree(const kvmem_pool& p, const TreeArgs& a, void* workspace,
     auto weights = [&](auto kernel, int tokens, int warps) {
         return launch_pdl(kernel, dim3((unsigned)(a.ns * LG), (unsigned)((a.cap + tokens - 1) / tokens)), dim3(32 * warps), 0, st, w);
     };
-    // few rows and enough tokens to fill the SMs in long runs: whole warps on tokens; else the rows are shared out (5.3 -> 3.3 us at
-    // 2,048 tokens)
+    // Few rows and enough tokens to fill the SMs in long runs: whole warps on tokens; else the rows are shared out (5.3 -> 3.3 us at
+    // 2,048 tokens).  The two sides are within 3 % of one another where they meet.
     const bool many = (long long)a.ns * LG * (a.cap / (8 * kMassTokens)) >= 2 * kSMs;
     return many && a.rows <= 4 ? weights(tree_mass_kernel<1, 8>, 8 * kMassTokens, 8) : many && a.rows <= 8 ? weights(tree_mass_kernel<2, 8>, 4 * kMassTokens, 8)
          : a.rows <= 16 ? weights(tree_mass_kernel<4, 4>, kMassTokens, 4) : weights(tree_mass_kernel<8, 8>, kMassTokens, 8);

@@ -639,7 +639,139 @@ int kvmem_view_evict(kvmem_pool_t* pool, int32_t n_sessions, const void* view_k 
                      int32_t* kept /*DEVICE, may be NULL*/, int32_t* n_sel_out /*DEVICE*/, void* workspace /*DEVICE*/,
                      size_t workspace_bytes, void* stream);
 
+/* ---- new tokens: rotary forms, tail and pages, prompt chunks -------------------------------------
+ * The way of new tokens into the loop (Sec. 4.1: the step begins with the prefill of the new tokens; Sec. 4.3: raw keys for
+ * the index; Sec. 4.4: keys at their positions for the view; Sec. 5.2: the current query is prefilled over the new view;
+ * Sec. 5.3 "Incremental Indexing").
+ *
+ * Rotary form of a model: which dims of a head are pairs, and how far a position turns each.  The pool itself rotates pairs
+ * (i, i + d/2) by the rows of its table.  Any form is that one in another order of the dims: pair p of the model's goes to dims
+ * p and d/2 + p, the n = head_dim - rotary_dim dims that pass go, in order, to rotary_dim/2 .. d/2 - 1 and d/2 + rotary_dim/2 .. d - 1,
+ * and turn by 0.  That is the "pool's order" of a query or key; no product of a query with a key, and no Mean-K score,
+ * depends on an order that both share.  Values have no order of their own.  kvmem_rope_apply and kvmem_append_tokens take
+ * queries and keys in the model's order and give the pool's; every other call of this library takes and gives the pool's. */
+#define KVMEM_ROPE_HALF 0        /* layout: pairs (i, i + rotary_dim/2) */
+#define KVMEM_ROPE_INTERLEAVED 1 /*         pairs (2i, 2i + 1) */
+#define KVMEM_ROPE_NONE 0        /* scaling: f_i = rope_theta^(-2i/rotary_dim) */
+#define KVMEM_ROPE_LINEAR 1      /*          f_i / factor */
+#define KVMEM_ROPE_BASE 2        /*          the same with base rope_theta * factor^(rotary_dim / (rotary_dim - 2)) */
+#define KVMEM_ROPE_RAMP 3        /*          f_i/factor * x + f_i * (1 - x), x = (i - lo) / max(hi - lo, 0.001) kept in [0, 1],
+                                             lo = max(floor(p(turns_fast)), 0), hi = min(ceil(p(turns_slow)), rotary_dim - 1),
+                                             p(t) = rotary_dim ln(original_positions / (2 pi t)) / (2 ln rope_theta): the pair
+                                             that makes t turns over the original window */
+#define KVMEM_ROPE_BANDS 4       /*          the same with x = (turns_fast - t_i) / (turns_fast - turns_slow) kept in [0, 1],
+                                             t_i = original_positions f_i / (2 pi): pair i's turns over the original window */
+#define KVMEM_ORDER_MODEL 0
+#define KVMEM_ORDER_POOL 1
+typedef struct {
+    int32_t layout;
+    int32_t rotary_dim;       /* the first rotary_dim dims rotate, a multiple of 16; 0: the whole head */
+    int32_t scaling;
+    float factor;             /* >= 1; not used with KVMEM_ROPE_NONE */
+    float original_positions; /* KVMEM_ROPE_RAMP, KVMEM_ROPE_BANDS: the window the unscaled frequencies were made for */
+    float turns_fast;         /* 0 selects 32 (ramp) or 4 (bands) */
+    float turns_slow;         /* 0 selects 1 */
+} kvmem_rope_t;
+
+/* The frequencies of a form (NULL: the pool's own) on a pool of this geometry, in radians per position and in the pool's
+ * order: HOST double [head_dim / 2], 0 for the dims that pass.  Pure host.  KVMEM_E_STATE without rotary support,
+ * KVMEM_E_INVALID, KVMEM_E_UNSUPPORTED (rotary_dim). */
+int kvmem_rope_frequencies(const kvmem_pool_config_t* cfg /*HOST*/, const kvmem_rope_t* rope /*HOST, may be NULL*/,
+                           double* frequencies /*HOST*/);
+
+/* Make the pool one of a model with this rotary form (NULL: the pool's own again): its table is rebuilt on `stream` with these
+ * frequencies (angles in 64 bits, cos and sin rounded once to fp32), so that every call that rotates uses them, and
+ * kvmem_rope_apply and kvmem_append_tokens go from the model's order to the pool's.  Before any block is appended or reserved
+ * (KVMEM_E_STATE otherwise): stored keys stay in the frame they were encoded in.  Work that reads the table must be ordered
+ * behind this call (same stream, or an event). */
+int kvmem_set_rope(kvmem_pool_t* pool, const kvmem_rope_t* rope /*HOST, may be NULL*/, void* stream);
+
+/* Rotate n_rows x n_vec vectors of head_dim elements, any head_dim that takes rotary support: vector (r, u) of y is vector (r, u) of x
+ * turned to positions[r], or back by it (inverse != 0; that is also the gradient of the forward rotation), its rotated dims
+ * times amplitude.  Row r, vector u starts r * row_stride + u * vec_stride elements behind x or y (multiples of 8, 16-byte
+ * aligned bases), so queries and keys can be read where a packed projection left them.  x_order, y_order say which order the
+ * dims come and go in.  fp32 products, sums and the amplitude's product, each rounded to fp32, one rounding to bf16; dims that
+ * pass are copied.
+ *   positions  DEVICE int32 [n_rows]; rows with a position outside the table are left unwritten and flagged in the status word
+ *   amplitude  0 selects 1.  (Where a form comes with a factor m on its cos and sin: m^2 on the queries and none on the keys
+ *              gives the same logits, and is what fits keys that this library rotates.)
+ * x and y may be the same vectors if the two orders are the same; any other overlap is refused (KVMEM_E_INVALID). */
+int kvmem_rope_apply(kvmem_pool_t* pool, const void* x /*DEVICE*/, int64_t x_row_stride, int64_t x_vec_stride, int32_t x_order,
+                     void* y /*DEVICE*/, int64_t y_row_stride, int64_t y_vec_stride, int32_t y_order, int64_t n_rows, int32_t n_vec,
+                     const int32_t* positions /*DEVICE*/, int32_t inverse, float amplitude, void* stream);
+
+/* Pages for n_blocks blocks behind a session's last: taken from the pool now (phys_ids as in kvmem_append_blocks), filled by
+ * kvmem_append_tokens, part of the session only once kvmem_commit_blocks makes them so.  While a session has reserved blocks
+ * kvmem_append_blocks refuses it; kvmem_session_reset gives them back.  Errors as kvmem_append_blocks; KVMEM_E_STATE on an FP8
+ * repository or with rope_in_block_keys (their pages do not hold the raw keys that the index is made from). */
+int kvmem_reserve_blocks(kvmem_pool_t* pool, int32_t session, int32_t n_blocks, const int32_t* phys_ids /*HOST, may be NULL*/,
+                         void* stream);
+
+/* Blocks a session has reserved and not committed, or a negative status. */
+int32_t kvmem_session_reserved(const kvmem_pool_t* pool, int32_t session);
+
+/* Rows of a batch as a projection leaves them: head h of layer l of token i of session s starts
+ * s * session_stride + i * token_stride + l * layer_stride + h * head_stride elements behind data (strides: multiples of 8). */
+typedef struct {
+    const void* data; /* DEVICE bf16, 16-byte aligned */
+    int64_t session_stride, token_stride, layer_stride, head_stride;
+} kvmem_rows_t;
+
+/* Append new tokens: token i < n_new[s] of session s takes row c = tail->n_tokens[s] + i of the tail, the one behind its committed
+ * and earlier new tokens, at position positions[s][i], or first_position + n_sel[s] * block_tokens + c without positions
+ * (n_sel NULL: 0), i.e. behind a view that starts at first_position.
+ *     q_out     [s][i] = the query turned to that position, times q_amplitude (its rotated dims; 0 selects 1)
+ *     tail->k, v [s][c] = the key turned to it, the value
+ *     page of block nblocks[s] + c / block_tokens, its token c mod block_tokens = the raw key, the value  (to_pages = 1; the block has to be
+ *                 reserved: a row without a reserved page is flagged as KVMEM_E_DEVICE_RANGE, and its tail row written)
+ * Queries and keys come in the model's order and leave in the pool's.  On a pool without rotary support nothing turns.
+ * tail->n_tokens is read, not changed: the tokens are drafted ones for kvmem_view_tree_attend and kvmem_view_prefill_attend;
+ * adding to it commits them, calling again replaces them.  Counts and lengths are read on the device, so a captured call appends
+ * wherever the tail then ends.  to_pages goes with a tail whose row 0 is the token behind the session's last block.
+ *   n_new     DEVICE int32 [n_sessions] (clamped to [0, n_new_tokens]); NULL: n_new_tokens each.  Rows behind are left as they were
+ *   q         HOST struct, n_q_heads heads per layer; NULL (with q_out NULL): keys and values alone.  k, v: n_kv_heads heads
+ *   positions DEVICE int32 [n_sessions][n_new_tokens], or NULL
+ *   q_out     DEVICE bf16 [n_sessions][n_new_tokens][L][H][d]
+ * A token whose position lies outside the table is left out as a whole and flagged.  An n_tokens[s] outside
+ * [0, cap_tokens - n_new[s]] is clamped to it and flagged.  Results must not overlap the inputs or each other (KVMEM_E_INVALID).
+ * KVMEM_E_UNSUPPORTED: head_dim not a multiple of 16, or 2^31 groups of 16 elements in one session's new tokens.  KVMEM_E_STATE: to_pages
+ * on an FP8 repository or with rope_in_block_keys. */
+int kvmem_append_tokens(kvmem_pool_t* pool, int32_t session_first, int32_t n_sessions, int32_t n_new_tokens,
+                        const int32_t* n_new /*DEVICE, may be NULL*/, const kvmem_rows_t* q /*HOST, may be NULL*/,
+                        const kvmem_rows_t* k /*HOST*/, const kvmem_rows_t* v /*HOST*/, const int32_t* positions /*DEVICE, may be NULL*/,
+                        const int32_t* n_sel /*DEVICE, may be NULL*/, int32_t first_position, float q_amplitude,
+                        const kvmem_tail_t* tail /*HOST*/, void* q_out /*DEVICE, may be NULL*/, int32_t to_pages, void* stream);
+
+/* Make the first n_blocks[s] reserved blocks of each session part of it: their Mean-K rows are computed from the raw keys in
+ * their pages (the bits that kvmem_append_blocks gives for the same keys), the session's length is raised and, with a tail, the
+ * rows behind them move to its front and n_tokens[s] drops by n_blocks[s] * block_tokens.  (n_tokens below that is flagged as
+ * KVMEM_E_DEVICE_RANGE: a block was committed before its tokens were there.)
+ *   n_blocks  HOST int32 [n_sessions]; KVMEM_E_STATE if a session has fewer reserved
+ *   tail      HOST struct, may be NULL; entry s is session session_first + s */
+int kvmem_commit_blocks(kvmem_pool_t* pool, int32_t session_first, int32_t n_sessions, const int32_t* n_blocks /*HOST*/,
+                        const kvmem_tail_t* tail /*HOST, may be NULL*/, void* stream);
+
+/* Attention of a prompt chunk over view and tail: kvmem_view_tree_attend for a chain (token i sees the view, the committed tail
+ * tokens and the chunk's tokens 0 .. i) of any length.  Same arguments (tail NULL: the view alone), definitions, guarantees and
+ * error values, and the same bits from run to run; n_q_tokens has no limit of its own, and the query heads that share a KV head are at
+ * most 128.
+ *   workspace  DEVICE, kvmem_prefill_workspace_bytes(), 256-byte aligned (about 40 MB whatever the call); calls that may overlap on
+ *              the GPU need one each
+ * A call is limited to 2^30 tiles, counted from the capacities: one for each 128 tokens of view and tail, either rounded up, and 2 more,
+ * for every two row tiles of floor(128 / (H/G)) tokens of every KV head, layer and session (KVMEM_E_UNSUPPORTED).
+ * Arithmetic bound: 4 d flops per query row and visible token on the tensor cores. */
+size_t kvmem_prefill_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens);
+int kvmem_view_prefill_attend(kvmem_pool_t* pool, int32_t n_sessions, const void* q /*DEVICE*/, int32_t n_q_tokens,
+                              const int32_t* n_q /*DEVICE, may be NULL*/, const void* view_k /*DEVICE*/, const void* view_v /*DEVICE*/,
+                              int32_t view_cap_tokens, const int32_t* n_sel /*DEVICE*/, const kvmem_tail_t* tail /*HOST, may be NULL*/,
+                              float scale, void* out /*DEVICE*/, float* lse /*DEVICE*/, void* workspace /*DEVICE*/,
+                              size_t workspace_bytes, void* stream);
+
 /* ---- inspection ------------------------------------------------------------------------------ */
+
+/* The pages of a bf16 repository: DEVICE bf16 [max_blocks][K | V][n_layers][n_kv_heads][block_tokens][head_dim] (of an FP8 one, the
+ * codes as described at kvmem_pool_config_t).  The pointer aliases pool storage. */
+int kvmem_get_pages(kvmem_pool_t* pool, const void** pages /*HOST, receives DEVICE ptr*/);
 
 /* Mean-K index of a session: DEVICE bf16 [n_layers][n_kv_heads][max_blocks_per_session][head_dim]
  * (rows >= *n_blocks undefined).  The pointer aliases pool storage. */

@@ -4,6 +4,7 @@ from .kvmem import (  # noqa: F401
     KvmemError,
     Pool,
     PoolConfig,
+    Rope,
     SelectParams,
     Tail,
     View,

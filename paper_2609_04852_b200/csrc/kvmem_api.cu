@@ -219,12 +219,15 @@ int kvmem_pool_create(const kvmem_pool_config_t* cfg, void* storage, size_t byte
     p->status_dev = (int32_t*)(p->base + lay.status_off);
     p->sess_blocks.assign(cfg->max_sessions, 0);
     p->sess_pages.assign(cfg->max_sessions, {});
+    p->sess_reserved.assign(cfg->max_sessions, {});
+    p->rope_form = RopeForm{cfg->head_dim, cfg->head_dim / 16, 0};
     p->page_used.assign(cfg->max_blocks, 0);
     p->free_hint = 0;
     p->sm_count = prop.multiProcessorCount;
     p->pos0_dev = cfg->rope_max_positions > 0 ? (int32_t*)(p->base + lay.pos0_off) : nullptr;
     p->rope_dev = cfg->rope_max_positions > 0 ? (float2*)(p->base + lay.rope_off) : nullptr;
-    e = cudaMemset(p->base + lay.tables_off, 0, lay.rope_off - lay.tables_off);
+    e = cudaMemset(p->base + lay.tables_off, 0xff, lay.nblocks_off - lay.tables_off);
+    if (e == cudaSuccess) e = cudaMemset(p->base + lay.nblocks_off, 0, lay.rope_off - lay.nblocks_off);
     if (e == cudaSuccess && cfg->rope_max_positions > 0) {
         // cos/sin of position * theta^(-2i/d): angle in fp64, one rounding to fp32 (built here, on the host)
         const int half = cfg->head_dim / 2;
@@ -270,8 +273,14 @@ int kvmem_session_reset(kvmem_pool_t* p, int32_t session, void* stream) {
     // the device's block count first: kernels that size their work from it see an empty session from here on in stream order
     cudaError_t e = cudaMemsetAsync(p->nblocks_dev + session, 0, 4, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail("clearing the session's block count", e);
+    // no entry of its table is a page from here on: what appends tokens to reserved blocks goes by that
+    const size_t entries = p->sess_pages[session].size() + p->sess_reserved[session].size();
+    if (entries) e = cudaMemsetAsync(p->tables + (size_t)session * p->cfg.max_blocks_per_session, 0xff, entries * 4, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("clearing the session's block table", e);
     for (int32_t pg : p->sess_pages[session]) p->page_used[pg] = 0;
+    for (int32_t pg : p->sess_reserved[session]) p->page_used[pg] = 0;
     p->sess_pages[session].clear();
+    p->sess_reserved[session].clear();
     p->sess_blocks[session] = 0;
     p->free_hint = 0;
     return KVMEM_OK;
@@ -283,21 +292,8 @@ int32_t kvmem_session_blocks(const kvmem_pool_t* p, int32_t session) {
     return p->sess_blocks[session];
 }
 
-static int append_impl(kvmem_pool_t* p, int32_t session, const void* k, const void* v, int32_t n_blocks,
-                       const int32_t* phys_ids, const int32_t* block_pos0, void* stream) {
-    if (!pool_live(p)) return KVMEM_E_STATE;
-    if (!sessions_ok(p, session, 1)) return KVMEM_E_INVALID;
-    if (n_blocks < 0) { set_error("n_blocks is negative"); return KVMEM_E_INVALID; }
-    if (n_blocks == 0) return KVMEM_OK;
-    if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) { set_error("k and v must be 16-byte aligned device pointers"); return KVMEM_E_INVALID; }
-    const int have = p->sess_blocks[session];
-    if ((int64_t)have + n_blocks > p->cfg.max_blocks_per_session) {
-        set_error("session %d holds %d blocks; %d more exceed max_blocks_per_session = %d", session, have, n_blocks,
-                  p->cfg.max_blocks_per_session);
-        return KVMEM_E_CAPACITY;
-    }
-    // choose pages without touching the pool until every id is known to be usable
-    std::vector<int32_t> ids(n_blocks);
+// n_blocks free pages, the caller's or the lowest, without touching the pool
+static int choose_pages(const kvmem_pool* p, int32_t n_blocks, const int32_t* phys_ids, std::vector<int32_t>& ids) {
     if (phys_ids) {
         std::vector<int32_t> sorted(phys_ids, phys_ids + n_blocks);
         std::sort(sorted.begin(), sorted.end());
@@ -314,6 +310,29 @@ static int append_impl(kvmem_pool_t* p, int32_t session, const void* k, const vo
             if (!p->page_used[pg]) ids[got++] = pg;
         if (got < n_blocks) { set_error("pool has %d free pages, %d needed", got, n_blocks); return KVMEM_E_CAPACITY; }
     }
+    return KVMEM_OK;
+}
+
+static int append_impl(kvmem_pool_t* p, int32_t session, const void* k, const void* v, int32_t n_blocks,
+                       const int32_t* phys_ids, const int32_t* block_pos0, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    if (!sessions_ok(p, session, 1)) return KVMEM_E_INVALID;
+    if (n_blocks < 0) { set_error("n_blocks is negative"); return KVMEM_E_INVALID; }
+    if (n_blocks == 0) return KVMEM_OK;
+    if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) { set_error("k and v must be 16-byte aligned device pointers"); return KVMEM_E_INVALID; }
+    const int have = p->sess_blocks[session];
+    if (!p->sess_reserved[session].empty()) {
+        set_error("session %d has %zu reserved blocks in front: commit them (kvmem_commit_blocks) or reset the session", session, p->sess_reserved[session].size());
+        return KVMEM_E_STATE;
+    }
+    if ((int64_t)have + n_blocks > p->cfg.max_blocks_per_session) {
+        set_error("session %d holds %d blocks; %d more exceed max_blocks_per_session = %d", session, have, n_blocks,
+                  p->cfg.max_blocks_per_session);
+        return KVMEM_E_CAPACITY;
+    }
+    std::vector<int32_t> ids(n_blocks);
+    const int rc = choose_pages(p, n_blocks, phys_ids, ids);
+    if (rc != KVMEM_OK) return rc;
     if (block_pos0) {
         if (p->cfg.rope_max_positions <= 0) { set_error("the pool was created without rotary support"); return KVMEM_E_STATE; }
         for (int i = 0; i < n_blocks; ++i)
@@ -1281,6 +1300,315 @@ int kvmem_view_evict(kvmem_pool_t* p, int32_t n_sessions, const void* view_k, co
     a.n_sink = n_sink_tokens; a.n_recent = n_recent_tokens;
     cudaError_t e = launch_evict(*p, a, workspace, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail("eviction kernel launch", e);
+    return KVMEM_OK;
+}
+
+// ---- new tokens: rotary forms, tail and pages, prompt chunks ----
+
+// form and frequencies of a rotary form; null: the pool's own
+static int rope_form(const kvmem_pool_config_t& c, const kvmem_rope_t* r, RopeForm* form, double* f) {
+    if (c.rope_max_positions <= 0) { set_error("the pool was created without rotary support"); return KVMEM_E_STATE; }
+    const kvmem_rope_t own{};
+    if (!r) r = &own;
+    const int d = c.head_dim, n = r->rotary_dim ? r->rotary_dim : d;
+    if (r->layout != KVMEM_ROPE_HALF && r->layout != KVMEM_ROPE_INTERLEAVED) { set_error("layout must be KVMEM_ROPE_HALF or KVMEM_ROPE_INTERLEAVED"); return KVMEM_E_INVALID; }
+    if (n < 0 || n > d) { set_error("rotary_dim %d outside [0, head_dim = %d]", n, d); return KVMEM_E_INVALID; }
+    if (n % 16 != 0) { set_error("rotary_dim %d is not a multiple of 16", n); return KVMEM_E_UNSUPPORTED; }
+    if (r->scaling < KVMEM_ROPE_NONE || r->scaling > KVMEM_ROPE_BANDS) { set_error("unknown scaling %d", r->scaling); return KVMEM_E_INVALID; }
+    const bool scaled = r->scaling != KVMEM_ROPE_NONE, windowed = r->scaling == KVMEM_ROPE_RAMP || r->scaling == KVMEM_ROPE_BANDS;
+    if (scaled && (!(r->factor >= 1.0f) || !std::isfinite(r->factor))) { set_error("factor must be finite and at least 1"); return KVMEM_E_INVALID; }
+    const double factor = scaled ? (double)r->factor : 1.0, theta = (double)c.rope_theta, two_pi = 6.283185307179586476925286766559;
+    const double fast = r->turns_fast != 0.0f ? (double)r->turns_fast : r->scaling == KVMEM_ROPE_RAMP ? 32.0 : 4.0;
+    const double slow = r->turns_slow != 0.0f ? (double)r->turns_slow : 1.0, window = (double)r->original_positions;
+    if (windowed && (!(window > 0.0) || !std::isfinite(window))) { set_error("original_positions must be positive and finite"); return KVMEM_E_INVALID; }
+    if (windowed && (!(slow > 0.0) || !(fast > slow) || !std::isfinite(fast))) { set_error("turns_fast must be finite and exceed turns_slow, which must be positive"); return KVMEM_E_INVALID; }
+    *form = RopeForm{n, n / 16, r->layout == KVMEM_ROPE_INTERLEAVED ? 1 : 0};
+    auto pair_of = [&](double turns) { return n * log(window / (turns * two_pi)) / (2.0 * log(theta)); };
+    const double lo = windowed ? std::max(floor(pair_of(fast)), 0.0) : 0.0, hi = windowed ? std::min(ceil(pair_of(slow)), n - 1.0) : 0.0;
+    for (int i = 0; i < d / 2; ++i) {
+        f[i] = 0.0;                                         // the dims that pass
+        if (2 * i >= n) continue;
+        f[i] = pow(theta, -2.0 * (double)i / (double)n);
+        if (r->scaling == KVMEM_ROPE_LINEAR) f[i] /= factor;
+        else if (r->scaling == KVMEM_ROPE_BASE) f[i] = pow(theta * pow(factor, n / (n - 2.0)), -2.0 * (double)i / (double)n);
+        else if (windowed) {
+            const double divided = r->scaling == KVMEM_ROPE_RAMP ? (i - lo) / std::max(hi - lo, 0.001)
+                                                                 : (fast - window * f[i] / two_pi) / (fast - slow);
+            const double x = std::min(std::max(divided, 0.0), 1.0);
+            f[i] = f[i] / factor * x + f[i] * (1.0 - x);
+        }
+    }
+    return KVMEM_OK;
+}
+
+int kvmem_rope_frequencies(const kvmem_pool_config_t* cfg, const kvmem_rope_t* rope, double* frequencies) {
+    const char* why = "";
+    if (!cfg || !config_valid(*cfg, &why) || !frequencies) { set_error("invalid arguments to kvmem_rope_frequencies: %s", why); return KVMEM_E_INVALID; }
+    RopeForm form;
+    double f[256];
+    const int rc = rope_form(*cfg, rope, &form, f);
+    if (rc == KVMEM_OK) memcpy(frequencies, f, sizeof(double) * (cfg->head_dim / 2));
+    return rc;
+}
+
+int kvmem_set_rope(kvmem_pool_t* p, const kvmem_rope_t* rope, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    RopeForm form;
+    RopeFrequencies f{};
+    const int rc = rope_form(p->cfg, rope, &form, f.f);
+    if (rc != KVMEM_OK) return rc;
+    for (int s = 0; s < p->cfg.max_sessions; ++s)
+        if (p->sess_blocks[s] || !p->sess_reserved[s].empty()) {
+            set_error("session %d holds blocks: the rotary form of a pool is set before tokens come in", s);
+            return KVMEM_E_STATE;
+        }
+    const cudaError_t e = launch_rope_table(*p, f, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("rotary table kernel launch", e);
+    p->rope_form = form;
+    return KVMEM_OK;
+}
+
+static bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s < (1ll << 40); }
+
+int kvmem_rope_apply(kvmem_pool_t* p, const void* x, int64_t x_row_stride, int64_t x_vec_stride, int32_t x_order, void* y,
+                     int64_t y_row_stride, int64_t y_vec_stride, int32_t y_order, int64_t n_rows, int32_t n_vec,
+                     const int32_t* positions, int32_t inverse, float amplitude, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    if (p->cfg.rope_max_positions <= 0) { set_error("the pool was created without rotary support"); return KVMEM_E_STATE; }
+    if (n_rows < 0 || n_rows >= (1ll << 40) || n_vec < 1 || n_vec > (1 << 24)) { set_error("kvmem_rope_apply: n_rows must be in [0, 2^40), n_vec in [1, 2^24]"); return KVMEM_E_INVALID; }
+    if ((x_order | 1) != 1 || (y_order | 1) != 1) { set_error("kvmem_rope_apply: an order is KVMEM_ORDER_MODEL or KVMEM_ORDER_POOL"); return KVMEM_E_INVALID; }
+    if (!std::isfinite(amplitude) || amplitude < 0.0f) { set_error("amplitude must be finite and non-negative (0 selects 1)"); return KVMEM_E_INVALID; }
+    if (n_rows == 0) return KVMEM_OK;
+    if (!x || !y || !positions || !aligned(x, 16) || !aligned(y, 16) || !stride_ok(x_row_stride) || !stride_ok(x_vec_stride) ||
+        !stride_ok(y_row_stride) || !stride_ok(y_vec_stride)) {
+        set_error("kvmem_rope_apply: null or misaligned pointer, or a stride that is negative or no multiple of 8 elements");
+        return KVMEM_E_INVALID;
+    }
+    const int64_t d = p->cfg.head_dim, rows1 = n_rows - 1, vec1 = n_vec - 1;
+    // every element of y is written once
+    const bool rows_outside = (vec1 == 0 || y_vec_stride >= d) && (rows1 == 0 || y_row_stride >= vec1 * y_vec_stride + d);
+    const bool vecs_outside = (rows1 == 0 || y_row_stride >= d) && (vec1 == 0 || y_vec_stride >= rows1 * y_row_stride + d);
+    if (!rows_outside && !vecs_outside) { set_error("kvmem_rope_apply: the strides of y make its vectors overlap"); return KVMEM_E_INVALID; }
+    const size_t xb = 2 * (size_t)(rows1 * x_row_stride + vec1 * x_vec_stride + d), yb = 2 * (size_t)(rows1 * y_row_stride + vec1 * y_vec_stride + d);
+    if (overlap(x, xb, y, yb)) {
+        const RopeForm& f = p->rope_form;
+        const bool same_order = x_order == y_order || (!f.interleaved && f.rotary == d);
+        if (x != y || (rows1 && x_row_stride != y_row_stride) || (vec1 && x_vec_stride != y_vec_stride) || !same_order) {
+            set_error("kvmem_rope_apply: x and y overlap without being the same vectors in the same order");
+            return KVMEM_E_INVALID;
+        }
+    }
+    RopeApplyArgs a{};
+    a.x = (const __nv_bfloat16*)x; a.y = (__nv_bfloat16*)y; a.x_row = x_row_stride; a.x_vec = x_vec_stride; a.y_row = y_row_stride; a.y_vec = y_vec_stride;
+    a.positions = positions; a.rope = p->rope_dev; a.status = p->status_dev; a.form = p->rope_form;
+    a.n_vec = n_vec; a.d = p->cfg.head_dim; a.rope_positions = p->cfg.rope_max_positions; a.x_pool = x_order; a.y_pool = y_order;
+    a.sgn = inverse ? -1.0f : 1.0f; a.amplitude = amplitude > 0.0f ? amplitude : 1.0f;
+    const cudaError_t e = launch_rope_apply(*p, a, n_rows, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("rotary kernel launch", e);
+    return KVMEM_OK;
+}
+
+int kvmem_reserve_blocks(kvmem_pool_t* p, int32_t session, int32_t n_blocks, const int32_t* phys_ids, void* stream) {
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    if (!sessions_ok(p, session, 1)) return KVMEM_E_INVALID;
+    if (!pages_are(p, false, "kvmem_reserve_blocks")) return KVMEM_E_STATE;
+    if (p->cfg.rope_in_block_keys) { set_error("kvmem_reserve_blocks: reserved pages hold raw keys until they are indexed; the pool's pages hold keys rotated by their offset in the block"); return KVMEM_E_STATE; }
+    if (n_blocks < 0) { set_error("n_blocks is negative"); return KVMEM_E_INVALID; }
+    if (n_blocks == 0) return KVMEM_OK;
+    std::vector<int32_t>& reserved = p->sess_reserved[session];
+    const int64_t have = (int64_t)p->sess_blocks[session] + (int64_t)reserved.size();
+    if (have + n_blocks > p->cfg.max_blocks_per_session) {
+        set_error("session %d holds %lld blocks with the reserved ones; %d more exceed max_blocks_per_session = %d", session, (long long)have, n_blocks, p->cfg.max_blocks_per_session);
+        return KVMEM_E_CAPACITY;
+    }
+    std::vector<int32_t> ids(n_blocks);
+    const int rc = choose_pages(p, n_blocks, phys_ids, ids);
+    if (rc != KVMEM_OK) return rc;
+    const cudaError_t e = cudaMemcpyAsync(p->tables + (size_t)session * p->cfg.max_blocks_per_session + have, ids.data(), (size_t)n_blocks * 4,
+                                          cudaMemcpyHostToDevice, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("block table upload", e);
+    for (int32_t pg : ids) { p->page_used[pg] = 1; reserved.push_back(pg); }
+    if (!phys_ids) p->free_hint = ids.back() + 1;
+    return KVMEM_OK;
+}
+
+int32_t kvmem_session_reserved(const kvmem_pool_t* p, int32_t session) {
+    if (!pool_ok(p)) return KVMEM_E_STATE;
+    if (!sessions_ok(p, session, 1)) return KVMEM_E_INVALID;
+    return (int32_t)p->sess_reserved[session].size();
+}
+
+// a tail whose rows are written, of n_sessions sessions and at least min_tokens tokens each
+static int tail_ok(const kvmem_tail_t* tail, int32_t n_sessions, int32_t min_tokens, const char* who) {
+    if (!tail || !tail->k || !tail->v || !tail->n_tokens || !aligned(tail->k, 16) || !aligned(tail->v, 16)) {
+        set_error("%s: null or misaligned tail pointer", who);
+        return KVMEM_E_INVALID;
+    }
+    if (tail->cap_tokens < min_tokens || tail->cap_tokens < 1 || (int64_t)tail->cap_tokens * n_sessions > INT32_MAX) {
+        set_error("the tail holds %d tokens per session: at least %d are needed, and n_sessions * cap_tokens must stay below 2^31", tail->cap_tokens, min_tokens);
+        return KVMEM_E_INVALID;
+    }
+    return KVMEM_OK;
+}
+
+// bytes from the first to behind the last element
+static size_t rows_bytes(const kvmem_rows_t& r, int64_t ns, int64_t M, int64_t L, int64_t heads, int64_t d) {
+    return 2 * (size_t)((ns - 1) * r.session_stride + (M - 1) * r.token_stride + (L - 1) * r.layer_stride + (heads - 1) * r.head_stride + d);
+}
+
+int kvmem_append_tokens(kvmem_pool_t* p, int32_t session_first, int32_t n_sessions, int32_t n_new_tokens, const int32_t* n_new,
+                        const kvmem_rows_t* q, const kvmem_rows_t* k, const kvmem_rows_t* v, const int32_t* positions,
+                        const int32_t* n_sel, int32_t first_position, float q_amplitude, const kvmem_tail_t* tail, void* q_out,
+                        int32_t to_pages, void* stream) {
+    const char* who = "kvmem_append_tokens";
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    const Geometry& g = p->geo;
+    if (n_sessions < 1 || n_sessions > 65535 || n_new_tokens < 1) { set_error("n_sessions must be in [1, 65535] and n_new_tokens positive"); return KVMEM_E_INVALID; }
+    if (to_pages != 0 && to_pages != 1) { set_error("to_pages must be 0 or 1"); return KVMEM_E_INVALID; }
+    if (to_pages) {
+        if (!sessions_ok(p, session_first, n_sessions)) return KVMEM_E_INVALID;
+        if (!pages_are(p, false, who)) return KVMEM_E_STATE;
+        if (p->cfg.rope_in_block_keys) { set_error("%s: pages that hold keys rotated by their offset in the block are filled by whole blocks", who); return KVMEM_E_STATE; }
+    }
+    if (g.d % 16 != 0) { set_error("%s needs head_dim to be a multiple of 16", who); return KVMEM_E_UNSUPPORTED; }
+    if (!append_tokens_fits(p->cfg, n_new_tokens)) { set_error("%d new tokens per session are more than 2^31 groups of 16 elements: append them in parts", n_new_tokens); return KVMEM_E_UNSUPPORTED; }
+    const int rc = tail_ok(tail, n_sessions, n_new_tokens, who);
+    if (rc != KVMEM_OK) return rc;
+    const kvmem_rows_t* in[3] = {q, k, v};
+    if (!k || !v || !q != !q_out || !aligned(q_out, 16)) { set_error("%s: k and v are required, q and q_out go together and are 16-byte aligned", who); return KVMEM_E_INVALID; }
+    for (const kvmem_rows_t* r : in)
+        if (r && (!r->data || !aligned(r->data, 16) || !stride_ok(r->session_stride) || !stride_ok(r->token_stride) || !stride_ok(r->layer_stride) || !stride_ok(r->head_stride))) {
+            set_error("%s: null or misaligned rows, or a stride that is negative or no multiple of 8 elements", who);
+            return KVMEM_E_INVALID;
+        }
+    if (!std::isfinite(q_amplitude) || q_amplitude < 0.0f) { set_error("q_amplitude must be finite and non-negative (0 selects 1)"); return KVMEM_E_INVALID; }
+    const bool rope = p->cfg.rope_max_positions > 0;
+    if (rope && !positions && (first_position < 0 || first_position >= p->cfg.rope_max_positions)) {
+        set_error("first_position %d outside the rotary table [0, %d)", first_position, p->cfg.rope_max_positions);
+        return KVMEM_E_INVALID;
+    }
+    const size_t tail_b = 2 * (size_t)n_sessions * tail->cap_tokens * g.L * g.G * g.d, q_b = 2 * (size_t)n_sessions * n_new_tokens * g.L * g.H * g.d;
+    const void* outs[3] = {tail->k, tail->v, q_out};
+    const size_t out_b[3] = {tail_b, tail_b, q_b};
+    for (int i = 0; i < 3; ++i) {
+        if (!outs[i]) continue;
+        for (int j = 0; j < i; ++j)
+            if (overlap(outs[i], out_b[i], outs[j], out_b[j])) { set_error("%s: two of tail.k, tail.v and q_out overlap", who); return KVMEM_E_INVALID; }
+        for (int j = 0; j < 3; ++j)
+            if (in[j] && overlap(outs[i], out_b[i], in[j]->data, rows_bytes(*in[j], n_sessions, n_new_tokens, g.L, j ? g.G : g.H, g.d))) {
+                set_error("%s: a result overlaps q, k or v", who);
+                return KVMEM_E_INVALID;
+            }
+    }
+    AppendTokensArgs a{};
+    auto rows = [](const kvmem_rows_t* r) { return r ? TokenRows{(const __nv_bfloat16*)r->data, r->session_stride, r->token_stride, r->layer_stride, r->head_stride} : TokenRows{}; };
+    a.q = rows(q); a.k = rows(k); a.v = rows(v);
+    a.q_out = (__nv_bfloat16*)q_out; a.tail_k = (__nv_bfloat16*)tail->k; a.tail_v = (__nv_bfloat16*)tail->v;
+    a.tail_n = tail->n_tokens; a.n_new = n_new; a.positions = positions; a.n_sel = n_sel;
+    a.rope = rope ? p->rope_dev : nullptr; a.pages = to_pages ? p->pages : nullptr; a.tables = p->tables; a.nblocks_dev = p->nblocks_dev;
+    a.status = p->status_dev; a.page_elems = p->lay.page_elems; a.form = p->rope_form;
+    if (!rope) a.form.chunks = 0;
+    a.ns = n_sessions; a.M = n_new_tokens; a.L = g.L; a.Hq = q ? g.H : 0; a.G = g.G; a.d = g.d; a.B = g.B; a.tail_cap = tail->cap_tokens;
+    a.first_position = first_position; a.rope_positions = p->cfg.rope_max_positions; a.session_first = session_first; a.max_bps = g.max_bps;
+    a.max_blocks = g.max_blocks; a.q_amplitude = q_amplitude > 0.0f ? q_amplitude : 1.0f;
+    const cudaError_t e = launch_append_tokens(*p, a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail("token append kernel launch", e);
+    return KVMEM_OK;
+}
+
+int kvmem_commit_blocks(kvmem_pool_t* p, int32_t session_first, int32_t n_sessions, const int32_t* n_blocks, const kvmem_tail_t* tail, void* stream) {
+    const char* who = "kvmem_commit_blocks";
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    if (!sessions_ok(p, session_first, n_sessions)) return KVMEM_E_INVALID;
+    if (!n_blocks) { set_error("%s: n_blocks is null", who); return KVMEM_E_INVALID; }
+    if (tail) {
+        const int rc = tail_ok(tail, n_sessions, 1, who);
+        if (rc != KVMEM_OK) return rc;
+    }
+    for (int i = 0; i < n_sessions; ++i) {
+        const size_t reserved = p->sess_reserved[session_first + i].size();
+        if (n_blocks[i] < 0) { set_error("n_blocks[%d] is negative", i); return KVMEM_E_INVALID; }
+        if ((size_t)n_blocks[i] > reserved) { set_error("session %d has %zu reserved blocks, %d are to be committed", session_first + i, reserved, n_blocks[i]); return KVMEM_E_STATE; }
+    }
+    const Geometry& g = p->geo;
+    for (int i0 = 0; i0 < n_sessions;) {
+        CommitArgs a{};
+        int i = i0;
+        for (; i < n_sessions && a.ns < kCommitSessions; ++i)
+            if (n_blocks[i]) a.s[a.ns++] = CommitSession{session_first + i, i, p->sess_blocks[session_first + i], n_blocks[i]};
+        i0 = i;
+        if (a.ns == 0) break;
+        a.pages = p->pages; a.index = p->index; a.tables = p->tables; a.nblocks = p->nblocks_dev; a.status = p->status_dev;
+        a.page_elems = p->lay.page_elems; a.index_elems = p->lay.index_elems_per_session;
+        a.L = g.L; a.G = g.G; a.d = g.d; a.B = g.B; a.max_bps = g.max_bps; a.max_blocks = g.max_blocks;
+        if (tail) { a.tail_n = const_cast<int32_t*>(tail->n_tokens); a.tail_k = (__nv_bfloat16*)tail->k; a.tail_v = (__nv_bfloat16*)tail->v; a.tail_cap = tail->cap_tokens; }
+        const cudaError_t e = launch_commit(a, (cudaStream_t)stream);
+        if (e != cudaSuccess) return cuda_fail("block commit kernel launch", e);
+        for (int k = 0; k < a.ns; ++k) {
+            std::vector<int32_t>&reserved = p->sess_reserved[a.s[k].session], &pages = p->sess_pages[a.s[k].session];
+            pages.insert(pages.end(), reserved.begin(), reserved.begin() + a.s[k].n);
+            reserved.erase(reserved.begin(), reserved.begin() + a.s[k].n);
+            p->sess_blocks[a.s[k].session] += a.s[k].n;
+        }
+    }
+    return KVMEM_OK;
+}
+
+int kvmem_get_pages(kvmem_pool_t* p, const void** pages) {
+    if (!pool_ok(p)) return KVMEM_E_STATE;
+    if (!pages) { set_error("null output pointer"); return KVMEM_E_INVALID; }
+    *pages = p->pages;
+    return KVMEM_OK;
+}
+
+// What the chunk attention refuses for its size alone, and its workspace size with it; capacities 0: any
+static int prefill_sizes(const kvmem_pool_config_t& c, int32_t n_sessions, int32_t n_q_tokens, int32_t cap, int32_t tail_cap) {
+    if (n_sessions < 1 || n_sessions > 65535) { set_error("n_sessions must be in [1, 65535]"); return KVMEM_E_INVALID; }
+    if (n_q_tokens < 1) { set_error("n_q_tokens must be positive"); return KVMEM_E_INVALID; }
+    if (c.head_dim != 128) { set_error("the attention kernel is built for head_dim 128"); return KVMEM_E_UNSUPPORTED; }
+    if (c.n_q_heads / c.n_kv_heads > 128) { set_error("more than 128 query heads share a KV head"); return KVMEM_E_UNSUPPORTED; }
+    if (!prefill_fits(c, n_sessions, n_q_tokens, cap, tail_cap)) {
+        set_error("%d sessions of %d new tokens over up to %d + %d tokens are more than a line of 2^30 tiles", n_sessions, n_q_tokens, cap, tail_cap);
+        return KVMEM_E_UNSUPPORTED;
+    }
+    return KVMEM_OK;
+}
+
+size_t kvmem_prefill_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t n_q_tokens) {
+    const char* why = "";
+    if (!cfg || !config_valid(*cfg, &why)) { set_error("invalid arguments to kvmem_prefill_workspace_bytes"); return 0; }
+    if (prefill_sizes(*cfg, n_sessions, n_q_tokens, 0, 0) != KVMEM_OK) return 0;
+    return prefill_workspace_bytes(*cfg);
+}
+
+int kvmem_view_prefill_attend(kvmem_pool_t* p, int32_t n_sessions, const void* q, int32_t n_q_tokens, const int32_t* n_q,
+                              const void* view_k, const void* view_v, int32_t view_cap_tokens, const int32_t* n_sel,
+                              const kvmem_tail_t* tail, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+    const char* who = "kvmem_view_prefill_attend";
+    if (!pool_live(p)) return KVMEM_E_STATE;
+    const Geometry& g = p->geo;
+    if (view_cap_tokens < g.B || view_cap_tokens % g.B != 0) { set_error("view_cap_tokens must be a positive multiple of block_tokens"); return KVMEM_E_INVALID; }
+    int rc = KVMEM_OK;
+    if (tail && n_sessions >= 1) rc = tail_ok(tail, n_sessions, n_q_tokens, who);
+    if (rc == KVMEM_OK) rc = prefill_sizes(p->cfg, n_sessions, n_q_tokens, view_cap_tokens, tail ? tail->cap_tokens : 0);
+    if (rc != KVMEM_OK) return rc;
+    if (!q || !view_k || !view_v || !n_sel || !out || !lse || !workspace || !aligned(q, 16) || !aligned(view_k, 128) || !aligned(view_v, 128) ||
+        !aligned(out, 16) || !aligned(workspace, 256)) {
+        set_error("%s: null or misaligned pointer (views need 128-byte alignment)", who);
+        return KVMEM_E_INVALID;
+    }
+    if (!(scale >= 0.0f) || !std::isfinite(scale)) { set_error("scale must be finite and non-negative (0 selects 1/sqrt(d))"); return KVMEM_E_INVALID; }
+    const size_t need = prefill_workspace_bytes(p->cfg);
+    if (workspace_bytes < need) { set_error("%s: the workspace holds %zu bytes, %zu needed", who, workspace_bytes, need); return KVMEM_E_CAPACITY; }
+    PrefillArgs a{};
+    a.q = (const __nv_bfloat16*)q; a.n_q = n_q; a.view_k = (const __nv_bfloat16*)view_k; a.view_v = (const __nv_bfloat16*)view_v; a.n_sel = n_sel;
+    if (tail) { a.tail_k = (const __nv_bfloat16*)tail->k; a.tail_v = (const __nv_bfloat16*)tail->v; a.n_tail = tail->n_tokens; a.tail_cap = tail->cap_tokens; }
+    a.out = (__nv_bfloat16*)out; a.lse = lse; a.status = p->status_dev;
+    a.ns = n_sessions; a.M = n_q_tokens; a.L = g.L; a.H = g.H; a.G = g.G; a.r = g.r; a.B = g.B; a.cap = view_cap_tokens;
+    a.scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)g.d);
+    const cudaError_t e = launch_prefill(*p, a, workspace, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(who, e);
     return KVMEM_OK;
 }
 

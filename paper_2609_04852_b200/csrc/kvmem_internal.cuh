@@ -19,7 +19,7 @@ constexpr uint64_t kWaitLimitNs = 1000ull * 1000 * 1000;  // ... or about one se
 // ---- device-resident layout inside the caller's storage --------------------------------------
 //   pages   [max_blocks][2 (K|V)][L][G][B][d] bf16   one (block, K|V, l, g) tile is B*d*2 contiguous bytes
 //   index   [max_sessions][L][G][max_blocks_per_session][d] bf16
-//   tables  [max_sessions][max_blocks_per_session] int32 (logical -> physical page)
+//   tables  [max_sessions][max_blocks_per_session] int32 (logical -> physical page; -1 behind the session's blocks and reserved blocks)
 //   nblocks [max_sessions] int32
 //   status  int32 (sticky device status word)
 //   pos0    [max_sessions][max_blocks_per_session] int32: original position of each block's first token (rotary pools)
@@ -34,6 +34,13 @@ struct Layout {
 struct Geometry {
     int L, H, G, d, B, r;
     int max_sessions, max_blocks, max_bps;
+};
+
+// how a model's rotary form lies in a head (kvmem_set_rope); the pool's own form is {d, d / 16, 0}
+struct RopeForm {
+    int rotary;        // dims that rotate
+    int chunks;        // of the d / 16 groups of 8 pairs, those that rotate
+    int interleaved;   // pairs (2i, 2i + 1)
 };
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -67,9 +74,11 @@ struct kvmem_pool {
     float2* rope_dev;
     std::vector<int32_t> sess_blocks;               // host mirror of nblocks
     std::vector<std::vector<int32_t>> sess_pages;   // host mirror of tables
+    std::vector<std::vector<int32_t>> sess_reserved;   // pages behind them that are reserved, in the device's table already
     std::vector<uint8_t> page_used;
     int32_t free_hint;
     int sm_count;
+    kvmem::RopeForm rope_form;          // of the model whose queries and keys come in; meaningless without a rotary table
     // host-resident index scoring: a copy stream and its events, created on first use
     cudaStream_t copy_stream = nullptr;
     cudaEvent_t ev_ready[2] = {nullptr, nullptr}, ev_free[2] = {nullptr, nullptr}, ev_start = nullptr;
@@ -280,5 +289,76 @@ struct EvictArgs {
 size_t evict_workspace_bytes(const kvmem_pool_config_t& c, int n_sessions, int keep_blocks);
 bool evict_grid_fits(const kvmem_pool_config_t& c, int n_sessions, int keep_blocks, int cap_tokens);   // launch_evict's limit; cap 0: one piece a head
 cudaError_t launch_evict(const kvmem_pool& p, const EvictArgs& a, void* workspace, cudaStream_t st);
+
+// ---- new tokens: rotary forms, tail and pages, prompt chunks ----
+struct RopeFrequencies { double f[256]; };       // by value to the kernel: d / 2 of them
+cudaError_t launch_rope_table(const kvmem_pool& p, const RopeFrequencies& f, cudaStream_t st);
+
+struct RopeApplyArgs {
+    const __nv_bfloat16* x;
+    __nv_bfloat16* y;
+    long long x_row, x_vec, y_row, y_vec;        // strides in elements
+    const int32_t* positions;
+    const float2* rope;
+    int32_t* status;
+    RopeForm form;
+    int n_rows, n_vec, d, rope_positions, x_pool, y_pool;
+    float sgn, amplitude;
+    int chunks, groups;                          // filled by the launcher
+};
+cudaError_t launch_rope_apply(const kvmem_pool& p, RopeApplyArgs a, long long n_rows, cudaStream_t st);
+
+struct TokenRows {
+    const __nv_bfloat16* data;
+    long long session, token, layer, head;       // strides in elements
+};
+struct AppendTokensArgs {
+    TokenRows q, k, v;
+    __nv_bfloat16* q_out;                        // [ns][M][L][H][d]
+    __nv_bfloat16 *tail_k, *tail_v;              // [ns][tail_cap][L][G][d]
+    const int32_t *tail_n, *n_new, *positions, *n_sel;
+    const float2* rope;                          // null: no rotation
+    __nv_bfloat16* pages;                        // null: the tail alone
+    const int32_t *tables, *nblocks_dev;
+    int32_t* status;
+    size_t page_elems;
+    RopeForm form;
+    int ns, M, L, Hq, G, d, B, tail_cap, first_position, rope_positions, session_first, max_bps, max_blocks;   // Hq: 0 without queries
+    float q_amplitude;
+    int chunks, groups, n_vec, s0;               // filled by the launcher
+};
+cudaError_t launch_append_tokens(const kvmem_pool& p, AppendTokensArgs a, cudaStream_t st);
+bool append_tokens_fits(const kvmem_pool_config_t& c, int n_q_tokens);      // one session's threads in 32 bits
+
+constexpr int kCommitSessions = 128;             // sessions of one set of launches
+struct CommitSession { int session, slot, have, n; };      // pool's number, the tail's row of sessions, blocks there, blocks to come
+struct CommitArgs {
+    CommitSession s[kCommitSessions];
+    const __nv_bfloat16* pages;
+    __nv_bfloat16* index;
+    const int32_t* tables;
+    int32_t *nblocks, *tail_n, *status;          // tail_n null: no tail
+    __nv_bfloat16 *tail_k, *tail_v;
+    size_t page_elems, index_elems;
+    int ns, L, G, d, B, tail_cap, max_bps, max_blocks;
+};
+cudaError_t launch_commit(const CommitArgs& a, cudaStream_t st);
+
+struct PrefillArgs {
+    const __nv_bfloat16* q;                      // [ns][M][L][H][d]
+    const int32_t* n_q;                          // [ns] or null
+    const __nv_bfloat16 *view_k, *view_v;        // [ns][LG][cap][d]
+    const int32_t* n_sel;
+    const __nv_bfloat16 *tail_k, *tail_v;        // [ns][tail_cap][LG][d]
+    const int32_t* n_tail;
+    __nv_bfloat16* out;                          // [ns][M][L][H][d]
+    float* lse;                                  // [ns][M][L][H]
+    int32_t* status;
+    int ns, M, L, H, G, r, B, cap, tail_cap;
+    float scale;
+};
+size_t prefill_workspace_bytes(const kvmem_pool_config_t& c);
+bool prefill_fits(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int cap_tokens, int tail_cap_tokens);
+cudaError_t launch_prefill(const kvmem_pool& p, const PrefillArgs& a, void* workspace, cudaStream_t st);
 
 }  // namespace kvmem

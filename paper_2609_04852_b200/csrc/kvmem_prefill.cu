@@ -1,0 +1,731 @@
+// Attention of a prompt chunk over a view and the tail of tokens behind it, the chunk's own tokens among them:
+//   out_i = sum_t p_it v_t,  p_it = exp(x_it - lse_i),  x_it = scale q_i . k_t  over the view's tokens, the committed tail tokens and
+//   the chunk tokens 0 .. i.
+//
+// The arithmetic is the tensor pipe's: 4 d flops per query row and token against 2 d bytes of key and value that many rows share.
+// A CTA works on two row tiles of 128 query rows at a time (whole tokens times the r query heads of a KV head), a slot each:
+//     S = Q K^T    tcgen05.mma, both operands in shared memory, 128 x 128 fp32 accumulators in tensor memory
+//     P = exp2(S scale log2e - ref)     four warps a slot, a thread per row: no exchange between threads
+//     O += P V     tcgen05.mma, P as bf16 in tensor memory (over S), V from shared memory
+// so that one slot's products run while the other's weights are computed.  S, P and O of the two slots fill tensor memory.  One
+// thread fetches Q, K and V tiles with TMA (128-byte swizzle), one thread issues the MMAs: those of one thread run in order, so a
+// slot's next S is issued right behind the product that reads its P, in whose place it goes.
+//
+// ref is a running maximum that moves only when a row's logits pass it by 8 (in powers of two): O is then rescaled in tensor
+// memory.  Until then the weights may reach 2^8, which costs neither fp32 nor bf16 any precision.
+//
+// Work: an item is (session, KV head, group of two row tiles); its tiles are those of the view and of the tail up to the group's last
+// token.  All items' tiles lie on one line, cut into as many equal parts as there are CTAs (one per SM): chunks over views of any
+// lengths keep all SMs busy to the end, and the causal part's short and long items need no other balance.  An item that a cut falls
+// into is left as partial sums, joined in line order by prefill_merge_kernel: the result depends on the sizes alone, not on
+// timing.  A CTA leaves at most two of them (its first and its last), so the workspace does not grow with the call.  Items of one KV
+// head are neighbours on the line: the CTAs that stream the same keys and values do so closely enough to find them in L2.
+//
+// Tokens that a row does not see: their logits are replaced before they are used, values behind the last token are cleared in shared
+// memory before the second product (0 x NaN), and so are values that are not finite of chunk tokens that only some rows see; the
+// rows that do see them get them at the end.
+#include <cudaTypedefs.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "kvmem_internal.cuh"
+#include "kvmem_ptx.cuh"
+#include "kvmem_t5.cuh"
+
+namespace kvmem {
+
+constexpr int kPreD = 128;
+constexpr int kPreTile = 128;                    // tokens per tile
+constexpr int kPreRows = 128;                    // rows per slot: TMEM lanes
+constexpr int kPreHalf = 128 * 128;              // bytes of one 64-dim half of a 128-row operand tile
+constexpr int kPreSlot = 2 * kPreHalf;           // a K, V or Q tile
+constexpr int kPreRing = 5;                      // K and V tiles in turn
+constexpr int kPreThreads = 320;                 // eight row warps, TMA warp, MMA warp: 200 registers a thread
+constexpr int kPreTmaWarp = 8, kPreMmaWarp = 9;
+constexpr int kPreLead = 1;                      // units on the line for an item's start and end
+constexpr float kPreSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
+constexpr uint32_t kPreIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
+constexpr uint32_t kPreIdescO = kPreIdescS | (1u << 16);                                         // B with dims contiguous (V as it lies)
+constexpr uint32_t kPreVStep = (uint32_t)kPreHalf >> 4;       // leading offset of V's descriptor: from dims 0..63 to 64..127
+constexpr int kPreMostUnits = 1 << 30;
+
+struct PreRecord { int s, lg, rg, flags; };      // flags: 1 the item's last share, 2 values that are not finite were cleared; s < 0: none
+
+struct PreWork {
+    PrefillArgs a;
+    int tpt;                                     // tokens per row tile
+    float* part_o;                               // [2 CTAs][256][128]
+    float2* part_ml;                             // [2 CTAs][256]: (reference, sum of weights), log2 domain
+    PreRecord* rec;                              // [2 CTAs]: what shares 2c (begun by an earlier CTA) and 2c + 1 (goes on in the next) hold
+};
+
+struct PreSpan {
+    int n_view, n_tail, n_q, view_tiles, groups;
+};
+
+__device__ __forceinline__ PreSpan pre_span(const PrefillArgs& a, int tpt, int s, bool report) {
+    PreSpan t;
+    t.n_view = (int)min((long long)max(a.n_sel[s], 0) * a.B, (long long)a.cap);
+    t.n_q = a.n_q ? min(max(a.n_q[s], 0), a.M) : a.M;
+    t.n_tail = 0;
+    if (a.tail_k) {
+        const int n = a.n_tail[s];
+        t.n_tail = min(max(n, 0), a.tail_cap - t.n_q);
+        if (report && t.n_tail != n) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
+    }
+    t.view_tiles = (t.n_view + kPreTile - 1) / kPreTile;
+    t.groups = (t.n_q + 2 * tpt - 1) / (2 * tpt);
+    return t;
+}
+
+// tail tokens that the last row of group rg sees, in tiles
+__device__ __forceinline__ int pre_tail_tiles(const PrefillArgs& a, const PreSpan& sp, int tpt, int rg) {
+    return a.tail_k ? (sp.n_tail + min((rg + 1) * 2 * tpt, sp.n_q) + kPreTile - 1) / kPreTile : 0;
+}
+
+// sum over i < n of floor((step i + from) / 128), by exchanging the axes of the triangle under the line
+__device__ __forceinline__ long long floor_sum(long long n, long long step, long long from) {
+    long long m = kPreTile, sum = 0;
+    while (n > 0) {
+        if (step >= m) { sum += (n - 1) * n / 2 * (step / m); step %= m; }
+        if (from >= m) { sum += n * (from / m); from %= m; }
+        const long long top = step * n + from;
+        if (top < m) break;
+        n = top / m;
+        from = top % m;
+        const long long t = m;
+        m = step;
+        step = t;
+    }
+    return sum;
+}
+
+// units of the row groups before group rg of a KV head (rg < groups), and of a whole KV head.  An item without a tile (no view, no
+// tail) has one unit beside its lead: somebody has to write its rows.
+__device__ __forceinline__ int pre_before(const PrefillArgs& a, const PreSpan& sp, int tpt, int rg) {
+    if (!a.tail_k) return rg * (max(sp.view_tiles, 1) + kPreLead);
+    return rg * (sp.view_tiles + kPreLead) + (int)floor_sum(rg, 2 * tpt, sp.n_tail + 2 * tpt + kPreTile - 1);
+}
+__device__ __forceinline__ int pre_tiles(const PrefillArgs& a, const PreSpan& sp, int tpt, int rg) { return sp.view_tiles + pre_tail_tiles(a, sp, tpt, rg); }
+__device__ __forceinline__ int pre_head(const PrefillArgs& a, const PreSpan& sp, int tpt) {
+    if (sp.groups == 0) return 0;
+    return pre_before(a, sp, tpt, sp.groups - 1) + max(pre_tiles(a, sp, tpt, sp.groups - 1), 1) + kPreLead;
+}
+
+// a role's walk over its CTA's shares of items
+struct PreWalk {
+    int pos, end, from;             // next unit of the line, the CTA's end, the item's first unit
+    int s, lg, rg;                  // the item at `from`
+    PreSpan sp;
+    int t0, t1, tiles;              // the share: tiles [t0, t1) of the item's `tiles` (0: nothing to see)
+    int cs, clg, crg, m0, rows2;    // its item; first token; whether the second row tile has any token
+    __device__ __forceinline__ bool next(const PreWork& w, int LG) {
+        const PrefillArgs& a = w.a;
+        while (pos < end) {
+            while (sp.groups == 0) sp = pre_span(a, w.tpt, ++s, false);     // (a session that has units follows: pos < end)
+            tiles = pre_tiles(a, sp, w.tpt, rg);
+            const int some = max(tiles, 1), first = from + kPreLead, item_end = first + some;
+            t0 = max(pos - first, 0);
+            t1 = min(some, end - first);
+            cs = s; clg = lg; crg = rg;
+            m0 = rg * 2 * w.tpt;
+            rows2 = sp.n_q - m0 > w.tpt;
+            n_view = sp.n_view; n_tail = sp.n_tail; n_q = sp.n_q; view_tiles = sp.view_tiles;
+            pos = min(end, item_end);
+            if (pos == item_end) {
+                from = item_end;
+                if (++rg == sp.groups) {
+                    rg = 0;
+                    if (++lg == LG) {
+                        lg = 0;
+                        if (pos < end) sp = pre_span(a, w.tpt, ++s, false);
+                    }
+                }
+            }
+            if (t0 < t1) return true;
+        }
+        return false;
+    }
+    int n_view, n_tail, n_q, view_tiles;      // of the share's session
+    __device__ __forceinline__ int units() const { return tiles ? t1 - t0 : 0; }
+};
+
+struct PreShared {
+    uint64_t full[kPreRing], empty[kPreRing], q_full, q_empty, s_full[2], p_full[2][2], o_full[2], o_empty[2], drained;
+    int plan_begin, plan_end, plan_from, plan_s, plan_lg, plan_rg;
+    uint32_t tmem;
+    int not_finite[2];                        // by the parity of the share: its number + 1, where values were cleared
+};
+constexpr size_t kPreSmem = (size_t)(2 + kPreRing) * kPreSlot + sizeof(PreShared);
+static_assert(kPreSmem <= 232448, "shared memory of a CTA");
+
+__device__ __forceinline__ void pre_zero_row(const PrefillArgs& a, size_t orow) {
+    uint4* o = reinterpret_cast<uint4*>(a.out + orow * kPreD);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = make_uint4(0u, 0u, 0u, 0u);
+    a.lse[orow] = -INFINITY;
+}
+
+__global__ void __launch_bounds__(kPreThreads, 1)
+prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+               const __grid_constant__ CUtensorMap map_tk, const __grid_constant__ CUtensorMap map_tv, const __grid_constant__ PreWork w) {
+    constexpr int RING = kPreRing;
+    extern __shared__ __align__(1024) unsigned char smem_q[];          // two Q tiles, the ring, then the small things
+    const PrefillArgs& a = w.a;
+    unsigned char* ring = smem_q + 2 * kPreSlot;
+    PreShared& sh = *reinterpret_cast<PreShared*>(ring + (size_t)RING * kPreSlot);
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int LG = a.L * a.G, tpt = w.tpt;
+
+    if (ptx::smem_u32(smem_q) & 1023u) {          // never: nothing static lies in front of the dynamic part
+        if (tid == 0) atomicExch(a.status, (int)KVMEM_E_UNSUPPORTED);
+        return;
+    }
+    if (tid == 0) {
+        for (int i = 0; i < RING; ++i) { ptx::mbar_init(&sh.full[i], 1); ptx::mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(&sh.s_full[i], 1);
+            ptx::mbar_init(&sh.p_full[i][0], 4);
+            ptx::mbar_init(&sh.p_full[i][1], 4);
+            ptx::mbar_init(&sh.o_full[i], 1);
+            ptx::mbar_init(&sh.o_empty[i], 4);
+            sh.not_finite[i] = 0;
+        }
+        ptx::mbar_init(&sh.q_full, 1);
+        ptx::mbar_init(&sh.q_empty, 1);
+        ptx::mbar_init(&sh.drained, 1);
+        ptx::fence_mbar_init();
+    }
+    if (warp == kPreMmaWarp) {
+        t5::tmem_alloc(&sh.tmem, 512);
+        t5::tmem_relinquish();
+    }
+    pdl_wait();        // everything earlier in the stream is complete and visible from here on
+    pdl_trigger();
+    if (warp == kPreTmaWarp) {
+        if (lane == 0) {
+            ptx::prefetch_tensormap(&map_q);
+            ptx::prefetch_tensormap(&map_k);
+            ptx::prefetch_tensormap(&map_v);
+            ptx::prefetch_tensormap(&map_tk);
+            ptx::prefetch_tensormap(&map_tv);
+        }
+        // the CTA's part of the line, and the item it starts in
+        int sum = 0;
+        for (int s = lane; s < a.ns; s += 32) sum += pre_head(a, pre_span(a, tpt, s, blockIdx.x == 0), tpt);
+        const int total = __reduce_add_sync(0xffffffffu, sum) * LG, n = min((int)gridDim.x, total);
+        const bool idle = (int)blockIdx.x >= n;
+        const int begin = idle ? 0 : (int)((long long)total * blockIdx.x / n), end = idle ? 0 : (int)((long long)total * (blockIdx.x + 1) / n);
+        int before = 0;
+        for (int s0 = 0; s0 < a.ns && !idle; s0 += 32) {
+            const int s = s0 + lane;
+            PreSpan sp{};
+            if (s < a.ns) sp = pre_span(a, tpt, s, false);
+            const int head = s < a.ns ? pre_head(a, sp, tpt) : 0, mine = head * LG;
+            int incl = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += up;
+            }
+            const int lo = before + incl - mine;
+            if (begin >= lo && begin < lo + mine) {
+                const int lg = (begin - lo) / head, at = begin - lo - lg * head;
+                int rg = 0;                                      // the last group that starts at `at` or before
+                for (int step = 1 << 15; step; step >>= 1)
+                    if (rg + step < sp.groups && pre_before(a, sp, tpt, rg + step) <= at) rg += step;
+                sh.plan_s = s;
+                sh.plan_lg = lg;
+                sh.plan_rg = rg;
+                sh.plan_from = lo + lg * head + pre_before(a, sp, tpt, rg);
+            }
+            before += __shfl_sync(0xffffffffu, incl, 31);
+            if (before > begin) break;
+        }
+        if (lane == 0) {
+            sh.plan_begin = begin;
+            sh.plan_end = end;
+            w.rec[2 * blockIdx.x].s = -1;
+            w.rec[2 * blockIdx.x + 1].s = -1;
+        }
+    }
+    t5::fence_before();
+    __syncthreads();
+    t5::fence_after();
+    const uint32_t tmem = sh.tmem;
+    PreWalk walk;
+    walk.pos = sh.plan_begin; walk.end = sh.plan_end;
+    if (walk.pos < walk.end) {
+        walk.from = sh.plan_from; walk.s = sh.plan_s; walk.lg = sh.plan_lg; walk.rg = sh.plan_rg;
+        walk.sp = pre_span(a, tpt, walk.s, false);
+    }
+
+    // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
+    // every role still reaches its end.
+    bool ok = true;
+    if (warp == kPreTmaWarp) {
+        // ------------------------------------------------ TMA: one thread
+        if (t5::elect()) {
+            int n = 0, seg = 0;                                       // loads of the ring, shares so far
+            auto slot = [&]() {                                       // the next ring slot, free
+                const int st = n % RING;
+                if (ok && n >= RING) ok = ptx::mbar_wait(&sh.empty[st], (uint32_t)(((n / RING) & 1) ^ 1));
+                ++n;
+                return st;
+            };
+            while (ok && walk.next(w, LG)) {
+                const int units = walk.units();
+                if (units == 0) continue;
+                if (seg > 0) ok = ptx::mbar_wait(&sh.q_empty, (uint32_t)((seg - 1) & 1));
+                if (!ok) break;
+                const int l = walk.clg / a.G, g = walk.clg % a.G, tok0 = walk.cs * a.M + walk.m0;
+                ptx::mbar_expect_tx(&sh.q_full, (uint32_t)((walk.rows2 ? 2 : 1) * 2 * 128 * a.r * tpt));
+                for (int x = 0; x <= walk.rows2; ++x)
+                    for (int h = 0; h < 2; ++h)
+                        ptx::tma_load_3d(smem_q + x * kPreSlot + h * kPreHalf, &map_q, 64 * h, l * a.H + g * a.r, tok0 + x * tpt, &sh.q_full);
+                const int z_view = walk.cs * LG + walk.clg, row_tail = walk.cs * a.tail_cap;
+                for (int t = walk.t0; t < walk.t1 && ok; ++t) {
+                    const bool in_view = t < walk.view_tiles;
+                    const int c0 = (in_view ? t : t - walk.view_tiles) * kPreTile;
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int st = slot();
+                        if (!ok) { --n; break; }
+                        unsigned char* dst = ring + (size_t)st * kPreSlot;
+                        ptx::mbar_expect_tx(&sh.full[st], kPreSlot);
+                        for (int h = 0; h < 2; ++h) {
+                            if (in_view) ptx::tma_load_3d(dst + h * kPreHalf, kv ? &map_v : &map_k, 64 * h, c0, z_view, &sh.full[st]);
+                            else ptx::tma_load_3d(dst + h * kPreHalf, kv ? &map_tv : &map_tk, 64 * h, walk.clg, row_tail + c0, &sh.full[st]);
+                        }
+                    }
+                }
+                ++seg;
+            }
+            // the copies still in flight land before the CTA gives its shared memory back
+            for (int i = max(0, n - RING); i < n; ++i) ok = ptx::mbar_wait(&sh.full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
+            if (seg > 0) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)((seg - 1) & 1)) && ok;
+            if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
+        }
+    } else if (warp == kPreMmaWarp) {
+        // ------------------------------------------------ MMA: one thread
+        if (t5::elect()) {
+            const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
+            struct Place {                                            // ring slot and phase of the next key / value tile
+                int st;
+                uint32_t ph;
+                __device__ __forceinline__ void next() { st += 2; if (st >= RING) { st -= RING; ph ^= 1u; } }
+            } kp{0, 0u}, vp{1, 0u};
+            int seg = 0;
+            uint32_t p_ph0 = 0, p_ph1 = 0;                            // phases of the slots' weights
+            int out0 = 0, out1 = 0;                                   // shares whose sums a slot's rows have to take out
+            auto logits = [&](int x) {
+                if (!ok) return;
+                t5::fence_after();
+                const uint32_t al = q_lo + (uint32_t)x * (kPreSlot >> 4), bl = ring_lo + (uint32_t)kp.st * (kPreSlot >> 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t o = (uint32_t)(i >> 2) * (kPreHalf >> 4) + (uint32_t)(i & 3) * 2u;
+                    t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kPreIdescS, i > 0 ? 1u : 0u);
+                }
+                t5::commit(&sh.s_full[x]);
+            };
+            auto half_product = [&](int x, int half, bool first) {
+                if (!ok) return;
+                t5::fence_after();
+                const uint32_t bl = (ring_lo + (uint32_t)vp.st * (kPreSlot >> 4)) | (kPreVStep << 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = half * 4 + i;
+                    t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)(k * 8),
+                                    t5::make_desc(bl + (uint32_t)k * (2048u >> 4)), kPreIdescO, !first || k > 0 ? 1u : 0u);
+                }
+            };
+            while (walk.next(w, LG)) {
+                const int units = walk.units();
+                if (units == 0) continue;
+                const bool two = walk.rows2;
+                if (ok) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)(seg & 1)) && ptx::mbar_wait(&sh.full[kp.st], kp.ph);
+                logits(0);
+                if (two) logits(1);
+                if (ok) t5::commit(&sh.empty[kp.st]);
+                if (ok && units == 1) t5::commit(&sh.q_empty);
+                kp.next();
+                for (int j = 0; j < units; ++j) {
+                    const bool more = j + 1 < units;
+                    if (ok) ok = ptx::mbar_wait(&sh.full[vp.st], vp.ph);
+                    // sums of the slots' last shares are out before new ones take their place (slot 1's too where it now rests: the flags of
+                    // cleared values are kept for two shares)
+                    if (j == 0) {
+                        if (ok && out0 > 0) ok = ptx::mbar_wait(&sh.o_empty[0], (uint32_t)((out0 - 1) & 1));
+                        if (ok && !two && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
+                    }
+                    if (ok) ok = ptx::mbar_wait(&sh.p_full[0][0], p_ph0);
+                    half_product(0, 0, j == 0);
+                    if (ok) ok = ptx::mbar_wait(&sh.p_full[0][1], p_ph0);
+                    half_product(0, 1, false);
+                    p_ph0 ^= 1u;
+                    if (ok && !more) t5::commit(&sh.o_full[0]);
+                    if (more) {
+                        if (ok) ok = ptx::mbar_wait(&sh.full[kp.st], kp.ph);
+                        logits(0);
+                    }
+                    if (two) {
+                        if (j == 0 && ok && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
+                        if (ok) ok = ptx::mbar_wait(&sh.p_full[1][0], p_ph1);
+                        half_product(1, 0, j == 0);
+                        if (ok) ok = ptx::mbar_wait(&sh.p_full[1][1], p_ph1);
+                        half_product(1, 1, false);
+                        p_ph1 ^= 1u;
+                        if (ok && !more) t5::commit(&sh.o_full[1]);
+                        if (more) logits(1);
+                    }
+                    if (ok) t5::commit(&sh.empty[vp.st]);
+                    vp.next();
+                    if (more) {
+                        if (ok) t5::commit(&sh.empty[kp.st]);
+                        if (ok && j + 2 == units) t5::commit(&sh.q_empty);
+                        kp.next();
+                    }
+                }
+                ++out0;
+                if (two) ++out1;
+                ++seg;
+            }
+            t5::commit(&sh.drained);                                  // MMAs in flight end before the tensor memory is given back
+            ok = ptx::mbar_wait(&sh.drained, 0u) && ok;
+            if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
+        }
+    } else {
+        // ------------------------------------------------ rows: a thread each
+        const int x = warp >> 2, row = (warp & 3) * 32 + lane, gt = tid & 127;
+        const uint32_t s_addr = tmem + (uint32_t)x * 256u + ((uint32_t)((warp & 3) * 32) << 16), o_addr = s_addr + 128u;
+        const float scale2 = a.scale * 1.4426950408889634f;
+        const int my_token = row / a.r, my_head = row - my_token * a.r;
+        int cnt = 0, done = 0, tiles = 0, seg = 0;       // units and shares of this slot; tiles and shares of the CTA
+        auto wait = [&](uint64_t* bar, int phase) {
+            if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1));
+            ok = __all_sync(0xffffffffu, ok);
+        };
+        while (walk.next(w, LG)) {
+            const int units = walk.units();
+            const bool mine = x == 0 || walk.rows2;
+            const int first_token = walk.m0 + x * tpt, token = first_token + my_token;
+            const bool live = mine && my_token < tpt && token < walk.n_q;
+            const int l = walk.clg / a.G, g = walk.clg % a.G;
+            const size_t orow = (((size_t)walk.cs * a.M + token) * a.L + l) * a.H + (size_t)g * a.r + my_head;
+            if (units == 0) {
+                if (live) pre_zero_row(a, orow);
+                continue;
+            }
+            if (mine) {
+                const bool warp_live = __any_sync(0xffffffffu, live);
+                float ref = -INFINITY, sum = 0.0f;
+                bool cleared = false;
+                for (int j = 0; j < units; ++j) {
+                    const int t = walk.t0 + j;
+                    const bool in_view = t < walk.view_tiles;
+                    const int c0 = (in_view ? t : t - walk.view_tiles) * kPreTile;        // the tile's first token in view or tail
+                    const int n_valid = (in_view ? walk.n_view : walk.n_tail + walk.n_q) - c0;
+                    wait(&sh.s_full[x], cnt);
+                    ++cnt;
+                    if (x == 0 && (n_valid < kPreTile || (!in_view && c0 + kPreTile > walk.n_tail + walk.m0 + 1))) {
+                        // Values behind the last token become zero, and those of tokens behind the group's first that are not finite.  The tile
+                        // that was in this ring slot before has landed for certain once these logits are there (a wait for a phase two
+                        // ahead of the barrier's would be over at once).
+                        const int v = 2 * (tiles + j) + 1, st = v % RING;
+                        wait(&sh.full[st], v / RING);
+                        unsigned char* vt = ring + (size_t)st * kPreSlot;
+                        const int first = in_view ? n_valid : min(max(walk.n_tail + walk.m0 + 1 - c0, 0), n_valid);
+                        for (int i = max(first, 0) * 16 + gt; i < kPreTile * 16; i += 128) {
+                            const int rr = i >> 4, c = i & 15;
+                            uint4* p = reinterpret_cast<uint4*>(vt + (size_t)(c >> 3) * kPreHalf + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
+                            uint4 val = make_uint4(0u, 0u, 0u, 0u);
+                            bool put = true;
+                            if (rr < n_valid) {
+                                val = *p;
+                                put = false;
+                                uint32_t* e = reinterpret_cast<uint32_t*>(&val);
+#pragma unroll
+                                for (int h = 0; h < 4; ++h) {
+                                    if ((e[h] & 0x00007f80u) == 0x00007f80u) { e[h] &= 0xffff0000u; put = true; }
+                                    if ((e[h] & 0x7f800000u) == 0x7f800000u) { e[h] &= 0x0000ffffu; put = true; }
+                                }
+                                cleared |= put;
+                            }
+                            if (put) *p = val;
+                        }
+                        if (cleared) sh.not_finite[seg & 1] = seg + 1;
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    if (warp_live) {
+                        t5::fence_after();
+                        uint32_t sv[4][32];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) t5::ld32_issue(s_addr + 32u * c, sv[c]);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) t5::ld_wait(sv[c]);
+                        // columns that this row sees: [0, seen)
+                        const int seen = in_view ? n_valid : min(walk.n_tail + token + 1 - c0, n_valid);
+                        if (__any_sync(0xffffffffu, seen < kPreTile)) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (32 * c + i >= seen) sv[c][i] = 0xff800000u;
+                        }
+                        float m[4];                                // the row's largest logit in this tile, NaN if one is
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            m[c] = f2::max3_nan(__uint_as_float(sv[c][0]), __uint_as_float(sv[c][1]), __uint_as_float(sv[c][2]));
+#pragma unroll
+                            for (int i = 3; i < 31; i += 2) m[c] = f2::max3_nan(m[c], __uint_as_float(sv[c][i]), __uint_as_float(sv[c][i + 1]));
+                            m[c] = f2::max3_nan(m[c], __uint_as_float(sv[c][31]), __uint_as_float(sv[c][31]));
+                        }
+                        const float m2 = scale2 * f2::max3_nan(f2::max3_nan(m[0], m[1], m[2]), m[3], m[3]);
+                        // true for the first logit that is not -inf (ref is), and for a NaN
+                        const bool moves = live && !(m2 <= ref + kPreSlack) && m2 != -INFINITY;
+                        if (__any_sync(0xffffffffu, moves)) {
+                            const float to = moves ? m2 : ref, corr = moves ? t5::ex2(ref - to) : 1.0f;
+                            if (j > 0) {
+                                // the last product into O is complete: this tile's logits were issued after it
+#pragma unroll 1
+                                for (int c = 0; c < 8; ++c) {
+                                    uint32_t ov[16];
+                                    t5::ld16_issue(o_addr + 16u * c, ov);
+                                    t5::ld_wait(ov);
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
+                                    t5::st16(o_addr + 16u * c, ov);
+                                }
+                            }
+                            sum *= corr;
+                            ref = to;
+                        }
+                        const float use = ref == -INFINITY ? 0.0f : ref;      // nothing seen yet: every weight is exp2(-inf) = 0
+                        const uint64_t sc2 = f2::pk(scale2, scale2), nm2 = f2::pk(-use, -use);
+                        uint64_t acc0 = f2::pk(0.0f, 0.0f), acc1 = acc0;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                float p0, p1;
+                                f2::unpk(f2::fma(f2::pk(sv[c][2 * i], sv[c][2 * i + 1]), sc2, nm2), p0, p1);
+                                p0 = t5::ex2(p0);
+                                p1 = t5::ex2(p1);
+                                if (i & 1) acc1 = f2::add(acc1, f2::pk(p0, p1)); else acc0 = f2::add(acc0, f2::pk(p0, p1));
+                                pk[i] = ptx::pack_bf16x2(p0, p1);
+                            }
+                            t5::st16(s_addr + 16u * c, pk);        // over logits that this thread has read
+                            if (c == 1) {                          // the first half of the tokens is ready for its product
+                                t5::st_wait();
+                                t5::fence_before();
+                                __syncwarp();
+                                if (lane == 0) ptx::mbar_arrive(&sh.p_full[x][0]);
+                            }
+                        }
+                        float a0, a1, a2, a3;
+                        f2::unpk(acc0, a0, a1);
+                        f2::unpk(acc1, a2, a3);
+                        sum += (a0 + a1) + (a2 + a3);
+                        t5::st_wait();
+                        t5::fence_before();
+                    } else if (lane == 0) {
+                        ptx::mbar_arrive(&sh.p_full[x][0]);
+                    }
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sh.p_full[x][1]);
+                }
+                // the share's sums
+                wait(&sh.o_full[x], done++);
+                const bool whole = walk.t0 == 0 && walk.t1 == walk.tiles;
+                const int share = 2 * blockIdx.x + (walk.t0 == 0 ? 1 : 0);
+                const bool nf = *(volatile int*)&sh.not_finite[seg & 1] == seg + 1;
+                if (warp_live) {
+                    t5::fence_after();
+                    const bool none = sum == 0.0f;
+                    const float inv = none ? 0.0f : 1.0f / sum;
+                    float* po = w.part_o + ((size_t)share * 2 * kPreRows + x * kPreRows + row) * kPreD;
+#pragma unroll 1
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t ov[16];
+                        t5::ld16_issue(o_addr + 16u * c, ov);
+                        t5::ld_wait(ov);
+                        if (live && !whole) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                *reinterpret_cast<uint4*>(po + 16 * c + 4 * i) = make_uint4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
+                        } else if (live) {
+                            float o[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = none ? 0.0f : __uint_as_float(ov[i]) * inv;
+                            if (nf && !none) {
+                                // values that were cleared and that this row sees
+                                for (int tok = walk.m0 + 1; tok <= token; ++tok) {
+                                    const __nv_bfloat16* vr = a.tail_v + (((size_t)walk.cs * a.tail_cap + walk.n_tail + tok) * LG + walk.clg) * kPreD + 16 * c;
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) {
+                                        const float v = __bfloat162float(vr[i]);
+                                        if (!isfinite(v)) o[i] += v;
+                                    }
+                                }
+                            }
+                            uint32_t pk[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) pk[i] = ptx::pack_bf16x2(o[2 * i], o[2 * i + 1]);
+                            uint4* dst = reinterpret_cast<uint4*>(a.out + orow * kPreD + 16 * c);
+                            dst[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                            dst[1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+                        }
+                        __syncwarp();
+                    }
+                    if (live) {
+                        if (whole) a.lse[orow] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+                        else w.part_ml[(size_t)share * 2 * kPreRows + x * kPreRows + row] = make_float2(ref, sum);
+                    }
+                    t5::fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.o_empty[x]);
+                if (!whole && x == 0 && tid == 0)
+                    w.rec[share] = PreRecord{walk.cs, walk.clg, walk.crg, (walk.t1 == walk.tiles ? 1 : 0) | (nf ? 2 : 0)};
+            }
+            tiles += units;
+            ++seg;
+        }
+        if (!ok && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
+    }
+    t5::fence_before();
+    __syncthreads();
+    if (warp == kPreMmaWarp) {
+        t5::fence_after();
+        t5::tmem_dealloc(tmem, 512);
+    }
+}
+
+// Joins the shares of an item that cuts of the line fall into, in line order: a warp per row, four dims a lane.  Block c of the grid's
+// first axis has the item whose first cut is the start of CTA c, if there is one.
+constexpr int kPreMergeRows = 16;
+__global__ void __launch_bounds__(32 * kPreMergeRows)
+prefill_merge_kernel(const __grid_constant__ PreWork w, int n_cta) {
+    pdl_wait();
+    pdl_trigger();
+    const PrefillArgs& a = w.a;
+    const int c = blockIdx.x + 1, lane = threadIdx.x & 31, rr = blockIdx.y * kPreMergeRows + (threadIdx.x >> 5);
+    const PreRecord it = w.rec[2 * c], head = w.rec[2 * c - 1];
+    if (it.s < 0 || head.s != it.s || head.lg != it.lg || head.rg != it.rg) return;
+    const int LG = a.L * a.G, x = rr >> 7, row = rr & 127, in_tile = row / a.r;
+    const int m0 = it.rg * 2 * w.tpt, token = m0 + x * w.tpt + in_tile;
+    const int n_q = a.n_q ? min(max(a.n_q[it.s], 0), a.M) : a.M;
+    if (in_tile >= w.tpt || token >= n_q) return;
+    float top = -INFINITY, z = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    int flags = 0;
+    for (int i = c - 1; i < n_cta; ++i) {
+        const int share = i < c ? 2 * c - 1 : 2 * i;
+        const PreRecord r = w.rec[share];
+        if (i > c && (r.s != it.s || r.lg != it.lg || r.rg != it.rg)) break;
+        flags |= r.flags;
+        const size_t at = (size_t)share * 2 * kPreRows + rr;
+        const float2 ml = w.part_ml[at];
+        if (ml.x > -INFINITY || ml.y != 0.0f) {                    // a share without a visible token holds no sums
+            const float4 v = *reinterpret_cast<const float4*>(w.part_o + at * kPreD + 4 * lane);
+            const float to = fmaxf(top, ml.x), back = top > -INFINITY ? t5::ex2(top - to) : (z == 0.0f ? 0.0f : 1.0f), f = t5::ex2(ml.x - to);
+            z = z * back + f * ml.y;
+            acc.x = acc.x * back + f * v.x; acc.y = acc.y * back + f * v.y; acc.z = acc.z * back + f * v.z; acc.w = acc.w * back + f * v.w;
+            top = to;
+        }
+        if (r.flags & 1) break;
+    }
+    const bool none = z == 0.0f;
+    float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (!none) { out[0] = acc.x / z; out[1] = acc.y / z; out[2] = acc.z / z; out[3] = acc.w / z; }
+    if ((flags & 2) && !none) {
+        const int n_tail = min(max(a.n_tail[it.s], 0), a.tail_cap - n_q);
+        for (int tok = m0 + 1; tok <= token; ++tok) {
+            const __nv_bfloat16* vr = a.tail_v + (((size_t)it.s * a.tail_cap + n_tail + tok) * LG + it.lg) * kPreD + 4 * lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = __bfloat162float(vr[i]);
+                if (!isfinite(v)) out[i] += v;
+            }
+        }
+    }
+    const size_t orow = (((size_t)it.s * a.M + token) * a.L + it.lg / a.G) * a.H + (size_t)(it.lg % a.G) * a.r + row % a.r;
+    *reinterpret_cast<uint2*>(a.out + orow * kPreD + 4 * lane) = make_uint2(ptx::pack_bf16x2(out[0], out[1]), ptx::pack_bf16x2(out[2], out[3]));
+    if (lane == 0) a.lse[orow] = none ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+}
+
+static size_t plan_prefill(char* base, PreWork* w) {
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return base ? base + at : nullptr; };
+    w->part_o = (float*)take((size_t)kSMs * 2 * 2 * kPreRows * kPreD * sizeof(float));
+    w->part_ml = (float2*)take((size_t)kSMs * 2 * 2 * kPreRows * sizeof(float2));
+    w->rec = (PreRecord*)take((size_t)kSMs * 2 * sizeof(PreRecord));
+    return off;
+}
+
+size_t prefill_workspace_bytes(const kvmem_pool_config_t&) {
+    PreWork w;
+    return plan_prefill(nullptr, &w);
+}
+
+static long long pre_most_units(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int cap, int tail_cap) {
+    const int tpt = kPreRows / (c.n_q_heads / c.n_kv_heads);
+    const long long groups = (n_q_tokens + 2ll * tpt - 1) / (2 * tpt);
+    const long long tiles = ((long long)cap + kPreTile - 1) / kPreTile + ((long long)tail_cap + kPreTile - 1) / kPreTile + 1 + kPreLead;
+    return (long long)n_sessions * c.n_layers * c.n_kv_heads * groups * tiles;
+}
+
+// the line in 30 bits, row groups of a head in 16, token rows in the 32 bits of a TMA coordinate
+bool prefill_fits(const kvmem_pool_config_t& c, int n_sessions, int n_q_tokens, int cap_tokens, int tail_cap_tokens) {
+    const int tpt = kPreRows / (c.n_q_heads / c.n_kv_heads);
+    return (long long)n_q_tokens <= 65535ll * 2 * tpt && (long long)n_sessions * n_q_tokens < INT32_MAX - 256 &&
+           (long long)n_sessions * c.n_layers * c.n_kv_heads < (1 << 30) &&
+           (double)pre_most_units(c, n_sessions, n_q_tokens, cap_tokens, tail_cap_tokens) < (double)kPreMostUnits;
+}
+
+static bool pre_map(CUtensorMap* map, const __nv_bfloat16* p, cuuint64_t d1, cuuint64_t d2, cuuint32_t box1, cuuint32_t box2) {
+    static PFN_cuTensorMapEncodeTiled_v12000 enc = [] {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr) : nullptr;
+    }();
+    if (!enc) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)kPreD, d1, d2};
+    cuuint64_t strides[2] = {(cuuint64_t)kPreD * 2, d1 * kPreD * 2};
+    cuuint32_t box[3] = {64, box1, box2}, step[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_prefill(const kvmem_pool& p, const PrefillArgs& a, void* workspace, cudaStream_t st) {
+    static PerDeviceOnce once;
+    if (once.pending(p.cfg.device)) {
+        const cudaError_t e = cudaFuncSetAttribute(prefill_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPreSmem);
+        if (e != cudaSuccess) return e;
+        once.mark(p.cfg.device);
+    }
+    PreWork w{};
+    plan_prefill((char*)workspace, &w);
+    w.a = a;
+    w.tpt = kPreRows / a.r;
+    const int LG = a.L * a.G;
+    CUtensorMap mq, mk, mv, mtk, mtv;
+    bool made = pre_map(&mq, a.q, (cuuint64_t)a.L * a.H, (cuuint64_t)a.ns * a.M, (cuuint32_t)a.r, (cuuint32_t)w.tpt) &&
+                pre_map(&mk, a.view_k, (cuuint64_t)a.cap, (cuuint64_t)a.ns * LG, kPreTile, 1) &&
+                pre_map(&mv, a.view_v, (cuuint64_t)a.cap, (cuuint64_t)a.ns * LG, kPreTile, 1);
+    if (a.tail_k)
+        made = made && pre_map(&mtk, a.tail_k, (cuuint64_t)LG, (cuuint64_t)a.ns * a.tail_cap, 1, kPreTile) &&
+               pre_map(&mtv, a.tail_v, (cuuint64_t)LG, (cuuint64_t)a.ns * a.tail_cap, 1, kPreTile);
+    else { mtk = mk; mtv = mv; }
+    if (!made) return cudaErrorInvalidValue;
+    const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), pre_most_units(p.cfg, a.ns, a.M, a.cap, a.tail_cap));
+    cudaError_t e = launch_pdl(prefill_kernel, dim3((unsigned)grid), dim3(kPreThreads), kPreSmem, st, mq, mk, mv, mtk, mtv, w);
+    if (e != cudaSuccess || grid < 2) return e;
+    return launch_pdl(prefill_merge_kernel, dim3((unsigned)grid - 1, 2 * kPreRows / kPreMergeRows), dim3(32 * kPreMergeRows), 0, st, w, grid);
+}
+
+}  // namespace kvmem

@@ -1,0 +1,309 @@
+// New tokens on their way into the cache: rotation from the model's rotary form, rows of the tail and of reserved pages, and the
+// step that makes whole reserved blocks part of the repository.
+//
+// Rotary forms.  Every pass of this library rotates pairs (i, i + d/2) by the angles of a table row.  A model that pairs
+// (2i, 2i + 1), or rotates only the first rotary_dim dims, is the same thing after a permutation of the dims, with angle 0 where
+// nothing turns: pair p goes to (p, d/2 + p), the dims that pass go behind the pairs of either half.  q . k and the Mean-K score do
+// not change under a permutation that queries and keys share, so only the way in knows of it ("pool's order").
+//
+// A thread takes 8 pairs of one vector: two 128-bit loads, the 8 (cos, sin) of the token, two 128-bit stores.  The head's dims lie
+// in three orders; in each the 8 + 8 elements are two runs of 8, or one of 16 to be taken apart (interleaved pairs).
+// Everything here moves bytes: bound by HBM where there are many tokens, by one launch where there are few.
+#include <algorithm>
+
+#include "kvmem_internal.cuh"
+#include "kvmem_rope.cuh"
+
+namespace kvmem {
+
+// ---- table of a rotary form -------------------------------------------------------------------------------------------------
+// Angles in 64 bits, one rounding of cos and sin to fp32; one thread per entry.  A frequency of 0 gives (1, 0) exactly.
+__global__ void __launch_bounds__(256)
+rope_table_kernel(float2* __restrict__ rope, int half, long long entries, const __grid_constant__ RopeFrequencies f) {
+    const long long e = blockIdx.x * 256ll + threadIdx.x;
+    if (e >= entries) return;
+    double s, c;
+    sincos((double)(e / half) * f.f[e % half], &s, &c);
+    rope[e] = make_float2((float)c, (float)s);
+}
+
+cudaError_t launch_rope_table(const kvmem_pool& p, const RopeFrequencies& f, cudaStream_t st) {
+    const int half = p.geo.d / 2;
+    const long long entries = (long long)p.cfg.rope_max_positions * half;
+    rope_table_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, st>>>(p.rope_dev, half, entries, f);
+    return cudaGetLastError();
+}
+
+// ---- the dims of a head ------------------------------------------------------------------------------------------------------
+
+// where the 8 + 8 elements of chunk c lie in a vector; woven: 16 elements from lo on, pair by pair
+struct Place {
+    int lo, hi;
+    bool woven;
+};
+__device__ __forceinline__ Place place_of(const RopeForm& f, bool pool_order, int c, int d) {
+    if (pool_order) return {8 * c, d / 2 + 8 * c, false};
+    if (c >= f.chunks) return {f.rotary + 8 * (c - f.chunks), f.rotary + (d - f.rotary) / 2 + 8 * (c - f.chunks), false};
+    return f.interleaved ? Place{16 * c, 16 * c + 8, true} : Place{8 * c, f.rotary / 2 + 8 * c, false};
+}
+
+// two runs of pairs (a0 b0 a1 b1 ...) to firsts and seconds, and back
+__device__ __forceinline__ void unweave(uint4& lo, uint4& hi) {
+    const uint4 x = lo, y = hi;
+    lo = make_uint4(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.z, x.w, 0x5410), __byte_perm(y.x, y.y, 0x5410), __byte_perm(y.z, y.w, 0x5410));
+    hi = make_uint4(__byte_perm(x.x, x.y, 0x7632), __byte_perm(x.z, x.w, 0x7632), __byte_perm(y.x, y.y, 0x7632), __byte_perm(y.z, y.w, 0x7632));
+}
+__device__ __forceinline__ void weave(uint4& lo, uint4& hi) {
+    const uint4 x = lo, y = hi;
+    lo = make_uint4(__byte_perm(x.x, y.x, 0x5410), __byte_perm(x.x, y.x, 0x7632), __byte_perm(x.y, y.y, 0x5410), __byte_perm(x.y, y.y, 0x7632));
+    hi = make_uint4(__byte_perm(x.z, y.z, 0x5410), __byte_perm(x.z, y.z, 0x7632), __byte_perm(x.w, y.w, 0x5410), __byte_perm(x.w, y.w, 0x7632));
+}
+
+// rotate8_cs with an amplitude: fp32 products, sums and the amplitude's product each rounded to fp32, then one rounding to bf16
+__device__ __forceinline__ void turn8(uint4& lo, uint4& hi, const float4 (&t4)[4], float sgn, float amplitude) {
+    uint32_t* l = reinterpret_cast<uint32_t*>(&lo);
+    uint32_t* h = reinterpret_cast<uint32_t*>(&hi);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float4 t = t4[w];
+        const float a0 = __uint_as_float(l[w] << 16), a1 = __uint_as_float(l[w] & 0xffff0000u);
+        const float b0 = __uint_as_float(h[w] << 16), b1 = __uint_as_float(h[w] & 0xffff0000u);
+        const float s0 = sgn * t.y, s1 = sgn * t.w;
+        const float l0 = __fsub_rn(__fmul_rn(a0, t.x), __fmul_rn(b0, s0)), h0 = __fadd_rn(__fmul_rn(b0, t.x), __fmul_rn(a0, s0));
+        const float l1 = __fsub_rn(__fmul_rn(a1, t.z), __fmul_rn(b1, s1)), h1 = __fadd_rn(__fmul_rn(b1, t.z), __fmul_rn(a1, s1));
+        const __nv_bfloat162 lp = __floats2bfloat162_rn(__fmul_rn(l0, amplitude), __fmul_rn(l1, amplitude));
+        const __nv_bfloat162 hp = __floats2bfloat162_rn(__fmul_rn(h0, amplitude), __fmul_rn(h1, amplitude));
+        l[w] = *reinterpret_cast<const uint32_t*>(&lp);
+        h[w] = *reinterpret_cast<const uint32_t*>(&hp);
+    }
+}
+
+__device__ __forceinline__ uint4 ld16(const __nv_bfloat16* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ void st16(__nv_bfloat16* p, const uint4& v) { *reinterpret_cast<uint4*>(p) = v; }
+
+// ---- rotation ----------------------------------------------------------------------------------------------------------------
+
+// One thread: chunk c of PER vectors of one row, so that a table row is fetched once for them and their loads are in flight together.
+template <int PER>
+__global__ void __launch_bounds__(256)
+rope_apply_kernel(const __grid_constant__ RopeApplyArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const unsigned e = blockIdx.x * 256u + threadIdx.x;
+    const unsigned c = e % (unsigned)a.chunks, g = e / (unsigned)a.chunks % (unsigned)a.groups, row = e / (unsigned)(a.chunks * a.groups);
+    if (row >= (unsigned)a.n_rows) return;
+    const bool turns = (int)c < a.form.chunks;
+    const int pos = a.positions[row];
+    if (pos < 0 || pos >= a.rope_positions) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); return; }
+    const Place in = place_of(a.form, a.x_pool, (int)c, a.d), out = place_of(a.form, a.y_pool, (int)c, a.d);
+    const __nv_bfloat16* x = a.x + (long long)row * a.x_row + (long long)g * a.x_vec;
+    __nv_bfloat16* y = a.y + (long long)row * a.y_row + (long long)g * a.y_vec;
+    const long long x_step = (long long)a.groups * a.x_vec, y_step = (long long)a.groups * a.y_vec;
+    uint4 lo[PER], hi[PER];
+    float4 t4[4];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if ((int)g + i * a.groups < a.n_vec) {
+            // (plain loads: y may be x)
+            lo[i] = *reinterpret_cast<const uint4*>(x + i * x_step + in.lo);
+            hi[i] = *reinterpret_cast<const uint4*>(x + i * x_step + in.hi);
+        }
+    if (turns) {
+        const float4* cs = reinterpret_cast<const float4*>(a.rope + (size_t)pos * (a.d / 2) + 8 * c);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) t4[w] = __ldg(cs + w);
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if ((int)g + i * a.groups < a.n_vec) {
+            if (turns) {
+                if (in.woven) unweave(lo[i], hi[i]);
+                turn8(lo[i], hi[i], t4, a.sgn, a.amplitude);
+                if (out.woven) weave(lo[i], hi[i]);
+            }
+            st16(y + i * y_step + out.lo, lo[i]);
+            st16(y + i * y_step + out.hi, hi[i]);
+        }
+}
+
+cudaError_t launch_rope_apply(const kvmem_pool& p, RopeApplyArgs a, long long n_rows, cudaStream_t st) {
+    constexpr int PER = 4;
+    a.chunks = p.geo.d / 16;
+    a.groups = (a.n_vec + PER - 1) / PER;
+    const long long per_row = (long long)a.chunks * a.groups, most = std::max<long long>(1, (1ll << 30) / per_row);
+    for (long long r0 = 0; r0 < n_rows; r0 += most) {
+        a.n_rows = (int)std::min(most, n_rows - r0);
+        const cudaError_t e = launch_pdl(rope_apply_kernel<PER>, dim3((unsigned)((a.n_rows * per_row + 255) / 256)), dim3(256), 0, st, a);
+        if (e != cudaSuccess) return e;
+        a.x += a.n_rows * a.x_row;
+        a.y += a.n_rows * a.y_row;
+        a.positions += a.n_rows;
+    }
+    return cudaSuccess;
+}
+
+// ---- append ------------------------------------------------------------------------------------------------------------------
+
+// One thread: chunk c of PER vectors of one new token, a vector being a query, key or value head of a layer.  Vectors are numbered
+// [layer][query heads | key heads | value heads].
+template <int PER>
+__global__ void __launch_bounds__(256)
+append_tokens_kernel(const __grid_constant__ AppendTokensArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const unsigned e = blockIdx.x * 256u + threadIdx.x;
+    const unsigned c = e % (unsigned)a.chunks, g = e / (unsigned)a.chunks % (unsigned)a.groups;
+    const unsigned token = e / (unsigned)(a.chunks * a.groups), s = token / (unsigned)a.M + (unsigned)a.s0, i = token % (unsigned)a.M;
+    if (s >= (unsigned)a.ns) return;
+    const int n_new = a.n_new ? min(max(a.n_new[s], 0), a.M) : a.M;
+    const int given = a.tail_n[s];
+    if ((int)i >= n_new) return;
+    const int n_tail = min(max(given, 0), a.tail_cap - n_new);
+    const int row = n_tail + (int)i;
+    bool ok = n_tail == given;
+    long long pos = 0;
+    if (a.rope) {
+        pos = a.positions ? a.positions[(size_t)s * a.M + i] : (long long)a.first_position + (a.n_sel ? (long long)max(a.n_sel[s], 0) * a.B : 0) + row;
+        if (pos < 0 || pos >= a.rope_positions) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); return; }
+    }
+    __nv_bfloat16* page = nullptr;
+    if (a.pages) {
+        const int b = a.nblocks_dev[a.session_first + s] + row / a.B;
+        const int pg = b < a.max_bps ? a.tables[(size_t)(a.session_first + s) * a.max_bps + b] : -1;
+        if (pg >= 0 && pg < a.max_blocks) page = a.pages + (size_t)pg * a.page_elems + (size_t)(row % a.B) * a.d;
+        else ok = false;
+    }
+    if (!ok) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
+    const bool turns = (int)c < a.form.chunks;
+    const Place in = place_of(a.form, a.rope == nullptr, (int)c, a.d);
+    const int per_layer = a.Hq + 2 * a.G, lo_at = 8 * (int)c, hi_at = a.d / 2 + 8 * (int)c;
+    uint4 lo[PER], hi[PER];
+    float4 t4[4];
+    int kind[PER], l[PER], h[PER];                       // 0 query, 1 key, 2 value; layer; head
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const int v = (int)g + u * a.groups;
+        kind[u] = -1;
+        if (v < a.n_vec) {
+            l[u] = v / per_layer;
+            const int at = v - l[u] * per_layer;
+            kind[u] = at < a.Hq ? 0 : at < a.Hq + a.G ? 1 : 2;
+            h[u] = kind[u] == 0 ? at : kind[u] == 1 ? at - a.Hq : at - a.Hq - a.G;
+            const TokenRows& t = kind[u] == 0 ? a.q : kind[u] == 1 ? a.k : a.v;
+            const __nv_bfloat16* src = t.data + (long long)s * t.session + (long long)i * t.token + (long long)l[u] * t.layer + (long long)h[u] * t.head;
+            lo[u] = ld16(src + (kind[u] == 2 ? lo_at : in.lo));
+            hi[u] = ld16(src + (kind[u] == 2 ? hi_at : in.hi));
+        }
+    }
+    if (turns) {
+        const float4* cs = reinterpret_cast<const float4*>(a.rope + (size_t)pos * (a.d / 2) + 8 * c);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) t4[w] = __ldg(cs + w);
+    }
+    const size_t tail_row = (size_t)s * a.tail_cap + row, tile = (size_t)a.B * a.d;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        if (kind[u] < 0) continue;
+        if (kind[u] < 2 && turns && in.woven) unweave(lo[u], hi[u]);
+        if (kind[u] > 0 && page) {
+            __nv_bfloat16* dst = page + ((size_t)((kind[u] - 1) * a.L + l[u]) * a.G + h[u]) * tile;
+            st16(dst + lo_at, lo[u]);
+            st16(dst + hi_at, hi[u]);
+        }
+        if (kind[u] < 2 && turns) turn8(lo[u], hi[u], t4, 1.0f, kind[u] == 0 ? a.q_amplitude : 1.0f);
+        __nv_bfloat16* dst = kind[u] == 0 ? a.q_out + ((((size_t)s * a.M + i) * a.L + l[u]) * a.Hq + h[u]) * a.d
+                                          : (kind[u] == 1 ? a.tail_k : a.tail_v) + ((tail_row * a.L + l[u]) * a.G + h[u]) * a.d;
+        st16(dst + lo_at, lo[u]);
+        st16(dst + hi_at, hi[u]);
+    }
+}
+
+cudaError_t launch_append_tokens(const kvmem_pool& p, AppendTokensArgs a, cudaStream_t st) {
+    constexpr int PER = 4;
+    a.chunks = p.geo.d / 16;
+    a.n_vec = a.L * (a.Hq + 2 * a.G);
+    a.groups = (a.n_vec + PER - 1) / PER;
+    // whole sessions per launch, as far as their threads are numbered in 32 bits (the caller keeps one session below that)
+    const long long per_session = (long long)a.M * a.chunks * a.groups;
+    const int most = (int)std::max<long long>(1, (1ll << 31) / per_session), all = a.ns;
+    for (int s0 = 0; s0 < all; s0 += most) {
+        a.s0 = s0;
+        a.ns = std::min(all, s0 + most);
+        const cudaError_t e = launch_pdl(append_tokens_kernel<PER>, dim3((unsigned)(((a.ns - s0) * per_session + 255) / 256)), dim3(256), 0, st, a);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+bool append_tokens_fits(const kvmem_pool_config_t& c, int n_q_tokens) {
+    return (long long)n_q_tokens * (c.head_dim / 16) * ((long long)c.n_layers * (c.n_q_heads + 2 * c.n_kv_heads)) < (1ll << 31);
+}
+
+// ---- commit ------------------------------------------------------------------------------------------------------------------
+
+// Index rows of blocks whose raw keys lie in pages already: the fp32 sum in token order, one product, one rounding of append_kernel,
+// a thread per dim.  Grid: (block of the session, layer and KV head, session).
+__global__ void __launch_bounds__(128)
+commit_index_kernel(const __grid_constant__ CommitArgs a) {
+    const CommitSession cs = a.s[blockIdx.z];
+    const int b = cs.have + (int)blockIdx.x, lg = blockIdx.y;
+    if ((int)blockIdx.x >= cs.n) return;
+    const int pg = a.tables[(size_t)cs.session * a.max_bps + b];
+    if (pg < 0 || pg >= a.max_blocks) { if (threadIdx.x == 0) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); return; }
+    const __nv_bfloat16* k = a.pages + (size_t)pg * a.page_elems + (size_t)lg * a.B * a.d;
+    __nv_bfloat16* row = a.index + (size_t)cs.session * a.index_elems + ((size_t)lg * a.max_bps + b) * a.d;
+    const float inv = 1.0f / (float)a.B;
+    for (int x = threadIdx.x; x < a.d; x += 128) {
+        float acc = 0.0f;
+#pragma unroll 16
+        for (int t = 0; t < a.B; ++t) acc = __fadd_rn(acc, __bfloat162float(k[(size_t)t * a.d + x]));
+        row[x] = __float2bfloat16_rn(__fmul_rn(acc, inv));
+    }
+}
+
+// The tail's rows behind the committed blocks move to its front: n B rows down, in runs of at most that many, so that a run's reads
+// and writes never meet; 16 bytes a thread.  Grid: (16-byte columns of a token row / 32, K | V, session).
+__global__ void __launch_bounds__(256)
+commit_tail_kernel(const __grid_constant__ CommitArgs a) {
+    const CommitSession cs = a.s[blockIdx.z];
+    const int down = cs.n * a.B, n = min(a.tail_n[cs.slot], a.tail_cap), left = n - down;
+    if (left <= 0) return;                              // fewer than the blocks hold: commit_counts_kernel reports it
+    const size_t width = (size_t)a.L * a.G * a.d / 8;   // 16-byte columns
+    const int col = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
+    uint4* t = reinterpret_cast<uint4*>(blockIdx.y ? a.tail_v : a.tail_k) + (size_t)cs.slot * a.tail_cap * width + col;
+    for (int r0 = 0; r0 < left; r0 += down) {
+        const int end = min(left, r0 + down);
+        if ((size_t)col < width)
+            for (int r = r0 + lane; r < end; r += 8) t[(size_t)r * width] = t[(size_t)(r + down) * width];
+        __syncthreads();
+    }
+}
+
+__global__ void commit_counts_kernel(const __grid_constant__ CommitArgs a) {
+    const CommitSession cs = a.s[threadIdx.x];
+    if ((int)threadIdx.x >= a.ns) return;
+    a.nblocks[cs.session] = cs.have + cs.n;
+    if (a.tail_n) {
+        const int n = a.tail_n[cs.slot], left = min(n, a.tail_cap) - cs.n * a.B;
+        if (left < 0 || n > a.tail_cap) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
+        a.tail_n[cs.slot] = max(left, 0);
+    }
+}
+
+cudaError_t launch_commit(const CommitArgs& a, cudaStream_t st) {
+    int most = 0;
+    for (int i = 0; i < a.ns; ++i) most = std::max(most, a.s[i].n);
+    commit_index_kernel<<<dim3((unsigned)most, (unsigned)(a.L * a.G), (unsigned)a.ns), 128, 0, st>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    if (a.tail_n) {
+        const unsigned cols = (unsigned)(((size_t)a.L * a.G * a.d / 8 + 31) / 32);
+        commit_tail_kernel<<<dim3(cols, 2, (unsigned)a.ns), 256, 0, st>>>(a);
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    commit_counts_kernel<<<1, kCommitSessions, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace kvmem

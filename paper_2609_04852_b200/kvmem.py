@@ -38,6 +38,15 @@ class TailStruct(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("cap_tokens", C.c_int32), ("n_tokens", C.c_void_p)]
 
 
+class RopeStruct(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layout", "rotary_dim", "scaling")] + \
+               [(n, C.c_float) for n in ("factor", "original_positions", "turns_fast", "turns_slow")]
+
+
+class RowsStruct(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("session_stride", "token_stride", "layer_stride", "head_stride")]
+
+
 class SelectParams(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("budget_blocks", "max_view_tokens", "mandatory_tokens",
                                           "n_sink_blocks", "n_recent_blocks")]
@@ -60,6 +69,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     L = C.CDLL(path)
     vp, i32, sz, f32 = C.c_void_p, C.c_int32, C.c_size_t, C.c_float
     cfgp, prmp, tailp = C.POINTER(PoolConfig), C.POINTER(SelectParams), C.POINTER(TailStruct)
+    ropep, rowsp, i64 = C.POINTER(RopeStruct), C.POINTER(RowsStruct), C.c_int64
     sig = {
         "kvmem_pool_bytes": (sz, [cfgp]),
         "kvmem_budget_blocks": (i32, [prmp, i32, i32]),
@@ -113,6 +123,16 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "kvmem_paged_tree_attend": (C.c_int, [vp, i32, i32, vp, i32, vp, vp, vp, i32, vp, tailp, f32, vp, vp, vp, sz, vp]),
         "kvmem_view_attend_mass": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i32, vp, tailp, f32, vp, f32, vp, vp, vp, sz, vp]),
         "kvmem_view_evict": (C.c_int, [vp, i32, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]),
+        "kvmem_rope_frequencies": (C.c_int, [cfgp, ropep, C.POINTER(C.c_double)]),
+        "kvmem_set_rope": (C.c_int, [vp, ropep, vp]),
+        "kvmem_rope_apply": (C.c_int, [vp, vp, i64, i64, i32, vp, i64, i64, i32, i64, i32, vp, i32, f32, vp]),
+        "kvmem_reserve_blocks": (C.c_int, [vp, i32, i32, C.POINTER(i32), vp]),
+        "kvmem_session_reserved": (i32, [vp, i32]),
+        "kvmem_append_tokens": (C.c_int, [vp, i32, i32, i32, vp, rowsp, rowsp, rowsp, vp, vp, i32, f32, tailp, vp, i32, vp]),
+        "kvmem_commit_blocks": (C.c_int, [vp, i32, i32, C.POINTER(i32), tailp, vp]),
+        "kvmem_prefill_workspace_bytes": (sz, [cfgp, i32, i32]),
+        "kvmem_view_prefill_attend": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i32, vp, tailp, f32, vp, vp, vp, sz, vp]),
+        "kvmem_get_pages": (C.c_int, [vp, C.POINTER(vp)]),
         "kvmem_step_staging_bytes": (sz, [cfgp, i32, i32]),
         "kvmem_recall_step_host": (C.c_int, [vp, i32, i32, vp, i32, prmp, vp, i32, vp, vp, vp, i32, f32, vp, vp,
                                              vp, sz, vp, sz, vp, sz, vp]),
@@ -138,7 +158,9 @@ EXPORTED = ("kvmem_pool_bytes", "kvmem_budget_blocks", "kvmem_select_workspace_b
             "kvmem_materialize_attend_rope", "kvmem_paged_attend_fp8", "kvmem_materialize_attend_fp8",
             "kvmem_paged_attend_fp8_rope", "kvmem_selftest_wait_timeout", "kvmem_selftest_joint_wait_timeout", "kvmem_materialize_delta",
             "kvmem_materialize_fp8_rope", "kvmem_tree_workspace_bytes", "kvmem_view_tree_attend", "kvmem_paged_tree_attend",
-            "kvmem_mass_workspace_bytes", "kvmem_view_attend_mass", "kvmem_evict_workspace_bytes", "kvmem_view_evict")
+            "kvmem_mass_workspace_bytes", "kvmem_view_attend_mass", "kvmem_evict_workspace_bytes", "kvmem_view_evict",
+            "kvmem_rope_frequencies", "kvmem_set_rope", "kvmem_rope_apply", "kvmem_reserve_blocks", "kvmem_session_reserved",
+            "kvmem_append_tokens", "kvmem_commit_blocks", "kvmem_prefill_workspace_bytes", "kvmem_view_prefill_attend", "kvmem_get_pages")
 
 
 def _check(status: int) -> None:
@@ -167,6 +189,26 @@ def _place(name: str, t: torch.Tensor, dtype, shape: tuple, device: int) -> int:
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on cuda:{device}, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (strided)'}")
     return t.data_ptr()
+
+
+def _rows(name: str, t: torch.Tensor, shape: tuple, device: int) -> RowsStruct:
+    """Rows [n_sessions][n_tokens][L][heads][d] of any strides but the last: a slice of a packed projection, read where it lies."""
+    if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != device or t.stride(4) != 1:
+        raise ValueError(f"{name}: expected a bf16 tensor {tuple(shape)} on cuda:{device} with contiguous heads, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
+    # (the stride of an axis of length 1 means nothing)
+    return RowsStruct(t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 else 0 for i in range(4)))
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
+ORDERS = {"model": 0, "pool": 1}
+
+
+def _one_of(name: str, value: str, choices: Dict[str, int]) -> int:
+    if value not in choices:
+        raise ValueError(f"{name}: expected one of {', '.join(choices)}, got {value!r}")
+    return choices[value]
 
 
 class HostStep:
@@ -201,6 +243,23 @@ def budget_blocks(params: SelectParams, block_tokens: int, n_blocks: int) -> int
 
 def set_option(name: str, value: int) -> None:
     _check(load_library().kvmem_set_option(name.encode(), value))
+
+
+@dataclass
+class Rope:
+    """Rotary form of a model (kvmem_rope_t): layout "half" or "interleaved", the dims that rotate (0: all), and how the
+    frequencies are scaled for long contexts: "none", "linear", "base", "ramp" or "bands"."""
+    layout: str = "half"
+    rotary_dim: int = 0
+    scaling: str = "none"
+    factor: float = 1.0
+    original_positions: float = 0.0
+    turns_fast: float = 0.0
+    turns_slow: float = 0.0
+
+    def struct(self) -> RopeStruct:
+        return RopeStruct(_one_of("layout", self.layout, ROPE_LAYOUTS), self.rotary_dim, _one_of("scaling", self.scaling, ROPE_SCALINGS),
+                          self.factor, self.original_positions, self.turns_fast, self.turns_slow)
 
 
 @dataclass
@@ -562,6 +621,101 @@ class Pool:
         _check(self.lib.kvmem_view_evict(self.handle, ns, vk, vv, cap, np_, ap, keep, n_sink_tokens, n_recent_tokens, dk, dv, dcap,
                                          dp, kp, no, wp, wn, st))
 
+    # ---- new tokens: rotary forms, tail and pages, prompt chunks
+    def rope_frequencies(self, rope: Optional[Rope] = None) -> List[float]:
+        """Radians per position of the pairs (i, i + d/2) in the pool's order; 0 where dims pass."""
+        f = (C.c_double * (self.cfg.head_dim // 2))()
+        _check(self.lib.kvmem_rope_frequencies(C.byref(self.cfg), None if rope is None else C.byref(rope.struct()), f))
+        return list(f)
+
+    def set_rope(self, rope: Optional[Rope] = None) -> None:
+        """Make this the pool of a model with this rotary form (None: the pool's own), before any block comes in."""
+        _check(self.lib.kvmem_set_rope(self.handle, None if rope is None else C.byref(rope.struct()), self._raw_stream()))
+
+    def rope_apply(self, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None, inverse: bool = False,
+                   amplitude: float = 1.0, x_order: str = "model", out_order: str = "pool") -> torch.Tensor:
+        """x bf16 [n_rows][n_vec][head_dim] (rows and vectors strided as they lie), positions int32 [n_rows] -> rotated vectors,
+        "model" or "pool" order of the dims on either side; out may be x if the orders are the same."""
+        d = self.cfg.head_dim
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        for name, t in (("x", x), ("out", out)):
+            if t.dim() != 3 or t.shape != x.shape or t.shape[2] != d or t.dtype is not torch.bfloat16 or t.get_device() != self._index or t.stride(2) != 1:
+                raise ValueError(f"{name}: expected a bf16 tensor [n_rows][n_vec][{d}] on cuda:{self._index} with contiguous vectors, got "
+                                 f"{t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
+        n_rows, n_vec = x.shape[0], x.shape[1]
+        pp = _place("positions", positions, torch.int32, (n_rows,), self._index)
+        xo, yo = _one_of("x_order", x_order, ORDERS), _one_of("out_order", out_order, ORDERS)
+        if n_rows and n_vec:
+            one = lambda t, i: t.stride(i) if t.shape[i] > 1 else 0          # (the stride of an axis of length 1 means nothing)
+            _check(self.lib.kvmem_rope_apply(self.handle, x.data_ptr(), one(x, 0), one(x, 1), xo, out.data_ptr(), one(out, 0), one(out, 1), yo,
+                                             n_rows, n_vec, pp, int(inverse), amplitude, self._raw_stream()))
+        return out
+
+    def reserve_blocks(self, session: int, n_blocks: int, phys_ids: Optional[Sequence[int]] = None) -> None:
+        """Pages for n_blocks blocks behind the session's last, to be filled by append_tokens(pages=True)."""
+        if phys_ids is not None and len(phys_ids) != n_blocks:
+            raise KvmemError(E_INVALID, "one page id per block")
+        ids = None if phys_ids is None else (C.c_int32 * n_blocks)(*[int(x) for x in phys_ids])
+        _check(self.lib.kvmem_reserve_blocks(self.handle, session, n_blocks, ids, self._raw_stream()))
+
+    def session_reserved(self, session: int) -> int:
+        n = self.lib.kvmem_session_reserved(self.handle, session)
+        if n < 0:
+            _check(n)
+        return n
+
+    def _tail_struct(self, tail: Tail, ns: int) -> TailStruct:
+        L, _, G, d = self._dims
+        cap = tail.k.shape[1] if tail.k.dim() == 5 else -1
+        shape = (ns, cap, L, G, d)
+        return TailStruct(_place("tail.k", tail.k, torch.bfloat16, shape, self._index), _place("tail.v", tail.v, torch.bfloat16, shape, self._index),
+                          cap, _place("tail.n_tokens", tail.n_tokens, torch.int32, (ns,), self._index))
+
+    def append_tokens(self, k: torch.Tensor, v: torch.Tensor, tail: Tail, q: Optional[torch.Tensor] = None,
+                      q_out: Optional[torch.Tensor] = None, n_new: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                      n_sel: Optional[torch.Tensor] = None, first_position: int = 0, q_amplitude: float = 1.0, pages: bool = False,
+                      session_first: int = 0) -> None:
+        """New tokens behind the tail's committed ones: q bf16 [n_sessions][M][L][H][d] (optional, with q_out of that shape), k, v
+        [n_sessions][M][L][G][d], strided as they lie.  Rotated queries go to q_out, rotated keys and values to the tail, with pages
+        raw keys and values to the reserved pages as well.  Positions are positions int32 [n_sessions][M], or first_position +
+        n_sel * block_tokens + the tail's row."""
+        L, H, G, d = self._dims
+        dev, i32 = self._index, torch.int32
+        if k.dim() != 5:
+            raise ValueError("k: expected [n_sessions][n_new_tokens][L][G][d]")
+        ns, M = k.shape[0], k.shape[1]
+        kr, vr = _rows("k", k, (ns, M, L, G, d), dev), _rows("v", v, (ns, M, L, G, d), dev)
+        qr, qo = None, None
+        if q is not None:
+            qr = _rows("q", q, (ns, M, L, H, d), dev)
+        if q_out is not None:
+            qo = _place("q_out", q_out, torch.bfloat16, (ns, M, L, H, d), dev)
+        nn = None if n_new is None else _place("n_new", n_new, i32, (ns,), dev)
+        pp = None if positions is None else _place("positions", positions, i32, (ns, M), dev)
+        np_ = None if n_sel is None else _place("n_sel", n_sel, i32, (ns,), dev)
+        _check(self.lib.kvmem_append_tokens(self.handle, session_first, ns, M, nn, qr, kr, vr, pp, np_, first_position, q_amplitude,
+                                            self._tail_struct(tail, ns), qo, int(pages), self._raw_stream()))
+
+    def commit_blocks(self, n_blocks: Sequence[int], tail: Optional[Tail] = None, session_first: int = 0) -> None:
+        """The first n_blocks[s] reserved blocks of each session become part of it, with their index rows; the tail's rows behind
+        them move to its front."""
+        ns = len(n_blocks)
+        ts = None if tail is None else self._tail_struct(tail, ns)
+        _check(self.lib.kvmem_commit_blocks(self.handle, session_first, ns, (C.c_int32 * max(ns, 1))(*[int(x) for x in n_blocks]), ts,
+                                            self._raw_stream()))
+
+    def view_prefill_attend(self, q: torch.Tensor, view: View, n_sel: torch.Tensor, tail: Optional[Tail], out: torch.Tensor,
+                            lse: torch.Tensor, n_q: Optional[torch.Tensor] = None, scale: float = 0.0,
+                            workspace: Optional[torch.Tensor] = None) -> None:
+        """view_tree_attend for a prompt chunk of any length: token i sees the view, the committed tail and the chunk's tokens 0 .. i.
+        Calls that may overlap on the GPU need a workspace each (kvmem_prefill_workspace_bytes); None: the pool's own."""
+        ns, M, qp, np_, tp, op, lp, nq = self._decode_common(q, n_sel, tail, out, lse, n_q)
+        vk, vv, cap = self._view_of("view", view, ns)
+        st = self._raw_stream()
+        wp, wn = self._decode_workspace(workspace, st, "prefill", ns, M)
+        _check(self.lib.kvmem_view_prefill_attend(self.handle, ns, qp, M, nq, vk, vv, cap, np_, tp, scale, op, lp, wp, wn, st))
+
     def materialize_attend(self, q: torch.Tensor, sel_ids: torch.Tensor, n_sel: torch.Tensor, view: View,
                            out: torch.Tensor, lse: torch.Tensor, scale: float = 0.0, session_first: int = 0) -> None:
         """materialize + view_attend in one pass over the selected blocks (same results, a third less HBM traffic)."""
@@ -732,6 +886,17 @@ class Pool:
         full = self.storage[off:off + 2 * elems].view(torch.bfloat16).view(c.n_layers, c.n_kv_heads,
                                                                               c.max_blocks_per_session, c.head_dim)
         return full[:, :, :n.value, :].clone()
+
+    def pages(self) -> torch.Tensor:
+        """bf16 [max_blocks][K | V][L][G][B][d]: the pages of a bf16 repository (a view of the pool's storage)."""
+        ptr = C.c_void_p()
+        _check(self.lib.kvmem_get_pages(self.handle, C.byref(ptr)))
+        c = self.cfg
+        if c.fp8_pages:
+            raise KvmemError(E_STATE, "the pool's pages hold FP8 codes")
+        shape = (c.max_blocks, 2, c.n_layers, c.n_kv_heads, c.block_tokens, c.head_dim)
+        off, n = (ptr.value or 0) - self.storage.data_ptr(), 2 * c.max_blocks * 2 * c.n_layers * c.n_kv_heads * c.block_tokens * c.head_dim
+        return self.storage[off:off + n].view(torch.bfloat16).view(shape)
 
     def block_table(self, session: int) -> torch.Tensor:
         ptr, n = C.c_void_p(), C.c_int32()

@@ -11,15 +11,20 @@
 // thread fetches Q, K and V tiles with TMA (128-byte swizzle), one thread issues the MMAs: those of one thread run in order, so a
 // slot's next S is issued right behind the product that reads its P, in whose place it goes.
 //
-// ref is a running maximum that moves only when a row's logits pass it by 8 (in powers of two): O is then rescaled in tensor
-// memory.  Until then the weights may reach 2^8, which costs neither fp32 nor bf16 any precision.
+// ref is the largest logit of the first tokens a row sees.  It moves only when half a tile's weights sum to more than 2^64: O is then
+// rescaled in tensor memory and the half's weights are computed again.  Until then they may be that large, which costs neither fp32
+// nor bf16 any precision, and no tile needs the maximum of its logits.
 //
 // Work: an item is (session, KV head, group of two row tiles); its tiles are those of the view and of the tail up to the group's last
-// token.  All items' tiles lie on one line, cut into as many equal parts as there are CTAs (one per SM): chunks over views of any
-// lengths keep all SMs busy to the end, and the causal part's short and long items need no other balance.  An item that a cut falls
-// into is left as partial sums, joined in line order by prefill_merge_kernel: the result depends on the sizes alone, not on
-// timing.  A CTA leaves at most two of them (its first and its last), so the workspace does not grow with the call.  Items of one KV
-// head are neighbours on the line: the CTAs that stream the same keys and values do so closely enough to find them in L2.
+// token.  All items' tiles lie on one line (with a lead for what starting and ending an item costs), cut into equal parts, one for each
+// CTA (one per SM): chunks over views of any lengths keep all SMs busy to the end, and the causal part's short and long items need
+// no other balance.  An item that a cut falls into is left as partial sums, joined in line order by prefill_merge_kernel: the
+// result depends on the sizes alone, not on timing.  A part leaves at most two of them (its first and its last), so the workspace
+// does not grow with the call.
+// Where the keys and values of all KV heads are more than L2 holds, the line is cut into several parts for each CTA, the c-th of n from
+// c on in steps of n: all CTAs then work on a few heads at a time and find their tiles in L2 after the first.  (In one sweep over
+// eight heads of 33 MB the CTAs are spread over all of them and read every tile from HBM: 2,048 tokens over 65,536 take 2,420 us at
+// 1,425 MHz under the power limit; in four sweeps 2,190 us at 1,640 MHz.)
 //
 // Tokens that a row does not see: their logits are replaced before they are used, values behind the last token are cleared in shared
 // memory before the second product (0 x NaN), and so are values that are not finite of chunk tokens that only some rows see; the
@@ -40,11 +45,19 @@ constexpr int kPreTile = 128;                    // tokens per tile
 constexpr int kPreRows = 128;                    // rows per slot: TMEM lanes
 constexpr int kPreHalf = 128 * 128;              // bytes of one 64-dim half of a 128-row operand tile
 constexpr int kPreSlot = 2 * kPreHalf;           // a K, V or Q tile
-constexpr int kPreRing = 5;                      // K and V tiles in turn
-constexpr int kPreThreads = 320;                 // eight row warps, TMA warp, MMA warp: 200 registers a thread
+constexpr int kPreRing = 4;                      // K and V tiles in turn
+constexpr int kPreStage = 4096;                  // bytes of a row warp's staging for stores
+constexpr int kPreThreads = 384;                 // eight row warps, TMA warp, MMA warp, two that only give registers away
 constexpr int kPreTmaWarp = 8, kPreMmaWarp = 9;
-constexpr int kPreLead = 1;                      // units on the line for an item's start and end
-constexpr float kPreSlack = 8.0f;                // a row's logits may pass its reference by this much (log2)
+// Registers a thread: the launch gives 168, the row warps take 216 and the others keep 64 (256 x 216 + 128 x 64 <= 384 x 168)
+#define PRE_ROW_REGS "216"
+#define PRE_OTHER_REGS "64"
+constexpr int kPreLead = 3;                      // units on the line for an item's start and end: what they cost a CTA, in tiles (1: 195 and 314 us
+                                                 // instead of 170 and 234 for a chunk of 4,096 alone and three ragged sessions)
+constexpr float kPreLimit = 18446744073709551616.0f;   // 2^64: half a tile's weights may sum to this before their reference moves
+constexpr int kPreParts = 4;                     // parts of the line a CTA can have
+constexpr int kPreBudget = 1024;                 // tiles of keys and values (64 KiB each) that a sweep of all CTAs may hold in L2
+constexpr int kPrePartUnits = 64;                // least units of a part, when there is more than one
 constexpr uint32_t kPreIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (16u << 17) | (8u << 24);   // bf16 x bf16 -> fp32, 128 x 128
 constexpr uint32_t kPreIdescO = kPreIdescS | (1u << 16);                                         // B with dims contiguous (V as it lies)
 constexpr uint32_t kPreVStep = (uint32_t)kPreHalf >> 4;       // leading offset of V's descriptor: from dims 0..63 to 64..127
@@ -55,9 +68,10 @@ struct PreRecord { int s, lg, rg, flags; };      // flags: 1 the item's last sha
 struct PreWork {
     PrefillArgs a;
     int tpt;                                     // tokens per row tile
-    float* part_o;                               // [2 CTAs][256][128]
-    float2* part_ml;                             // [2 CTAs][256]: (reference, sum of weights), log2 domain
-    PreRecord* rec;                              // [2 CTAs]: what shares 2c (begun by an earlier CTA) and 2c + 1 (goes on in the next) hold
+    float* part_o;                               // [2 parts][slot][dims / 4][128 rows][4]
+    float2* part_ml;                             // [2 parts][256]: (reference, sum of weights), log2 domain
+    PreRecord* rec;                              // [2 parts]: what shares 2c (begun in an earlier part) and 2c + 1 (goes on in the next) hold
+    int* n_parts;                                // parts of the line in all
 };
 
 struct PreSpan {
@@ -84,17 +98,18 @@ __device__ __forceinline__ int pre_tail_tiles(const PrefillArgs& a, const PreSpa
     return a.tail_k ? (sp.n_tail + min((rg + 1) * 2 * tpt, sp.n_q) + kPreTile - 1) / kPreTile : 0;
 }
 
-// sum over i < n of floor((step i + from) / 128), by exchanging the axes of the triangle under the line
-__device__ __forceinline__ long long floor_sum(long long n, long long step, long long from) {
-    long long m = kPreTile, sum = 0;
+// sum over i < n of floor((step i + from) / 128), by exchanging the axes of the triangle under the line.  In 32 bits: the sum is
+// at most the line's 2^30 units, and so are the products that it is made of.
+__device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t step, uint32_t from) {
+    uint32_t m = kPreTile, sum = 0;
     while (n > 0) {
-        if (step >= m) { sum += (n - 1) * n / 2 * (step / m); step %= m; }
-        if (from >= m) { sum += n * (from / m); from %= m; }
-        const long long top = step * n + from;
+        if (step >= m) { const uint32_t k = step / m; sum += (n - 1) * n / 2 * k; step -= k * m; }
+        if (from >= m) { const uint32_t k = from / m; sum += n * k; from -= k * m; }
+        const uint32_t top = step * n + from;
         if (top < m) break;
         n = top / m;
-        from = top % m;
-        const long long t = m;
+        from = top - n * m;
+        const uint32_t t = m;
         m = step;
         step = t;
     }
@@ -113,16 +128,27 @@ __device__ __forceinline__ int pre_head(const PrefillArgs& a, const PreSpan& sp,
     return pre_before(a, sp, tpt, sp.groups - 1) + max(pre_tiles(a, sp, tpt, sp.groups - 1), 1) + kPreLead;
 }
 
+// where a part of the line begins and ends, and the item at its beginning: its first unit, session, KV head, row group
+struct PrePart { int begin, end, from, s, lg, rg; };
+
 // a role's walk over its CTA's shares of items
 struct PreWalk {
-    int pos, end, from;             // next unit of the line, the CTA's end, the item's first unit
+    const PrePart* parts;           // the CTA's, in shared memory
+    int part, n_parts;              // the next one, how many
+    int pos, end, from;             // next unit of the line, the part's end, the item's first unit
     int s, lg, rg;                  // the item at `from`
     PreSpan sp;
     int t0, t1, tiles;              // the share: tiles [t0, t1) of the item's `tiles` (0: nothing to see)
     int cs, clg, crg, m0, rows2;    // its item; first token; whether the second row tile has any token
     __device__ __forceinline__ bool next(const PreWork& w, int LG) {
         const PrefillArgs& a = w.a;
-        while (pos < end) {
+        while (true) {
+            if (pos >= end) {
+                if (part >= n_parts) return false;
+                const PrePart p = parts[part++];
+                pos = p.begin; end = p.end; from = p.from; s = p.s; lg = p.lg; rg = p.rg;
+                sp = pre_span(a, w.tpt, s, false);
+            }
             while (sp.groups == 0) sp = pre_span(a, w.tpt, ++s, false);     // (a session that has units follows: pos < end)
             tiles = pre_tiles(a, sp, w.tpt, rg);
             const int some = max(tiles, 1), first = from + kPreLead, item_end = first + some;
@@ -145,19 +171,19 @@ struct PreWalk {
             }
             if (t0 < t1) return true;
         }
-        return false;
     }
     int n_view, n_tail, n_q, view_tiles;      // of the share's session
     __device__ __forceinline__ int units() const { return tiles ? t1 - t0 : 0; }
 };
 
 struct PreShared {
-    uint64_t full[kPreRing], empty[kPreRing], q_full, q_empty, s_full[2], p_full[2][2], o_full[2], o_empty[2], drained;
-    int plan_begin, plan_end, plan_from, plan_s, plan_lg, plan_rg;
+    uint64_t full[kPreRing], empty[kPreRing], q_full, q_empty, s_full[2], p_full[2][2], h_full[2], o_full[2], o_empty[2], drained;
+    PrePart parts[kPreParts];
+    int n_parts, n_cta;                       // the CTA's; CTAs that share the line
     uint32_t tmem;
     int not_finite[2];                        // by the parity of the share: its number + 1, where values were cleared
 };
-constexpr size_t kPreSmem = (size_t)(2 + kPreRing) * kPreSlot + sizeof(PreShared);
+constexpr size_t kPreSmem = (size_t)(2 + kPreRing) * kPreSlot + 8 * kPreStage + sizeof(PreShared);
 static_assert(kPreSmem <= 232448, "shared memory of a CTA");
 
 __device__ __forceinline__ void pre_zero_row(const PrefillArgs& a, size_t orow) {
@@ -174,7 +200,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     extern __shared__ __align__(1024) unsigned char smem_q[];          // two Q tiles, the ring, then the small things
     const PrefillArgs& a = w.a;
     unsigned char* ring = smem_q + 2 * kPreSlot;
-    PreShared& sh = *reinterpret_cast<PreShared*>(ring + (size_t)RING * kPreSlot);
+    unsigned char* staging = ring + (size_t)RING * kPreSlot;
+    PreShared& sh = *reinterpret_cast<PreShared*>(staging + 8 * kPreStage);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int LG = a.L * a.G, tpt = w.tpt;
 
@@ -188,6 +215,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             ptx::mbar_init(&sh.s_full[i], 1);
             ptx::mbar_init(&sh.p_full[i][0], 4);
             ptx::mbar_init(&sh.p_full[i][1], 4);
+            ptx::mbar_init(&sh.h_full[i], 1);
             ptx::mbar_init(&sh.o_full[i], 1);
             ptx::mbar_init(&sh.o_empty[i], 4);
             sh.not_finite[i] = 0;
@@ -203,51 +231,79 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     }
     pdl_wait();        // everything earlier in the stream is complete and visible from here on
     pdl_trigger();
-    if (warp == kPreTmaWarp) {
-        if (lane == 0) {
-            ptx::prefetch_tensormap(&map_q);
-            ptx::prefetch_tensormap(&map_k);
-            ptx::prefetch_tensormap(&map_v);
-            ptx::prefetch_tensormap(&map_tk);
-            ptx::prefetch_tensormap(&map_tv);
+    if (tid == 32 * kPreTmaWarp) {
+        ptx::prefetch_tensormap(&map_q);
+        ptx::prefetch_tensormap(&map_k);
+        ptx::prefetch_tensormap(&map_v);
+        ptx::prefetch_tensormap(&map_tk);
+        ptx::prefetch_tensormap(&map_tv);
+    }
+    {
+        // the CTA's parts of the line, and the item each starts in: a warp a part, each counting the line for itself
+        const PreSpan first = lane < a.ns ? pre_span(a, tpt, lane, blockIdx.x == 0 && warp == 0) : PreSpan{};
+        const int first_head = pre_head(a, first, tpt);
+        int sum = first_head, held = first.groups ? pre_tiles(a, first, tpt, first.groups - 1) : 0;
+        for (int s = lane + 32; s < a.ns; s += 32) {
+            const PreSpan sp = pre_span(a, tpt, s, blockIdx.x == 0 && warp == 0);
+            sum += pre_head(a, sp, tpt);
+            held += sp.groups ? pre_tiles(a, sp, tpt, sp.groups - 1) : 0;
         }
-        // the CTA's part of the line, and the item it starts in
-        int sum = 0;
-        for (int s = lane; s < a.ns; s += 32) sum += pre_head(a, pre_span(a, tpt, s, blockIdx.x == 0), tpt);
         const int total = __reduce_add_sync(0xffffffffu, sum) * LG, n = min((int)gridDim.x, total);
-        const bool idle = (int)blockIdx.x >= n;
-        const int begin = idle ? 0 : (int)((long long)total * blockIdx.x / n), end = idle ? 0 : (int)((long long)total * (blockIdx.x + 1) / n);
-        int before = 0;
-        for (int s0 = 0; s0 < a.ns && !idle; s0 += 32) {
-            const int s = s0 + lane;
-            PreSpan sp{};
-            if (s < a.ns) sp = pre_span(a, tpt, s, false);
-            const int head = s < a.ns ? pre_head(a, sp, tpt) : 0, mine = head * LG;
-            int incl = mine;
+        const unsigned tiles = __reduce_add_sync(0xffffffffu, held) * (unsigned)LG;
+        int sweeps = (int)min((unsigned)kPreParts, (tiles + kPreBudget - 1) / kPreBudget);
+        sweeps = max(1, min(sweeps, n ? total / (n * kPrePartUnits) : 1));
+        const int all = n * sweeps, mine_n = (int)blockIdx.x < n ? sweeps : 0;
+        for (int b = warp; b < mine_n; b += kPreThreads / 32) {
+            const int part = b * n + (int)blockIdx.x;
+            const int begin = (int)((unsigned long long)total * part / all), end = (int)((unsigned long long)total * (part + 1) / all);
+            int before = 0;
+            for (int s0 = 0; s0 < a.ns; s0 += 32) {
+                const int s = s0 + lane;
+                PreSpan sp{};
+                int head = 0;
+                if (s0 == 0) { sp = first; head = first_head; }
+                else if (s < a.ns) { sp = pre_span(a, tpt, s, false); head = pre_head(a, sp, tpt); }
+                const int mine = head * LG;
+                int incl = mine;
+                if (a.ns > 1) {
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int up = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += up;
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const int up = __shfl_up_sync(0xffffffffu, incl, d);
+                        if (lane >= d) incl += up;
+                    }
+                }
+                const int lo = before + incl - mine;
+                const unsigned here = __ballot_sync(0xffffffffu, begin >= lo && begin < lo + mine);
+                if (here) {
+                    // that lane's session; the last of its row groups that starts at the part's beginning or before, 32 tried at a time
+                    const int from = __ffs(here) - 1;
+                    const int at_s = s0 + from, lo_s = __shfl_sync(0xffffffffu, lo, from), head_s = __shfl_sync(0xffffffffu, head, from);
+                    sp.n_view = __shfl_sync(0xffffffffu, sp.n_view, from); sp.n_tail = __shfl_sync(0xffffffffu, sp.n_tail, from);
+                    sp.n_q = __shfl_sync(0xffffffffu, sp.n_q, from); sp.view_tiles = __shfl_sync(0xffffffffu, sp.view_tiles, from);
+                    sp.groups = __shfl_sync(0xffffffffu, sp.groups, from);
+                    const int lg = (begin - lo_s) / head_s, at = begin - lo_s - lg * head_s;
+                    int rg = 0, units = 0;
+                    for (int span = sp.groups; span > 0;) {
+                        const int step = (span + 31) / 32, try_rg = rg + lane * step, u = lane * step < span ? pre_before(a, sp, tpt, try_rg) : 0;
+                        const int k = 31 - __clz(__ballot_sync(0xffffffffu, lane * step < span && u <= at));
+                        units = __shfl_sync(0xffffffffu, u, k);
+                        rg += k * step;
+                        span = step == 1 ? 0 : min(step, span - k * step);
+                    }
+                    if (lane == 0) sh.parts[b] = PrePart{begin, end, lo_s + lg * head_s + units, at_s, lg, rg};
+                    break;
+                }
+                before += __shfl_sync(0xffffffffu, incl, 31);
             }
-            const int lo = before + incl - mine;
-            if (begin >= lo && begin < lo + mine) {
-                const int lg = (begin - lo) / head, at = begin - lo - lg * head;
-                int rg = 0;                                      // the last group that starts at `at` or before
-                for (int step = 1 << 15; step; step >>= 1)
-                    if (rg + step < sp.groups && pre_before(a, sp, tpt, rg + step) <= at) rg += step;
-                sh.plan_s = s;
-                sh.plan_lg = lg;
-                sh.plan_rg = rg;
-                sh.plan_from = lo + lg * head + pre_before(a, sp, tpt, rg);
+            if (lane == 0) {
+                w.rec[2 * part].s = -1;
+                w.rec[2 * part + 1].s = -1;
             }
-            before += __shfl_sync(0xffffffffu, incl, 31);
-            if (before > begin) break;
         }
-        if (lane == 0) {
-            sh.plan_begin = begin;
-            sh.plan_end = end;
-            w.rec[2 * blockIdx.x].s = -1;
-            w.rec[2 * blockIdx.x + 1].s = -1;
+        if (tid == 0) {
+            sh.n_parts = mine_n;
+            sh.n_cta = n;
+            if (blockIdx.x == 0) *w.n_parts = all;
         }
     }
     t5::fence_before();
@@ -255,15 +311,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     t5::fence_after();
     const uint32_t tmem = sh.tmem;
     PreWalk walk;
-    walk.pos = sh.plan_begin; walk.end = sh.plan_end;
-    if (walk.pos < walk.end) {
-        walk.from = sh.plan_from; walk.s = sh.plan_s; walk.lg = sh.plan_lg; walk.rg = sh.plan_rg;
-        walk.sp = pre_span(a, tpt, walk.s, false);
-    }
+    walk.parts = sh.parts; walk.n_parts = sh.n_parts;
+    walk.part = walk.pos = walk.end = 0;
 
     // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
     // every role still reaches its end.
     bool ok = true;
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 " PRE_OTHER_REGS ";");
     if (warp == kPreTmaWarp) {
         // ------------------------------------------------ TMA: one thread
         if (t5::elect()) {
@@ -361,6 +416,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     }
                     if (ok) ok = ptx::mbar_wait(&sh.p_full[0][0], p_ph0);
                     half_product(0, 0, j == 0);
+                    if (ok) t5::commit(&sh.h_full[0]);
                     if (ok) ok = ptx::mbar_wait(&sh.p_full[0][1], p_ph0);
                     half_product(0, 1, false);
                     p_ph0 ^= 1u;
@@ -373,6 +429,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         if (j == 0 && ok && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
                         if (ok) ok = ptx::mbar_wait(&sh.p_full[1][0], p_ph1);
                         half_product(1, 0, j == 0);
+                        if (ok) t5::commit(&sh.h_full[1]);
                         if (ok) ok = ptx::mbar_wait(&sh.p_full[1][1], p_ph1);
                         half_product(1, 1, false);
                         p_ph1 ^= 1u;
@@ -395,12 +452,15 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             ok = ptx::mbar_wait(&sh.drained, 0u) && ok;
             if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 " PRE_ROW_REGS ";");
         // ------------------------------------------------ rows: a thread each
         const int x = warp >> 2, row = (warp & 3) * 32 + lane, gt = tid & 127;
         const uint32_t s_addr = tmem + (uint32_t)x * 256u + ((uint32_t)((warp & 3) * 32) << 16), o_addr = s_addr + 128u;
         const float scale2 = a.scale * 1.4426950408889634f;
         const int my_token = row / a.r, my_head = row - my_token * a.r;
+        const int n_cta = sh.n_cta;
         int cnt = 0, done = 0, tiles = 0, seg = 0;       // units and shares of this slot; tiles and shares of the CTA
         auto wait = [&](uint64_t* bar, int phase) {
             if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1));
@@ -474,63 +534,69 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                                 for (int i = 0; i < 32; ++i)
                                     if (32 * c + i >= seen) sv[c][i] = 0xff800000u;
                         }
-                        float m[4];                                // the row's largest logit in this tile, NaN if one is
+                        const uint64_t sc2 = f2::pk(scale2, scale2);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            m[c] = f2::max3_nan(__uint_as_float(sv[c][0]), __uint_as_float(sv[c][1]), __uint_as_float(sv[c][2]));
+                        for (int half = 0; half < 2; ++half) {
+                            float part;
+                            for (bool again = false;; again = true) {
+                                const float use = ref == -INFINITY ? 0.0f : ref;      // nothing seen yet: every weight is exp2(-inf) = 0
+                                const uint64_t nm2 = f2::pk(-use, -use);
+                                uint64_t acc0 = f2::pk(0.0f, 0.0f), acc1 = acc0;
 #pragma unroll
-                            for (int i = 3; i < 31; i += 2) m[c] = f2::max3_nan(m[c], __uint_as_float(sv[c][i]), __uint_as_float(sv[c][i + 1]));
-                            m[c] = f2::max3_nan(m[c], __uint_as_float(sv[c][31]), __uint_as_float(sv[c][31]));
-                        }
-                        const float m2 = scale2 * f2::max3_nan(f2::max3_nan(m[0], m[1], m[2]), m[3], m[3]);
-                        // true for the first logit that is not -inf (ref is), and for a NaN
-                        const bool moves = live && !(m2 <= ref + kPreSlack) && m2 != -INFINITY;
-                        if (__any_sync(0xffffffffu, moves)) {
-                            const float to = moves ? m2 : ref, corr = moves ? t5::ex2(ref - to) : 1.0f;
-                            if (j > 0) {
-                                // the last product into O is complete: this tile's logits were issued after it
-#pragma unroll 1
-                                for (int c = 0; c < 8; ++c) {
-                                    uint32_t ov[16];
-                                    t5::ld16_issue(o_addr + 16u * c, ov);
-                                    t5::ld_wait(ov);
+                                for (int c = 0; c < 2; ++c) {
+                                    uint32_t pk[16];
+                                    const uint32_t (&v)[32] = sv[2 * half + c];
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
-                                    t5::st16(o_addr + 16u * c, ov);
+                                    for (int i = 0; i < 16; ++i) {
+                                        float p0, p1;
+                                        f2::unpk(f2::fma(f2::pk(v[2 * i], v[2 * i + 1]), sc2, nm2), p0, p1);
+                                        p0 = t5::ex2(p0);
+                                        p1 = t5::ex2(p1);
+                                        if (i & 1) acc1 = f2::add(acc1, f2::pk(p0, p1)); else acc0 = f2::add(acc0, f2::pk(p0, p1));
+                                        pk[i] = ptx::pack_bf16x2(p0, p1);
+                                    }
+                                    t5::st16(s_addr + 32u * half + 16u * c, pk);      // over logits that this thread has read
                                 }
-                            }
-                            sum *= corr;
-                            ref = to;
-                        }
-                        const float use = ref == -INFINITY ? 0.0f : ref;      // nothing seen yet: every weight is exp2(-inf) = 0
-                        const uint64_t sc2 = f2::pk(scale2, scale2), nm2 = f2::pk(-use, -use);
-                        uint64_t acc0 = f2::pk(0.0f, 0.0f), acc1 = acc0;
+                                float a0, a1, a2, a3;
+                                f2::unpk(acc0, a0, a1);
+                                f2::unpk(acc1, a2, a3);
+                                part = (a0 + a1) + (a2 + a3);
+                                // rows without a reference yet, and those whose weights have grown past the limit (a NaN too)
+                                const bool moves = live && (ref == -INFINITY || !(part <= kPreLimit));
+                                if (again || !__any_sync(0xffffffffu, moves)) break;
+                                float m = -INFINITY;                   // largest logit of this half, NaN if one is
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t pk[16];
+                                for (int i = 0; i < 32; ++i)
+                                    m = f2::max3_nan(m, __uint_as_float(sv[2 * half + (i >> 4)][2 * (i & 15)]), __uint_as_float(sv[2 * half + (i >> 4)][2 * (i & 15) + 1]));
+                                m *= scale2;
+                                const float to = moves && m != -INFINITY ? m : ref, corr = to == ref ? 1.0f : t5::ex2(ref - to);
+                                // what O holds: the products before this tile's logits were issued, and the first half's
+                                if (half == 1) {
+                                    wait(&sh.h_full[x], cnt - 1);
+                                    t5::fence_after();
+                                }
+                                if (j > 0 || half == 1) {
+#pragma unroll 1
+                                    for (int c = 0; c < 8; ++c) {
+                                        uint32_t ov[16];
+                                        t5::ld16_issue(o_addr + 16u * c, ov);
+                                        t5::ld_wait(ov);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                float p0, p1;
-                                f2::unpk(f2::fma(f2::pk(sv[c][2 * i], sv[c][2 * i + 1]), sc2, nm2), p0, p1);
-                                p0 = t5::ex2(p0);
-                                p1 = t5::ex2(p1);
-                                if (i & 1) acc1 = f2::add(acc1, f2::pk(p0, p1)); else acc0 = f2::add(acc0, f2::pk(p0, p1));
-                                pk[i] = ptx::pack_bf16x2(p0, p1);
+                                        for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr);
+                                        t5::st16(o_addr + 16u * c, ov);
+                                    }
+                                }
+                                sum *= corr;
+                                ref = to;
                             }
-                            t5::st16(s_addr + 16u * c, pk);        // over logits that this thread has read
-                            if (c == 1) {                          // the first half of the tokens is ready for its product
-                                t5::st_wait();
-                                t5::fence_before();
+                            sum += part;
+                            t5::st_wait();
+                            t5::fence_before();
+                            if (half == 0) {                       // the first half of the tokens is ready for its product
                                 __syncwarp();
                                 if (lane == 0) ptx::mbar_arrive(&sh.p_full[x][0]);
                             }
                         }
-                        float a0, a1, a2, a3;
-                        f2::unpk(acc0, a0, a1);
-                        f2::unpk(acc1, a2, a3);
-                        sum += (a0 + a1) + (a2 + a3);
-                        t5::st_wait();
-                        t5::fence_before();
                     } else if (lane == 0) {
                         ptx::mbar_arrive(&sh.p_full[x][0]);
                     }
@@ -540,49 +606,75 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 // the share's sums
                 wait(&sh.o_full[x], done++);
                 const bool whole = walk.t0 == 0 && walk.t1 == walk.tiles;
-                const int share = 2 * blockIdx.x + (walk.t0 == 0 ? 1 : 0);
+                const int share = 2 * ((walk.part - 1) * n_cta + (int)blockIdx.x) + (walk.t0 == 0 ? 1 : 0);
                 const bool nf = *(volatile int*)&sh.not_finite[seg & 1] == seg + 1;
                 if (warp_live) {
                     t5::fence_after();
                     const bool none = sum == 0.0f;
-                    const float inv = none ? 0.0f : 1.0f / sum;
-                    float* po = w.part_o + ((size_t)share * 2 * kPreRows + x * kPreRows + row) * kPreD;
-#pragma unroll 1
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t ov[16];
-                        t5::ld16_issue(o_addr + 16u * c, ov);
-                        t5::ld_wait(ov);
-                        if (live && !whole) {
+                    if (whole) {
+                        // 64 dims of each row at a time through the warp's staging, so that eight lanes write a row's 128 bytes together (a
+                        // lane with 16 bytes of a row of its own takes eight times as many cycles of the store path)
+                        const uint32_t stage = ptx::smem_u32(staging + warp * kPreStage);
+                        const float inv = none ? 0.0f : 1.0f / sum;
+                        unsigned long long to[8];                      // the rows that this lane writes a part of; 0: none
+                        {
+                            const unsigned long long mine_to = live ? (unsigned long long)(a.out + orow * kPreD) : 0ull;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                *reinterpret_cast<uint4*>(po + 16 * c + 4 * i) = make_uint4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
-                        } else if (live) {
-                            float o[16];
+                            for (int i = 0; i < 8; ++i) to[i] = __shfl_sync(0xffffffffu, mine_to, i * 4 + (lane >> 3));
+                        }
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = none ? 0.0f : __uint_as_float(ov[i]) * inv;
-                            if (nf && !none) {
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t ov[2][32], pk[32];
+                            t5::ld32_issue(o_addr + 64u * c, ov[0]);
+                            t5::ld32_issue(o_addr + 64u * c + 32u, ov[1]);
+                            t5::ld_wait(ov[0]);
+                            t5::ld_wait(ov[1]);
+                            float* o = reinterpret_cast<float*>(ov);
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) o[i] = none ? 0.0f : o[i] * inv;
+                            if (nf && live && !none) {
                                 // values that were cleared and that this row sees
                                 for (int tok = walk.m0 + 1; tok <= token; ++tok) {
-                                    const __nv_bfloat16* vr = a.tail_v + (((size_t)walk.cs * a.tail_cap + walk.n_tail + tok) * LG + walk.clg) * kPreD + 16 * c;
+                                    const __nv_bfloat16* vr = a.tail_v + (((size_t)walk.cs * a.tail_cap + walk.n_tail + tok) * LG + walk.clg) * kPreD + 64 * c;
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) {
+                                    for (int i = 0; i < 64; ++i) {
                                         const float v = __bfloat162float(vr[i]);
                                         if (!isfinite(v)) o[i] += v;
                                     }
                                 }
                             }
-                            uint32_t pk[8];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) pk[i] = ptx::pack_bf16x2(o[2 * i], o[2 * i + 1]);
-                            uint4* dst = reinterpret_cast<uint4*>(a.out + orow * kPreD + 16 * c);
-                            dst[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                            dst[1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+                            for (int i = 0; i < 32; ++i) pk[i] = ptx::pack_bf16x2(o[2 * i], o[2 * i + 1]);
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + 128u * lane + 16u * (i ^ (lane & 7))), "r"(pk[4 * i]), "r"(pk[4 * i + 1]), "r"(pk[4 * i + 2]), "r"(pk[4 * i + 3]) : "memory");
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const int rr = i * 4 + (lane >> 3);
+                                uint32_t v[4];
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(stage + 128u * rr + 16u * ((lane & 7) ^ (rr & 7))) : "memory");
+                                if (to[i]) asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to[i] + 128 * c + 16 * (lane & 7)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                            }
                         }
-                        __syncwarp();
-                    }
-                    if (live) {
-                        if (whole) a.lse[orow] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
-                        else w.part_ml[(size_t)share * 2 * kPreRows + x * kPreRows + row] = make_float2(ref, sum);
+                        if (live) a.lse[orow] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+                    } else {
+                        // partial sums lie four dims at a time, a row's behind another's: a warp's stores are whole lines as they are
+                        float4* po = reinterpret_cast<float4*>(w.part_o) + ((size_t)share * 2 + x) * (kPreD / 4) * kPreRows + row;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t ov[32];
+                            t5::ld32_issue(o_addr + 32u * c, ov);
+                            t5::ld_wait(ov);
+                            if (live) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    po[(size_t)(8 * c + i) * kPreRows] = make_float4(__uint_as_float(ov[4 * i]), __uint_as_float(ov[4 * i + 1]), __uint_as_float(ov[4 * i + 2]), __uint_as_float(ov[4 * i + 3]));
+                            }
+                            __syncwarp();
+                        }
+                        if (live) w.part_ml[(size_t)share * 2 * kPreRows + x * kPreRows + row] = make_float2(ref, sum);
                     }
                     t5::fence_before();
                 }
@@ -604,65 +696,90 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     }
 }
 
-// Joins the shares of an item that cuts of the line fall into, in line order: a warp per row, four dims a lane.  Block c of the grid's
-// first axis has the item whose first cut is the start of CTA c, if there is one.
-constexpr int kPreMergeRows = 16;
-__global__ void __launch_bounds__(32 * kPreMergeRows)
-prefill_merge_kernel(const __grid_constant__ PreWork w, int n_cta) {
+// Joins the shares of an item that cuts of the line fall into, in line order.  Block c - 1 of the grid's first axis has the item whose
+// first cut is the start of part c, if there is one; the second axis is the slot.  A warp has 32 rows, a lane each, and 16 dims: its
+// reads are whole lines, and the next share's are in flight while one is added.
+constexpr int kPreMergeThreads = 1024;
+__global__ void __launch_bounds__(kPreMergeThreads)
+prefill_merge_kernel(const __grid_constant__ PreWork w) {
     pdl_wait();
     pdl_trigger();
     const PrefillArgs& a = w.a;
-    const int c = blockIdx.x + 1, lane = threadIdx.x & 31, rr = blockIdx.y * kPreMergeRows + (threadIdx.x >> 5);
+    const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, x = blockIdx.y;
+    const int n_parts = *w.n_parts;
+    if (c >= n_parts) return;
     const PreRecord it = w.rec[2 * c], head = w.rec[2 * c - 1];
     if (it.s < 0 || head.s != it.s || head.lg != it.lg || head.rg != it.rg) return;
-    const int LG = a.L * a.G, x = rr >> 7, row = rr & 127, in_tile = row / a.r;
-    const int m0 = it.rg * 2 * w.tpt, token = m0 + x * w.tpt + in_tile;
+    const int LG = a.L * a.G, m0 = it.rg * 2 * w.tpt, first_token = m0 + x * w.tpt;
     const int n_q = a.n_q ? min(max(a.n_q[it.s], 0), a.M) : a.M;
-    if (in_tile >= w.tpt || token >= n_q) return;
+    const int rows = min(w.tpt, n_q - first_token) * a.r;               // live ones of this row tile
+    const int row = (warp & 3) * 32 + (threadIdx.x & 31), d0 = (warp >> 2) * 16;
+    if (row >= rows) return;
     float top = -INFINITY, z = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float4 acc[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     int flags = 0;
-    for (int i = c - 1; i < n_cta; ++i) {
+    for (int i = c - 1; i < n_parts; ++i) {
         const int share = i < c ? 2 * c - 1 : 2 * i;
         const PreRecord r = w.rec[share];
         if (i > c && (r.s != it.s || r.lg != it.lg || r.rg != it.rg)) break;
         flags |= r.flags;
-        const size_t at = (size_t)share * 2 * kPreRows + rr;
-        const float2 ml = w.part_ml[at];
-        if (ml.x > -INFINITY || ml.y != 0.0f) {                    // a share without a visible token holds no sums
-            const float4 v = *reinterpret_cast<const float4*>(w.part_o + at * kPreD + 4 * lane);
+        const float2 ml = w.part_ml[(size_t)share * 2 * kPreRows + x * kPreRows + row];
+        const float4* po = reinterpret_cast<const float4*>(w.part_o) + (((size_t)share * 2 + x) * (kPreD / 4) + d0 / 4) * kPreRows + row;
+        float4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = po[(size_t)k * kPreRows];
+        if (ml.x > -INFINITY || ml.y != 0.0f) {                        // a share without a visible token holds no sums
             const float to = fmaxf(top, ml.x), back = top > -INFINITY ? t5::ex2(top - to) : (z == 0.0f ? 0.0f : 1.0f), f = t5::ex2(ml.x - to);
             z = z * back + f * ml.y;
-            acc.x = acc.x * back + f * v.x; acc.y = acc.y * back + f * v.y; acc.z = acc.z * back + f * v.z; acc.w = acc.w * back + f * v.w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                acc[k].x = acc[k].x * back + f * v[k].x; acc[k].y = acc[k].y * back + f * v[k].y;
+                acc[k].z = acc[k].z * back + f * v[k].z; acc[k].w = acc[k].w * back + f * v[k].w;
+            }
             top = to;
         }
         if (r.flags & 1) break;
     }
+    const int token = first_token + row / a.r;
     const bool none = z == 0.0f;
-    float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (!none) { out[0] = acc.x / z; out[1] = acc.y / z; out[2] = acc.z / z; out[3] = acc.w / z; }
+    const float inv = none ? 0.0f : 1.0f / z;
+    float out[16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        out[4 * k] = none ? 0.0f : acc[k].x * inv; out[4 * k + 1] = none ? 0.0f : acc[k].y * inv;
+        out[4 * k + 2] = none ? 0.0f : acc[k].z * inv; out[4 * k + 3] = none ? 0.0f : acc[k].w * inv;
+    }
     if ((flags & 2) && !none) {
         const int n_tail = min(max(a.n_tail[it.s], 0), a.tail_cap - n_q);
         for (int tok = m0 + 1; tok <= token; ++tok) {
-            const __nv_bfloat16* vr = a.tail_v + (((size_t)it.s * a.tail_cap + n_tail + tok) * LG + it.lg) * kPreD + 4 * lane;
+            const __nv_bfloat16* vr = a.tail_v + (((size_t)it.s * a.tail_cap + n_tail + tok) * LG + it.lg) * kPreD + d0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 16; ++i) {
                 const float v = __bfloat162float(vr[i]);
                 if (!isfinite(v)) out[i] += v;
             }
         }
     }
     const size_t orow = (((size_t)it.s * a.M + token) * a.L + it.lg / a.G) * a.H + (size_t)(it.lg % a.G) * a.r + row % a.r;
-    *reinterpret_cast<uint2*>(a.out + orow * kPreD + 4 * lane) = make_uint2(ptx::pack_bf16x2(out[0], out[1]), ptx::pack_bf16x2(out[2], out[3]));
-    if (lane == 0) a.lse[orow] = none ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+    uint32_t pk[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pk[i] = ptx::pack_bf16x2(out[2 * i], out[2 * i + 1]);
+    uint4* dst = reinterpret_cast<uint4*>(a.out + orow * kPreD + d0);
+    dst[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+    dst[1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+    if (d0 == 0) a.lse[orow] = none ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
 }
 
 static size_t plan_prefill(char* base, PreWork* w) {
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return base ? base + at : nullptr; };
-    w->part_o = (float*)take((size_t)kSMs * 2 * 2 * kPreRows * kPreD * sizeof(float));
-    w->part_ml = (float2*)take((size_t)kSMs * 2 * 2 * kPreRows * sizeof(float2));
-    w->rec = (PreRecord*)take((size_t)kSMs * 2 * sizeof(PreRecord));
+    constexpr size_t shares = (size_t)kSMs * kPreParts * 2;
+    w->part_o = (float*)take(shares * 2 * kPreRows * kPreD * sizeof(float));
+    w->part_ml = (float2*)take(shares * 2 * kPreRows * sizeof(float2));
+    w->rec = (PreRecord*)take(shares * sizeof(PreRecord));
+    w->n_parts = (int*)take(sizeof(int));
     return off;
 }
 
@@ -724,8 +841,9 @@ cudaError_t launch_prefill(const kvmem_pool& p, const PrefillArgs& a, void* work
     if (!made) return cudaErrorInvalidValue;
     const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), pre_most_units(p.cfg, a.ns, a.M, a.cap, a.tail_cap));
     cudaError_t e = launch_pdl(prefill_kernel, dim3((unsigned)grid), dim3(kPreThreads), kPreSmem, st, mq, mk, mv, mtk, mtv, w);
-    if (e != cudaSuccess || grid < 2) return e;
-    return launch_pdl(prefill_merge_kernel, dim3((unsigned)grid - 1, 2 * kPreRows / kPreMergeRows), dim3(32 * kPreMergeRows), 0, st, w, grid);
+    const long long parts = std::min<long long>(grid * (long long)kPreParts, pre_most_units(p.cfg, a.ns, a.M, a.cap, a.tail_cap));
+    if (e != cudaSuccess || parts < 2) return e;
+    return launch_pdl(prefill_merge_kernel, dim3((unsigned)parts - 1, 2), dim3(kPreMergeThreads), 0, st, w);
 }
 
 }  // namespace kvmem

@@ -688,8 +688,8 @@ int kvmem_set_rope(kvmem_pool_t* pool, const kvmem_rope_t* rope /*HOST, may be N
 
 /* Rotate n_rows x n_vec vectors of head_dim elements, any head_dim that takes rotary support: vector (r, u) of y is vector (r, u) of x
  * turned to positions[r], or back by it (inverse != 0; that is also the gradient of the forward rotation), its rotated dims
- * times amplitude.  Row r, vector u starts r * row_stride + u * vec_stride elements behind x or y (multiples of 8, 16-byte
- * aligned bases), so queries and keys can be read where a packed projection left them.  x_order, y_order say which order the
+ * times amplitude.  Row r, vector u starts r * row_stride + u * vec_stride elements behind x or y (not negative, multiples of 8;
+ * that of an axis of length 1 is not looked at; bases 16-byte aligned), so queries and keys can be read where a packed projection left them.  x_order, y_order say which order the
  * dims come and go in.  fp32 products, sums and the amplitude's product, each rounded to fp32, one rounding to bf16; dims that
  * pass are copied.
  *   positions  DEVICE int32 [n_rows]; rows with a position outside the table are left unwritten and flagged in the status word
@@ -711,7 +711,8 @@ int kvmem_reserve_blocks(kvmem_pool_t* pool, int32_t session, int32_t n_blocks, 
 int32_t kvmem_session_reserved(const kvmem_pool_t* pool, int32_t session);
 
 /* Rows of a batch as a projection leaves them: head h of layer l of token i of session s starts
- * s * session_stride + i * token_stride + l * layer_stride + h * head_stride elements behind data (strides: multiples of 8). */
+ * s * session_stride + i * token_stride + l * layer_stride + h * head_stride elements behind data (strides: not negative, multiples of
+ * 8; that of an axis of length 1 is not looked at). */
 typedef struct {
     const void* data; /* DEVICE bf16, 16-byte aligned */
     int64_t session_stride, token_stride, layer_stride, head_stride;

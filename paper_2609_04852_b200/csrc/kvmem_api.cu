@@ -1379,6 +1379,8 @@ int kvmem_rope_apply(kvmem_pool_t* p, const void* x, int64_t x_row_stride, int64
     if ((x_order | 1) != 1 || (y_order | 1) != 1) { set_error("kvmem_rope_apply: an order is KVMEM_ORDER_MODEL or KVMEM_ORDER_POOL"); return KVMEM_E_INVALID; }
     if (!std::isfinite(amplitude) || amplitude < 0.0f) { set_error("amplitude must be finite and non-negative (0 selects 1)"); return KVMEM_E_INVALID; }
     if (n_rows == 0) return KVMEM_OK;
+    if (n_rows == 1) x_row_stride = y_row_stride = 0;
+    if (n_vec == 1) x_vec_stride = y_vec_stride = 0;
     if (!x || !y || !positions || !aligned(x, 16) || !aligned(y, 16) || !stride_ok(x_row_stride) || !stride_ok(x_vec_stride) ||
         !stride_ok(y_row_stride) || !stride_ok(y_vec_stride)) {
         set_error("kvmem_rope_apply: null or misaligned pointer, or a stride that is negative or no multiple of 8 elements");
@@ -1474,7 +1476,17 @@ int kvmem_append_tokens(kvmem_pool_t* p, int32_t session_first, int32_t n_sessio
     if (!append_tokens_fits(p->cfg, n_new_tokens)) { set_error("%d new tokens per session are more than 2^31 groups of 16 elements: append them in parts", n_new_tokens); return KVMEM_E_UNSUPPORTED; }
     const int rc = tail_ok(tail, n_sessions, n_new_tokens, who);
     if (rc != KVMEM_OK) return rc;
+    kvmem_rows_t copies[3];
     const kvmem_rows_t* in[3] = {q, k, v};
+    for (int i = 0; i < 3; ++i) {                       // the stride of an axis of length 1 means nothing
+        if (!in[i]) continue;
+        copies[i] = *in[i];
+        in[i] = &copies[i];
+        if (n_sessions == 1) copies[i].session_stride = 0;
+        if (n_new_tokens == 1) copies[i].token_stride = 0;
+        if (g.L == 1) copies[i].layer_stride = 0;
+        if ((i ? g.G : g.H) == 1) copies[i].head_stride = 0;
+    }
     if (!k || !v || !q != !q_out || !aligned(q_out, 16)) { set_error("%s: k and v are required, q and q_out go together and are 16-byte aligned", who); return KVMEM_E_INVALID; }
     for (const kvmem_rows_t* r : in)
         if (r && (!r->data || !aligned(r->data, 16) || !stride_ok(r->session_stride) || !stride_ok(r->token_stride) || !stride_ok(r->layer_stride) || !stride_ok(r->head_stride))) {
@@ -1502,7 +1514,7 @@ int kvmem_append_tokens(kvmem_pool_t* p, int32_t session_first, int32_t n_sessio
     }
     AppendTokensArgs a{};
     auto rows = [](const kvmem_rows_t* r) { return r ? TokenRows{(const __nv_bfloat16*)r->data, r->session_stride, r->token_stride, r->layer_stride, r->head_stride} : TokenRows{}; };
-    a.q = rows(q); a.k = rows(k); a.v = rows(v);
+    a.q = rows(in[0]); a.k = rows(in[1]); a.v = rows(in[2]);
     a.q_out = (__nv_bfloat16*)q_out; a.tail_k = (__nv_bfloat16*)tail->k; a.tail_v = (__nv_bfloat16*)tail->v;
     a.tail_n = tail->n_tokens; a.n_new = n_new; a.positions = positions; a.n_sel = n_sel;
     a.rope = rope ? p->rope_dev : nullptr; a.pages = to_pages ? p->pages : nullptr; a.tables = p->tables; a.nblocks_dev = p->nblocks_dev;

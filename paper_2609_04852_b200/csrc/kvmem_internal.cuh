@@ -306,7 +306,7 @@ struct RopeApplyArgs {
     float sgn, amplitude;
     int chunks, groups;                          // filled by the launcher
 };
-cudaError_t launch_rope_apply(const kvmem_pool& p, RopeApplyArgs a, long long n_rows, cudaStream_t st);
+cudaError_t launch_rope_apply(const kvmem_pool& p, const RopeApplyArgs& a, long long n_rows, cudaStream_t st);
 
 struct TokenRows {
     const __nv_bfloat16* data;

@@ -9,6 +9,12 @@
 // A thread takes 8 pairs of one vector: two 128-bit loads, the 8 (cos, sin) of the token, two 128-bit stores.  The head's dims lie
 // in three orders; in each the 8 + 8 elements are two runs of 8, or one of 16 to be taken apart (interleaved pairs).
 // Everything here moves bytes: bound by HBM where there are many tokens, by one launch where there are few.
+//
+// A thread takes one vector where all threads are resident together anyway (the shortest way through: 2.1 us instead of 2.8 with four
+// vectors for 8 tokens of 40 heads, 2.5 instead of 3.8 for an append of 8 tokens with 48), and several beyond, whose loads are then in
+// flight together behind one table row: rotation four (24,576 tokens of 40 heads 85 us, 108 with one, 94 with two), append three
+// in blocks of 128 (16,383 tokens with 48 heads 90 us, 127 with one, 103 with four in blocks of 256, whose 106 registers leave room
+// for 16 warps an SM).
 #include <algorithm>
 
 #include "kvmem_internal.cuh"
@@ -84,6 +90,7 @@ __device__ __forceinline__ void st16(__nv_bfloat16* p, const uint4& v) { *reinte
 // ---- rotation ----------------------------------------------------------------------------------------------------------------
 
 // One thread: chunk c of PER vectors of one row, so that a table row is fetched once for them and their loads are in flight together.
+constexpr long long kTokensFew = (long long)kSMs * 1024;      // threads that are resident together at any register count here
 template <int PER>
 __global__ void __launch_bounds__(256)
 rope_apply_kernel(const __grid_constant__ RopeApplyArgs a) {
@@ -126,8 +133,8 @@ rope_apply_kernel(const __grid_constant__ RopeApplyArgs a) {
         }
 }
 
-cudaError_t launch_rope_apply(const kvmem_pool& p, RopeApplyArgs a, long long n_rows, cudaStream_t st) {
-    constexpr int PER = 4;
+template <int PER>
+static cudaError_t rope_apply(const kvmem_pool& p, RopeApplyArgs a, long long n_rows, cudaStream_t st) {
     a.chunks = p.geo.d / 16;
     a.groups = (a.n_vec + PER - 1) / PER;
     const long long per_row = (long long)a.chunks * a.groups, most = std::max<long long>(1, (1ll << 30) / per_row);
@@ -142,64 +149,71 @@ cudaError_t launch_rope_apply(const kvmem_pool& p, RopeApplyArgs a, long long n_
     return cudaSuccess;
 }
 
+cudaError_t launch_rope_apply(const kvmem_pool& p, const RopeApplyArgs& a, long long n_rows, cudaStream_t st) {
+    const bool few = n_rows <= kTokensFew / ((long long)a.n_vec * (p.geo.d / 16));
+    return few ? rope_apply<1>(p, a, n_rows, st) : rope_apply<4>(p, a, n_rows, st);
+}
+
 // ---- append ------------------------------------------------------------------------------------------------------------------
 
 // One thread: chunk c of PER vectors of one new token, a vector being a query, key or value head of a layer.  Vectors are numbered
-// [layer][query heads | key heads | value heads].
+// [layer][query heads | key heads | value heads].  What a thread needs comes in two rounds of loads: counts, lengths and its vectors,
+// then the table row and the page.
+constexpr int kAppendThreads = 128;
 template <int PER>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kAppendThreads)
 append_tokens_kernel(const __grid_constant__ AppendTokensArgs a) {
     pdl_wait();
     pdl_trigger();
-    const unsigned e = blockIdx.x * 256u + threadIdx.x;
-    const unsigned c = e % (unsigned)a.chunks, g = e / (unsigned)a.chunks % (unsigned)a.groups;
-    const unsigned token = e / (unsigned)(a.chunks * a.groups), s = token / (unsigned)a.M + (unsigned)a.s0, i = token % (unsigned)a.M;
+    const unsigned e = blockIdx.x * (unsigned)kAppendThreads + threadIdx.x;
+    const unsigned c = e % (unsigned)a.chunks, eg = e / (unsigned)a.chunks, token = eg / (unsigned)a.groups, g = eg - token * (unsigned)a.groups;
+    const unsigned s = token / (unsigned)a.M + (unsigned)a.s0, i = token - (s - (unsigned)a.s0) * (unsigned)a.M;
     if (s >= (unsigned)a.ns) return;
-    const int n_new = a.n_new ? min(max(a.n_new[s], 0), a.M) : a.M;
-    const int given = a.tail_n[s];
-    if ((int)i >= n_new) return;
-    const int n_tail = min(max(given, 0), a.tail_cap - n_new);
-    const int row = n_tail + (int)i;
-    bool ok = n_tail == given;
-    long long pos = 0;
-    if (a.rope) {
-        pos = a.positions ? a.positions[(size_t)s * a.M + i] : (long long)a.first_position + (a.n_sel ? (long long)max(a.n_sel[s], 0) * a.B : 0) + row;
-        if (pos < 0 || pos >= a.rope_positions) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); return; }
-    }
-    __nv_bfloat16* page = nullptr;
-    if (a.pages) {
-        const int b = a.nblocks_dev[a.session_first + s] + row / a.B;
-        const int pg = b < a.max_bps ? a.tables[(size_t)(a.session_first + s) * a.max_bps + b] : -1;
-        if (pg >= 0 && pg < a.max_blocks) page = a.pages + (size_t)pg * a.page_elems + (size_t)(row % a.B) * a.d;
-        else ok = false;
-    }
-    if (!ok) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
+    const int given_new = a.n_new ? a.n_new[s] : a.M, given = a.tail_n[s];
+    const int n_sel = a.rope && a.n_sel ? a.n_sel[s] : 0, at = a.rope && a.positions ? a.positions[(size_t)s * a.M + i] : 0;
+    const int blocks = a.pages ? a.nblocks_dev[a.session_first + s] : 0;
     const bool turns = (int)c < a.form.chunks;
     const Place in = place_of(a.form, a.rope == nullptr, (int)c, a.d);
     const int per_layer = a.Hq + 2 * a.G, lo_at = 8 * (int)c, hi_at = a.d / 2 + 8 * (int)c;
     uint4 lo[PER], hi[PER];
-    float4 t4[4];
-    int kind[PER], l[PER], h[PER];                       // 0 query, 1 key, 2 value; layer; head
+    int kind[PER], l[PER], h[PER];                       // 0 query, 1 key, 2 value, -1 none; layer; head
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
         const int v = (int)g + u * a.groups;
         kind[u] = -1;
         if (v < a.n_vec) {
-            l[u] = v / per_layer;
-            const int at = v - l[u] * per_layer;
-            kind[u] = at < a.Hq ? 0 : at < a.Hq + a.G ? 1 : 2;
-            h[u] = kind[u] == 0 ? at : kind[u] == 1 ? at - a.Hq : at - a.Hq - a.G;
+            l[u] = a.L == 1 ? 0 : v / per_layer;
+            const int w = v - l[u] * per_layer;
+            kind[u] = w < a.Hq ? 0 : w < a.Hq + a.G ? 1 : 2;
+            h[u] = kind[u] == 0 ? w : kind[u] == 1 ? w - a.Hq : w - a.Hq - a.G;
             const TokenRows& t = kind[u] == 0 ? a.q : kind[u] == 1 ? a.k : a.v;
             const __nv_bfloat16* src = t.data + (long long)s * t.session + (long long)i * t.token + (long long)l[u] * t.layer + (long long)h[u] * t.head;
             lo[u] = ld16(src + (kind[u] == 2 ? lo_at : in.lo));
             hi[u] = ld16(src + (kind[u] == 2 ? hi_at : in.hi));
         }
     }
-    if (turns) {
-        const float4* cs = reinterpret_cast<const float4*>(a.rope + (size_t)pos * (a.d / 2) + 8 * c);
+    const int n_new = min(max(given_new, 0), a.M);
+    if ((int)i >= n_new) return;
+    const int n_tail = min(max(given, 0), a.tail_cap - n_new), row = n_tail + (int)i;
+    bool ok = n_tail == given;
+    float4 t4[4];
+    if (a.rope) {
+        const long long pos = a.positions ? at : (long long)a.first_position + (long long)max(n_sel, 0) * a.B + row;
+        if (pos < 0 || pos >= a.rope_positions) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); return; }
+        if (turns) {
+            const float4* cs = reinterpret_cast<const float4*>(a.rope + (size_t)pos * (a.d / 2) + 8 * c);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) t4[w] = __ldg(cs + w);
+            for (int w = 0; w < 4; ++w) t4[w] = __ldg(cs + w);
+        }
     }
+    __nv_bfloat16* page = nullptr;
+    if (a.pages) {
+        const int b = blocks + row / a.B;
+        const int pg = b < a.max_bps ? a.tables[(size_t)(a.session_first + s) * a.max_bps + b] : -1;
+        if (pg >= 0 && pg < a.max_blocks) page = a.pages + (size_t)pg * a.page_elems + (size_t)(row % a.B) * a.d;
+        else ok = false;
+    }
+    if (!ok) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
     const size_t tail_row = (size_t)s * a.tail_cap + row, tile = (size_t)a.B * a.d;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
@@ -218,10 +232,8 @@ append_tokens_kernel(const __grid_constant__ AppendTokensArgs a) {
     }
 }
 
-cudaError_t launch_append_tokens(const kvmem_pool& p, AppendTokensArgs a, cudaStream_t st) {
-    constexpr int PER = 4;
-    a.chunks = p.geo.d / 16;
-    a.n_vec = a.L * (a.Hq + 2 * a.G);
+template <int PER>
+static cudaError_t append_tokens(AppendTokensArgs a, cudaStream_t st) {
     a.groups = (a.n_vec + PER - 1) / PER;
     // whole sessions per launch, as far as their threads are numbered in 32 bits (the caller keeps one session below that)
     const long long per_session = (long long)a.M * a.chunks * a.groups;
@@ -229,10 +241,18 @@ cudaError_t launch_append_tokens(const kvmem_pool& p, AppendTokensArgs a, cudaSt
     for (int s0 = 0; s0 < all; s0 += most) {
         a.s0 = s0;
         a.ns = std::min(all, s0 + most);
-        const cudaError_t e = launch_pdl(append_tokens_kernel<PER>, dim3((unsigned)(((a.ns - s0) * per_session + 255) / 256)), dim3(256), 0, st, a);
+        const long long blocks = ((a.ns - s0) * per_session + kAppendThreads - 1) / kAppendThreads;
+        const cudaError_t e = launch_pdl(append_tokens_kernel<PER>, dim3((unsigned)blocks), dim3(kAppendThreads), 0, st, a);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
+}
+
+cudaError_t launch_append_tokens(const kvmem_pool& p, AppendTokensArgs a, cudaStream_t st) {
+    a.chunks = p.geo.d / 16;
+    a.n_vec = a.L * (a.Hq + 2 * a.G);
+    const bool few = (long long)a.ns * a.M <= kTokensFew / ((long long)a.n_vec * a.chunks);
+    return few ? append_tokens<1>(a, st) : append_tokens<3>(a, st);
 }
 
 bool append_tokens_fits(const kvmem_pool_config_t& c, int n_q_tokens) {

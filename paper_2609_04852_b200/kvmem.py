@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -43,16 +44,13 @@ class RopeStruct(C.Structure):
                [(n, C.c_float) for n in ("factor", "original_positions", "turns_fast", "turns_slow")]
 
 
-class RowsStruct(C.Structure):
-    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("session_stride", "token_stride", "layer_stride", "head_stride")]
-
-
 class SelectParams(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("budget_blocks", "max_view_tokens", "mandatory_tokens",
                                           "n_sink_blocks", "n_recent_blocks")]
 
 
 _lib = None
+_BF16, _I32 = torch.bfloat16, torch.int32
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
@@ -69,7 +67,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     L = C.CDLL(path)
     vp, i32, sz, f32 = C.c_void_p, C.c_int32, C.c_size_t, C.c_float
     cfgp, prmp, tailp = C.POINTER(PoolConfig), C.POINTER(SelectParams), C.POINTER(TailStruct)
-    ropep, rowsp, i64 = C.POINTER(RopeStruct), C.POINTER(RowsStruct), C.c_int64
+    ropep, i64 = C.POINTER(RopeStruct), C.c_int64
     sig = {
         "kvmem_pool_bytes": (sz, [cfgp]),
         "kvmem_budget_blocks": (i32, [prmp, i32, i32]),
@@ -128,7 +126,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "kvmem_rope_apply": (C.c_int, [vp, vp, i64, i64, i32, vp, i64, i64, i32, i64, i32, vp, i32, f32, vp]),
         "kvmem_reserve_blocks": (C.c_int, [vp, i32, i32, C.POINTER(i32), vp]),
         "kvmem_session_reserved": (i32, [vp, i32]),
-        "kvmem_append_tokens": (C.c_int, [vp, i32, i32, i32, vp, rowsp, rowsp, rowsp, vp, vp, i32, f32, tailp, vp, i32, vp]),
+        "kvmem_append_tokens": (C.c_int, [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, i32, vp]),
         "kvmem_commit_blocks": (C.c_int, [vp, i32, i32, C.POINTER(i32), tailp, vp]),
         "kvmem_prefill_workspace_bytes": (sz, [cfgp, i32, i32]),
         "kvmem_view_prefill_attend": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i32, vp, tailp, f32, vp, vp, vp, sz, vp]),
@@ -191,13 +189,18 @@ def _place(name: str, t: torch.Tensor, dtype, shape: tuple, device: int) -> int:
     return t.data_ptr()
 
 
-def _rows(name: str, t: torch.Tensor, shape: tuple, device: int) -> RowsStruct:
+# kvmem_rows_t and kvmem_tail_t as the append call takes them: packed into a buffer that the pool keeps (building ctypes structures takes
+# longer than the call)
+_ROWS, _TAIL = struct.Struct("P4q"), struct.Struct("PPiP")
+
+
+def _rows(name: str, t: torch.Tensor, shape: tuple, device: int, buf, at: int) -> None:
     """Rows [n_sessions][n_tokens][L][heads][d] of any strides but the last: a slice of a packed projection, read where it lies."""
-    if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != device or t.stride(4) != 1:
+    st = t.stride()
+    if t.dtype is not _BF16 or t.shape != shape or t.get_device() != device or st[4] != 1:
         raise ValueError(f"{name}: expected a bf16 tensor {tuple(shape)} on cuda:{device} with contiguous heads, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
-    # (the stride of an axis of length 1 means nothing)
-    return RowsStruct(t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 else 0 for i in range(4)))
+                         f"{tuple(t.shape)} on {t.device} with strides {st}")
+    _ROWS.pack_into(buf, at, t.data_ptr(), *st[:4])
 
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -310,6 +313,8 @@ class Pool:
         self._decode_pinned = False                                    # a captured graph or another stream may still write it
         self._decode_kept: List[torch.Tensor] = []                     # smaller ones of which that holds
         self._decode_need: Dict[tuple, int] = {}
+        self._append_buf = C.create_string_buffer(3 * _ROWS.size + _TAIL.size)         # rows of k, v, q and the tail of an append
+        self._append_at = C.addressof(self._append_buf)
 
     # ---- lifetime
     def close(self) -> None:
@@ -636,20 +641,23 @@ class Pool:
                    amplitude: float = 1.0, x_order: str = "model", out_order: str = "pool") -> torch.Tensor:
         """x bf16 [n_rows][n_vec][head_dim] (rows and vectors strided as they lie), positions int32 [n_rows] -> rotated vectors,
         "model" or "pool" order of the dims on either side; out may be x if the orders are the same."""
-        d = self.cfg.head_dim
+        d, dev = self._dims[3], self._index
+        shape = x.shape
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        for name, t in (("x", x), ("out", out)):
-            if t.dim() != 3 or t.shape != x.shape or t.shape[2] != d or t.dtype is not torch.bfloat16 or t.get_device() != self._index or t.stride(2) != 1:
-                raise ValueError(f"{name}: expected a bf16 tensor [n_rows][n_vec][{d}] on cuda:{self._index} with contiguous vectors, got "
-                                 f"{t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
-        n_rows, n_vec = x.shape[0], x.shape[1]
-        pp = _place("positions", positions, torch.int32, (n_rows,), self._index)
+            out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        xs, ys = x.stride(), out.stride()
+        if (len(shape) != 3 or shape[2] != d or out.shape != shape or x.dtype is not _BF16 or out.dtype is not _BF16 or x.get_device() != dev or
+                out.get_device() != dev or xs[2] != 1 or ys[2] != 1):
+            raise ValueError(f"x, out: expected bf16 tensors [n_rows][n_vec][{d}] on cuda:{dev} with contiguous vectors, got {x.dtype} "
+                             f"{tuple(shape)} on {x.device} with strides {xs}, {out.dtype} {tuple(out.shape)} on {out.device} with strides {ys}")
+        n_rows, n_vec, _ = shape
+        pp = _place("positions", positions, _I32, (n_rows,), dev)
         xo, yo = _one_of("x_order", x_order, ORDERS), _one_of("out_order", out_order, ORDERS)
         if n_rows and n_vec:
-            one = lambda t, i: t.stride(i) if t.shape[i] > 1 else 0          # (the stride of an axis of length 1 means nothing)
-            _check(self.lib.kvmem_rope_apply(self.handle, x.data_ptr(), one(x, 0), one(x, 1), xo, out.data_ptr(), one(out, 0), one(out, 1), yo,
-                                             n_rows, n_vec, pp, int(inverse), amplitude, self._raw_stream()))
+            rc = self.lib.kvmem_rope_apply(self.handle, x.data_ptr(), xs[0], xs[1], xo, out.data_ptr(), ys[0], ys[1], yo, n_rows, n_vec, pp,
+                                           int(inverse), amplitude, self._raw_stream())
+            if rc:
+                _check(rc)
         return out
 
     def reserve_blocks(self, session: int, n_blocks: int, phys_ids: Optional[Sequence[int]] = None) -> None:
@@ -667,10 +675,11 @@ class Pool:
 
     def _tail_struct(self, tail: Tail, ns: int) -> TailStruct:
         L, _, G, d = self._dims
-        cap = tail.k.shape[1] if tail.k.dim() == 5 else -1
+        tk, dev = tail.k, self._index
+        cap = tk.shape[1] if tk.dim() == 5 else -1
         shape = (ns, cap, L, G, d)
-        return TailStruct(_place("tail.k", tail.k, torch.bfloat16, shape, self._index), _place("tail.v", tail.v, torch.bfloat16, shape, self._index),
-                          cap, _place("tail.n_tokens", tail.n_tokens, torch.int32, (ns,), self._index))
+        return TailStruct(_place("tail.k", tk, _BF16, shape, dev), _place("tail.v", tail.v, _BF16, shape, dev), cap,
+                          _place("tail.n_tokens", tail.n_tokens, _I32, (ns,), dev))
 
     def append_tokens(self, k: torch.Tensor, v: torch.Tensor, tail: Tail, q: Optional[torch.Tensor] = None,
                       q_out: Optional[torch.Tensor] = None, n_new: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
@@ -681,21 +690,30 @@ class Pool:
         raw keys and values to the reserved pages as well.  Positions are positions int32 [n_sessions][M], or first_position +
         n_sel * block_tokens + the tail's row."""
         L, H, G, d = self._dims
-        dev, i32 = self._index, torch.int32
-        if k.dim() != 5:
+        dev = self._index
+        shape = k.shape
+        if len(shape) != 5:
             raise ValueError("k: expected [n_sessions][n_new_tokens][L][G][d]")
-        ns, M = k.shape[0], k.shape[1]
-        kr, vr = _rows("k", k, (ns, M, L, G, d), dev), _rows("v", v, (ns, M, L, G, d), dev)
-        qr, qo = None, None
+        ns, M, _, _, _ = shape
+        kv, qs, per_session = (ns, M, L, G, d), (ns, M, L, H, d), (ns,)
+        buf, at, size = self._append_buf, self._append_at, _ROWS.size
+        _rows("k", k, kv, dev, buf, 0)
+        _rows("v", v, kv, dev, buf, size)
         if q is not None:
-            qr = _rows("q", q, (ns, M, L, H, d), dev)
-        if q_out is not None:
-            qo = _place("q_out", q_out, torch.bfloat16, (ns, M, L, H, d), dev)
-        nn = None if n_new is None else _place("n_new", n_new, i32, (ns,), dev)
-        pp = None if positions is None else _place("positions", positions, i32, (ns, M), dev)
-        np_ = None if n_sel is None else _place("n_sel", n_sel, i32, (ns,), dev)
-        _check(self.lib.kvmem_append_tokens(self.handle, session_first, ns, M, nn, qr, kr, vr, pp, np_, first_position, q_amplitude,
-                                            self._tail_struct(tail, ns), qo, int(pages), self._raw_stream()))
+            _rows("q", q, qs, dev, buf, 2 * size)
+        tk = tail.k
+        cap = tk.shape[1] if tk.dim() == 5 else -1
+        ts = (ns, cap, L, G, d)
+        _TAIL.pack_into(buf, 3 * size, _place("tail.k", tk, _BF16, ts, dev), _place("tail.v", tail.v, _BF16, ts, dev), cap,
+                        _place("tail.n_tokens", tail.n_tokens, _I32, per_session, dev))
+        qo = None if q_out is None else _place("q_out", q_out, _BF16, qs, dev)
+        nn = None if n_new is None else _place("n_new", n_new, _I32, per_session, dev)
+        pp = None if positions is None else _place("positions", positions, _I32, (ns, M), dev)
+        np_ = None if n_sel is None else _place("n_sel", n_sel, _I32, per_session, dev)
+        rc = self.lib.kvmem_append_tokens(self.handle, session_first, ns, M, nn, None if q is None else at + 2 * size, at, at + size, pp, np_,
+                                          first_position, q_amplitude, at + 3 * size, qo, int(pages), self._raw_stream())
+        if rc:
+            _check(rc)
 
     def commit_blocks(self, n_blocks: Sequence[int], tail: Optional[Tail] = None, session_first: int = 0) -> None:
         """The first n_blocks[s] reserved blocks of each session become part of it, with their index rows; the tail's rows behind

@@ -754,13 +754,12 @@ int kvmem_commit_blocks(kvmem_pool_t* pool, int32_t session_first, int32_t n_ses
 
 /* Attention of a prompt chunk over view and tail: kvmem_view_tree_attend for a chain (token i sees the view, the committed tail
  * tokens and the chunk's tokens 0 .. i) of any length.  Same arguments (tail NULL: the view alone), definitions, guarantees and
- * error values, and the same bits from run to run; n_q_tokens has no limit of its own, and the query heads that share a KV head are at
- * most 128.
- *   workspace  DEVICE, kvmem_prefill_workspace_bytes(), 256-byte aligned (about 40 MB whatever the call); calls that may overlap on
+ * error values, and the same bits from run to run.  Chunks of up to 64 tokens are that call, with its kernel, workspace and limits.
+ * Longer ones: 4 head_dim flops per query row and visible token on the tensor cores; at most 128 query heads may share a KV head;
+ *   workspace  DEVICE, kvmem_prefill_workspace_bytes(), 256-byte aligned (about 160 MB whatever the call); calls that may overlap on
  *              the GPU need one each
- * A call is limited to 2^30 tiles, counted from the capacities: one for each 128 tokens of view and tail, either rounded up, and 2 more,
- * for every two row tiles of floor(128 / (H/G)) tokens of every KV head, layer and session (KVMEM_E_UNSUPPORTED).
- * Arithmetic bound: 4 d flops per query row and visible token on the tensor cores. */
+ * A call is limited to 2^30 tiles, counted from the capacities: one for each 128 tokens of view and tail, either rounded up, and 4 more,
+ * for every two row tiles of floor(128 / (H/G)) tokens of every KV head, layer and session (KVMEM_E_UNSUPPORTED). */
 size_t kvmem_prefill_workspace_bytes(const kvmem_pool_config_t* cfg /*HOST*/, int32_t n_sessions, int32_t n_q_tokens);
 int kvmem_view_prefill_attend(kvmem_pool_t* pool, int32_t n_sessions, const void* q /*DEVICE*/, int32_t n_q_tokens,
                               const int32_t* n_q /*DEVICE, may be NULL*/, const void* view_k /*DEVICE*/, const void* view_v /*DEVICE*/,

@@ -1586,9 +1586,16 @@ static int prefill_sizes(const kvmem_pool_config_t& c, int32_t n_sessions, int32
     return KVMEM_OK;
 }
 
+// A chunk of up to 64 tokens is a chain of drafted ones: the decode kernel, which shares a tile's two slots out between tokens where rows
+// are few (32 query heads on 8 KV heads, 1 / 33 / 64 tokens: 12 / 18 / 20 us instead of 24 / 27 / 29 at 2,048, 29 / 47 / 50 instead of
+// 52 / 62 / 61 at 32,768, 85 / 133 / 150 instead of 125 / 136 / 165 at 131,072; 64 heads on 8, 64 tokens: 25 and 29, 82 and 83, 300 and
+// 310).
+static bool chunk_is_chain(int32_t n_q_tokens) { return n_q_tokens >= 1 && n_q_tokens <= kMaxDrafted; }
+
 size_t kvmem_prefill_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t n_q_tokens) {
     const char* why = "";
     if (!cfg || !config_valid(*cfg, &why)) { set_error("invalid arguments to kvmem_prefill_workspace_bytes"); return 0; }
+    if (chunk_is_chain(n_q_tokens)) return tree_bytes(cfg, n_sessions, n_q_tokens, 0, "kvmem_prefill_workspace_bytes");
     if (prefill_sizes(*cfg, n_sessions, n_q_tokens, 0, 0) != KVMEM_OK) return 0;
     return prefill_workspace_bytes(*cfg);
 }
@@ -1599,6 +1606,9 @@ int kvmem_view_prefill_attend(kvmem_pool_t* p, int32_t n_sessions, const void* q
                               void* stream) {
     const char* who = "kvmem_view_prefill_attend";
     if (!pool_live(p)) return KVMEM_E_STATE;
+    if (chunk_is_chain(n_q_tokens))
+        return kvmem_view_tree_attend(p, n_sessions, q, n_q_tokens, n_q, nullptr, view_k, view_v, view_cap_tokens, n_sel, tail, scale, out, lse, workspace,
+                                      workspace_bytes, stream);
     const Geometry& g = p->geo;
     if (view_cap_tokens < g.B || view_cap_tokens % g.B != 0) { set_error("view_cap_tokens must be a positive multiple of block_tokens"); return KVMEM_E_INVALID; }
     int rc = KVMEM_OK;

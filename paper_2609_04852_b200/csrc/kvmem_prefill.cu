@@ -63,14 +63,16 @@ constexpr uint32_t kPreIdescO = kPreIdescS | (1u << 16);                        
 constexpr uint32_t kPreVStep = (uint32_t)kPreHalf >> 4;       // leading offset of V's descriptor: from dims 0..63 to 64..127
 constexpr int kPreMostUnits = 1 << 30;
 
-struct PreRecord { int s, lg, rg, flags; };      // flags: 1 the item's last share, 2 values that are not finite were cleared; s < 0: none
+struct PreRecord { int s, lg, rg, last; };       // an item, and the part its last share lies in; s < 0: none
 
 struct PreWork {
     PrefillArgs a;
     int tpt;                                     // tokens per row tile
+    int log_group;                               // log2 of the tokens of a group, where they are a power of two; else -1
     float* part_o;                               // [2 parts][slot][dims / 4][128 rows][4]
     float2* part_ml;                             // [2 parts][256]: (reference, sum of weights), log2 domain
     PreRecord* rec;                              // [2 parts]: what shares 2c (begun in an earlier part) and 2c + 1 (goes on in the next) hold
+    int* nf;                                     // [2 parts]: whether values that are not finite were cleared
     int* n_parts;                                // parts of the line in all
 };
 
@@ -116,16 +118,26 @@ __device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t step, uint32_
     return sum;
 }
 
+// the same where step is 2^log: without a division
+__device__ __forceinline__ uint32_t floor_sum_pow2(uint32_t n, int log, uint32_t from) {
+    constexpr int m = 7;                                                // log2 of 128
+    if (log >= m) return ((n * (n - 1) / 2) << (log - m)) + n * (from >> m);
+    const int k = m - log;                                              // floor((2^log i + from) / 128) = floor((i + from / 2^log) / 2^k)
+    auto upto = [&](uint32_t x) { const uint32_t q = x >> k; return ((q * (q - 1) / 2) << k) + q * (x - (q << k)); };       // over i < x of floor(i / 2^k)
+    return upto(n + (from >> log)) - upto(from >> log);
+}
+
 // units of the row groups before group rg of a KV head (rg < groups), and of a whole KV head.  An item without a tile (no view, no
 // tail) has one unit beside its lead: somebody has to write its rows.
-__device__ __forceinline__ int pre_before(const PrefillArgs& a, const PreSpan& sp, int tpt, int rg) {
-    if (!a.tail_k) return rg * (max(sp.view_tiles, 1) + kPreLead);
-    return rg * (sp.view_tiles + kPreLead) + (int)floor_sum(rg, 2 * tpt, sp.n_tail + 2 * tpt + kPreTile - 1);
+__device__ __forceinline__ int pre_before(const PreWork& w, const PreSpan& sp, int rg) {
+    if (!w.a.tail_k) return rg * (max(sp.view_tiles, 1) + kPreLead);
+    const uint32_t from = (uint32_t)(sp.n_tail + 2 * w.tpt + kPreTile - 1);
+    return rg * (sp.view_tiles + kPreLead) + (int)(w.log_group >= 0 ? floor_sum_pow2(rg, w.log_group, from) : floor_sum(rg, 2 * w.tpt, from));
 }
 __device__ __forceinline__ int pre_tiles(const PrefillArgs& a, const PreSpan& sp, int tpt, int rg) { return sp.view_tiles + pre_tail_tiles(a, sp, tpt, rg); }
-__device__ __forceinline__ int pre_head(const PrefillArgs& a, const PreSpan& sp, int tpt) {
+__device__ __forceinline__ int pre_head(const PreWork& w, const PreSpan& sp) {
     if (sp.groups == 0) return 0;
-    return pre_before(a, sp, tpt, sp.groups - 1) + max(pre_tiles(a, sp, tpt, sp.groups - 1), 1) + kPreLead;
+    return pre_before(w, sp, sp.groups - 1) + max(pre_tiles(w.a, sp, w.tpt, sp.groups - 1), 1) + kPreLead;
 }
 
 // where a part of the line begins and ends, and the item at its beginning: its first unit, session, KV head, row group
@@ -140,6 +152,7 @@ struct PreWalk {
     PreSpan sp;
     int t0, t1, tiles;              // the share: tiles [t0, t1) of the item's `tiles` (0: nothing to see)
     int cs, clg, crg, m0, rows2;    // its item; first token; whether the second row tile has any token
+    int last;                       // the item's last unit
     __device__ __forceinline__ bool next(const PreWork& w, int LG) {
         const PrefillArgs& a = w.a;
         while (true) {
@@ -154,7 +167,7 @@ struct PreWalk {
             const int some = max(tiles, 1), first = from + kPreLead, item_end = first + some;
             t0 = max(pos - first, 0);
             t1 = min(some, end - first);
-            cs = s; clg = lg; crg = rg;
+            cs = s; clg = lg; crg = rg; last = item_end - 1;
             m0 = rg * 2 * w.tpt;
             rows2 = sp.n_q - m0 > w.tpt;
             n_view = sp.n_view; n_tail = sp.n_tail; n_q = sp.n_q; view_tiles = sp.view_tiles;
@@ -179,7 +192,7 @@ struct PreWalk {
 struct PreShared {
     uint64_t full[kPreRing], empty[kPreRing], q_full, q_empty, s_full[2], p_full[2][2], h_full[2], o_full[2], o_empty[2], drained;
     PrePart parts[kPreParts];
-    int n_parts, n_cta;                       // the CTA's; CTAs that share the line
+    int n_parts, n_cta, total;                // the CTA's; CTAs that share the line, its units
     uint32_t tmem;
     int not_finite[2];                        // by the parity of the share: its number + 1, where values were cleared
 };
@@ -241,11 +254,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     {
         // the CTA's parts of the line, and the item each starts in: a warp a part, each counting the line for itself
         const PreSpan first = lane < a.ns ? pre_span(a, tpt, lane, blockIdx.x == 0 && warp == 0) : PreSpan{};
-        const int first_head = pre_head(a, first, tpt);
+        const int first_head = pre_head(w, first);
         int sum = first_head, held = first.groups ? pre_tiles(a, first, tpt, first.groups - 1) : 0;
         for (int s = lane + 32; s < a.ns; s += 32) {
             const PreSpan sp = pre_span(a, tpt, s, blockIdx.x == 0 && warp == 0);
-            sum += pre_head(a, sp, tpt);
+            sum += pre_head(w, sp);
             held += sp.groups ? pre_tiles(a, sp, tpt, sp.groups - 1) : 0;
         }
         const int total = __reduce_add_sync(0xffffffffu, sum) * LG, n = min((int)gridDim.x, total);
@@ -253,16 +266,18 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         int sweeps = (int)min((unsigned)kPreParts, (tiles + kPreBudget - 1) / kPreBudget);
         sweeps = max(1, min(sweeps, n ? total / (n * kPrePartUnits) : 1));
         const int all = n * sweeps, mine_n = (int)blockIdx.x < n ? sweeps : 0;
+        // parts begin at floor(total part / all): in 32 bits, all being at most kSMs kPreParts
+        const unsigned each = all ? (unsigned)total / (unsigned)all : 0u, over = (unsigned)total - each * (unsigned)all;
         for (int b = warp; b < mine_n; b += kPreThreads / 32) {
             const int part = b * n + (int)blockIdx.x;
-            const int begin = (int)((unsigned long long)total * part / all), end = (int)((unsigned long long)total * (part + 1) / all);
+            const int begin = (int)(each * part + over * part / (unsigned)all), end = (int)(each * (part + 1) + over * (part + 1) / (unsigned)all);
             int before = 0;
             for (int s0 = 0; s0 < a.ns; s0 += 32) {
                 const int s = s0 + lane;
                 PreSpan sp{};
                 int head = 0;
                 if (s0 == 0) { sp = first; head = first_head; }
-                else if (s < a.ns) { sp = pre_span(a, tpt, s, false); head = pre_head(a, sp, tpt); }
+                else if (s < a.ns) { sp = pre_span(a, tpt, s, false); head = pre_head(w, sp); }
                 const int mine = head * LG;
                 int incl = mine;
                 if (a.ns > 1) {
@@ -284,7 +299,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     const int lg = (begin - lo_s) / head_s, at = begin - lo_s - lg * head_s;
                     int rg = 0, units = 0;
                     for (int span = sp.groups; span > 0;) {
-                        const int step = (span + 31) / 32, try_rg = rg + lane * step, u = lane * step < span ? pre_before(a, sp, tpt, try_rg) : 0;
+                        const int step = (span + 31) / 32, try_rg = rg + lane * step, u = lane * step < span ? pre_before(w, sp, try_rg) : 0;
                         const int k = 31 - __clz(__ballot_sync(0xffffffffu, lane * step < span && u <= at));
                         units = __shfl_sync(0xffffffffu, u, k);
                         rg += k * step;
@@ -303,6 +318,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (tid == 0) {
             sh.n_parts = mine_n;
             sh.n_cta = n;
+            sh.total = total;
             if (blockIdx.x == 0) *w.n_parts = all;
         }
     }
@@ -680,8 +696,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 }
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&sh.o_empty[x]);
-                if (!whole && x == 0 && tid == 0)
-                    w.rec[share] = PreRecord{walk.cs, walk.clg, walk.crg, (walk.t1 == walk.tiles ? 1 : 0) | (nf ? 2 : 0)};
+                if (!whole && tid == 0) {
+                    const int all = n_cta * sh.n_parts;
+                    w.rec[share] = PreRecord{walk.cs, walk.clg, walk.crg, (int)(((unsigned long long)(walk.last + 1) * all - 1) / sh.total)};
+                    w.nf[share] = nf;
+                }
             }
             tiles += units;
             ++seg;
@@ -696,80 +715,92 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     }
 }
 
-// Joins the shares of an item that cuts of the line fall into, in line order.  Block c - 1 of the grid's first axis has the item whose
-// first cut is the start of part c, if there is one; the second axis is the slot.  A warp has 32 rows, a lane each, and 16 dims: its
-// reads are whole lines, and the next share's are in flight while one is added.
-constexpr int kPreMergeThreads = 1024;
-__global__ void __launch_bounds__(kPreMergeThreads)
+// Joins the shares of the items that cuts of the line fall into, in line order: for every part c, the item whose first cut is the part's
+// start, if there is one.  The grid's first axis goes over the parts, the second is the slot and 32 of the dims.  A warp has 32 rows, a
+// lane each, and 16 dims: its reads are whole lines.  Bound by latency (a round of dependent reads costs some 0.6 us): two shares
+// are requested together, and blocks go on to the next part rather than be many and mostly empty (three ragged sessions: 221
+// us; with a block a part 229).
+constexpr int kPreMergeThreads = 256, kPreMergeBatch = 2;
+__global__ void __launch_bounds__(kPreMergeThreads, 4)
 prefill_merge_kernel(const __grid_constant__ PreWork w) {
     pdl_wait();
     pdl_trigger();
     const PrefillArgs& a = w.a;
-    const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, x = blockIdx.y;
-    const int n_parts = *w.n_parts;
-    if (c >= n_parts) return;
-    const PreRecord it = w.rec[2 * c], head = w.rec[2 * c - 1];
-    if (it.s < 0 || head.s != it.s || head.lg != it.lg || head.rg != it.rg) return;
-    const int LG = a.L * a.G, m0 = it.rg * 2 * w.tpt, first_token = m0 + x * w.tpt;
-    const int n_q = a.n_q ? min(max(a.n_q[it.s], 0), a.M) : a.M;
-    const int rows = min(w.tpt, n_q - first_token) * a.r;               // live ones of this row tile
-    const int row = (warp & 3) * 32 + (threadIdx.x & 31), d0 = (warp >> 2) * 16;
-    if (row >= rows) return;
-    float top = -INFINITY, z = 0.0f;
-    float4 acc[4];
+    const int warp = threadIdx.x >> 5, x = blockIdx.y >> 2, n_parts = *w.n_parts;
+    for (int c = blockIdx.x + 1; c < n_parts; c += gridDim.x) {
+        const PreRecord it = w.rec[2 * c], head = w.rec[2 * c - 1];
+        if (it.s < 0 || head.s != it.s || head.lg != it.lg || head.rg != it.rg) continue;
+        const int LG = a.L * a.G, m0 = it.rg * 2 * w.tpt, first_token = m0 + x * w.tpt, shares = it.last - c + 2;
+        const int n_q = a.n_q ? min(max(a.n_q[it.s], 0), a.M) : a.M;
+        const int rows = min(w.tpt, n_q - first_token) * a.r;               // live ones of this row tile
+        const int row = (warp & 3) * 32 + (threadIdx.x & 31), d0 = (blockIdx.y & 3) * 32 + (warp >> 2) * 16;
+        if (row >= rows) continue;
+        auto share = [&](int i) { return i == 0 ? 2 * c - 1 : 2 * (c - 1 + i); };
+        float top = -INFINITY, z = 0.0f;
+        float4 acc[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    int flags = 0;
-    for (int i = c - 1; i < n_parts; ++i) {
-        const int share = i < c ? 2 * c - 1 : 2 * i;
-        const PreRecord r = w.rec[share];
-        if (i > c && (r.s != it.s || r.lg != it.lg || r.rg != it.rg)) break;
-        flags |= r.flags;
-        const float2 ml = w.part_ml[(size_t)share * 2 * kPreRows + x * kPreRows + row];
-        const float4* po = reinterpret_cast<const float4*>(w.part_o) + (((size_t)share * 2 + x) * (kPreD / 4) + d0 / 4) * kPreRows + row;
-        float4 v[4];
+        for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        int nf = 0;
+        for (int i0 = 0; i0 < shares; i0 += kPreMergeBatch) {
+            float2 ml[kPreMergeBatch];
+            float4 v[kPreMergeBatch][4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = po[(size_t)k * kPreRows];
-        if (ml.x > -INFINITY || ml.y != 0.0f) {                        // a share without a visible token holds no sums
-            const float to = fmaxf(top, ml.x), back = top > -INFINITY ? t5::ex2(top - to) : (z == 0.0f ? 0.0f : 1.0f), f = t5::ex2(ml.x - to);
-            z = z * back + f * ml.y;
+            for (int i = 0; i < kPreMergeBatch; ++i) {
+                ml[i] = make_float2(-INFINITY, 0.0f);
+                if (i0 + i < shares) {
+                    ml[i] = w.part_ml[(size_t)share(i0 + i) * 2 * kPreRows + x * kPreRows + row];
+                    nf |= w.nf[share(i0 + i)];
+                    const float4* po = reinterpret_cast<const float4*>(w.part_o) + (((size_t)share(i0 + i) * 2 + x) * (kPreD / 4) + d0 / 4) * kPreRows + row;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                acc[k].x = acc[k].x * back + f * v[k].x; acc[k].y = acc[k].y * back + f * v[k].y;
-                acc[k].z = acc[k].z * back + f * v[k].z; acc[k].w = acc[k].w * back + f * v[k].w;
+                    for (int k = 0; k < 4; ++k) v[i][k] = po[(size_t)k * kPreRows];
+                }
             }
+            float to = top;
+#pragma unroll
+            for (int i = 0; i < kPreMergeBatch; ++i) to = fmaxf(to, ml[i].x);
+            const float back = top > -INFINITY ? t5::ex2(top - to) : 1.0f;            // (without a reference z and acc are 0, or NaN)
+            z *= back;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { acc[k].x *= back; acc[k].y *= back; acc[k].z *= back; acc[k].w *= back; }
+#pragma unroll
+            for (int i = 0; i < kPreMergeBatch; ++i)
+                if (ml[i].x > -INFINITY || ml[i].y != 0.0f) {                          // a share without a visible token holds no sums
+                    const float f = t5::ex2(ml[i].x - to);
+                    z += f * ml[i].y;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { acc[k].x += f * v[i][k].x; acc[k].y += f * v[i][k].y; acc[k].z += f * v[i][k].z; acc[k].w += f * v[i][k].w; }
+                }
             top = to;
         }
-        if (r.flags & 1) break;
-    }
-    const int token = first_token + row / a.r;
-    const bool none = z == 0.0f;
-    const float inv = none ? 0.0f : 1.0f / z;
-    float out[16];
+        const int token = first_token + row / a.r;
+        const bool none = z == 0.0f;
+        const float inv = none ? 0.0f : 1.0f / z;
+        float out[16];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        out[4 * k] = none ? 0.0f : acc[k].x * inv; out[4 * k + 1] = none ? 0.0f : acc[k].y * inv;
-        out[4 * k + 2] = none ? 0.0f : acc[k].z * inv; out[4 * k + 3] = none ? 0.0f : acc[k].w * inv;
-    }
-    if ((flags & 2) && !none) {
-        const int n_tail = min(max(a.n_tail[it.s], 0), a.tail_cap - n_q);
-        for (int tok = m0 + 1; tok <= token; ++tok) {
-            const __nv_bfloat16* vr = a.tail_v + (((size_t)it.s * a.tail_cap + n_tail + tok) * LG + it.lg) * kPreD + d0;
+        for (int k = 0; k < 4; ++k) {
+            out[4 * k] = none ? 0.0f : acc[k].x * inv; out[4 * k + 1] = none ? 0.0f : acc[k].y * inv;
+            out[4 * k + 2] = none ? 0.0f : acc[k].z * inv; out[4 * k + 3] = none ? 0.0f : acc[k].w * inv;
+        }
+        if (nf && !none) {
+            const int n_tail = min(max(a.n_tail[it.s], 0), a.tail_cap - n_q);
+            for (int tok = m0 + 1; tok <= token; ++tok) {
+                const __nv_bfloat16* vr = a.tail_v + (((size_t)it.s * a.tail_cap + n_tail + tok) * LG + it.lg) * kPreD + d0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float v = __bfloat162float(vr[i]);
-                if (!isfinite(v)) out[i] += v;
+                for (int i = 0; i < 16; ++i) {
+                    const float v = __bfloat162float(vr[i]);
+                    if (!isfinite(v)) out[i] += v;
+                }
             }
         }
-    }
-    const size_t orow = (((size_t)it.s * a.M + token) * a.L + it.lg / a.G) * a.H + (size_t)(it.lg % a.G) * a.r + row % a.r;
-    uint32_t pk[8];
+        const size_t orow = (((size_t)it.s * a.M + token) * a.L + it.lg / a.G) * a.H + (size_t)(it.lg % a.G) * a.r + row % a.r;
+        uint32_t pk[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pk[i] = ptx::pack_bf16x2(out[2 * i], out[2 * i + 1]);
-    uint4* dst = reinterpret_cast<uint4*>(a.out + orow * kPreD + d0);
-    dst[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-    dst[1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
-    if (d0 == 0) a.lse[orow] = none ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+        for (int i = 0; i < 8; ++i) pk[i] = ptx::pack_bf16x2(out[2 * i], out[2 * i + 1]);
+        uint4* dst = reinterpret_cast<uint4*>(a.out + orow * kPreD + d0);
+        dst[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+        dst[1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+        if (d0 == 0) a.lse[orow] = none ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+    }
 }
 
 static size_t plan_prefill(char* base, PreWork* w) {
@@ -779,6 +810,7 @@ static size_t plan_prefill(char* base, PreWork* w) {
     w->part_o = (float*)take(shares * 2 * kPreRows * kPreD * sizeof(float));
     w->part_ml = (float2*)take(shares * 2 * kPreRows * sizeof(float2));
     w->rec = (PreRecord*)take(shares * sizeof(PreRecord));
+    w->nf = (int*)take(shares * sizeof(int));
     w->n_parts = (int*)take(sizeof(int));
     return off;
 }
@@ -829,6 +861,9 @@ cudaError_t launch_prefill(const kvmem_pool& p, const PrefillArgs& a, void* work
     plan_prefill((char*)workspace, &w);
     w.a = a;
     w.tpt = kPreRows / a.r;
+    w.log_group = -1;
+    for (int i = 0; i <= 8; ++i)
+        if (2 * w.tpt == 1 << i) w.log_group = i;
     const int LG = a.L * a.G;
     CUtensorMap mq, mk, mv, mtk, mtv;
     bool made = pre_map(&mq, a.q, (cuuint64_t)a.L * a.H, (cuuint64_t)a.ns * a.M, (cuuint32_t)a.r, (cuuint32_t)w.tpt) &&
@@ -841,9 +876,11 @@ cudaError_t launch_prefill(const kvmem_pool& p, const PrefillArgs& a, void* work
     if (!made) return cudaErrorInvalidValue;
     const int grid = (int)std::min<long long>(std::min(p.sm_count, kSMs), pre_most_units(p.cfg, a.ns, a.M, a.cap, a.tail_cap));
     cudaError_t e = launch_pdl(prefill_kernel, dim3((unsigned)grid), dim3(kPreThreads), kPreSmem, st, mq, mk, mv, mtk, mtv, w);
-    const long long parts = std::min<long long>(grid * (long long)kPreParts, pre_most_units(p.cfg, a.ns, a.M, a.cap, a.tail_cap));
+    // as many parts as the line can have
+    const long long units = pre_most_units(p.cfg, a.ns, a.M, a.cap, a.tail_cap);
+    const long long parts = std::min(units, grid * std::max(1ll, std::min<long long>(kPreParts, units / ((long long)grid * kPrePartUnits))));
     if (e != cudaSuccess || parts < 2) return e;
-    return launch_pdl(prefill_merge_kernel, dim3((unsigned)parts - 1, 2), dim3(kPreMergeThreads), 0, st, w);
+    return launch_pdl(prefill_merge_kernel, dim3((unsigned)std::min<long long>(parts - 1, grid), 8), dim3(kPreMergeThreads), 0, st, w);
 }
 
 }  // namespace kvmem

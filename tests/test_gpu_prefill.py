@@ -101,8 +101,12 @@ GEOMETRIES = [
     dict(M=257, H=2, G=2, lens=(2,), tails=(127,)),
     dict(M=333, H=10, G=2, B=16, lens=(9,), tails=(1,)),               # five heads on a KV head, 16-token blocks: 125 rows of 128
     dict(M=70, H=21, G=3, B=48, lens=(4,), tails=(60,)),               # seven heads on a KV head
-    dict(M=5, H=128, G=1, lens=(2,), tails=(3,)),                      # 128 heads on a KV head: a token fills a row tile
-    dict(M=7, H=71, G=1, lens=(2,), tails=(3,)),                       # 71: a token a row tile, 57 rows idle
+    dict(M=5, H=128, G=1, lens=(2,), tails=(3,)),                      # 128 heads on a KV head, few tokens
+    dict(M=70, H=128, G=1, lens=(2,), tails=(3,)),                     # a token fills a row tile
+    dict(M=67, H=71, G=1, lens=(2,), tails=(3,)),                      # 71: a token a row tile, 57 rows idle
+    dict(M=66, H=3, G=3, lens=(1,), tails=(0,)),                       # one item a head, half of it idle
+    dict(M=66, lens=(0,), tails=None),                                 # nothing to see, in a long chunk
+    dict(ns=3, M=100, lens=(0, 2, 0), n_q=(100, 3, 100), tails=None),  # nothing or a view
     dict(M=90, H=66, G=2, lens=(1,), tails=(0,)),                      # 33: three tokens a row tile
     dict(ns=3, L=2, M=150, lens=(3, 0, 11), n_q=(150, 1, 77), tails=(5, 0, 130), B=32),    # ragged batch, one empty view
     dict(ns=4, M=90, lens=(1, 40, 2, 0), n_q=(0, 90, 3, 0), tails=(3, 64, 0, 0), B=16),    # sessions without a token

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <thread>
 
 #include "kvmem_internal.cuh"
 
@@ -115,6 +116,24 @@ static bool pages_are(const kvmem_pool* p, bool fp8, const char* who) {
 static int cuda_fail(const char* what, cudaError_t e) {
     set_error("%s: %s", what, cudaGetErrorString(e));
     return KVMEM_E_CUDA;
+}
+
+// f(begin, end) over [0, n), shared out over up to 16 host threads (a rotary table of 262,144 positions takes one of them 0.24 s); where no
+// thread is to be had, on this one
+template <typename F>
+static void on_threads(int n, const F& f) {
+    const int most = std::max(1, std::min({16, (int)std::thread::hardware_concurrency(), n / 256}));
+    std::thread t[16];
+    int started = 1;                       // pieces that have a thread; this one takes the first and what is left
+    try {
+        for (; started < most; ++started) {
+            const int a = (int)((int64_t)n * started / most), b = (int)((int64_t)n * (started + 1) / most);
+            t[started] = std::thread([&f, a, b] { f(a, b); });
+        }
+    } catch (...) {}
+    f(0, (int)((int64_t)n / most));
+    if (started < most) f((int)((int64_t)n * started / most), n);
+    for (int i = 1; i < started; ++i) t[i].join();
 }
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
@@ -233,15 +252,17 @@ int kvmem_pool_create(const kvmem_pool_config_t* cfg, void* storage, size_t byte
         const int half = cfg->head_dim / 2;
         std::vector<double> freq(half);
         for (int i = 0; i < half; ++i) freq[i] = pow((double)cfg->rope_theta, -2.0 * (double)i / (double)cfg->head_dim);
-        const int chunk = 4096;
-        std::vector<float2> rows((size_t)chunk * half);
+        const int chunk = 32768;
+        std::vector<float2> rows((size_t)std::min(chunk, cfg->rope_max_positions) * half);
         for (int p0 = 0; e == cudaSuccess && p0 < cfg->rope_max_positions; p0 += chunk) {
             const int n = std::min(chunk, cfg->rope_max_positions - p0);
-            for (int r = 0; r < n; ++r)
-                for (int i = 0; i < half; ++i) {
-                    const double ang = (double)(p0 + r) * freq[i];
-                    rows[(size_t)r * half + i] = make_float2((float)cos(ang), (float)sin(ang));
-                }
+            on_threads(n, [&](int r0, int r1) {
+                for (int r = r0; r < r1; ++r)
+                    for (int i = 0; i < half; ++i) {
+                        const double ang = (double)(p0 + r) * freq[i];
+                        rows[(size_t)r * half + i] = make_float2((float)cos(ang), (float)sin(ang));
+                    }
+            });
             e = cudaMemcpy(p->rope_dev + (size_t)p0 * half, rows.data(), (size_t)n * half * sizeof(float2), cudaMemcpyHostToDevice);
         }
     }
@@ -1423,9 +1444,13 @@ int kvmem_reserve_blocks(kvmem_pool_t* p, int32_t session, int32_t n_blocks, con
         set_error("session %d holds %lld blocks with the reserved ones; %d more exceed max_blocks_per_session = %d", session, (long long)have, n_blocks, p->cfg.max_blocks_per_session);
         return KVMEM_E_CAPACITY;
     }
-    std::vector<int32_t> ids(n_blocks);
-    const int rc = choose_pages(p, n_blocks, phys_ids, ids);
-    if (rc != KVMEM_OK) return rc;
+    std::vector<int32_t> ids;
+    try {
+        ids.resize(n_blocks);
+        const int rc = choose_pages(p, n_blocks, phys_ids, ids);
+        if (rc != KVMEM_OK) return rc;
+        reserved.reserve(reserved.size() + n_blocks);
+    } catch (const std::bad_alloc&) { set_error("host allocation failed"); return KVMEM_E_CAPACITY; }
     const cudaError_t e = cudaMemcpyAsync(p->tables + (size_t)session * p->cfg.max_blocks_per_session + have, ids.data(), (size_t)n_blocks * 4,
                                           cudaMemcpyHostToDevice, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail("block table upload", e);
@@ -1493,6 +1518,11 @@ int kvmem_append_tokens(kvmem_pool_t* p, int32_t session_first, int32_t n_sessio
             set_error("%s: null or misaligned rows, or a stride that is negative or no multiple of 8 elements", who);
             return KVMEM_E_INVALID;
         }
+    for (int i = 0; i < 3; ++i)
+        if (in[i] && (g.L - 1) * in[i]->layer_stride + ((i ? g.G : g.H) - 1) * in[i]->head_stride >= (1ll << 31)) {
+            set_error("%s: the layers and heads of a token lie more than 2^31 elements apart", who);
+            return KVMEM_E_UNSUPPORTED;
+        }
     if (!std::isfinite(q_amplitude) || q_amplitude < 0.0f) { set_error("q_amplitude must be finite and non-negative (0 selects 1)"); return KVMEM_E_INVALID; }
     const bool rope = p->cfg.rope_max_positions > 0;
     if (rope && !positions && (first_position < 0 || first_position >= p->cfg.rope_max_positions)) {
@@ -1513,7 +1543,7 @@ int kvmem_append_tokens(kvmem_pool_t* p, int32_t session_first, int32_t n_sessio
             }
     }
     AppendTokensArgs a{};
-    auto rows = [](const kvmem_rows_t* r) { return r ? TokenRows{(const __nv_bfloat16*)r->data, r->session_stride, r->token_stride, r->layer_stride, r->head_stride} : TokenRows{}; };
+    auto rows = [](const kvmem_rows_t* r) { return r ? TokenRows{(const __nv_bfloat16*)r->data, r->session_stride, r->token_stride, (int)r->layer_stride, (int)r->head_stride} : TokenRows{}; };
     a.q = rows(in[0]); a.k = rows(in[1]); a.v = rows(in[2]);
     a.q_out = (__nv_bfloat16*)q_out; a.tail_k = (__nv_bfloat16*)tail->k; a.tail_v = (__nv_bfloat16*)tail->v;
     a.tail_n = tail->n_tokens; a.n_new = n_new; a.positions = positions; a.n_sel = n_sel;
@@ -1543,6 +1573,10 @@ int kvmem_commit_blocks(kvmem_pool_t* p, int32_t session_first, int32_t n_sessio
         if ((size_t)n_blocks[i] > reserved) { set_error("session %d has %zu reserved blocks, %d are to be committed", session_first + i, reserved, n_blocks[i]); return KVMEM_E_STATE; }
     }
     const Geometry& g = p->geo;
+    try {
+        for (int i = 0; i < n_sessions; ++i)
+            if (n_blocks[i]) p->sess_pages[session_first + i].reserve(p->sess_pages[session_first + i].size() + n_blocks[i]);
+    } catch (const std::bad_alloc&) { set_error("host allocation failed"); return KVMEM_E_CAPACITY; }
     for (int i0 = 0; i0 < n_sessions;) {
         CommitArgs a{};
         int i = i0;

@@ -294,6 +294,21 @@ cudaError_t launch_evict(const kvmem_pool& p, const EvictArgs& a, void* workspac
 struct RopeFrequencies { double f[256]; };       // by value to the kernel: d / 2 of them
 cudaError_t launch_rope_table(const kvmem_pool& p, const RopeFrequencies& f, cudaStream_t st);
 
+// Division of numbers below 2^31 by one that the host knows, as a product: with l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1,
+// floor(n / d) = (floor(m n / 2^32) + n) / 2^l (Granlund and Montgomery, Division by Invariant Integers using Multiplication, 1994)
+struct Divisor {
+    uint32_t d, mul, shift;
+    Divisor() = default;
+    explicit Divisor(uint32_t by) : d(by), mul(0), shift(0) {
+        while ((1ull << shift) < by) ++shift;
+        mul = (uint32_t)((((1ull << shift) - by) << 32) / by + 1);
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(mul, n) + n) >> shift; }
+    __device__ __forceinline__ uint32_t rest(uint32_t n, uint32_t q) const { return n - q * d; }
+#endif
+};
+
 struct RopeApplyArgs {
     const __nv_bfloat16* x;
     __nv_bfloat16* y;
@@ -304,13 +319,14 @@ struct RopeApplyArgs {
     RopeForm form;
     int n_rows, n_vec, d, rope_positions, x_pool, y_pool;
     float sgn, amplitude;
-    int chunks, groups;                          // filled by the launcher
+    Divisor chunks, groups;                      // filled by the launcher
 };
 cudaError_t launch_rope_apply(const kvmem_pool& p, const RopeApplyArgs& a, long long n_rows, cudaStream_t st);
 
 struct TokenRows {
     const __nv_bfloat16* data;
-    long long session, token, layer, head;       // strides in elements
+    long long session, token;                    // strides in elements
+    int layer, head;                             // (inside a token's row: below 2^31)
 };
 struct AppendTokensArgs {
     TokenRows q, k, v;
@@ -325,7 +341,8 @@ struct AppendTokensArgs {
     RopeForm form;
     int ns, M, L, Hq, G, d, B, tail_cap, first_position, rope_positions, session_first, max_bps, max_blocks;   // Hq: 0 without queries
     float q_amplitude;
-    int chunks, groups, n_vec, s0;               // filled by the launcher
+    int n_vec, s0;                               // filled by the launcher
+    Divisor chunks, groups, tokens, per_layer, block;
 };
 cudaError_t launch_append_tokens(const kvmem_pool& p, AppendTokensArgs a, cudaStream_t st);
 bool append_tokens_fits(const kvmem_pool_config_t& c, int n_q_tokens);      // one session's threads in 32 bits

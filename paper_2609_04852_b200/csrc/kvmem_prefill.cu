@@ -49,9 +49,11 @@ constexpr int kPreRing = 4;                      // K and V tiles in turn
 constexpr int kPreStage = 4096;                  // bytes of a row warp's staging for stores
 constexpr int kPreThreads = 384;                 // eight row warps, TMA warp, MMA warp, two that only give registers away
 constexpr int kPreTmaWarp = 8, kPreMmaWarp = 9;
-// Registers a thread: the launch gives 168, the row warps take 216 and the others keep 64 (256 x 216 + 128 x 64 <= 384 x 168)
-#define PRE_ROW_REGS "216"
-#define PRE_OTHER_REGS "64"
+// Registers a thread: the launch gives 168, the row warps take 208 and the others keep 80.  (Without: a row's 128 logits do not fit, and a
+// spill is slow here, where shared memory leaves the L1 no room for it: 220 us instead of 206 for a chunk of 4,096 alone.)
+#define PRE_ROW_REGS "208"
+#define PRE_OTHER_REGS "80"
+static_assert(256 * 208 + 128 * 80 <= kPreThreads * 168, "the registers that the row warps take are those the others give");
 constexpr int kPreLead = 3;                      // units on the line for an item's start and end: what they cost a CTA, in tiles (1: 195 and 314 us
                                                  // instead of 170 and 234 for a chunk of 4,096 alone and three ragged sessions)
 constexpr float kPreLimit = 18446744073709551616.0f;   // 2^64: half a tile's weights may sum to this before their reference moves
@@ -333,142 +335,142 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
     // every role still reaches its end.
     bool ok = true;
-    if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 " PRE_OTHER_REGS ";");
-    if (warp == kPreTmaWarp) {
-        // ------------------------------------------------ TMA: one thread
-        if (t5::elect()) {
-            int n = 0, seg = 0;                                       // loads of the ring, shares so far
-            auto slot = [&]() {                                       // the next ring slot, free
-                const int st = n % RING;
-                if (ok && n >= RING) ok = ptx::mbar_wait(&sh.empty[st], (uint32_t)(((n / RING) & 1) ^ 1));
-                ++n;
-                return st;
-            };
-            while (ok && walk.next(w, LG)) {
-                const int units = walk.units();
-                if (units == 0) continue;
-                if (seg > 0) ok = ptx::mbar_wait(&sh.q_empty, (uint32_t)((seg - 1) & 1));
-                if (!ok) break;
-                const int l = walk.clg / a.G, g = walk.clg % a.G, tok0 = walk.cs * a.M + walk.m0;
-                ptx::mbar_expect_tx(&sh.q_full, (uint32_t)((walk.rows2 ? 2 : 1) * 2 * 128 * a.r * tpt));
-                for (int x = 0; x <= walk.rows2; ++x)
-                    for (int h = 0; h < 2; ++h)
-                        ptx::tma_load_3d(smem_q + x * kPreSlot + h * kPreHalf, &map_q, 64 * h, l * a.H + g * a.r, tok0 + x * tpt, &sh.q_full);
-                const int z_view = walk.cs * LG + walk.clg, row_tail = walk.cs * a.tail_cap;
-                for (int t = walk.t0; t < walk.t1 && ok; ++t) {
-                    const bool in_view = t < walk.view_tiles;
-                    const int c0 = (in_view ? t : t - walk.view_tiles) * kPreTile;
-                    for (int kv = 0; kv < 2; ++kv) {
-                        const int st = slot();
-                        if (!ok) { --n; break; }
-                        unsigned char* dst = ring + (size_t)st * kPreSlot;
-                        ptx::mbar_expect_tx(&sh.full[st], kPreSlot);
-                        for (int h = 0; h < 2; ++h) {
-                            if (in_view) ptx::tma_load_3d(dst + h * kPreHalf, kv ? &map_v : &map_k, 64 * h, c0, z_view, &sh.full[st]);
-                            else ptx::tma_load_3d(dst + h * kPreHalf, kv ? &map_tv : &map_tk, 64 * h, walk.clg, row_tail + c0, &sh.full[st]);
+    if (warp >= kPreTmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PRE_OTHER_REGS ";");
+        if (warp == kPreTmaWarp) {
+            // ------------------------------------------------ TMA: one thread
+            if (t5::elect()) {
+                int n = 0, seg = 0;                                       // loads of the ring, shares so far
+                auto slot = [&]() {                                       // the next ring slot, free
+                    const int st = n % RING;
+                    if (ok && n >= RING) ok = ptx::mbar_wait(&sh.empty[st], (uint32_t)(((n / RING) & 1) ^ 1));
+                    ++n;
+                    return st;
+                };
+                while (ok && walk.next(w, LG)) {
+                    const int units = walk.units();
+                    if (units == 0) continue;
+                    if (seg > 0) ok = ptx::mbar_wait(&sh.q_empty, (uint32_t)((seg - 1) & 1));
+                    if (!ok) break;
+                    const int l = walk.clg / a.G, g = walk.clg % a.G, tok0 = walk.cs * a.M + walk.m0;
+                    ptx::mbar_expect_tx(&sh.q_full, (uint32_t)((walk.rows2 ? 2 : 1) * 2 * 128 * a.r * tpt));
+                    for (int x = 0; x <= walk.rows2; ++x)
+                        for (int h = 0; h < 2; ++h)
+                            ptx::tma_load_3d(smem_q + x * kPreSlot + h * kPreHalf, &map_q, 64 * h, l * a.H + g * a.r, tok0 + x * tpt, &sh.q_full);
+                    const int z_view = walk.cs * LG + walk.clg, row_tail = walk.cs * a.tail_cap;
+                    for (int t = walk.t0; t < walk.t1 && ok; ++t) {
+                        const bool in_view = t < walk.view_tiles;
+                        const int c0 = (in_view ? t : t - walk.view_tiles) * kPreTile;
+                        for (int kv = 0; kv < 2; ++kv) {
+                            const int st = slot();
+                            if (!ok) { --n; break; }
+                            unsigned char* dst = ring + (size_t)st * kPreSlot;
+                            ptx::mbar_expect_tx(&sh.full[st], kPreSlot);
+                            for (int h = 0; h < 2; ++h) {
+                                if (in_view) ptx::tma_load_3d(dst + h * kPreHalf, kv ? &map_v : &map_k, 64 * h, c0, z_view, &sh.full[st]);
+                                else ptx::tma_load_3d(dst + h * kPreHalf, kv ? &map_tv : &map_tk, 64 * h, walk.clg, row_tail + c0, &sh.full[st]);
+                            }
                         }
                     }
+                    ++seg;
                 }
-                ++seg;
+                // the copies still in flight land before the CTA gives its shared memory back
+                for (int i = max(0, n - RING); i < n; ++i) ok = ptx::mbar_wait(&sh.full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
+                if (seg > 0) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)((seg - 1) & 1)) && ok;
+                if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
             }
-            // the copies still in flight land before the CTA gives its shared memory back
-            for (int i = max(0, n - RING); i < n; ++i) ok = ptx::mbar_wait(&sh.full[i % RING], (uint32_t)((i / RING) & 1)) && ok;
-            if (seg > 0) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)((seg - 1) & 1)) && ok;
-            if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
-        }
-    } else if (warp == kPreMmaWarp) {
-        // ------------------------------------------------ MMA: one thread
-        if (t5::elect()) {
-            const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
-            struct Place {                                            // ring slot and phase of the next key / value tile
-                int st;
-                uint32_t ph;
-                __device__ __forceinline__ void next() { st += 2; if (st >= RING) { st -= RING; ph ^= 1u; } }
-            } kp{0, 0u}, vp{1, 0u};
-            int seg = 0;
-            uint32_t p_ph0 = 0, p_ph1 = 0;                            // phases of the slots' weights
-            int out0 = 0, out1 = 0;                                   // shares whose sums a slot's rows have to take out
-            auto logits = [&](int x) {
-                if (!ok) return;
-                t5::fence_after();
-                const uint32_t al = q_lo + (uint32_t)x * (kPreSlot >> 4), bl = ring_lo + (uint32_t)kp.st * (kPreSlot >> 4);
+        } else if (warp == kPreMmaWarp) {
+            // ------------------------------------------------ MMA: one thread
+            if (t5::elect()) {
+                const uint32_t q_lo = t5::desc_lo(ptx::smem_u32(smem_q)), ring_lo = t5::desc_lo(ptx::smem_u32(ring));
+                struct Place {                                            // ring slot and phase of the next key / value tile
+                    int st;
+                    uint32_t ph;
+                    __device__ __forceinline__ void next() { st += 2; if (st >= RING) { st -= RING; ph ^= 1u; } }
+                } kp{0, 0u}, vp{1, 0u};
+                int seg = 0;
+                uint32_t p_ph0 = 0, p_ph1 = 0;                            // phases of the slots' weights
+                int out0 = 0, out1 = 0;                                   // shares whose sums a slot's rows have to take out
+                auto logits = [&](int x) {
+                    if (!ok) return;
+                    t5::fence_after();
+                    const uint32_t al = q_lo + (uint32_t)x * (kPreSlot >> 4), bl = ring_lo + (uint32_t)kp.st * (kPreSlot >> 4);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t o = (uint32_t)(i >> 2) * (kPreHalf >> 4) + (uint32_t)(i & 3) * 2u;
-                    t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kPreIdescS, i > 0 ? 1u : 0u);
-                }
-                t5::commit(&sh.s_full[x]);
-            };
-            auto half_product = [&](int x, int half, bool first) {
-                if (!ok) return;
-                t5::fence_after();
-                const uint32_t bl = (ring_lo + (uint32_t)vp.st * (kPreSlot >> 4)) | (kPreVStep << 16);
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t o = (uint32_t)(i >> 2) * (kPreHalf >> 4) + (uint32_t)(i & 3) * 2u;
+                        t5::mma_bf16(tmem + (uint32_t)x * 256u, t5::make_desc(al + o), t5::make_desc(bl + o), kPreIdescS, i > 0 ? 1u : 0u);
+                    }
+                    t5::commit(&sh.s_full[x]);
+                };
+                auto half_product = [&](int x, int half, bool first) {
+                    if (!ok) return;
+                    t5::fence_after();
+                    const uint32_t bl = (ring_lo + (uint32_t)vp.st * (kPreSlot >> 4)) | (kPreVStep << 16);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = half * 4 + i;
-                    t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)(k * 8),
-                                    t5::make_desc(bl + (uint32_t)k * (2048u >> 4)), kPreIdescO, !first || k > 0 ? 1u : 0u);
+                    for (int i = 0; i < 4; ++i) {
+                        const int k = half * 4 + i;
+                        t5::mma_bf16_ta(tmem + (uint32_t)x * 256u + 128u, tmem + (uint32_t)x * 256u + (uint32_t)(k * 8),
+                                        t5::make_desc(bl + (uint32_t)k * (2048u >> 4)), kPreIdescO, !first || k > 0 ? 1u : 0u);
+                    }
+                };
+                while (walk.next(w, LG)) {
+                    const int units = walk.units();
+                    if (units == 0) continue;
+                    const bool two = walk.rows2;
+                    if (ok) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)(seg & 1)) && ptx::mbar_wait(&sh.full[kp.st], kp.ph);
+                    logits(0);
+                    if (two) logits(1);
+                    if (ok) t5::commit(&sh.empty[kp.st]);
+                    if (ok && units == 1) t5::commit(&sh.q_empty);
+                    kp.next();
+                    for (int j = 0; j < units; ++j) {
+                        const bool more = j + 1 < units;
+                        if (ok) ok = ptx::mbar_wait(&sh.full[vp.st], vp.ph);
+                        // sums of the slots' last shares are out before new ones take their place (slot 1's too where it now rests: the flags of
+                        // cleared values are kept for two shares)
+                        if (j == 0) {
+                            if (ok && out0 > 0) ok = ptx::mbar_wait(&sh.o_empty[0], (uint32_t)((out0 - 1) & 1));
+                            if (ok && !two && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
+                        }
+                        if (ok) ok = ptx::mbar_wait(&sh.p_full[0][0], p_ph0);
+                        half_product(0, 0, j == 0);
+                        if (ok) t5::commit(&sh.h_full[0]);
+                        if (ok) ok = ptx::mbar_wait(&sh.p_full[0][1], p_ph0);
+                        half_product(0, 1, false);
+                        p_ph0 ^= 1u;
+                        if (ok && !more) t5::commit(&sh.o_full[0]);
+                        if (more) {
+                            if (ok) ok = ptx::mbar_wait(&sh.full[kp.st], kp.ph);
+                            logits(0);
+                        }
+                        if (two) {
+                            if (j == 0 && ok && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
+                            if (ok) ok = ptx::mbar_wait(&sh.p_full[1][0], p_ph1);
+                            half_product(1, 0, j == 0);
+                            if (ok) t5::commit(&sh.h_full[1]);
+                            if (ok) ok = ptx::mbar_wait(&sh.p_full[1][1], p_ph1);
+                            half_product(1, 1, false);
+                            p_ph1 ^= 1u;
+                            if (ok && !more) t5::commit(&sh.o_full[1]);
+                            if (more) logits(1);
+                        }
+                        if (ok) t5::commit(&sh.empty[vp.st]);
+                        vp.next();
+                        if (more) {
+                            if (ok) t5::commit(&sh.empty[kp.st]);
+                            if (ok && j + 2 == units) t5::commit(&sh.q_empty);
+                            kp.next();
+                        }
+                    }
+                    ++out0;
+                    if (two) ++out1;
+                    ++seg;
                 }
-            };
-            while (walk.next(w, LG)) {
-                const int units = walk.units();
-                if (units == 0) continue;
-                const bool two = walk.rows2;
-                if (ok) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)(seg & 1)) && ptx::mbar_wait(&sh.full[kp.st], kp.ph);
-                logits(0);
-                if (two) logits(1);
-                if (ok) t5::commit(&sh.empty[kp.st]);
-                if (ok && units == 1) t5::commit(&sh.q_empty);
-                kp.next();
-                for (int j = 0; j < units; ++j) {
-                    const bool more = j + 1 < units;
-                    if (ok) ok = ptx::mbar_wait(&sh.full[vp.st], vp.ph);
-                    // sums of the slots' last shares are out before new ones take their place (slot 1's too where it now rests: the flags of
-                    // cleared values are kept for two shares)
-                    if (j == 0) {
-                        if (ok && out0 > 0) ok = ptx::mbar_wait(&sh.o_empty[0], (uint32_t)((out0 - 1) & 1));
-                        if (ok && !two && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
-                    }
-                    if (ok) ok = ptx::mbar_wait(&sh.p_full[0][0], p_ph0);
-                    half_product(0, 0, j == 0);
-                    if (ok) t5::commit(&sh.h_full[0]);
-                    if (ok) ok = ptx::mbar_wait(&sh.p_full[0][1], p_ph0);
-                    half_product(0, 1, false);
-                    p_ph0 ^= 1u;
-                    if (ok && !more) t5::commit(&sh.o_full[0]);
-                    if (more) {
-                        if (ok) ok = ptx::mbar_wait(&sh.full[kp.st], kp.ph);
-                        logits(0);
-                    }
-                    if (two) {
-                        if (j == 0 && ok && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
-                        if (ok) ok = ptx::mbar_wait(&sh.p_full[1][0], p_ph1);
-                        half_product(1, 0, j == 0);
-                        if (ok) t5::commit(&sh.h_full[1]);
-                        if (ok) ok = ptx::mbar_wait(&sh.p_full[1][1], p_ph1);
-                        half_product(1, 1, false);
-                        p_ph1 ^= 1u;
-                        if (ok && !more) t5::commit(&sh.o_full[1]);
-                        if (more) logits(1);
-                    }
-                    if (ok) t5::commit(&sh.empty[vp.st]);
-                    vp.next();
-                    if (more) {
-                        if (ok) t5::commit(&sh.empty[kp.st]);
-                        if (ok && j + 2 == units) t5::commit(&sh.q_empty);
-                        kp.next();
-                    }
-                }
-                ++out0;
-                if (two) ++out1;
-                ++seg;
+                t5::commit(&sh.drained);                                  // MMAs in flight end before the tensor memory is given back
+                ok = ptx::mbar_wait(&sh.drained, 0u) && ok;
+                if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
             }
-            t5::commit(&sh.drained);                                  // MMAs in flight end before the tensor memory is given back
-            ok = ptx::mbar_wait(&sh.drained, 0u) && ok;
-            if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
         }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 " PRE_ROW_REGS ";");
         // ------------------------------------------------ rows: a thread each

@@ -143,6 +143,11 @@ __device__ __forceinline__ uint64_t add(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+__device__ __forceinline__ uint64_t mul(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // NaN if any operand is
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     float d;

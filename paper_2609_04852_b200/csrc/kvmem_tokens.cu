@@ -11,14 +11,15 @@
 // Everything here moves bytes: bound by HBM where there are many tokens, by one launch where there are few.
 //
 // A thread takes one vector where all threads are resident together anyway (the shortest way through: 2.1 us instead of 2.8 with four
-// vectors for 8 tokens of 40 heads, 2.5 instead of 3.8 for an append of 8 tokens with 48), and several beyond, whose loads are then in
-// flight together behind one table row: rotation four (24,576 tokens of 40 heads 85 us, 108 with one, 94 with two), append three
-// in blocks of 128 (16,383 tokens with 48 heads 90 us, 127 with one, 103 with four in blocks of 256, whose 106 registers leave room
-// for 16 warps an SM).
+// vectors for 8 tokens of 40 heads, 2.5 instead of 3.8 for an append of 8 tokens with 48 heads), and several beyond, whose loads are then in
+// flight together behind one table row: rotation four (24,576 tokens of 40 heads 80 us, 89 with two),
+// append three (16,383 tokens with 48 heads 80 us, 83 with two, 82 with four, 101 with six).  Issue slots count beside the bytes (56 %
+// busy at 65 % of HBM's cycles): indices are divided by products, the products of a rotation taken two at a time (append 90 -> 80 us).
 #include <algorithm>
 
 #include "kvmem_internal.cuh"
-#include "kvmem_rope.cuh"
+#include "kvmem_ptx.cuh"
+#include "kvmem_t5.cuh"
 
 namespace kvmem {
 
@@ -65,23 +66,41 @@ __device__ __forceinline__ void weave(uint4& lo, uint4& hi) {
     hi = make_uint4(__byte_perm(x.z, y.z, 0x5410), __byte_perm(x.z, y.z, 0x7632), __byte_perm(x.w, y.w, 0x5410), __byte_perm(x.w, y.w, 0x7632));
 }
 
-// rotate8_cs with an amplitude: fp32 products, sums and the amplitude's product each rounded to fp32, then one rounding to bf16
-__device__ __forceinline__ void turn8(uint4& lo, uint4& hi, const float4 (&t4)[4], float sgn, float amplitude) {
+// a chunk's angles, two pairs to a register pair
+struct Angles { uint64_t c[4], s[4]; };
+__device__ __forceinline__ Angles angles_at(const float2* cs, float sgn) {
+    Angles t;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(cs) + w);
+        t.c[w] = f2::pk(v.x, v.z);
+        t.s[w] = f2::pk(sgn * v.y, sgn * v.w);
+    }
+    return t;
+}
+
+// 8 pairs turned: a c - b s and b c + a s, products and sums each rounded to fp32, then the amplitude's product where there is one, one
+// rounding to bf16.  Products two at a time; the sums are scalar, since packed ones are contracted with the products before them.
+template <bool AMPLITUDE>
+__device__ __forceinline__ void turn8(uint4& lo, uint4& hi, const Angles& t, float amplitude) {
     uint32_t* l = reinterpret_cast<uint32_t*>(&lo);
     uint32_t* h = reinterpret_cast<uint32_t*>(&hi);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        const float4 t = t4[w];
-        const float a0 = __uint_as_float(l[w] << 16), a1 = __uint_as_float(l[w] & 0xffff0000u);
-        const float b0 = __uint_as_float(h[w] << 16), b1 = __uint_as_float(h[w] & 0xffff0000u);
-        const float s0 = sgn * t.y, s1 = sgn * t.w;
-        const float l0 = __fsub_rn(__fmul_rn(a0, t.x), __fmul_rn(b0, s0)), h0 = __fadd_rn(__fmul_rn(b0, t.x), __fmul_rn(a0, s0));
-        const float l1 = __fsub_rn(__fmul_rn(a1, t.z), __fmul_rn(b1, s1)), h1 = __fadd_rn(__fmul_rn(b1, t.z), __fmul_rn(a1, s1));
-        const __nv_bfloat162 lp = __floats2bfloat162_rn(__fmul_rn(l0, amplitude), __fmul_rn(l1, amplitude));
-        const __nv_bfloat162 hp = __floats2bfloat162_rn(__fmul_rn(h0, amplitude), __fmul_rn(h1, amplitude));
-        l[w] = *reinterpret_cast<const uint32_t*>(&lp);
-        h[w] = *reinterpret_cast<const uint32_t*>(&hp);
+        const uint64_t a = f2::pk(l[w] << 16, l[w] & 0xffff0000u), b = f2::pk(h[w] << 16, h[w] & 0xffff0000u);
+        float ac0, ac1, bs0, bs1, bc0, bc1, as0, as1;
+        f2::unpk(f2::mul(a, t.c[w]), ac0, ac1);
+        f2::unpk(f2::mul(b, t.s[w]), bs0, bs1);
+        f2::unpk(f2::mul(b, t.c[w]), bc0, bc1);
+        f2::unpk(f2::mul(a, t.s[w]), as0, as1);
+        float x0 = __fsub_rn(ac0, bs0), x1 = __fsub_rn(ac1, bs1), y0 = __fadd_rn(bc0, as0), y1 = __fadd_rn(bc1, as1);
+        if (AMPLITUDE) { x0 = __fmul_rn(x0, amplitude); x1 = __fmul_rn(x1, amplitude); y0 = __fmul_rn(y0, amplitude); y1 = __fmul_rn(y1, amplitude); }
+        l[w] = ptx::pack_bf16x2(x0, x1);
+        h[w] = ptx::pack_bf16x2(y0, y1);
     }
+}
+__device__ __forceinline__ void turn8(uint4& lo, uint4& hi, const Angles& t, float amplitude) {
+    if (amplitude != 1.0f) turn8<true>(lo, hi, t, amplitude); else turn8<false>(lo, hi, t, 1.0f);
 }
 
 __device__ __forceinline__ uint4 ld16(const __nv_bfloat16* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
@@ -90,14 +109,15 @@ __device__ __forceinline__ void st16(__nv_bfloat16* p, const uint4& v) { *reinte
 // ---- rotation ----------------------------------------------------------------------------------------------------------------
 
 // One thread: chunk c of PER vectors of one row, so that a table row is fetched once for them and their loads are in flight together.
+constexpr int kTokensThreads = 128;                            // (256: 83 us instead of 80.5 for 24,576 tokens, 10.6 instead of 9.7 for 2,048)
 constexpr long long kTokensFew = (long long)kSMs * 1024;      // threads that are resident together at any register count here
 template <int PER>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kTokensThreads)
 rope_apply_kernel(const __grid_constant__ RopeApplyArgs a) {
     pdl_wait();
     pdl_trigger();
-    const unsigned e = blockIdx.x * 256u + threadIdx.x;
-    const unsigned c = e % (unsigned)a.chunks, g = e / (unsigned)a.chunks % (unsigned)a.groups, row = e / (unsigned)(a.chunks * a.groups);
+    const unsigned e = blockIdx.x * (unsigned)kTokensThreads + threadIdx.x;
+    const unsigned eg = a.chunks.of(e), c = a.chunks.rest(e, eg), row = a.groups.of(eg), g = a.groups.rest(eg, row);
     if (row >= (unsigned)a.n_rows) return;
     const bool turns = (int)c < a.form.chunks;
     const int pos = a.positions[row];
@@ -105,27 +125,23 @@ rope_apply_kernel(const __grid_constant__ RopeApplyArgs a) {
     const Place in = place_of(a.form, a.x_pool, (int)c, a.d), out = place_of(a.form, a.y_pool, (int)c, a.d);
     const __nv_bfloat16* x = a.x + (long long)row * a.x_row + (long long)g * a.x_vec;
     __nv_bfloat16* y = a.y + (long long)row * a.y_row + (long long)g * a.y_vec;
-    const long long x_step = (long long)a.groups * a.x_vec, y_step = (long long)a.groups * a.y_vec;
+    const long long x_step = (long long)a.groups.d * a.x_vec, y_step = (long long)a.groups.d * a.y_vec;
     uint4 lo[PER], hi[PER];
-    float4 t4[4];
+    Angles t;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        if ((int)g + i * a.groups < a.n_vec) {
+        if ((int)(g + i * a.groups.d) < a.n_vec) {
             // (plain loads: y may be x)
             lo[i] = *reinterpret_cast<const uint4*>(x + i * x_step + in.lo);
             hi[i] = *reinterpret_cast<const uint4*>(x + i * x_step + in.hi);
         }
-    if (turns) {
-        const float4* cs = reinterpret_cast<const float4*>(a.rope + (size_t)pos * (a.d / 2) + 8 * c);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) t4[w] = __ldg(cs + w);
-    }
+    if (turns) t = angles_at(a.rope + (size_t)pos * (a.d / 2) + 8 * c, a.sgn);
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        if ((int)g + i * a.groups < a.n_vec) {
+        if ((int)(g + i * a.groups.d) < a.n_vec) {
             if (turns) {
                 if (in.woven) unweave(lo[i], hi[i]);
-                turn8(lo[i], hi[i], t4, a.sgn, a.amplitude);
+                turn8(lo[i], hi[i], t, a.amplitude);
                 if (out.woven) weave(lo[i], hi[i]);
             }
             st16(y + i * y_step + out.lo, lo[i]);
@@ -135,12 +151,12 @@ rope_apply_kernel(const __grid_constant__ RopeApplyArgs a) {
 
 template <int PER>
 static cudaError_t rope_apply(const kvmem_pool& p, RopeApplyArgs a, long long n_rows, cudaStream_t st) {
-    a.chunks = p.geo.d / 16;
-    a.groups = (a.n_vec + PER - 1) / PER;
-    const long long per_row = (long long)a.chunks * a.groups, most = std::max<long long>(1, (1ll << 30) / per_row);
+    a.chunks = Divisor(p.geo.d / 16);
+    a.groups = Divisor((a.n_vec + PER - 1) / PER);
+    const long long per_row = (long long)a.chunks.d * a.groups.d, most = std::max<long long>(1, (1ll << 30) / per_row);
     for (long long r0 = 0; r0 < n_rows; r0 += most) {
         a.n_rows = (int)std::min(most, n_rows - r0);
-        const cudaError_t e = launch_pdl(rope_apply_kernel<PER>, dim3((unsigned)((a.n_rows * per_row + 255) / 256)), dim3(256), 0, st, a);
+        const cudaError_t e = launch_pdl(rope_apply_kernel<PER>, dim3((unsigned)((a.n_rows * per_row + kTokensThreads - 1) / kTokensThreads)), dim3(kTokensThreads), 0, st, a);
         if (e != cudaSuccess) return e;
         a.x += a.n_rows * a.x_row;
         a.y += a.n_rows * a.y_row;
@@ -159,35 +175,35 @@ cudaError_t launch_rope_apply(const kvmem_pool& p, const RopeApplyArgs& a, long 
 // One thread: chunk c of PER vectors of one new token, a vector being a query, key or value head of a layer.  Vectors are numbered
 // [layer][query heads | key heads | value heads].  What a thread needs comes in two rounds of loads: counts, lengths and its vectors,
 // then the table row and the page.
-constexpr int kAppendThreads = 128;
 template <int PER>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kTokensThreads)
 append_tokens_kernel(const __grid_constant__ AppendTokensArgs a) {
     pdl_wait();
     pdl_trigger();
-    const unsigned e = blockIdx.x * (unsigned)kAppendThreads + threadIdx.x;
-    const unsigned c = e % (unsigned)a.chunks, eg = e / (unsigned)a.chunks, token = eg / (unsigned)a.groups, g = eg - token * (unsigned)a.groups;
-    const unsigned s = token / (unsigned)a.M + (unsigned)a.s0, i = token - (s - (unsigned)a.s0) * (unsigned)a.M;
+    const unsigned e = blockIdx.x * (unsigned)kTokensThreads + threadIdx.x;
+    const unsigned eg = a.chunks.of(e), c = a.chunks.rest(e, eg), token = a.groups.of(eg), g = a.groups.rest(eg, token);
+    const unsigned s1 = a.tokens.of(token), i = a.tokens.rest(token, s1), s = s1 + (unsigned)a.s0;
     if (s >= (unsigned)a.ns) return;
     const int given_new = a.n_new ? a.n_new[s] : a.M, given = a.tail_n[s];
     const int n_sel = a.rope && a.n_sel ? a.n_sel[s] : 0, at = a.rope && a.positions ? a.positions[(size_t)s * a.M + i] : 0;
     const int blocks = a.pages ? a.nblocks_dev[a.session_first + s] : 0;
     const bool turns = (int)c < a.form.chunks;
     const Place in = place_of(a.form, a.rope == nullptr, (int)c, a.d);
-    const int per_layer = a.Hq + 2 * a.G, lo_at = 8 * (int)c, hi_at = a.d / 2 + 8 * (int)c;
+    const int lo_at = 8 * (int)c, hi_at = a.d / 2 + 8 * (int)c;
     uint4 lo[PER], hi[PER];
     int kind[PER], l[PER], h[PER];                       // 0 query, 1 key, 2 value, -1 none; layer; head
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-        const int v = (int)g + u * a.groups;
+        const unsigned v = g + u * a.groups.d;
         kind[u] = -1;
-        if (v < a.n_vec) {
-            l[u] = a.L == 1 ? 0 : v / per_layer;
-            const int w = v - l[u] * per_layer;
-            kind[u] = w < a.Hq ? 0 : w < a.Hq + a.G ? 1 : 2;
-            h[u] = kind[u] == 0 ? w : kind[u] == 1 ? w - a.Hq : w - a.Hq - a.G;
+        if ((int)v < a.n_vec) {
+            l[u] = (int)a.per_layer.of(v);
+            h[u] = (int)a.per_layer.rest(v, l[u]);
+            kind[u] = 0;
+            if (h[u] >= a.Hq) { h[u] -= a.Hq; kind[u] = 1; }
+            if (kind[u] == 1 && h[u] >= a.G) { h[u] -= a.G; kind[u] = 2; }
             const TokenRows& t = kind[u] == 0 ? a.q : kind[u] == 1 ? a.k : a.v;
-            const __nv_bfloat16* src = t.data + (long long)s * t.session + (long long)i * t.token + (long long)l[u] * t.layer + (long long)h[u] * t.head;
+            const __nv_bfloat16* src = t.data + (long long)s * t.session + (long long)i * t.token + (l[u] * t.layer + h[u] * t.head);
             lo[u] = ld16(src + (kind[u] == 2 ? lo_at : in.lo));
             hi[u] = ld16(src + (kind[u] == 2 ? hi_at : in.hi));
         }
@@ -196,37 +212,36 @@ append_tokens_kernel(const __grid_constant__ AppendTokensArgs a) {
     if ((int)i >= n_new) return;
     const int n_tail = min(max(given, 0), a.tail_cap - n_new), row = n_tail + (int)i;
     bool ok = n_tail == given;
-    float4 t4[4];
+    Angles t;
     if (a.rope) {
         const long long pos = a.positions ? at : (long long)a.first_position + (long long)max(n_sel, 0) * a.B + row;
         if (pos < 0 || pos >= a.rope_positions) { atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE); return; }
-        if (turns) {
-            const float4* cs = reinterpret_cast<const float4*>(a.rope + (size_t)pos * (a.d / 2) + 8 * c);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) t4[w] = __ldg(cs + w);
-        }
+        if (turns) t = angles_at(a.rope + (size_t)pos * (a.d / 2) + 8 * c, 1.0f);
     }
     __nv_bfloat16* page = nullptr;
     if (a.pages) {
-        const int b = blocks + row / a.B;
+        const int rb = (int)a.block.of(row), b = blocks + rb;
         const int pg = b < a.max_bps ? a.tables[(size_t)(a.session_first + s) * a.max_bps + b] : -1;
-        if (pg >= 0 && pg < a.max_blocks) page = a.pages + (size_t)pg * a.page_elems + (size_t)(row % a.B) * a.d;
+        if (pg >= 0 && pg < a.max_blocks) page = a.pages + (size_t)pg * a.page_elems + (int)a.block.rest(row, rb) * a.d;
         else ok = false;
     }
     if (!ok) atomicExch(a.status, (int)KVMEM_E_DEVICE_RANGE);
-    const size_t tail_row = (size_t)s * a.tail_cap + row, tile = (size_t)a.B * a.d;
+    // a token's vectors lie within 2^31 elements of one another, in every result
+    __nv_bfloat16 *const q_out = a.q_out + ((size_t)s * a.M + i) * (size_t)(a.L * a.Hq * a.d);
+    const size_t tail_row = ((size_t)s * a.tail_cap + row) * (size_t)(a.L * a.G * a.d);
+    const int tile = a.B * a.d;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
         if (kind[u] < 0) continue;
         if (kind[u] < 2 && turns && in.woven) unweave(lo[u], hi[u]);
+        const int place = l[u] * a.G + h[u];                               // of a key or value
         if (kind[u] > 0 && page) {
-            __nv_bfloat16* dst = page + ((size_t)((kind[u] - 1) * a.L + l[u]) * a.G + h[u]) * tile;
+            __nv_bfloat16* dst = page + (place + (kind[u] == 2 ? a.L * a.G : 0)) * (size_t)tile;
             st16(dst + lo_at, lo[u]);
             st16(dst + hi_at, hi[u]);
         }
-        if (kind[u] < 2 && turns) turn8(lo[u], hi[u], t4, 1.0f, kind[u] == 0 ? a.q_amplitude : 1.0f);
-        __nv_bfloat16* dst = kind[u] == 0 ? a.q_out + ((((size_t)s * a.M + i) * a.L + l[u]) * a.Hq + h[u]) * a.d
-                                          : (kind[u] == 1 ? a.tail_k : a.tail_v) + ((tail_row * a.L + l[u]) * a.G + h[u]) * a.d;
+        if (kind[u] < 2 && turns) turn8(lo[u], hi[u], t, kind[u] == 0 ? a.q_amplitude : 1.0f);
+        __nv_bfloat16* dst = kind[u] == 0 ? q_out + (l[u] * a.Hq + h[u]) * a.d : (kind[u] == 1 ? a.tail_k : a.tail_v) + tail_row + place * a.d;
         st16(dst + lo_at, lo[u]);
         st16(dst + hi_at, hi[u]);
     }
@@ -234,29 +249,33 @@ append_tokens_kernel(const __grid_constant__ AppendTokensArgs a) {
 
 template <int PER>
 static cudaError_t append_tokens(AppendTokensArgs a, cudaStream_t st) {
-    a.groups = (a.n_vec + PER - 1) / PER;
-    // whole sessions per launch, as far as their threads are numbered in 32 bits (the caller keeps one session below that)
-    const long long per_session = (long long)a.M * a.chunks * a.groups;
-    const int most = (int)std::max<long long>(1, (1ll << 31) / per_session), all = a.ns;
+    a.groups = Divisor((a.n_vec + PER - 1) / PER);
+    // whole sessions per launch, as far as their threads stay below 2^30 (the caller keeps one session below that)
+    const long long per_session = (long long)a.M * a.chunks.d * a.groups.d;
+    const int most = (int)std::max<long long>(1, (1ll << 30) / per_session), all = a.ns;
     for (int s0 = 0; s0 < all; s0 += most) {
         a.s0 = s0;
         a.ns = std::min(all, s0 + most);
-        const long long blocks = ((a.ns - s0) * per_session + kAppendThreads - 1) / kAppendThreads;
-        const cudaError_t e = launch_pdl(append_tokens_kernel<PER>, dim3((unsigned)blocks), dim3(kAppendThreads), 0, st, a);
+        const long long blocks = ((a.ns - s0) * per_session + kTokensThreads - 1) / kTokensThreads;
+        const cudaError_t e = launch_pdl(append_tokens_kernel<PER>, dim3((unsigned)blocks), dim3(kTokensThreads), 0, st, a);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
 cudaError_t launch_append_tokens(const kvmem_pool& p, AppendTokensArgs a, cudaStream_t st) {
-    a.chunks = p.geo.d / 16;
+    a.chunks = Divisor(p.geo.d / 16);
     a.n_vec = a.L * (a.Hq + 2 * a.G);
-    const bool few = (long long)a.ns * a.M <= kTokensFew / ((long long)a.n_vec * a.chunks);
+    a.tokens = Divisor(a.M);
+    a.per_layer = Divisor(a.Hq + 2 * a.G);
+    a.block = Divisor(a.B);
+    const bool few = (long long)a.ns * a.M <= kTokensFew / ((long long)a.n_vec * a.chunks.d);
     return few ? append_tokens<1>(a, st) : append_tokens<3>(a, st);
 }
 
 bool append_tokens_fits(const kvmem_pool_config_t& c, int n_q_tokens) {
-    return (long long)n_q_tokens * (c.head_dim / 16) * ((long long)c.n_layers * (c.n_q_heads + 2 * c.n_kv_heads)) < (1ll << 31);
+    const long long vectors = (long long)c.n_layers * (c.n_q_heads + 2ll * c.n_kv_heads);
+    return vectors * c.head_dim < (1ll << 31) && (double)n_q_tokens * (c.head_dim / 16) * (double)vectors < (double)(1ll << 31);
 }
 
 // ---- commit ------------------------------------------------------------------------------------------------------------------

@@ -701,7 +701,8 @@ int kvmem_rope_apply(kvmem_pool_t* pool, const void* x /*DEVICE*/, int64_t x_row
                      const int32_t* positions /*DEVICE*/, int32_t inverse, float amplitude, void* stream);
 
 /* Pages for n_blocks blocks behind a session's last: taken from the pool now (phys_ids as in kvmem_append_blocks), filled by
- * kvmem_append_tokens, part of the session only once kvmem_commit_blocks makes them so.  While a session has reserved blocks
+ * kvmem_append_tokens, part of the session only once kvmem_commit_blocks makes them so (this call, that one and kvmem_set_rope are
+ * refused as KVMEM_E_STATE on a stream that is being captured: they change what the host knows of the pool).  While a session has reserved blocks
  * kvmem_append_blocks refuses it; kvmem_session_reset gives them back.  Errors as kvmem_append_blocks; KVMEM_E_STATE on an FP8
  * repository or with rope_in_block_keys (their pages do not hold the raw keys that the index is made from). */
 int kvmem_reserve_blocks(kvmem_pool_t* pool, int32_t session, int32_t n_blocks, const int32_t* phys_ids /*HOST, may be NULL*/,

@@ -1372,8 +1372,19 @@ int kvmem_rope_frequencies(const kvmem_pool_config_t* cfg, const kvmem_rope_t* r
     return rc;
 }
 
+// Calls that change what the host knows of a pool run once: a captured one would be replayed without the host's part.
+static bool captured(void* stream, const char* who) {
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    const cudaError_t e = cudaStreamIsCapturing((cudaStream_t)stream, &st);
+    if (e == cudaSuccess && st == cudaStreamCaptureStatusNone) return false;
+    (void)cudaGetLastError();
+    set_error("%s changes the pool's bookkeeping on the host: it cannot be part of a captured graph", who);
+    return true;
+}
+
 int kvmem_set_rope(kvmem_pool_t* p, const kvmem_rope_t* rope, void* stream) {
     if (!pool_live(p)) return KVMEM_E_STATE;
+    if (captured(stream, "kvmem_set_rope")) return KVMEM_E_STATE;
     RopeForm form;
     RopeFrequencies f{};
     const int rc = rope_form(p->cfg, rope, &form, f.f);
@@ -1434,7 +1445,7 @@ int kvmem_rope_apply(kvmem_pool_t* p, const void* x, int64_t x_row_stride, int64
 int kvmem_reserve_blocks(kvmem_pool_t* p, int32_t session, int32_t n_blocks, const int32_t* phys_ids, void* stream) {
     if (!pool_live(p)) return KVMEM_E_STATE;
     if (!sessions_ok(p, session, 1)) return KVMEM_E_INVALID;
-    if (!pages_are(p, false, "kvmem_reserve_blocks")) return KVMEM_E_STATE;
+    if (captured(stream, "kvmem_reserve_blocks") || !pages_are(p, false, "kvmem_reserve_blocks")) return KVMEM_E_STATE;
     if (p->cfg.rope_in_block_keys) { set_error("kvmem_reserve_blocks: reserved pages hold raw keys until they are indexed; the pool's pages hold keys rotated by their offset in the block"); return KVMEM_E_STATE; }
     if (n_blocks < 0) { set_error("n_blocks is negative"); return KVMEM_E_INVALID; }
     if (n_blocks == 0) return KVMEM_OK;
@@ -1563,6 +1574,7 @@ int kvmem_commit_blocks(kvmem_pool_t* p, int32_t session_first, int32_t n_sessio
     if (!pool_live(p)) return KVMEM_E_STATE;
     if (!sessions_ok(p, session_first, n_sessions)) return KVMEM_E_INVALID;
     if (!n_blocks) { set_error("%s: n_blocks is null", who); return KVMEM_E_INVALID; }
+    if (captured(stream, who)) return KVMEM_E_STATE;
     if (tail) {
         const int rc = tail_ok(tail, n_sessions, 1, who);
         if (rc != KVMEM_OK) return rc;

@@ -11,7 +11,7 @@
 // thread fetches Q, K and V tiles with TMA (128-byte swizzle), one thread issues the MMAs: those of one thread run in order, so a
 // slot's next S is issued right behind the product that reads its P, in whose place it goes.
 //
-// ref is the largest logit of the first tokens a row sees.  It moves only when half a tile's weights sum to more than 2^64: O is then
+// ref is the largest logit of the first tokens a row sees.  It moves only when half a tile's weights sum to more than 2^12: O is then
 // rescaled in tensor memory and the half's weights are computed again.  Until then they may be that large, which costs neither fp32
 // nor bf16 any precision, and no tile needs the maximum of its logits.
 //
@@ -56,7 +56,8 @@ constexpr int kPreTmaWarp = 8, kPreMmaWarp = 9;
 static_assert(256 * 208 + 128 * 80 <= kPreThreads * 168, "the registers that the row warps take are those the others give");
 constexpr int kPreLead = 3;                      // units on the line for an item's start and end: what they cost a CTA, in tiles (1: 195 and 314 us
                                                  // instead of 170 and 234 for a chunk of 4,096 alone and three ragged sessions)
-constexpr float kPreLimit = 18446744073709551616.0f;   // 2^64: half a tile's weights may sum to this before their reference moves
+constexpr float kPreLimit = 4096.0f;              // half a tile's weights may sum to this before their reference moves (2^8 and 2^64 instead: 2,152 and
+                                                  // 2,081 us against 2,090 for 2,048 tokens over 65,536; a value may be 2^115 before its sum overflows)
 constexpr int kPreParts = 4;                     // parts of the line a CTA can have
 constexpr int kPreBudget = 1024;                 // tiles of keys and values (64 KiB each) that a sweep of all CTAs may hold in L2
 constexpr int kPrePartUnits = 64;                // least units of a part, when there is more than one

@@ -133,6 +133,10 @@ LONG = [
     dict(M=65, H=4, G=1, lens=(501,), tails=(10,)),                    # one KV head on all SMs
     dict(ns=9, M=129, H=8, G=8, lens=[5 * s for s in range(9)], n_q=[129 - 15 * s for s in range(9)], tails=(0, 200, 7)),
     dict(M=1111, H=6, G=2, lens=(17,), tails=(777,), B=80),
+    # more keys and values than L2 holds: the line in two and in four parts a CTA
+    dict(M=700, H=32, G=8, lens=(512,), tails=(40,)),
+    dict(ns=2, M=450, H=32, G=8, lens=(1024, 500), n_q=(450, 449), tails=(3, 200)),
+    dict(M=800, H=40, G=8, B=128, lens=(512,), tails=(127,)),
 ]
 
 
@@ -207,6 +211,20 @@ def test_nothing_reaches_a_result_that_it_does_not_see(value):
             assert bool(got[:, 7].isnan().all() if math.isnan(value) else (got[:, 7] == value).all())
     assert torch.equal(c.lse[:, :, :, r:], clean.lse[:, :, :, r:])
     c.guards.check()
+
+
+def test_the_largest_values_do_not_overflow():
+    """Values of 2^110 behind logits that grow from tile to tile: the weights before a reference moves are below 2^12, a product's sums
+    below 2^122 times a few."""
+    c, big = Chunk(lens=(24,), M=130, seed=8), Chunk(lens=(24,), M=130, seed=8)
+    ramp = torch.linspace(0.1, 2.0, c.k.shape[3], device="cuda").view(1, 1, 1, -1, 1)
+    for x in (c, big):
+        x.k = (x.k.float() * ramp).to(torch.bfloat16)
+    big.v, big.tv = big.v * 2.0 ** 110, big.tv * 2.0 ** 110
+    c.call()
+    big.call()
+    torch.cuda.synchronize()
+    assert torch.equal(big.out.float(), c.out.float() * 2.0 ** 110) and torch.equal(big.lse, c.lse)
 
 
 @pytest.mark.parametrize("M,H,lens", [(140, 8, (3,)), (700, 16, (300,))])

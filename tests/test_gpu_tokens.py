@@ -287,6 +287,68 @@ def test_what_rotation_refuses():
     assert bool((out == 3.0).all())
 
 
+@pytest.mark.parametrize("in_block", [False, True])
+@pytest.mark.parametrize("i", [1, 2, 5, 6])
+def test_every_pass_rotates_by_the_pools_form(i, in_block):
+    """Materialised, fused, copy-free and cached views of a pool with a model's form: keys as the definition has them from raw keys in
+    the pool's order, and the attention of each pass is that over the keys it wrote or would write.
+
+    Bounds: a key of the materialised view on raw pages is one rotation (`close`), with in-block keys two roundings more of at most
+    2^-8 of the pair each.  Attention results are compared with one another at the 2e-3 of the other passes' tests (unit-scale values;
+    one bf16 step of some keys apart)."""
+    rope, B, NB, G, H = FORMS[i], 64, 12, 2, 8
+    pool = make_pool(1, H, G, B=B, blocks=NB, positions=2048, rope=rope, rope_in_block_keys=in_block)
+    raw = randn(i, NB * B, 1, G, 128)                                       # the pool's order
+    v = randn(50 + i, NB * B, 1, G, 128)
+    # as a prefill left them: rotated at positions of their own, block by block
+    pos0 = [(37 * b) % 1900 for b in range(NB)]
+    at = torch.cat([torch.arange(p, p + B) for p in pos0]).to(torch.int32).cuda()
+    roped = pool.rope_apply(raw[:, 0], at, x_order="pool")
+    pool.append_blocks_rope(0, roped.unsqueeze(1).contiguous(), v, pos0)
+    back = pool.rope_apply(roped, at, inverse=True, x_order="pool", out_order="pool")        # what the pages hold or are made from
+    kbar = torch.zeros(NB, G, 128, device="cuda")
+    for t in range(B):
+        kbar = kbar + back.view(NB, B, G, 128)[:, t].float()
+    assert torch.equal(pool.index(0)[0].transpose(0, 1), (kbar * (1.0 / B)).to(torch.bfloat16))
+    sel, n_sel = ints([[0, 3, 4, 9, 11]]), ints([5])
+    first = 100
+    view = pool.new_view(1, 5 * B)
+    pool.materialize_rope(sel, n_sel, view, first)
+    keys = torch.cat([back.view(NB, B, G, 128)[b] for b in sel[0].tolist()]).double()
+    where = (first + torch.arange(5 * B, device="cuda")).view(-1, 1)
+    ref, mag = turned(keys, where, rope)
+    got = view.k[0, 0].transpose(0, 1).double()
+    if in_block:
+        # the stored key is a rounded rotation, and its rotation is rounded: 2^-8 of an element's pair each
+        n = (rope.rotary_dim or 128) // 2
+        size = mag.clone()
+        size[..., n:64] = keys[..., n:64].abs()
+        size[..., 64 + n:] = keys[..., 64 + n:].abs()
+        assert bool(((got - ref).abs() <= 2 * 2.0 ** -8 * size * 1.02 + 1e-30).all())
+    else:
+        close(view.k[0, 0].transpose(0, 1), ref, mag)
+    q = pool.rope_apply(randn(90 + i, 3, H, 128), ints([first + 5 * B] * 3)).view(1, 3, 1, H, 128)
+    outs = [pool.new_outputs(1, 3) for _ in range(4)]
+    pool.view_attend(q, view, n_sel, *outs[0])
+    pool.paged_attend_rope(q, sel, n_sel, *outs[1], first_position=first)
+    view2 = pool.new_view(1, 5 * B)
+    pool.materialize_attend_rope(q, sel, n_sel, view2, *outs[2], first_position=first)
+    n_out = 3
+    if not in_block:
+        cache = pool.new_view_cache(5, 2, first)
+        cache.update(0, ints([0, 1, 2, 9, 11]), n_sel)
+        cache.update(0, sel[0].contiguous(), n_sel)                         # two blocks keep their slots and turn on by a delta
+        cache.attend(q[0], outs[3][0][0], outs[3][1][0])
+        n_out = 4
+    assert torch.equal(view2.v, view.v)
+    for o, l in outs[1:n_out]:
+        assert float((o - outs[0][0]).abs().max()) <= 2e-2 and float((l - outs[0][1]).abs().max()) <= 2e-2
+    # and they follow the positions: the same keys a few positions on are others
+    pool.materialize_rope(sel, n_sel, view2, first + 5)
+    assert not torch.equal(view2.k, view.k)
+    assert pool.device_status() == 0
+
+
 # ---- append ---------------------------------------------------------------------------------------------------------------------
 
 class Append:
@@ -533,6 +595,23 @@ def test_a_captured_append_follows_the_tail():
         c.pool.pages().fill_(4.0)
         g.replay()
         c.check()
+
+
+def test_what_changes_the_hosts_bookkeeping_is_not_captured():
+    pool = make_pool(blocks=4)
+    tail = Tail(torch.zeros(1, 64, 1, 2, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 64, 1, 2, 128, dtype=torch.bfloat16, device="cuda"), ints([0]))
+    pool.reserve_blocks(0, 1)
+    g, st = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    refused = []
+    with torch.cuda.graph(g, stream=st):
+        tail.n_tokens.add_(0)
+        for f in (lambda: pool.reserve_blocks(0, 1), lambda: pool.commit_blocks([1], tail), lambda: pool.set_rope(Rope())):
+            try:
+                f()
+            except KvmemError as e:
+                refused.append(e.status)
+    assert refused == [kvmem.E_STATE] * 3
+    assert pool.session_reserved(0) == 1 and pool.session_blocks(0) == 0
 
 
 def test_append_and_commit_on_another_stream():

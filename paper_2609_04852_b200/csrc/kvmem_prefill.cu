@@ -47,13 +47,13 @@ constexpr int kPreHalf = 128 * 128;              // bytes of one 64-dim half of 
 constexpr int kPreSlot = 2 * kPreHalf;           // a K, V or Q tile
 constexpr int kPreRing = 4;                      // K and V tiles in turn
 constexpr int kPreStage = 4096;                  // bytes of a row warp's staging for stores
-constexpr int kPreThreads = 384;                 // eight row warps, TMA warp, MMA warp, two that only give registers away
+constexpr int kPreThreads = 384;                 // eight row warps, TMA warp, MMA warp, two for values that rows do not see
 constexpr int kPreTmaWarp = 8, kPreMmaWarp = 9;
 // Registers a thread: the launch gives 168, the row warps take 208 and the others keep 80.  (Without: a row's 128 logits do not fit, and a
 // spill is slow here, where shared memory leaves the L1 no room for it: 220 us instead of 206 for a chunk of 4,096 alone.)
 #define PRE_ROW_REGS "208"
-#define PRE_OTHER_REGS "80"
-static_assert(256 * 208 + 128 * 80 <= kPreThreads * 168, "the registers that the row warps take are those the others give");
+#define PRE_OTHER_REGS "88"
+static_assert(256 * 208 + 128 * 88 <= kPreThreads * 168, "the registers that the row warps take are those the others give");
 constexpr int kPreLead = 3;                      // units on the line for an item's start and end: what they cost a CTA, in tiles (1: 195 and 314 us
                                                  // instead of 170 and 234 for a chunk of 4,096 alone and three ragged sessions)
 constexpr float kPreLimit = 4096.0f;              // half a tile's weights may sum to this before their reference moves (2^8 and 2^64 instead: 2,152 and
@@ -156,6 +156,7 @@ struct PreWalk {
     int t0, t1, tiles;              // the share: tiles [t0, t1) of the item's `tiles` (0: nothing to see)
     int cs, clg, crg, m0, rows2;    // its item; first token; whether the second row tile has any token
     int last;                       // the item's last unit
+    bool more;
     __device__ __forceinline__ bool next(const PreWork& w, int LG) {
         const PrefillArgs& a = w.a;
         while (true) {
@@ -190,15 +191,32 @@ struct PreWalk {
     }
     int n_view, n_tail, n_q, view_tiles;      // of the share's session
     __device__ __forceinline__ int units() const { return tiles ? t1 - t0 : 0; }
+    // of the share's tile t: its first token in view or tail, its tokens, those that every row sees, whether some do not
+    __device__ __forceinline__ int first_of(int t) const { return (t < view_tiles ? t : t - view_tiles) * kPreTile; }
+    __device__ __forceinline__ int valid_of(int t) const { return (t < view_tiles ? n_view : n_tail + n_q) - first_of(t); }
+    __device__ __forceinline__ int plain_of(int t) const { return t < view_tiles ? valid_of(t) : min(valid_of(t), n_tail + m0 + 1 - first_of(t)); }
+    __device__ __forceinline__ bool cleans(int t) const { return plain_of(t) < kPreTile; }
 };
 
 struct PreShared {
-    uint64_t full[kPreRing], empty[kPreRing], q_full, q_empty, s_full[2], p_full[2][2], h_full[2], o_full[2], o_empty[2], drained;
+    uint64_t full[kPreRing], empty[kPreRing], q_full, q_empty, s_full[2], p_full[2][2], h_full[2], o_full[2], o_empty[2], v_ask, v_clean, drained;
     PrePart parts[kPreParts];
+    PreWalk walk[8];                          // of the row warps
     int n_parts, n_cta, total;                // the CTA's; CTAs that share the line, its units
     uint32_t tmem;
-    int not_finite[2];                        // by the parity of the share: its number + 1, where values were cleared
+    int loads;                                // tiles requested so far: waits of many tiles' length look at it
+    int not_finite[4];                        // by the share's number mod 4: that number + 1, where values were cleared
 };
+// A wait that may last as long as a share (seconds, where one head's view fills the device): given up when no tile was requested
+// between two limits.
+__device__ __forceinline__ bool pre_wait_long(const PreShared& sh, uint64_t* bar, uint32_t ph) {
+    for (int seen = -1;;) {
+        if (ptx::mbar_wait(bar, ph)) return true;
+        const int now = *(const volatile int*)&sh.loads;
+        if (now == seen) return false;
+        seen = now;
+    }
+}
 constexpr size_t kPreSmem = (size_t)(2 + kPreRing) * kPreSlot + 8 * kPreStage + sizeof(PreShared);
 static_assert(kPreSmem <= 232448, "shared memory of a CTA");
 
@@ -234,11 +252,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             ptx::mbar_init(&sh.h_full[i], 1);
             ptx::mbar_init(&sh.o_full[i], 1);
             ptx::mbar_init(&sh.o_empty[i], 4);
-            sh.not_finite[i] = 0;
+            sh.not_finite[i] = sh.not_finite[2 + i] = 0;
         }
         ptx::mbar_init(&sh.q_full, 1);
         ptx::mbar_init(&sh.q_empty, 1);
+        ptx::mbar_init(&sh.v_ask, 1);
+        ptx::mbar_init(&sh.v_clean, 2);
         ptx::mbar_init(&sh.drained, 1);
+        sh.loads = 0;
         ptx::fence_mbar_init();
     }
     if (warp == kPreMmaWarp) {
@@ -329,15 +350,16 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     __syncthreads();
     t5::fence_after();
     const uint32_t tmem = sh.tmem;
-    PreWalk walk;
-    walk.parts = sh.parts; walk.n_parts = sh.n_parts;
-    walk.part = walk.pos = walk.end = 0;
+    PreWalk walk0;
+    walk0.parts = sh.parts; walk0.n_parts = sh.n_parts;
+    walk0.part = walk0.pos = walk0.end = 0;
 
     // A wait that runs out is recorded and the role goes on without waiting (and without issuing what would need it), so that
     // every role still reaches its end.
     bool ok = true;
     if (warp >= kPreTmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " PRE_OTHER_REGS ";");
+        PreWalk walk = walk0;
         if (warp == kPreTmaWarp) {
             // ------------------------------------------------ TMA: one thread
             if (t5::elect()) {
@@ -372,6 +394,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                                 else ptx::tma_load_3d(dst + h * kPreHalf, kv ? &map_tv : &map_tk, 64 * h, walk.clg, row_tail + c0, &sh.full[st]);
                             }
                         }
+                        *(volatile int*)&sh.loads = n;
                     }
                     ++seg;
                 }
@@ -403,6 +426,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     }
                     t5::commit(&sh.s_full[x]);
                 };
+                int look_view = 0, look_tail = 0;                         // a share's tiles with values to look at: one, and all from one on
+                bool clean = false;                                       // the next tile to be multiplied has values to look at first
+                uint32_t c_ph = 0;
+                auto ask = [&](int j) {
+                    clean = j == look_view || j >= look_tail;
+                    if (ok && clean) ptx::mbar_arrive(&sh.v_ask);
+                };
                 auto half_product = [&](int x, int half, bool first) {
                     if (!ok) return;
                     t5::fence_after();
@@ -414,37 +444,65 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                                         t5::make_desc(bl + (uint32_t)k * (2048u >> 4)), kPreIdescO, !first || k > 0 ? 1u : 0u);
                     }
                 };
-                while (walk.next(w, LG)) {
-                    const int units = walk.units();
-                    if (units == 0) continue;
-                    const bool two = walk.rows2;
-                    if (ok) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)(seg & 1)) && ptx::mbar_wait(&sh.full[kp.st], kp.ph);
+                int units = 0;                                            // of the share at hand; two: both row tiles have tokens
+                bool two = false;
+                auto open = [&]() {                                       // the next share that has tiles
+                    while (walk.next(w, LG)) {
+                        units = walk.units();
+                        two = walk.rows2;
+                        if (units == 0) continue;
+                        look_view = walk.n_view % kPreTile ? walk.view_tiles - walk.t0 - 1 : -1;
+                        look_tail = walk.view_tiles - walk.t0 + (walk.n_tail + walk.m0 + 1) / kPreTile;
+                        return true;
+                    }
+                    return false;
+                };
+                bool have = open();
+                if (have) {
+                    if (ok) ok = ptx::mbar_wait(&sh.q_full, 0u) && ptx::mbar_wait(&sh.full[kp.st], kp.ph);
                     logits(0);
+                    ask(0);
                     if (two) logits(1);
                     if (ok) t5::commit(&sh.empty[kp.st]);
                     if (ok && units == 1) t5::commit(&sh.q_empty);
                     kp.next();
-                    for (int j = 0; j < units; ++j) {
-                        const bool more = j + 1 < units;
+                }
+                while (have) {
+                    const int n = units;
+                    const bool both = two;
+                    for (int j = 0; j < n; ++j) {
+                        const bool more = j + 1 < n;
+                        bool ahead = more;                                // a next tile: this share's, or the first of the next one
                         if (ok) ok = ptx::mbar_wait(&sh.full[vp.st], vp.ph);
                         // sums of the slots' last shares are out before new ones take their place (slot 1's too where it now rests: the flags of
-                        // cleared values are kept for two shares)
+                        // cleared values are kept for four shares)
                         if (j == 0) {
                             if (ok && out0 > 0) ok = ptx::mbar_wait(&sh.o_empty[0], (uint32_t)((out0 - 1) & 1));
-                            if (ok && !two && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
+                            if (ok && !both && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
                         }
+                        if (clean) {
+                            if (ok) ok = ptx::mbar_wait(&sh.v_clean, c_ph);
+                            c_ph ^= 1u;
+                        }
+                        if (more) ask(j + 1);
                         if (ok) ok = ptx::mbar_wait(&sh.p_full[0][0], p_ph0);
                         half_product(0, 0, j == 0);
                         if (ok) t5::commit(&sh.h_full[0]);
                         if (ok) ok = ptx::mbar_wait(&sh.p_full[0][1], p_ph0);
                         half_product(0, 1, false);
                         p_ph0 ^= 1u;
-                        if (ok && !more) t5::commit(&sh.o_full[0]);
-                        if (more) {
+                        if (!more) {
+                            if (ok) t5::commit(&sh.o_full[0]);
+                            ++seg;
+                            ahead = have = open();
+                            if (ok && ahead) ok = ptx::mbar_wait(&sh.q_full, (uint32_t)(seg & 1));
+                        }
+                        if (ahead) {
                             if (ok) ok = ptx::mbar_wait(&sh.full[kp.st], kp.ph);
                             logits(0);
+                            if (!more) ask(0);
                         }
-                        if (two) {
+                        if (both) {
                             if (j == 0 && ok && out1 > 0) ok = ptx::mbar_wait(&sh.o_empty[1], (uint32_t)((out1 - 1) & 1));
                             if (ok) ok = ptx::mbar_wait(&sh.p_full[1][0], p_ph1);
                             half_product(1, 0, j == 0);
@@ -453,39 +511,102 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                             half_product(1, 1, false);
                             p_ph1 ^= 1u;
                             if (ok && !more) t5::commit(&sh.o_full[1]);
-                            if (more) logits(1);
                         }
+                        if (ahead && two) logits(1);
                         if (ok) t5::commit(&sh.empty[vp.st]);
                         vp.next();
-                        if (more) {
+                        if (ahead) {
                             if (ok) t5::commit(&sh.empty[kp.st]);
-                            if (ok && j + 2 == units) t5::commit(&sh.q_empty);
+                            if (ok && (more ? j + 2 == n : units == 1)) t5::commit(&sh.q_empty);
                             kp.next();
                         }
                     }
                     ++out0;
-                    if (two) ++out1;
-                    ++seg;
+                    if (both) ++out1;
                 }
                 t5::commit(&sh.drained);                                  // MMAs in flight end before the tensor memory is given back
                 ok = ptx::mbar_wait(&sh.drained, 0u) && ok;
                 if (!ok) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
             }
+        } else {
+            // ------------------------------------------------ values that rows do not see: two warps
+            const int ht = tid & 63;
+            int tiles = 0, asked = 0, seg = 0;
+            while (walk.next(w, LG)) {
+                const int units = walk.units();
+                if (units == 0) continue;
+                for (int j = 0; j < units && ok; ++j) {
+                    const int t = walk.t0 + j;
+                    if (!walk.cleans(t)) continue;
+                    // The MMA thread asks when the tile that was in this ring slot before has landed for certain (a wait for a phase two
+                    // ahead of the barrier's would be over at once).
+                    const int v = 2 * (tiles + j) + 1, st = v % RING;
+                    ok = pre_wait_long(sh, &sh.v_ask, (uint32_t)(asked & 1)) && ptx::mbar_wait(&sh.full[st], (uint32_t)((v / RING) & 1));
+                    ok = __all_sync(0xffffffffu, ok);
+                    ++asked;
+                    if (!ok) break;
+                    unsigned char* vt = ring + (size_t)st * kPreSlot;
+                    const int n_valid = walk.valid_of(t), first = max(walk.plain_of(t), 0);
+                    auto at = [&](int i) {                                // 16 bytes of the tile, the swizzle's way
+                        const int rr = i >> 4, c = i & 15;
+                        return reinterpret_cast<uint4*>(vt + (size_t)(c >> 3) * kPreHalf + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
+                    };
+                    const int held = min(n_valid, kPreTile) * 16;
+                    bool cleared = false;
+#pragma unroll 4
+                    for (int i = first * 16 + ht; i < held; i += 64) {
+                        uint4 val = *at(i);
+                        uint32_t* e = reinterpret_cast<uint32_t*>(&val);
+                        __nv_bfloat162 any = __float2bfloat162_rn(0.0f);  // 0 x value summed up: NaN where one is not finite
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) any = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&e[h]), __float2bfloat162_rn(0.0f), any);
+                        if (__hbeq2(any, any)) continue;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            if ((e[h] & 0x00007f80u) == 0x00007f80u) e[h] &= 0xffff0000u;
+                            if ((e[h] & 0x7f800000u) == 0x7f800000u) e[h] &= 0x0000ffffu;
+                        }
+                        *at(i) = val;
+                        cleared = true;
+                    }
+                    for (int i = max(held, 0) + ht; i < kPreTile * 16; i += 64) *at(i) = make_uint4(0u, 0u, 0u, 0u);
+                    if (cleared) sh.not_finite[seg & 3] = seg + 1;
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sh.v_clean);
+                }
+                tiles += units;
+                ++seg;
+            }
+            if (!ok && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 " PRE_ROW_REGS ";");
         // ------------------------------------------------ rows: a thread each
-        const int x = warp >> 2, row = (warp & 3) * 32 + lane, gt = tid & 127;
+        const int x = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t s_addr = tmem + (uint32_t)x * 256u + ((uint32_t)((warp & 3) * 32) << 16), o_addr = s_addr + 128u;
         const float scale2 = a.scale * 1.4426950408889634f;
         const int my_token = row / a.r, my_head = row - my_token * a.r;
         const int n_cta = sh.n_cta;
-        int cnt = 0, done = 0, tiles = 0, seg = 0;       // units and shares of this slot; tiles and shares of the CTA
+        int cnt = 0, done = 0, seg = 0;                  // units and shares of this slot; shares of the CTA
         auto wait = [&](uint64_t* bar, int phase) {
             if (ok) ok = ptx::mbar_wait(bar, (uint32_t)(phase & 1));
             ok = __all_sync(0xffffffffu, ok);
         };
-        while (walk.next(w, LG)) {
+        // The walk's state lies in shared memory, a copy a warp: beside a row's 128 logits there is no room for it in registers.
+        PreWalk& walk = sh.walk[warp];
+        if (lane == 0) walk = walk0;
+        auto next = [&]() {
+            __syncwarp();
+            if (lane == 0) {
+                PreWalk t = walk;
+                t.more = t.next(w, LG);
+                walk = t;
+            }
+            __syncwarp();
+            return walk.more;
+        };
+        while (next()) {
             const int units = walk.units();
             const bool mine = x == 0 || walk.rows2;
             const int first_token = walk.m0 + x * tpt, token = first_token + my_token;
@@ -499,44 +620,16 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             if (mine) {
                 const bool warp_live = __any_sync(0xffffffffu, live);
                 float ref = -INFINITY, sum = 0.0f;
-                bool cleared = false;
+                // tokens that this row sees from the share's first tile on, as far as tiles are the view's, and behind
+                const int view_units = walk.view_tiles - walk.t0, view_seen = walk.n_view - walk.t0 * kPreTile;
+                const int tail_seen = walk.n_tail + min(token + 1, walk.n_q) + view_units * kPreTile;
+                if (x == 1) {                                          // (slot 0 may have had shares to itself in between)
+                    if (ok) ok = pre_wait_long(sh, &sh.s_full[1], (uint32_t)(cnt & 1));
+                    ok = __all_sync(0xffffffffu, ok);
+                }
                 for (int j = 0; j < units; ++j) {
-                    const int t = walk.t0 + j;
-                    const bool in_view = t < walk.view_tiles;
-                    const int c0 = (in_view ? t : t - walk.view_tiles) * kPreTile;        // the tile's first token in view or tail
-                    const int n_valid = (in_view ? walk.n_view : walk.n_tail + walk.n_q) - c0;
                     wait(&sh.s_full[x], cnt);
                     ++cnt;
-                    if (x == 0 && (n_valid < kPreTile || (!in_view && c0 + kPreTile > walk.n_tail + walk.m0 + 1))) {
-                        // Values behind the last token become zero, and those of tokens behind the group's first that are not finite.  The tile
-                        // that was in this ring slot before has landed for certain once these logits are there (a wait for a phase two
-                        // ahead of the barrier's would be over at once).
-                        const int v = 2 * (tiles + j) + 1, st = v % RING;
-                        wait(&sh.full[st], v / RING);
-                        unsigned char* vt = ring + (size_t)st * kPreSlot;
-                        const int first = in_view ? n_valid : min(max(walk.n_tail + walk.m0 + 1 - c0, 0), n_valid);
-                        for (int i = max(first, 0) * 16 + gt; i < kPreTile * 16; i += 128) {
-                            const int rr = i >> 4, c = i & 15;
-                            uint4* p = reinterpret_cast<uint4*>(vt + (size_t)(c >> 3) * kPreHalf + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
-                            uint4 val = make_uint4(0u, 0u, 0u, 0u);
-                            bool put = true;
-                            if (rr < n_valid) {
-                                val = *p;
-                                put = false;
-                                uint32_t* e = reinterpret_cast<uint32_t*>(&val);
-#pragma unroll
-                                for (int h = 0; h < 4; ++h) {
-                                    if ((e[h] & 0x00007f80u) == 0x00007f80u) { e[h] &= 0xffff0000u; put = true; }
-                                    if ((e[h] & 0x7f800000u) == 0x7f800000u) { e[h] &= 0x0000ffffu; put = true; }
-                                }
-                                cleared |= put;
-                            }
-                            if (put) *p = val;
-                        }
-                        if (cleared) sh.not_finite[seg & 1] = seg + 1;
-                        ptx::fence_proxy_async_smem();
-                        __syncwarp();
-                    }
                     if (warp_live) {
                         t5::fence_after();
                         uint32_t sv[4][32];
@@ -545,7 +638,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
                         for (int c = 0; c < 4; ++c) t5::ld_wait(sv[c]);
                         // columns that this row sees: [0, seen)
-                        const int seen = in_view ? n_valid : min(walk.n_tail + token + 1 - c0, n_valid);
+                        const int seen = (j < view_units ? view_seen : tail_seen) - j * kPreTile;
                         if (__any_sync(0xffffffffu, seen < kPreTile)) {
 #pragma unroll
                             for (int c = 0; c < 4; ++c)
@@ -626,7 +719,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 wait(&sh.o_full[x], done++);
                 const bool whole = walk.t0 == 0 && walk.t1 == walk.tiles;
                 const int share = 2 * ((walk.part - 1) * n_cta + (int)blockIdx.x) + (walk.t0 == 0 ? 1 : 0);
-                const bool nf = *(volatile int*)&sh.not_finite[seg & 1] == seg + 1;
+                const bool nf = *(volatile int*)&sh.not_finite[seg & 3] == seg + 1;
                 if (warp_live) {
                     t5::fence_after();
                     const bool none = sum == 0.0f;
@@ -650,7 +743,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                             t5::ld_wait(ov[1]);
                             float* o = reinterpret_cast<float*>(ov);
 #pragma unroll
-                            for (int i = 0; i < 64; ++i) o[i] = none ? 0.0f : o[i] * inv;
+                            for (int i = 0; i < 32; ++i) f2::unpk(f2::mul(f2::pk(o[2 * i], o[2 * i + 1]), f2::pk(inv, inv)), o[2 * i], o[2 * i + 1]);
                             if (nf && live && !none) {
                                 // values that were cleared and that this row sees
                                 for (int tok = walk.m0 + 1; tok <= token; ++tok) {
@@ -663,19 +756,22 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                                 }
                             }
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) pk[i] = ptx::pack_bf16x2(o[2 * i], o[2 * i + 1]);
+                            for (int i = 0; i < 32; ++i) pk[i] = none ? 0u : ptx::pack_bf16x2(o[2 * i], o[2 * i + 1]);
                             __syncwarp();
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + 128u * lane + 16u * (i ^ (lane & 7))), "r"(pk[4 * i]), "r"(pk[4 * i + 1]), "r"(pk[4 * i + 2]), "r"(pk[4 * i + 3]) : "memory");
                             __syncwarp();
+                            uint32_t vv[8][4];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 const int rr = i * 4 + (lane >> 3);
-                                uint32_t v[4];
+                                uint32_t (&v)[4] = vv[i];
                                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(stage + 128u * rr + 16u * ((lane & 7) ^ (rr & 7))) : "memory");
-                                if (to[i]) asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to[i] + 128 * c + 16 * (lane & 7)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
                             }
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if (to[i]) asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to[i] + 128 * c + 16 * (lane & 7)), "r"(vv[i][0]), "r"(vv[i][1]), "r"(vv[i][2]), "r"(vv[i][3]) : "memory");
                         }
                         if (live) a.lse[orow] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
                     } else {
@@ -705,7 +801,6 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     w.nf[share] = nf;
                 }
             }
-            tiles += units;
             ++seg;
         }
         if (!ok && lane == 0) atomicExch(a.status, (int)KVMEM_E_TIMEOUT);

@@ -755,8 +755,9 @@ int kvmem_commit_blocks(kvmem_pool_t* pool, int32_t session_first, int32_t n_ses
 
 /* Attention of a prompt chunk over view and tail: kvmem_view_tree_attend for a chain (token i sees the view, the committed tail
  * tokens and the chunk's tokens 0 .. i) of any length.  Same arguments (tail NULL: the view alone), definitions, guarantees and
- * error values, and the same bits from run to run.  Chunks of up to 64 tokens are that call, with its kernel, workspace and limits.
- * Longer ones: 4 head_dim flops per query row and visible token on the tensor cores; at most 128 query heads may share a KV head;
+ * error values, and the same bits from run to run.  Chunks of up to 64 tokens with few query rows (H/G n_q_tokens below 448, or
+ * n_sessions L H n_q_tokens below 2,560, or H/G above 128) are that call, with its kernel, workspace and limits.
+ * Others: 4 head_dim flops per query row and visible token on the tensor cores; at most 128 query heads may share a KV head;
  *   workspace  DEVICE, kvmem_prefill_workspace_bytes(), 256-byte aligned (about 160 MB whatever the call); calls that may overlap on
  *              the GPU need one each
  * A call is limited to 2^30 tiles, counted from the capacities: one for each 128 tokens of view and tail, either rounded up, and 4 more,

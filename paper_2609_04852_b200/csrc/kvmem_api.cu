@@ -1632,16 +1632,26 @@ static int prefill_sizes(const kvmem_pool_config_t& c, int32_t n_sessions, int32
     return KVMEM_OK;
 }
 
-// A chunk of up to 64 tokens is a chain of drafted ones: the decode kernel, which shares a tile's two slots out between tokens where rows
-// are few (32 query heads on 8 KV heads, 1 / 33 / 64 tokens: 12 / 18 / 20 us instead of 24 / 27 / 29 at 2,048, 29 / 47 / 50 instead of
-// 52 / 62 / 61 at 32,768, 85 / 133 / 150 instead of 125 / 136 / 165 at 131,072; 64 heads on 8, 64 tokens: 25 and 29, 82 and 83, 300 and
-// 310).
-static bool chunk_is_chain(int32_t n_q_tokens) { return n_q_tokens >= 1 && n_q_tokens <= kMaxDrafted; }
+// A chunk of up to 64 tokens is a chain of drafted ones, and where its query rows are few the decode kernel is faster: it shares a tile's
+// two slots out between tokens.  With more rows the chunk's own kernel is.  Measured, 64-token blocks, tail of 40, us at 2,048 / 16,384 /
+// 65,536 tokens, decode kernel and chunk kernel:
+//   64 heads on 8, 48 tokens (384 rows a KV head, 3,072 in all)     24 / 43 / 129    23 / 47 / 131
+//   64 heads on 8, 64 tokens (512 and 4,096)                        25 / 51 / 170    25 / 50 / 143
+//   64 heads on 4, 33 tokens (528 and 2,112)                        25 / 37 / 102    26 / 40 / 108
+//   64 heads on 4, 64 tokens (1,024 and 4,096)                      25 / 51 / 179    25 / 47 / 137
+//   128 heads on 4, 16 tokens (512 and 2,048)                       23 / 34 / 80     29 / 38 / 80
+//   128 heads on 4, 24 tokens (768 and 3,072)                       26 / 44 / 120    26 / 42 / 108
+//   32 heads on 8, 64 tokens (256 and 2,048), 2,048 / 32,768        20 / 50          26 / 57
+static bool chunk_is_chain(const kvmem_pool_config_t& c, int32_t n_sessions, int32_t n_q_tokens) {
+    if (n_q_tokens < 1 || n_q_tokens > kMaxDrafted) return false;
+    const int64_t share = c.n_q_heads / c.n_kv_heads, rows = (int64_t)n_sessions * c.n_layers * c.n_q_heads * n_q_tokens;
+    return share > 128 || share * n_q_tokens < 448 || rows < 2560;
+}
 
 size_t kvmem_prefill_workspace_bytes(const kvmem_pool_config_t* cfg, int32_t n_sessions, int32_t n_q_tokens) {
     const char* why = "";
     if (!cfg || !config_valid(*cfg, &why)) { set_error("invalid arguments to kvmem_prefill_workspace_bytes"); return 0; }
-    if (chunk_is_chain(n_q_tokens)) return tree_bytes(cfg, n_sessions, n_q_tokens, 0, "kvmem_prefill_workspace_bytes");
+    if (chunk_is_chain(*cfg, n_sessions, n_q_tokens)) return tree_bytes(cfg, n_sessions, n_q_tokens, 0, "kvmem_prefill_workspace_bytes");
     if (prefill_sizes(*cfg, n_sessions, n_q_tokens, 0, 0) != KVMEM_OK) return 0;
     return prefill_workspace_bytes(*cfg);
 }
@@ -1652,7 +1662,7 @@ int kvmem_view_prefill_attend(kvmem_pool_t* p, int32_t n_sessions, const void* q
                               void* stream) {
     const char* who = "kvmem_view_prefill_attend";
     if (!pool_live(p)) return KVMEM_E_STATE;
-    if (chunk_is_chain(n_q_tokens))
+    if (chunk_is_chain(p->cfg, n_sessions, n_q_tokens))
         return kvmem_view_tree_attend(p, n_sessions, q, n_q_tokens, n_q, nullptr, view_k, view_v, view_cap_tokens, n_sel, tail, scale, out, lse, workspace,
                                       workspace_bytes, stream);
     const Geometry& g = p->geo;

@@ -23,12 +23,21 @@
 // does not grow with the call.
 // Where the keys and values of all KV heads are more than L2 holds, the line is cut into several parts for each CTA, the c-th of n from
 // c on in steps of n: all CTAs then work on a few heads at a time and find their tiles in L2 after the first.  (In one sweep over
-// eight heads of 33 MB the CTAs are spread over all of them and read every tile from HBM: 2,048 tokens over 65,536 take 2,420 us at
-// 1,425 MHz under the power limit; in four sweeps 2,190 us at 1,640 MHz.)
+// eight heads of 33 MB the CTAs are spread over all of them and read every tile from HBM: 2,048 tokens over 65,536 take 2,200 us at
+// 1,342 MHz under the power limit; in four sweeps 1,937 us at 1,567 MHz.)
 //
 // Tokens that a row does not see: their logits are replaced before they are used, values behind the last token are cleared in shared
 // memory before the second product (0 x NaN), and so are values that are not finite of chunk tokens that only some rows see; the
-// rows that do see them get them at the end.
+// rows that do see them get them at the end.  Two warps of their own look at those values while the logits are on their way (by the row
+// warps: 159 us instead of 155 for a chunk of 4,096 alone).
+//
+// What bounds it: under a long view the power limit (960 W at 1,567 MHz) and the chain S -> weights -> O of each slot: 3,300 cycles per
+// 128 tokens of 256 rows, where the products alone take 2,048 by their rate, 2,724 with operands that lie in shared memory already, some
+// 2,900 with the tiles' loads beside them.  2,048 tokens of 32 heads on 8 over 65,536: 1,705 us before the power limit bites, 1,915 behind
+// it (1,310 and 1,168 TFLOP/s).  Short calls: 2 us of plan, 2.6 to the first tile, 2 us for a CTA's every further item, 5 of joining.
+// Measured and dropped: two threads a row (16 row warps; 221 us instead of 197 for 4,096 alone), an MMA thread a slot (170, 163), S in two
+// halves of 64 tokens (211, 195), a part of the exponentials by a polynomial (an eighth: 174, 155), fewer tokens in the last product of
+// a causal item (171, 162: what the MMA thread does between two products costs more).
 #include <cudaTypedefs.h>
 #include <math.h>
 
@@ -49,15 +58,16 @@ constexpr int kPreRing = 4;                      // K and V tiles in turn
 constexpr int kPreStage = 4096;                  // bytes of a row warp's staging for stores
 constexpr int kPreThreads = 384;                 // eight row warps, TMA warp, MMA warp, two for values that rows do not see
 constexpr int kPreTmaWarp = 8, kPreMmaWarp = 9;
-// Registers a thread: the launch gives 168, the row warps take 208 and the others keep 80.  (Without: a row's 128 logits do not fit, and a
-// spill is slow here, where shared memory leaves the L1 no room for it: 220 us instead of 206 for a chunk of 4,096 alone.)
+// Registers a thread: the launch gives 168, the row warps take 208 and the others keep 88.  (Without: a row's 128 logits do not fit, and a
+// spill is slow here, where shared memory leaves the L1 no room for it: 220 us instead of 206 for a chunk of 4,096 alone.  With 80 for
+// the others 161 instead of 159.)
 #define PRE_ROW_REGS "208"
 #define PRE_OTHER_REGS "88"
 static_assert(256 * 208 + 128 * 88 <= kPreThreads * 168, "the registers that the row warps take are those the others give");
-constexpr int kPreLead = 3;                      // units on the line for an item's start and end: what they cost a CTA, in tiles (1: 195 and 314 us
-                                                 // instead of 170 and 234 for a chunk of 4,096 alone and three ragged sessions)
-constexpr float kPreLimit = 4096.0f;              // half a tile's weights may sum to this before their reference moves (2^8 and 2^64 instead: 2,152 and
-                                                  // 2,081 us against 2,090 for 2,048 tokens over 65,536; a value may be 2^115 before its sum overflows)
+constexpr int kPreLead = 3;                      // units on the line for an item's start and end: what they cost a CTA, in tiles (1: 170 and 243 us,
+                                                 // 5: 159 and 212, instead of 155 and 214 for a chunk of 4,096 alone and three ragged sessions)
+constexpr float kPreLimit = 4096.0f;              // half a tile's weights may sum to this before their reference moves (2^8 and 2^64 instead: 2,012 and
+                                                  // 1,918 us against 1,919 for 2,048 tokens over 65,536; a value may be 2^115 before its sum overflows)
 constexpr int kPreParts = 4;                     // parts of the line a CTA can have
 constexpr int kPreBudget = 1024;                 // tiles of keys and values (64 KiB each) that a sweep of all CTAs may hold in L2
 constexpr int kPrePartUnits = 64;                // least units of a part, when there is more than one
@@ -816,8 +826,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 // Joins the shares of the items that cuts of the line fall into, in line order: for every part c, the item whose first cut is the part's
 // start, if there is one.  The grid's first axis goes over the parts, the second is the slot and 32 of the dims.  A warp has 32 rows, a
 // lane each, and 16 dims: its reads are whole lines.  Bound by latency (a round of dependent reads costs some 0.6 us): two shares
-// are requested together, and blocks go on to the next part rather than be many and mostly empty (three ragged sessions: 221
-// us; with a block a part 229).
+// are requested together, and blocks go on to the next part rather than be many and mostly empty.
 constexpr int kPreMergeThreads = 256, kPreMergeBatch = 2;
 __global__ void __launch_bounds__(kPreMergeThreads, 4)
 prefill_merge_kernel(const __grid_constant__ PreWork w) {

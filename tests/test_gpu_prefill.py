@@ -115,6 +115,11 @@ GEOMETRIES = [
     dict(M=200, B=256, lens=(2,), tails=(300,)),
     dict(M=130, lens=(30,), scale=0.02),
     dict(M=64, H=32, G=8, lens=(9,), tails=(11,)),
+    # up to 64 tokens with many query rows, and one token fewer than that takes
+    dict(M=64, H=64, G=8, lens=(9,), tails=(11,)),
+    dict(M=56, H=64, G=8, lens=(0,), tails=(129,)),
+    dict(M=55, H=64, G=8, lens=(5,), tails=(100,)),
+    dict(ns=3, M=4, H=256, G=2, lens=(0, 3, 1), n_q=(4, 0, 3), tails=(3, 0, 200)),
 ]
 
 

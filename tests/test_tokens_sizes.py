@@ -87,6 +87,13 @@ def test_chunk_workspace_sizes():
     assert size(cfg, 1, 65) == size(cfg, 4, 100000) > 0                                     # the same whatever the call
     for M in (1, 17, 64):
         assert size(cfg, 3, M) == lib.kvmem_tree_workspace_bytes(C.byref(cfg), 3, M) > 0    # the decode kernel's
+    many = config(n_q_heads=64)                                                             # 448 rows of a KV head and 2,560 in all
+    assert size(many, 1, 56) == size(cfg, 1, 65) and size(many, 1, 55) == lib.kvmem_tree_workspace_bytes(C.byref(many), 1, 55)
+    many = config(n_q_heads=64, n_kv_heads=1)
+    assert size(many, 1, 40) == size(cfg, 1, 65) and size(many, 1, 39) == lib.kvmem_tree_workspace_bytes(C.byref(many), 1, 39)
+    assert size(many, 2, 20) == size(cfg, 1, 65) and size(many, 5, 6) == lib.kvmem_tree_workspace_bytes(C.byref(many), 5, 6)
+    many = config(n_q_heads=129, n_kv_heads=1)
+    assert size(many, 1, 64) == lib.kvmem_tree_workspace_bytes(C.byref(many), 1, 64)
     for bad, ns, M in ((cfg, 0, 100), (cfg, 65536, 100), (cfg, 1, 0), (cfg, 1, -5), (config(head_dim=64), 1, 100), (config(n_q_heads=129, n_kv_heads=1), 1, 100),
                        (config(n_kv_heads=5), 1, 100), (cfg, 1, 65535 * 64 + 1), (cfg, 65535, 65535)):
         assert size(bad, ns, M) == 0 and lib.kvmem_last_error()

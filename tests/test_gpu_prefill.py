@@ -248,6 +248,31 @@ def test_values_that_are_not_finite_in_the_last_tokens(M, H, lens):
     assert torch.equal(c.out[0, M - 1][..., same], clean.out[0, M - 1][..., same])
 
 
+def test_values_that_are_not_finite_in_many_short_items():
+    """Every CTA with several items in turn, of one and of two row tiles, each with an infinite value at another token: it reaches the
+    tokens from its own on and nothing else."""
+    ns = 60
+    kw = dict(ns=ns, H=16, G=8, B=16, M=150, lens=[(5 * s) % 19 for s in range(ns)], n_q=[150 - (17 * s) % 90 for s in range(ns)],
+              tails=[(29 * s) % 150 for s in range(ns)], seed=13)
+    c, clean = Chunk(**kw), Chunk(**kw)
+    at = [(31 * s) % c.n_q[s] for s in range(ns)]
+    for s in range(ns):
+        c.tv[s, c.tails[s] + at[s], :, :, s] = math.inf
+    clean.call()
+    for _ in range(3):
+        c.call()
+        torch.cuda.synchronize()
+        for s in range(ns):
+            i, n = at[s], c.n_q[s]
+            assert torch.equal(c.out[s, :i], clean.out[s, :i]), s
+            assert bool((c.out[s, i:n, :, :, s] == math.inf).all()), s
+            same = torch.ones(D, dtype=torch.bool, device="cuda")
+            same[s] = False
+            assert torch.equal(c.out[s, i:n][..., same], clean.out[s, i:n][..., same]), s
+        assert torch.equal(c.lse, clean.lse)
+    c.guards.check()
+
+
 def test_large_logits_and_growing_maxima():
     """Keys that grow along the view, so that the running maximum moves in every tile; logits up to about 200."""
     c = Chunk(lens=(24,), M=130, seed=8, scale=0.5)

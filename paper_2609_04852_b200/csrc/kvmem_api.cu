@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <memory>
 #include <new>
 #include <thread>
 
@@ -252,8 +253,9 @@ int kvmem_pool_create(const kvmem_pool_config_t* cfg, void* storage, size_t byte
         const int half = cfg->head_dim / 2;
         std::vector<double> freq(half);
         for (int i = 0; i < half; ++i) freq[i] = pow((double)cfg->rope_theta, -2.0 * (double)i / (double)cfg->head_dim);
-        const int chunk = 32768;
-        std::vector<float2> rows((size_t)std::min(chunk, cfg->rope_max_positions) * half);
+        const int chunk = 8192;
+        const std::unique_ptr<float2[]> rows(new (std::nothrow) float2[(size_t)std::min(chunk, cfg->rope_max_positions) * half]);
+        if (!rows) { delete p; set_error("host allocation failed"); return KVMEM_E_CAPACITY; }
         for (int p0 = 0; e == cudaSuccess && p0 < cfg->rope_max_positions; p0 += chunk) {
             const int n = std::min(chunk, cfg->rope_max_positions - p0);
             on_threads(n, [&](int r0, int r1) {
@@ -263,7 +265,7 @@ int kvmem_pool_create(const kvmem_pool_config_t* cfg, void* storage, size_t byte
                         rows[(size_t)r * half + i] = make_float2((float)cos(ang), (float)sin(ang));
                     }
             });
-            e = cudaMemcpy(p->rope_dev + (size_t)p0 * half, rows.data(), (size_t)n * half * sizeof(float2), cudaMemcpyHostToDevice);
+            e = cudaMemcpy(p->rope_dev + (size_t)p0 * half, rows.get(), (size_t)n * half * sizeof(float2), cudaMemcpyHostToDevice);
         }
     }
     if (e == cudaSuccess) e = cudaDeviceSynchronize();

@@ -700,6 +700,20 @@ int kvmem_rope_apply(kvmem_pool_t* pool, const void* x /*DEVICE*/, int64_t x_row
                      void* y /*DEVICE*/, int64_t y_row_stride, int64_t y_vec_stride, int32_t y_order, int64_t n_rows, int32_t n_vec,
                      const int32_t* positions /*DEVICE*/, int32_t inverse, float amplitude, void* stream);
 
+/* The same call with its arguments in one struct, for callers that pay for each argument (a foreign-function interface): the launch of
+ * a few tokens takes 2.5 us of host time, sixteen converted arguments half of that again. */
+typedef struct {
+    kvmem_pool_t* pool;
+    const void* x;            /* DEVICE */
+    void* y;                  /* DEVICE */
+    const int32_t* positions; /* DEVICE */
+    void* stream;
+    int64_t n_rows, x_row_stride, x_vec_stride, y_row_stride, y_vec_stride;
+    int32_t n_vec, x_order, y_order, inverse;
+    float amplitude;
+} kvmem_rope_call_t;
+int kvmem_rope_apply_call(const kvmem_rope_call_t* call /*HOST*/);
+
 /* Pages for n_blocks blocks behind a session's last: taken from the pool now (phys_ids as in kvmem_append_blocks), filled by
  * kvmem_append_tokens, part of the session only once kvmem_commit_blocks makes them so (this call, that one and kvmem_set_rope are
  * refused as KVMEM_E_STATE on a stream that is being captured: they change what the host knows of the pool).  While a session has reserved blocks
@@ -743,6 +757,21 @@ int kvmem_append_tokens(kvmem_pool_t* pool, int32_t session_first, int32_t n_ses
                         const kvmem_rows_t* k /*HOST*/, const kvmem_rows_t* v /*HOST*/, const int32_t* positions /*DEVICE, may be NULL*/,
                         const int32_t* n_sel /*DEVICE, may be NULL*/, int32_t first_position, float q_amplitude,
                         const kvmem_tail_t* tail /*HOST*/, void* q_out /*DEVICE, may be NULL*/, int32_t to_pages, void* stream);
+
+/* The same call with its arguments in one struct (see kvmem_rope_apply_call); q.data NULL: no queries. */
+typedef struct {
+    kvmem_pool_t* pool;
+    const int32_t* n_new;     /* DEVICE, may be NULL */
+    kvmem_rows_t q, k, v;
+    const int32_t* positions; /* DEVICE, may be NULL */
+    const int32_t* n_sel;     /* DEVICE, may be NULL */
+    kvmem_tail_t tail;
+    void* q_out;              /* DEVICE, may be NULL */
+    void* stream;
+    int32_t session_first, n_sessions, n_new_tokens, first_position, to_pages;
+    float q_amplitude;
+} kvmem_append_call_t;
+int kvmem_append_tokens_call(const kvmem_append_call_t* call /*HOST*/);
 
 /* Make the first n_blocks[s] reserved blocks of each session part of it: their Mean-K rows are computed from the raw keys in
  * their pages (the bits that kvmem_append_blocks gives for the same keys), the session's length is raised and, with a tail, the

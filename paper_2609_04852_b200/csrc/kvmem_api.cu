@@ -1444,6 +1444,12 @@ int kvmem_rope_apply(kvmem_pool_t* p, const void* x, int64_t x_row_stride, int64
     return KVMEM_OK;
 }
 
+int kvmem_rope_apply_call(const kvmem_rope_call_t* c) {
+    if (!c) { set_error("null call"); return KVMEM_E_INVALID; }
+    return kvmem_rope_apply(c->pool, c->x, c->x_row_stride, c->x_vec_stride, c->x_order, c->y, c->y_row_stride, c->y_vec_stride, c->y_order, c->n_rows,
+                            c->n_vec, c->positions, c->inverse, c->amplitude, c->stream);
+}
+
 int kvmem_reserve_blocks(kvmem_pool_t* p, int32_t session, int32_t n_blocks, const int32_t* phys_ids, void* stream) {
     if (!pool_live(p)) return KVMEM_E_STATE;
     if (!sessions_ok(p, session, 1)) return KVMEM_E_INVALID;
@@ -1569,6 +1575,12 @@ int kvmem_append_tokens(kvmem_pool_t* p, int32_t session_first, int32_t n_sessio
     const cudaError_t e = launch_append_tokens(*p, a, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail("token append kernel launch", e);
     return KVMEM_OK;
+}
+
+int kvmem_append_tokens_call(const kvmem_append_call_t* c) {
+    if (!c) { set_error("null call"); return KVMEM_E_INVALID; }
+    return kvmem_append_tokens(c->pool, c->session_first, c->n_sessions, c->n_new_tokens, c->n_new, c->q.data ? &c->q : nullptr, &c->k, &c->v, c->positions,
+                               c->n_sel, c->first_position, c->q_amplitude, &c->tail, c->q_out, c->to_pages, c->stream);
 }
 
 int kvmem_commit_blocks(kvmem_pool_t* p, int32_t session_first, int32_t n_sessions, const int32_t* n_blocks, const kvmem_tail_t* tail, void* stream) {

@@ -124,9 +124,11 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "kvmem_rope_frequencies": (C.c_int, [cfgp, ropep, C.POINTER(C.c_double)]),
         "kvmem_set_rope": (C.c_int, [vp, ropep, vp]),
         "kvmem_rope_apply": (C.c_int, [vp, vp, i64, i64, i32, vp, i64, i64, i32, i64, i32, vp, i32, f32, vp]),
+        "kvmem_rope_apply_call": (C.c_int, [vp]),
         "kvmem_reserve_blocks": (C.c_int, [vp, i32, i32, C.POINTER(i32), vp]),
         "kvmem_session_reserved": (i32, [vp, i32]),
         "kvmem_append_tokens": (C.c_int, [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, i32, vp]),
+        "kvmem_append_tokens_call": (C.c_int, [vp]),
         "kvmem_commit_blocks": (C.c_int, [vp, i32, i32, C.POINTER(i32), tailp, vp]),
         "kvmem_prefill_workspace_bytes": (sz, [cfgp, i32, i32]),
         "kvmem_view_prefill_attend": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i32, vp, tailp, f32, vp, vp, vp, sz, vp]),
@@ -157,8 +159,8 @@ EXPORTED = ("kvmem_pool_bytes", "kvmem_budget_blocks", "kvmem_select_workspace_b
             "kvmem_paged_attend_fp8_rope", "kvmem_selftest_wait_timeout", "kvmem_selftest_joint_wait_timeout", "kvmem_materialize_delta",
             "kvmem_materialize_fp8_rope", "kvmem_tree_workspace_bytes", "kvmem_view_tree_attend", "kvmem_paged_tree_attend",
             "kvmem_mass_workspace_bytes", "kvmem_view_attend_mass", "kvmem_evict_workspace_bytes", "kvmem_view_evict",
-            "kvmem_rope_frequencies", "kvmem_set_rope", "kvmem_rope_apply", "kvmem_reserve_blocks", "kvmem_session_reserved",
-            "kvmem_append_tokens", "kvmem_commit_blocks", "kvmem_prefill_workspace_bytes", "kvmem_view_prefill_attend", "kvmem_get_pages")
+            "kvmem_rope_frequencies", "kvmem_set_rope", "kvmem_rope_apply", "kvmem_rope_apply_call", "kvmem_reserve_blocks", "kvmem_session_reserved",
+            "kvmem_append_tokens", "kvmem_append_tokens_call", "kvmem_commit_blocks", "kvmem_prefill_workspace_bytes", "kvmem_view_prefill_attend", "kvmem_get_pages")
 
 
 def _check(status: int) -> None:
@@ -189,18 +191,20 @@ def _place(name: str, t: torch.Tensor, dtype, shape: tuple, device: int) -> int:
     return t.data_ptr()
 
 
-# kvmem_rows_t and kvmem_tail_t as the append call takes them: packed into a buffer that the pool keeps (building ctypes structures takes
-# longer than the call)
-_ROWS, _TAIL = struct.Struct("P4q"), struct.Struct("PPiP")
+# kvmem_append_call_t and kvmem_rope_call_t, packed into buffers that the pool keeps (building ctypes structures, or converting sixteen
+# arguments, takes as long as the launch)
+_APPEND, _ROPE = struct.Struct("PP" + 3 * "P4q" + "PP" + "PPiP" + "PP" + "5if"), struct.Struct("5P5q4if")
+_NO_ROWS = (0, 0, 0, 0, 0)
 
 
-def _rows(name: str, t: torch.Tensor, shape: tuple, device: int, buf, at: int) -> None:
-    """Rows [n_sessions][n_tokens][L][heads][d] of any strides but the last: a slice of a packed projection, read where it lies."""
+def _rows(name: str, t: torch.Tensor, shape: tuple, device: int) -> tuple:
+    """Pointer and strides of rows [n_sessions][n_tokens][L][heads][d] of any strides but the last: a slice of a packed projection, read
+    where it lies."""
     st = t.stride()
     if t.dtype is not _BF16 or t.shape != shape or t.get_device() != device or st[4] != 1:
         raise ValueError(f"{name}: expected a bf16 tensor {tuple(shape)} on cuda:{device} with contiguous heads, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device} with strides {st}")
-    _ROWS.pack_into(buf, at, t.data_ptr(), *st[:4])
+    return (t.data_ptr(), *st[:4])
 
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -313,8 +317,8 @@ class Pool:
         self._decode_pinned = False                                    # a captured graph or another stream may still write it
         self._decode_kept: List[torch.Tensor] = []                     # smaller ones of which that holds
         self._decode_need: Dict[tuple, int] = {}
-        self._append_buf = C.create_string_buffer(3 * _ROWS.size + _TAIL.size)         # rows of k, v, q and the tail of an append
-        self._append_at = C.addressof(self._append_buf)
+        self._append_buf, self._rope_buf = C.create_string_buffer(_APPEND.size), C.create_string_buffer(_ROPE.size)
+        self._append_at, self._rope_at = C.addressof(self._append_buf), C.addressof(self._rope_buf)
 
     # ---- lifetime
     def close(self) -> None:
@@ -654,8 +658,9 @@ class Pool:
         pp = _place("positions", positions, _I32, (n_rows,), dev)
         xo, yo = _one_of("x_order", x_order, ORDERS), _one_of("out_order", out_order, ORDERS)
         if n_rows and n_vec:
-            rc = self.lib.kvmem_rope_apply(self.handle, x.data_ptr(), xs[0], xs[1], xo, out.data_ptr(), ys[0], ys[1], yo, n_rows, n_vec, pp,
-                                           int(inverse), amplitude, self._raw_stream())
+            _ROPE.pack_into(self._rope_buf, 0, self.handle.value or 0, x.data_ptr(), out.data_ptr(), pp, self._raw_stream(), n_rows, xs[0], xs[1],
+                            ys[0], ys[1], n_vec, xo, yo, bool(inverse), amplitude)
+            rc = self.lib.kvmem_rope_apply_call(self._rope_at)
             if rc:
                 _check(rc)
         return out
@@ -696,22 +701,18 @@ class Pool:
             raise ValueError("k: expected [n_sessions][n_new_tokens][L][G][d]")
         ns, M, _, _, _ = shape
         kv, qs, per_session = (ns, M, L, G, d), (ns, M, L, H, d), (ns,)
-        buf, at, size = self._append_buf, self._append_at, _ROWS.size
-        _rows("k", k, kv, dev, buf, 0)
-        _rows("v", v, kv, dev, buf, size)
-        if q is not None:
-            _rows("q", q, qs, dev, buf, 2 * size)
         tk = tail.k
         cap = tk.shape[1] if tk.dim() == 5 else -1
         ts = (ns, cap, L, G, d)
-        _TAIL.pack_into(buf, 3 * size, _place("tail.k", tk, _BF16, ts, dev), _place("tail.v", tail.v, _BF16, ts, dev), cap,
-                        _place("tail.n_tokens", tail.n_tokens, _I32, per_session, dev))
-        qo = None if q_out is None else _place("q_out", q_out, _BF16, qs, dev)
-        nn = None if n_new is None else _place("n_new", n_new, _I32, per_session, dev)
-        pp = None if positions is None else _place("positions", positions, _I32, (ns, M), dev)
-        np_ = None if n_sel is None else _place("n_sel", n_sel, _I32, per_session, dev)
-        rc = self.lib.kvmem_append_tokens(self.handle, session_first, ns, M, nn, None if q is None else at + 2 * size, at, at + size, pp, np_,
-                                          first_position, q_amplitude, at + 3 * size, qo, int(pages), self._raw_stream())
+        _APPEND.pack_into(
+            self._append_buf, 0, self.handle.value or 0, 0 if n_new is None else _place("n_new", n_new, _I32, per_session, dev),
+            *(_NO_ROWS if q is None else _rows("q", q, qs, dev)), *_rows("k", k, kv, dev), *_rows("v", v, kv, dev),
+            0 if positions is None else _place("positions", positions, _I32, (ns, M), dev),
+            0 if n_sel is None else _place("n_sel", n_sel, _I32, per_session, dev),
+            _place("tail.k", tk, _BF16, ts, dev), _place("tail.v", tail.v, _BF16, ts, dev), cap,
+            _place("tail.n_tokens", tail.n_tokens, _I32, per_session, dev), 0 if q_out is None else _place("q_out", q_out, _BF16, qs, dev),
+            self._raw_stream(), session_first, ns, M, first_position, bool(pages), q_amplitude)
+        rc = self.lib.kvmem_append_tokens_call(self._append_at)
         if rc:
             _check(rc)
 

@@ -107,6 +107,9 @@ def test_calls_without_a_pool_fail_cleanly():
     assert lib.kvmem_set_rope(None, None, None) == kvmem.E_STATE
     assert lib.kvmem_rope_apply(None, None, 0, 0, 0, None, 0, 0, 0, 1, 1, None, 0, 1.0, None) == kvmem.E_STATE
     assert lib.kvmem_reserve_blocks(None, 0, 1, None, None) == kvmem.E_STATE
+    assert lib.kvmem_rope_apply_call(None) == kvmem.E_INVALID and lib.kvmem_append_tokens_call(None) == kvmem.E_INVALID
+    assert lib.kvmem_rope_apply_call(C.create_string_buffer(1024)) == kvmem.E_STATE                    # all zeros: no pool
+    assert lib.kvmem_append_tokens_call(C.create_string_buffer(1024)) == kvmem.E_STATE
     assert lib.kvmem_session_reserved(None, 0) == kvmem.E_STATE
     assert lib.kvmem_append_tokens(None, 0, 1, 1, None, None, None, None, None, None, 0, 1.0, None, None, 0, None) == kvmem.E_STATE
     assert lib.kvmem_commit_blocks(None, 0, 1, one, None, None) == kvmem.E_STATE

@@ -744,6 +744,8 @@ typedef struct {
  * tail->n_tokens is read, not changed: the tokens are drafted ones for kvmem_view_tree_attend and kvmem_view_prefill_attend;
  * adding to it commits them, calling again replaces them.  Counts and lengths are read on the device, so a captured call appends
  * wherever the tail then ends.  to_pages goes with a tail whose row 0 is the token behind the session's last block.
+ * A tail's keys stay at the positions that they were turned to.  The positions counted here from rows go on behind them only as long as
+ * row 0 of the tail and the view in front of it are those of the calls before: see kvmem_commit_blocks for what to do when they are not.
  *   n_new     DEVICE int32 [n_sessions] (clamped to [0, n_new_tokens]); NULL: n_new_tokens each.  Rows behind are left as they were
  *   q         HOST struct, n_q_heads heads per layer; NULL (with q_out NULL): keys and values alone.  k, v: n_kv_heads heads
  *   positions DEVICE int32 [n_sessions][n_new_tokens], or NULL
@@ -777,6 +779,15 @@ int kvmem_append_tokens_call(const kvmem_append_call_t* call /*HOST*/);
  * their pages (the bits that kvmem_append_blocks gives for the same keys), the session's length is raised and, with a tail, the
  * rows behind them move to its front and n_tokens[s] drops by n_blocks[s] * block_tokens.  (n_tokens below that is flagged as
  * KVMEM_E_DEVICE_RANGE: a block was committed before its tokens were there.)
+ * The rows that move keep their bits: row r then holds a key at the position of row r + n_blocks[s] * block_tokens.  Whatever changes
+ * where the rows or the view in front of them begin (a commit; another view, i.e. every recall that changes n_sel or first_position) asks
+ * for one of these before the next call that appends to the tail or attends over it; nothing on the device can tell that it is missing:
+ *   - the view grows at its end by the committed blocks (n_sel[s] by n_blocks[s], first_position as it was): positions fit as they are;
+ *   - the view stays as it was, the committed tokens out of sight until a recall: kvmem_append_tokens with first_position larger by
+ *     n_blocks[s] * block_tokens (or with positions, where sessions differ), so that new tokens go on behind the tail's;
+ *   - any other view: the tail's keys come to their new positions.  Either n_tokens[s] = 0 and the raw keys and values of the rows are
+ *     appended again (one rounding, as at first), or the tail's keys are turned in place by the difference, kvmem_rope_apply from
+ *     KVMEM_ORDER_POOL to KVMEM_ORDER_POOL, inverse where they go down (no raw keys needed, but one rounding to bf16 more each time).
  *   n_blocks  HOST int32 [n_sessions]; KVMEM_E_STATE if a session has fewer reserved
  *   tail      HOST struct, may be NULL; entry s is session session_first + s */
 int kvmem_commit_blocks(kvmem_pool_t* pool, int32_t session_first, int32_t n_sessions, const int32_t* n_blocks /*HOST*/,

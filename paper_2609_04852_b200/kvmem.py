@@ -693,7 +693,7 @@ class Pool:
         """New tokens behind the tail's committed ones: q bf16 [n_sessions][M][L][H][d] (optional, with q_out of that shape), k, v
         [n_sessions][M][L][G][d], strided as they lie.  Rotated queries go to q_out, rotated keys and values to the tail, with pages
         raw keys and values to the reserved pages as well.  Positions are positions int32 [n_sessions][M], or first_position +
-        n_sel * block_tokens + the tail's row."""
+        n_sel * block_tokens + the tail's row; what the tail holds already stays where it is (see commit_blocks)."""
         L, H, G, d = self._dims
         dev = self._index
         shape = k.shape
@@ -718,7 +718,9 @@ class Pool:
 
     def commit_blocks(self, n_blocks: Sequence[int], tail: Optional[Tail] = None, session_first: int = 0) -> None:
         """The first n_blocks[s] reserved blocks of each session become part of it, with their index rows; the tail's rows behind
-        them move to its front."""
+        them move to its front, their keys at the positions that they had.  Before the next append or attention: a view that has grown by
+        these blocks, or a first_position that has grown by their tokens, or keys brought to their new positions by rope_apply in the
+        "pool" order or by appending them again (kvmem_commit_blocks in the header)."""
         ns = len(n_blocks)
         ts = None if tail is None else self._tail_struct(tail, ns)
         _check(self.lib.kvmem_commit_blocks(self.handle, session_first, ns, (C.c_int32 * max(ns, 1))(*[int(x) for x in n_blocks]), ts,

@@ -11,9 +11,10 @@
 // thread fetches Q, K and V tiles with TMA (128-byte swizzle), one thread issues the MMAs: those of one thread run in order, so a
 // slot's next S is issued right behind the product that reads its P, in whose place it goes.
 //
-// ref is the largest logit of the first tokens a row sees.  It moves only when half a tile's weights sum to more than 2^12: O is then
-// rescaled in tensor memory and the half's weights are computed again.  Until then they may be that large, which costs neither fp32
-// nor bf16 any precision, and no tile needs the maximum of its logits.
+// ref is the largest logit of the first tokens a row sees.  It moves only when the row's weights sum to more than 2^15, to that sum's
+// logarithm or to the half tile's largest logit, whichever is more: O is then rescaled in tensor memory and the half's weights are
+// computed again.  Until then they may be that large, which costs neither fp32 nor bf16 any precision, and no tile needs the maximum of
+// its logits.  O stays below 2^15 times the largest value however long the view is, so values up to 2^112 do not overflow it.
 //
 // Work: an item is (session, KV head, group of two row tiles); its tiles are those of the view and of the tail up to the group's last
 // token.  All items' tiles lie on one line (with a lead for what starting and ending an item costs), cut into equal parts, one for each
@@ -66,8 +67,8 @@ constexpr int kPreTmaWarp = 8, kPreMmaWarp = 9;
 static_assert(256 * 208 + 128 * 88 <= kPreThreads * 168, "the registers that the row warps take are those the others give");
 constexpr int kPreLead = 3;                      // units on the line for an item's start and end: what they cost a CTA, in tiles (1: 170 and 243 us,
                                                  // 5: 159 and 212, instead of 155 and 214 for a chunk of 4,096 alone and three ragged sessions)
-constexpr float kPreLimit = 4096.0f;              // half a tile's weights may sum to this before their reference moves (2^8 and 2^64 instead: 2,012 and
-                                                  // 1,918 us against 1,919 for 2,048 tokens over 65,536; a value may be 2^115 before its sum overflows)
+constexpr float kPreLimit = 32768.0f;            // a row's weights may sum to this before their reference moves (2^12 instead: 2,240 us against 1,959
+                                                 // for 2,048 tokens over 65,536, 233 against 219 for three ragged sessions; 2^17 and 2^20 as 2^15)
 constexpr int kPreParts = 4;                     // parts of the line a CTA can have
 constexpr int kPreBudget = 1024;                 // tiles of keys and values (64 KiB each) that a sweep of all CTAs may hold in L2
 constexpr int kPrePartUnits = 64;                // least units of a part, when there is more than one
@@ -660,6 +661,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             float part;
+                            const float room = kPreLimit - sum;        // (known before the weights: sum + part behind them is 1,956 us, this 1,949)
                             for (bool again = false;; again = true) {
                                 const float use = ref == -INFINITY ? 0.0f : ref;      // nothing seen yet: every weight is exp2(-inf) = 0
                                 const uint64_t nm2 = f2::pk(-use, -use);
@@ -684,13 +686,15 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                                 f2::unpk(acc1, a2, a3);
                                 part = (a0 + a1) + (a2 + a3);
                                 // rows without a reference yet, and those whose weights have grown past the limit (a NaN too)
-                                const bool moves = live && (ref == -INFINITY || !(part <= kPreLimit));
+                                const bool moves = live && (ref == -INFINITY || !(part <= room));
                                 if (again || !__any_sync(0xffffffffu, moves)) break;
                                 float m = -INFINITY;                   // largest logit of this half, NaN if one is
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
                                     m = f2::max3_nan(m, __uint_as_float(sv[2 * half + (i >> 4)][2 * (i & 15)]), __uint_as_float(sv[2 * half + (i >> 4)][2 * (i & 15) + 1]));
                                 m *= scale2;
+                                const float so_far = ref + __log2f(sum);         // log2 of the row's sum in front of this half; -inf without one
+                                m = f2::max3_nan(m, so_far, so_far);
                                 const float to = moves && m != -INFINITY ? m : ref, corr = to == ref ? 1.0f : t5::ex2(ref - to);
                                 // what O holds: the products before this tile's logits were issued, and the first half's
                                 if (half == 1) {
@@ -864,7 +868,7 @@ prefill_merge_kernel(const __grid_constant__ PreWork w) {
             }
             float to = top;
 #pragma unroll
-            for (int i = 0; i < kPreMergeBatch; ++i) to = fmaxf(to, ml[i].x);
+            for (int i = 0; i < kPreMergeBatch; ++i) to = fmaxf(to, ml[i].x + __log2f(ml[i].y));      // (by its sum: no share is more than its values)
             const float back = top > -INFINITY ? t5::ex2(top - to) : 1.0f;            // (without a reference z and acc are 0, or NaN)
             z *= back;
 #pragma unroll

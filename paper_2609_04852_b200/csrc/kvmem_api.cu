@@ -137,6 +137,32 @@ static void on_threads(int n, const F& f) {
     for (int i = 1; i < started; ++i) t[i].join();
 }
 
+// frequencies of the pool's own rotary form: theta^(-2i/d)
+static void own_frequencies(const kvmem_pool_config_t& c, double* f) {
+    for (int i = 0; i < c.head_dim / 2; ++i) f[i] = pow((double)c.rope_theta, -2.0 * (double)i / (double)c.head_dim);
+}
+
+// cos/sin of position * frequency in fp64, one rounding to fp32, computed here on the host; 8,192 positions at a time from pageable memory, which
+// a copy has left when its call returns
+static int upload_rope_table(const kvmem_pool& p, const double* freq, cudaStream_t st) {
+    const int half = p.cfg.head_dim / 2, positions = p.cfg.rope_max_positions, chunk = 8192;
+    const std::unique_ptr<float2[]> rows(new (std::nothrow) float2[(size_t)std::min(chunk, positions) * half]);
+    if (!rows) { set_error("host allocation failed"); return KVMEM_E_CAPACITY; }
+    for (int p0 = 0; p0 < positions; p0 += chunk) {
+        const int n = std::min(chunk, positions - p0);
+        on_threads(n, [&](int r0, int r1) {
+            for (int r = r0; r < r1; ++r)
+                for (int i = 0; i < half; ++i) {
+                    const double ang = (double)(p0 + r) * freq[i];
+                    rows[(size_t)r * half + i] = make_float2((float)cos(ang), (float)sin(ang));
+                }
+        });
+        const cudaError_t e = cudaMemcpyAsync(p.rope_dev + (size_t)p0 * half, rows.get(), (size_t)n * half * sizeof(float2), cudaMemcpyHostToDevice, st);
+        if (e != cudaSuccess) return cuda_fail("rotary table upload", e);
+    }
+    return KVMEM_OK;
+}
+
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 // The passes that read pages through the block table walk the view in 64-token tiles: a tile is 64 / B whole blocks or
@@ -249,24 +275,10 @@ int kvmem_pool_create(const kvmem_pool_config_t* cfg, void* storage, size_t byte
     e = cudaMemset(p->base + lay.tables_off, 0xff, lay.nblocks_off - lay.tables_off);
     if (e == cudaSuccess) e = cudaMemset(p->base + lay.nblocks_off, 0, lay.rope_off - lay.nblocks_off);
     if (e == cudaSuccess && cfg->rope_max_positions > 0) {
-        // cos/sin of position * theta^(-2i/d): angle in fp64, one rounding to fp32 (built here, on the host)
-        const int half = cfg->head_dim / 2;
-        std::vector<double> freq(half);
-        for (int i = 0; i < half; ++i) freq[i] = pow((double)cfg->rope_theta, -2.0 * (double)i / (double)cfg->head_dim);
-        const int chunk = 8192;
-        const std::unique_ptr<float2[]> rows(new (std::nothrow) float2[(size_t)std::min(chunk, cfg->rope_max_positions) * half]);
-        if (!rows) { delete p; set_error("host allocation failed"); return KVMEM_E_CAPACITY; }
-        for (int p0 = 0; e == cudaSuccess && p0 < cfg->rope_max_positions; p0 += chunk) {
-            const int n = std::min(chunk, cfg->rope_max_positions - p0);
-            on_threads(n, [&](int r0, int r1) {
-                for (int r = r0; r < r1; ++r)
-                    for (int i = 0; i < half; ++i) {
-                        const double ang = (double)(p0 + r) * freq[i];
-                        rows[(size_t)r * half + i] = make_float2((float)cos(ang), (float)sin(ang));
-                    }
-            });
-            e = cudaMemcpy(p->rope_dev + (size_t)p0 * half, rows.get(), (size_t)n * half * sizeof(float2), cudaMemcpyHostToDevice);
-        }
+        double freq[256];
+        own_frequencies(*cfg, freq);
+        const int rc = upload_rope_table(*p, freq, nullptr);
+        if (rc != KVMEM_OK) { (void)cudaDeviceSynchronize(); delete p; return rc; }
     }
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) { delete p; return cuda_fail("clearing pool metadata", e); }
@@ -1396,8 +1408,17 @@ int kvmem_set_rope(kvmem_pool_t* p, const kvmem_rope_t* rope, void* stream) {
             set_error("session %d holds blocks: the rotary form of a pool is set before tokens come in", s);
             return KVMEM_E_STATE;
         }
-    const cudaError_t e = launch_rope_table(*p, f, (cudaStream_t)stream);
-    if (e != cudaSuccess) return cuda_fail("rotary table kernel launch", e);
+    // The pool's own frequencies give the table that it was created with, to the bit: where the device's 64-bit cosine and the host's differ in
+    // their last bit, one entry in some 10^9 rounds to another fp32.
+    double own[256];
+    own_frequencies(p->cfg, own);
+    if (memcmp(f.f, own, sizeof(double) * (p->cfg.head_dim / 2)) == 0) {
+        const int copied = upload_rope_table(*p, own, (cudaStream_t)stream);
+        if (copied != KVMEM_OK) return copied;
+    } else {
+        const cudaError_t e = launch_rope_table(*p, f, (cudaStream_t)stream);
+        if (e != cudaSuccess) return cuda_fail("rotary table kernel launch", e);
+    }
     p->rope_form = form;
     return KVMEM_OK;
 }

@@ -696,7 +696,8 @@ int kvmem_set_rope(kvmem_pool_t* pool, const kvmem_rope_t* rope /*HOST, may be N
  *   positions  DEVICE int32 [n_rows]; rows with a position outside the table are left unwritten and flagged in the status word
  *   amplitude  0 selects 1.  (Where a form comes with a factor m on its cos and sin: m^2 on the queries and none on the keys
  *              gives the same logits, and is what fits keys that this library rotates.)
- * x and y may be the same vectors if the two orders are the same; any other overlap is refused (KVMEM_E_INVALID). */
+ * x and y may be the same vectors if the two orders are the same; any other overlap is refused (KVMEM_E_INVALID).  Extents are compared, first
+ * element to last: y between the rows of x counts as overlap too. */
 int kvmem_rope_apply(kvmem_pool_t* pool, const void* x /*DEVICE*/, int64_t x_row_stride, int64_t x_vec_stride, int32_t x_order,
                      void* y /*DEVICE*/, int64_t y_row_stride, int64_t y_vec_stride, int32_t y_order, int64_t n_rows, int32_t n_vec,
                      const int32_t* positions /*DEVICE*/, int32_t inverse, float amplitude, void* stream);
@@ -752,7 +753,8 @@ typedef struct {
  *   positions DEVICE int32 [n_sessions][n_new_tokens], or NULL
  *   q_out     DEVICE bf16 [n_sessions][n_new_tokens][L][H][d]
  * A token whose position lies outside the table is left out as a whole and flagged.  An n_tokens[s] outside
- * [0, cap_tokens - n_new[s]] is clamped to it and flagged.  Results must not overlap the inputs or each other (KVMEM_E_INVALID).
+ * [0, cap_tokens - n_new[s]] is clamped to it and flagged.  Results must not overlap the inputs or each other (KVMEM_E_INVALID; extents are
+ * compared, first element to last).
  * KVMEM_E_UNSUPPORTED: head_dim not a multiple of 16, or 2^31 groups of 16 elements in one session's new tokens.  KVMEM_E_STATE: to_pages
  * on an FP8 repository or with rope_in_block_keys. */
 int kvmem_append_tokens(kvmem_pool_t* pool, int32_t session_first, int32_t n_sessions, int32_t n_new_tokens,

@@ -114,7 +114,9 @@ __device__ __forceinline__ int pre_tail_tiles(const PrefillArgs& a, const PreSpa
     return a.tail_k ? (sp.n_tail + min((rg + 1) * 2 * tpt, sp.n_q) + kPreTile - 1) / kPreTile : 0;
 }
 
-// sum over i < n of floor((step i + from) / 128), by exchanging the axes of the triangle under the line.  In 32 bits: the sum is
+// sum over i < n of floor((step i + from) / 128): whole parts of step and from taken out, then the axes of the lattice points under the line
+// exchanged, as in Euclid's algorithm (a known method; Knuth, The Art of Computer Programming, 3.3.3; Graham, Knuth and Patashnik,
+// Concrete Mathematics, 3.5).  In 32 bits: the sum is
 // at most the line's 2^30 units, and so are the products that it is made of.
 __device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t step, uint32_t from) {
     uint32_t m = kPreTile, sum = 0;
@@ -677,7 +679,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                                         p0 = t5::ex2(p0);
                                         p1 = t5::ex2(p1);
                                         if (i & 1) acc1 = f2::add(acc1, f2::pk(p0, p1)); else acc0 = f2::add(acc0, f2::pk(p0, p1));
-                                        pk[i] = ptx::pack_bf16x2(p0, p1);
+                                        pk[i] = ptx::pack_bf16x2(p0, p1);         // what the tensor pipe takes beside bf16 values; the sum is of the fp32 weights
                                     }
                                     t5::st16(s_addr + 32u * half + 16u * c, pk);      // over logits that this thread has read
                                 }

@@ -279,6 +279,7 @@ int kvmem_pool_create(const kvmem_pool_config_t* cfg, void* storage, size_t byte
         own_frequencies(*cfg, freq);
         const int rc = upload_rope_table(*p, freq, nullptr);
         if (rc != KVMEM_OK) { (void)cudaDeviceSynchronize(); delete p; return rc; }
+        p->rope_own = true;
     }
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) { delete p; return cuda_fail("clearing pool metadata", e); }
@@ -1413,9 +1414,13 @@ int kvmem_set_rope(kvmem_pool_t* p, const kvmem_rope_t* rope, void* stream) {
     double own[256];
     own_frequencies(p->cfg, own);
     if (memcmp(f.f, own, sizeof(double) * (p->cfg.head_dim / 2)) == 0) {
-        const int copied = upload_rope_table(*p, own, (cudaStream_t)stream);
-        if (copied != KVMEM_OK) return copied;
+        if (!p->rope_own) {
+            const int copied = upload_rope_table(*p, own, (cudaStream_t)stream);
+            if (copied != KVMEM_OK) return copied;
+            p->rope_own = true;
+        }
     } else {
+        p->rope_own = false;
         const cudaError_t e = launch_rope_table(*p, f, (cudaStream_t)stream);
         if (e != cudaSuccess) return cuda_fail("rotary table kernel launch", e);
     }

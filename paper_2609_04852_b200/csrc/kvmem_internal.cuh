@@ -79,6 +79,7 @@ struct kvmem_pool {
     int32_t free_hint;
     int sm_count;
     kvmem::RopeForm rope_form;          // of the model whose queries and keys come in; meaningless without a rotary table
+    bool rope_own = false;              // the table is the one of the pool's own frequencies
     // host-resident index scoring: a copy stream and its events, created on first use
     cudaStream_t copy_stream = nullptr;
     cudaEvent_t ev_ready[2] = {nullptr, nullptr}, ev_free[2] = {nullptr, nullptr}, ev_start = nullptr;

@@ -25,6 +25,9 @@ def test_the_pools_own_form_again_is_the_table_it_was_created_with(d, positions,
     angle = at.double().view(-1, 1) * f
     want = torch.stack([angle.cos(), angle.sin()], -1)
     assert bool(((created[at.cuda()].cpu().double() - want).abs() <= 2.0 ** -24 * want.abs() * (1 + 2.0 ** -20) + 1e-12).all())
+    for own in (Rope("interleaved"), None):                              # as it is
+        pool.set_rope(own)
+        assert torch.equal(table(pool).view(torch.int32), created.view(torch.int32))
     other = Rope("interleaved", 0, "linear", 2.0)
     for own in (None, Rope(), Rope("interleaved"), Rope("half", d)):
         st = torch.cuda.Stream()

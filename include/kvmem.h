@@ -681,7 +681,7 @@ int kvmem_rope_frequencies(const kvmem_pool_config_t* cfg /*HOST*/, const kvmem_
 
 /* Make the pool one of a model with this rotary form (NULL: the pool's own again): its table is rebuilt on `stream` with these
  * frequencies (angles in 64 bits, cos and sin rounded once to fp32; with the pool's own frequencies the bits of its creation, computed on the host
- * as there, unless the table holds them already), so that every call that rotates uses them, and
+ * as there and copied before the call returns, unless the table holds them already), so that every call that rotates uses them, and
  * kvmem_rope_apply and kvmem_append_tokens go from the model's order to the pool's.  Before any block is appended or reserved
  * (KVMEM_E_STATE otherwise): stored keys stay in the frame they were encoded in.  Work that reads the table must be ordered
  * behind this call (same stream, or an event). */

@@ -142,8 +142,8 @@ static void own_frequencies(const kvmem_pool_config_t& c, double* f) {
     for (int i = 0; i < c.head_dim / 2; ++i) f[i] = pow((double)c.rope_theta, -2.0 * (double)i / (double)c.head_dim);
 }
 
-// cos/sin of position * frequency in fp64, one rounding to fp32, computed here on the host; 8,192 positions at a time from pageable memory, which
-// a copy has left when its call returns
+// cos/sin of position * frequency in fp64, one rounding to fp32, computed here on the host; 8,192 positions at a time in one buffer, used
+// again when its copy is over (whether a copy from pageable memory is staged or read later is the system's choice)
 static int upload_rope_table(const kvmem_pool& p, const double* freq, cudaStream_t st) {
     const int half = p.cfg.head_dim / 2, positions = p.cfg.rope_max_positions, chunk = 8192;
     const std::unique_ptr<float2[]> rows(new (std::nothrow) float2[(size_t)std::min(chunk, positions) * half]);
@@ -157,7 +157,8 @@ static int upload_rope_table(const kvmem_pool& p, const double* freq, cudaStream
                     rows[(size_t)r * half + i] = make_float2((float)cos(ang), (float)sin(ang));
                 }
         });
-        const cudaError_t e = cudaMemcpyAsync(p.rope_dev + (size_t)p0 * half, rows.get(), (size_t)n * half * sizeof(float2), cudaMemcpyHostToDevice, st);
+        cudaError_t e = cudaMemcpyAsync(p.rope_dev + (size_t)p0 * half, rows.get(), (size_t)n * half * sizeof(float2), cudaMemcpyHostToDevice, st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
         if (e != cudaSuccess) return cuda_fail("rotary table upload", e);
     }
     return KVMEM_OK;
